@@ -305,6 +305,99 @@ typedef enum {
 int skd_profile_enable(skd_state *st, int32_t on);
 int skd_profile_read(skd_state *st, double *ms, int64_t *launches);
 
+/* Operators outside of a state ------------------------------------------- */
+
+/* A paged cache of keys and values in the caller's memory: a pool of pages, and
+ * for every row (sequence) the pages that hold its positions, page_tokens of
+ * them each, in a block table.  One layer's; layers have a pool or block tables
+ * each.  Everything is device memory of the current device; the calls only
+ * enqueue work on hip_stream (NULL: the default stream), allocate nothing, wait
+ * for nothing and may be captured into a graph.  Calls that run at the same time
+ * (two streams, two graphs) need workspaces of their own; rows of one pool may be
+ * appended to and read at the same time if they share no page.
+ *
+ * SKD_KV_BF16 pages hold bf16 values.  In elements, per kv head h (of
+ * page_tokens * 2 * head_dim) and block of 32 positions (of 64 * head_dim):
+ *   keys   [half of the block][head_dim / 32][4][16 positions][8]
+ *          position 16 half + p, element 32 i + 8 j + e at [half][i][j][p][e]
+ *   values [head_dim / 16][4][16][2][4]
+ *          position 16 x + 4 j + y, element 16 i + e at [i][j][e][x][y]
+ * SKD_KV_FP8 pages hold 8 bits a value: e4m3 codes in bytes, per head and block
+ *   keys   [half][head_dim / 64][4][16 positions][2][8]
+ *          position 16 half + p, element 64 i + 32 w + 8 j + e at [half][i][j][p][w][e]
+ *   values [head_dim / 32][4][16][2][2][4]
+ *          position 16 x + 4 j + y, element 32 i + 16 w + e at [i][j][e][w][x][y]
+ * and behind the codes of all heads [kv_heads][page_tokens / 32][k | v][32]
+ * bytes: the values of a position are code * 2^(byte - 127), where the exponent is
+ * the smallest from -127 on with which no magnitude exceeds 448 * 2^exponent, and
+ * codes are rounded to nearest even (those of exponent 120 end at 240, so that
+ * what is finite stays so).  A position and head whose values held an
+ * infinity or NaN has byte 255, codes 0, and reads as NaN.
+ * The bf16 pages of a state have the same layout. */
+enum { SKD_KV_BF16 = 0, SKD_KV_FP8 = 1 }; /* skd_kv.elem */
+typedef struct {
+  int32_t elem;
+  int32_t kv_heads, head_dim; /* head_dim 64 or 128 */
+  int32_t page_tokens;        /* multiple of 32 */
+  int32_t pages;              /* of the pool */
+  int32_t rows, max_pages;    /* of the block table */
+  void *pool;                 /* pages * skd_kv_page_bytes, 16-byte aligned */
+  const int32_t *block_table; /* [rows][max_pages]: entries outside [0, pages) are no page: what would be filed there is
+                                 dropped, and their positions are neither read nor attended to */
+} skd_kv;
+
+/* The tokens of a call: those of row r are tokens first[r] .. first[r + 1] - 1 of
+ * the call's arrays and have the positions past[r], past[r] + 1, ... of the row.
+ * Rows may have none.  max_new and max_past are upper bounds of the counts and of
+ * past[], known to the host: tokens of a row beyond max_new are left out, and
+ * max_past only decides how the work is shared out.  Counts that do not fit into
+ * [0, tokens) are cut; a row whose past is negative, or more than its pages
+ * hold, is left out.  max_pages * page_tokens is below 2^30. */
+typedef struct {
+  int32_t tokens;             /* rows of the call's arrays */
+  int32_t max_new, max_past;
+  const int32_t *first;       /* [rows + 1] */
+  const int32_t *past;        /* [rows] */
+} skd_kv_chunk;
+
+/* Bytes of a page; nothing but the shape is read.  Negative skd_err. */
+int64_t skd_kv_page_bytes(const skd_kv *kv);
+
+/* File the keys and values of new tokens: k, v [tokens][kv_heads * head_dim] bf16,
+ * strides in elements from token to token (multiples of 8, pointers 16-byte
+ * aligned).  What the pages hold at other positions stays.  Errors:
+ * SKD_ERR_NULL; SKD_ERR_SHAPE (unknown elem, head_dim, page_tokens, counts below
+ * 1, strides, alignment); SKD_ERR_RANGE (negative counts, sizes beyond 32 bits of
+ * positions or workgroups, memory that is not the current device's);
+ * SKD_ERR_HIP. */
+int skd_kv_append(const skd_kv *kv, const skd_kv_chunk *chunk, const void *k, int64_t k_stride, const void *v,
+                  int64_t v_stride, void *hip_stream);
+
+/* Read back the keys and values at the tokens' positions (past = 0 and as many
+ * tokens as it holds: a whole row) into k_out, v_out [tokens][kv_heads * head_dim],
+ * fp32 (SKD_W_FP32: exact) or bf16 (SKD_W_BF16).  Tokens whose positions have no
+ * page keep what was there.  Errors as skd_kv_append. */
+int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t elem, void *k_out, int64_t k_stride, void *v_out,
+                int64_t v_stride, void *hip_stream);
+
+/* Attention of new tokens over the cache: query head h of a token at position p of
+ * its row attends, with softmax(scale * q . k), to positions 0 .. p of kv head
+ * h / (heads / kv_heads).  q, out [tokens][heads * head_dim] bf16, heads a multiple of
+ * kv_heads.  k and v (both or neither): the new tokens' keys and values, filed by
+ * this call as by skd_kv_append before they are attended to (as they are held, so
+ * in 8 bits as rounded); NULL: the cache holds them already.  A query that sees
+ * no position gets zeros.  Positions behind a row's last one may hold anything.
+ * Sums and softmax are in fp32, weights are rounded to bf16 for the matrix
+ * instructions.  workspace: skd_kv_attend_workspace bytes for this kv, chunk and
+ * heads (16-byte aligned; NULL where that is 0), nothing in it is kept from call
+ * to call.  The same call gives the same bits.  Errors as skd_kv_append, and
+ * SKD_ERR_SHAPE (heads), SKD_ERR_RANGE (scale not above 0), SKD_ERR_NOMEM
+ * (workspace_bytes). */
+int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, float scale, const void *q, int64_t q_stride,
+                  const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
+                  void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads);
+
 void skd_destroy(skd_state *st);
 const char *skd_strerror(int err);
 /* hipError_t (as int) of the most recent failing HIP call on this thread, 0 if none. */

@@ -32,6 +32,24 @@ constexpr long kv_v_off(int h, int tt, int e, const KvGeom &g) {
          ((long)(e >> 4) * 64 + 16 * ((kk & 15) >> 2) + (e & 15)) * 8 + 4 * (kk >> 4) + (kk & 3);
 }
 
+// 8-bit page (one row): codes [head][32-key block][K block | V block], then exponents [head][32-key block][k | v][32].
+// K block = [tile 0..1][pair of chunks][lane][2][8]: a lane's 16 bytes are its 8 elements of two neighbouring chunks of the
+// bf16 layout; V block = [pair of 16 elements][lane][2][8] likewise.  Offsets in bytes.
+constexpr long kv8_page_bytes(int H, int dh, int page_tokens) { return (long)H * page_tokens * (2 * dh + 2); }
+constexpr long kv8_k_off(int h, int tt, int e, const KvGeom &g) {
+  const int kk = tt & 31;
+  return kv_block_base(h, tt, g) +
+         ((long)((kk >> 4) * (g.dh >> 6) + (e >> 6)) * 64 + (kk & 15) + 16 * ((e & 31) >> 3)) * 16 + ((e >> 5) & 1) * 8 + (e & 7);
+}
+constexpr long kv8_v_off(int h, int tt, int e, const KvGeom &g) {
+  const int kk = tt & 31;
+  return kv_block_base(h, tt, g) + 32 * g.dh +
+         ((long)(e >> 5) * 64 + 16 * ((kk & 15) >> 2) + (e & 15)) * 16 + ((e >> 4) & 1) * 8 + 4 * (kk >> 4) + (kk & 3);
+}
+constexpr long kv8_exp_off(int h, int tt, int v, const KvGeom &g) {
+  return (long)g.H * g.page_tokens * 2 * g.dh + ((long)h * (g.page_tokens >> 5) + (tt >> 5)) * 64 + 32 * v + (tt & 31);
+}
+
 // The same in parts, for 16 positions (half `half` of a block) at a time: kv_block_base + kv_k_half + kv_k_at is where the
 // eight elements from e on (a multiple of 8) of the key at position `key` of the 16 begin, kv_block_base + kv_v_half + kv_v_at
 // where the values of element e at four positions from `key` on (a multiple of 4) do.  Parts inside a block fit 32 bits.

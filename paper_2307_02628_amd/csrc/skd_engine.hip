@@ -74,6 +74,10 @@ struct GemmPlan {
 
 namespace skd {
 thread_local LaunchTimer *g_launch_timer = nullptr;
+int hip_failed(hipError_t e) {
+  g_last_hip = (int)e;
+  return e == hipErrorOutOfMemory ? SKD_ERR_NOMEM : SKD_ERR_HIP;
+}
 }
 
 // hands the launches of one kernel class their event pairs (skd_profile_enable mode 1)

@@ -1,0 +1,193 @@
+// C entry points of the operators outside of a state: argument checks and launches.
+#include <math.h>
+
+#include <limits>
+
+#include "../../include/skd.h"
+#include "kv_ops.h"
+
+using namespace skd;
+
+namespace {
+
+bool aligned(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+int check_kv(const skd_kv *kv) {
+  if (!kv) return SKD_ERR_NULL;
+  if (kv->elem != SKD_KV_BF16 && kv->elem != SKD_KV_FP8) return SKD_ERR_SHAPE;
+  if (kv->head_dim != 64 && kv->head_dim != 128) return SKD_ERR_SHAPE;
+  if (kv->kv_heads < 1 || kv->kv_heads > 65536 || kv->page_tokens < 32 || kv->page_tokens % 32 || kv->pages < 1 || kv->rows < 0 || kv->max_pages < 1) return SKD_ERR_SHAPE;
+  if ((int64_t)kv->max_pages * kv->page_tokens >= 1 << 30) return SKD_ERR_RANGE;  // positions are counted in 32 bits
+  return SKD_OK;
+}
+int check_call(const skd_kv *kv, const skd_kv_chunk *ch) {
+  const int rc = check_kv(kv);
+  if (rc != SKD_OK) return rc;
+  if (!ch) return SKD_ERR_NULL;
+  if (ch->tokens < 0 || ch->max_new < 0 || ch->max_past < 0) return SKD_ERR_RANGE;
+  return SKD_OK;
+}
+// The device memory of a call, which is the current device's: a pointer that is not, or is no device memory, is refused
+// before it reaches a kernel.
+int check_memory(std::initializer_list<const void *> ps) {
+  int device = 0;
+  if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return hip_failed(e);
+  for (const void *p : ps) {
+    hipPointerAttribute_t at{};
+    if (hipPointerGetAttributes(&at, p) != hipSuccess) {
+      (void)hipGetLastError();
+      return SKD_ERR_RANGE;
+    }
+    if (at.type == hipMemoryTypeUnregistered || (at.type == hipMemoryTypeDevice && at.device != device)) return SKD_ERR_RANGE;
+  }
+  return SKD_OK;
+}
+int check_rows(const void *p, int64_t stride, int64_t width) {
+  if (!p) return SKD_ERR_NULL;
+  if (stride < width || stride % 8 || !aligned(p)) return SKD_ERR_SHAPE;
+  return SKD_OK;
+}
+
+KvView view(const skd_kv *kv) {
+  KvView v{};
+  v.g.page_tokens = kv->page_tokens;
+  v.g.max_pages = kv->max_pages;
+  v.g.H = kv->kv_heads;
+  v.g.dh = kv->head_dim;
+  v.fp8 = kv->elem == SKD_KV_FP8;
+  v.pages = kv->pages;
+  v.rows = kv->rows;
+  v.page_bytes = (long)skd_kv_page_bytes(kv);
+  v.pool = (unsigned char *)kv->pool;
+  v.table = kv->block_table;
+  return v;
+}
+KvTokens tokens(const skd_kv *kv, const skd_kv_chunk *ch) {
+  KvTokens t{};
+  t.kind = KvTokens::RAGGED;
+  t.first = ch->first;
+  t.past = ch->past;
+  t.tokens = ch->tokens;
+  t.step = 1;
+  // no row has more positions than its pages hold, nor more new tokens than there are
+  const int64_t room = (int64_t)kv->max_pages * kv->page_tokens;
+  t.max_new = (int)std::min<int64_t>(std::min(ch->max_new, ch->tokens), room);
+  t.max_past = (int)std::min<int64_t>(ch->max_past, room);
+  t.room = (int)room;
+  return t;
+}
+KvRows rows_of(const void *p, int64_t stride) { return KvRows{const_cast<void *>(p), (long)stride, 0, false}; }
+
+int launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SKD_OK : hip_failed(e);
+}
+bool fits_grid(int64_t wgs) { return wgs <= std::numeric_limits<int32_t>::max(); }
+
+#define CHECK(expr)          \
+  do {                       \
+    const int r_ = (expr);   \
+    if (r_ < 0) return r_;   \
+  } while (0)
+
+}  // namespace
+
+extern "C" int64_t skd_kv_page_bytes(const skd_kv *kv) {
+  CHECK(check_kv(kv));
+  return kv->elem == SKD_KV_FP8 ? (int64_t)kv8_page_bytes(kv->kv_heads, kv->head_dim, kv->page_tokens)
+                                : (int64_t)kv->kv_heads * kv->page_tokens * 4 * kv->head_dim;
+}
+
+extern "C" int skd_kv_append(const skd_kv *kv, const skd_kv_chunk *ch, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                             void *hip_stream) {
+  CHECK(check_call(kv, ch));
+  const KvTokens tk = tokens(kv, ch);
+  if (!tk.max_new || !kv->rows) return SKD_OK;
+  if (!kv->pool || !kv->block_table || !ch->first || !ch->past) return SKD_ERR_NULL;
+  const int64_t width = (int64_t)kv->kv_heads * kv->head_dim;
+  CHECK(check_rows(k, k_stride, width));
+  CHECK(check_rows(v, v_stride, width));
+  if (!aligned(kv->pool)) return SKD_ERR_SHAPE;
+  if (!fits_grid(((int64_t)tk.max_new + 62) / 32 * kv->kv_heads * kv->rows)) return SKD_ERR_RANGE;
+  CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, k, v}));
+  kv_append((hipStream_t)hip_stream, view(kv), tk, rows_of(k, k_stride), rows_of(v, v_stride));
+  return launched();
+}
+
+extern "C" int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *ch, int32_t elem, void *k_out, int64_t k_stride, void *v_out,
+                           int64_t v_stride, void *hip_stream) {
+  CHECK(check_call(kv, ch));
+  if (elem != SKD_W_FP32 && elem != SKD_W_BF16) return SKD_ERR_SHAPE;
+  const KvTokens tk = tokens(kv, ch);
+  if (!tk.max_new || !kv->rows) return SKD_OK;
+  if (!kv->pool || !kv->block_table || !ch->first || !ch->past) return SKD_ERR_NULL;
+  const int64_t width = (int64_t)kv->kv_heads * kv->head_dim;
+  CHECK(check_rows(k_out, k_stride, width));
+  CHECK(check_rows(v_out, v_stride, width));
+  if (!aligned(kv->pool)) return SKD_ERR_SHAPE;
+  if (!fits_grid(((int64_t)tk.max_new + 62) / 32 * kv->kv_heads * kv->rows)) return SKD_ERR_RANGE;
+  CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, k_out, v_out}));
+  kv_read((hipStream_t)hip_stream, view(kv), tk, elem == SKD_W_BF16, rows_of(k_out, k_stride), rows_of(v_out, v_stride));
+  return launched();
+}
+
+static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads) {
+  CHECK(check_call(kv, ch));
+  if (heads < 1 || heads % kv->kv_heads) return SKD_ERR_SHAPE;
+  const KvTokens tk = tokens(kv, ch);
+  const int64_t group = heads / kv->kv_heads;
+  if (!fits_grid(((int64_t)tk.max_new * group + 15) / 16 * kv->kv_heads * std::max(kv->rows, 1)) || (int64_t)tk.max_new * group > std::numeric_limits<int32_t>::max() - 16)
+    return SKD_ERR_RANGE;
+  return SKD_OK;
+}
+
+extern "C" int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads) {
+  CHECK(check_attend(kv, ch, heads));
+  const KvView v = view(kv);
+  const KvTokens tk = tokens(kv, ch);
+  if (!tk.max_new || !kv->rows) return 0;
+  return (int64_t)(kv_attend_part(v, tk, heads, kv_attend_splits(v, tk, heads)) * sizeof(float));
+}
+
+extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float scale, const void *q, int64_t q_stride,
+                             const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
+                             void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  CHECK(check_attend(kv, ch, heads));
+  if (!(scale > 0.f) || !std::isfinite(scale)) return SKD_ERR_RANGE;
+  KvAttend a{};
+  a.kv = view(kv);
+  a.tk = tokens(kv, ch);
+  if (!a.tk.max_new || !kv->rows) return SKD_OK;
+  if (!kv->pool || !kv->block_table || !ch->first || !ch->past || !k != !v) return SKD_ERR_NULL;
+  const int64_t width = (int64_t)kv->kv_heads * kv->head_dim;
+  CHECK(check_rows(q, q_stride, (int64_t)heads * kv->head_dim));
+  CHECK(check_rows(out, out_stride, (int64_t)heads * kv->head_dim));
+  if (k) {
+    CHECK(check_rows(k, k_stride, width));
+    CHECK(check_rows(v, v_stride, width));
+  }
+  if (!aligned(kv->pool)) return SKD_ERR_SHAPE;
+  a.heads = heads;
+  a.group = heads / kv->kv_heads;
+  a.c = scale * 1.4426950408889634f;
+  a.q = rows_of(q, q_stride);
+  a.o = rows_of(out, out_stride);
+  a.splits = kv_attend_splits(a.kv, a.tk, heads);
+  if (a.splits > 1) {
+    if (!workspace) return SKD_ERR_NULL;
+    if (!aligned(workspace)) return SKD_ERR_SHAPE;
+    if (workspace_bytes < (int64_t)(kv_attend_part(a.kv, a.tk, heads, a.splits) * sizeof(float))) return SKD_ERR_NOMEM;
+    a.part = (float *)workspace;
+  }
+  CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, q, out}));
+  if (k) CHECK(check_memory({k, v}));
+  if (a.splits > 1) CHECK(check_memory({workspace}));
+  if (k && a.tk.max_new == 1) {  // one launch
+    a.k = rows_of(k, k_stride);
+    a.v = rows_of(v, v_stride);
+  } else if (k) {
+    kv_append((hipStream_t)hip_stream, a.kv, a.tk, rows_of(k, k_stride), rows_of(v, v_stride));
+  }
+  kv_attend((hipStream_t)hip_stream, a);
+  return launched();
+}

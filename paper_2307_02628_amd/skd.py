@@ -20,11 +20,12 @@ OK, ERR_NULL, ERR_SHAPE, ERR_RANGE, ERR_ORDER, ERR_SCHEDULE, ERR_NOMEM, ERR_HIP 
 BF16, FP32 = 0, 1
 HOST, DEVICE = 0, 1
 W_FP32, W_BF16 = 0, 1
+KV_BF16, KV_FP8 = 0, 1
 
 EXPORTS = ["skd_schedule", "skd_active_layers", "skd_create", "skd_create_with_schedule", "skd_state_active_layers", "skd_prefill", "skd_decode_step",
            "skd_logits_argmax", "skd_logits_argmax_noalloc", "skd_logits_sample", "skd_rewind", "skd_profile_enable", "skd_profile_read", "skd_kv_len", "skd_kv_pages_reserved", "skd_kv_pages_dense", "skd_synchronize",
            "skd_debug_read_hidden", "skd_debug_kv_load", "skd_debug_kv_read", "skd_destroy", "skd_strerror",
-           "skd_last_hip_error"]
+           "skd_last_hip_error", "skd_kv_page_bytes", "skd_kv_append", "skd_kv_read", "skd_kv_attend", "skd_kv_attend_workspace"]
 
 
 class Config(C.Structure):
@@ -86,6 +87,12 @@ def lib() -> C.CDLL:
         l.skd_strerror.argtypes = [C.c_int]
         l.skd_strerror.restype = C.c_char_p
         l.skd_last_hip_error.argtypes = []
+        P, I32, I64 = C.c_void_p, C.c_int32, C.c_int64
+        l.skd_kv_page_bytes.argtypes, l.skd_kv_page_bytes.restype = [P], I64
+        l.skd_kv_append.argtypes = [P, P, P, I64, P, I64, P]
+        l.skd_kv_read.argtypes = [P, P, I32, P, I64, P, I64, P]
+        l.skd_kv_attend.argtypes = [P, P, I32, C.c_float, P, I64, P, I64, P, I64, P, I64, P, I64, P]
+        l.skd_kv_attend_workspace.argtypes, l.skd_kv_attend_workspace.restype = [P, P, I32], I64
         _lib = l
     return _lib
 
@@ -304,3 +311,84 @@ class Decoder:
         v = np.zeros((n, self.cfg.d_model), dtype=np.float32)
         _check(self._lib.skd_debug_kv_read(self._h, layer, b, k.ctypes.data, v.ctypes.data), "skd_debug_kv_read")
         return k, v
+
+
+class Kv(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("elem", "kv_heads", "head_dim", "page_tokens", "pages", "rows", "max_pages")] +
+                [("pool", C.c_void_p), ("block_table", C.c_void_p)])
+
+
+class Chunk(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("tokens", "max_new", "max_past")] + [("first", C.c_void_p), ("past", C.c_void_p)]
+
+
+class KvChunk:
+    """The tokens of a call on a KvCache (skd_kv_chunk): first [rows + 1] and past [rows] are int32 device tensors."""
+
+    def __init__(self, first, past, tokens: int, max_new: int, max_past: int):
+        _expect(first, "int32", 1)
+        _expect(past, "int32", 1)
+        if len(first) != len(past) + 1:
+            raise ValueError("first needs one entry more than past")
+        self._keep = (first, past)
+        self.rows, self.tokens = len(past), tokens
+        self.c = Chunk(tokens, max_new, max_past, _ptr_of(first), _ptr_of(past))
+        self.ref = C.byref(self.c)
+
+
+class KvCache:
+    """Keys and values in pages of the caller's memory (skd_kv): pool [pages][..] and block_table [rows][max_pages] (int32) are
+    contiguous device tensors, kept alive by this object; calls run on `stream` (0: the default stream)."""
+
+    def __init__(self, pool, block_table, kv_heads: int, head_dim: int, page_tokens: int, elem: int = KV_BF16):
+        self._lib = lib()
+        _expect(block_table, "int32", 2)
+        if not pool.is_contiguous() or pool.dim() < 1:
+            raise ValueError("pool must be contiguous, pages first")
+        self._keep = (pool, block_table)
+        self.rows, self.heads, self.dh = block_table.shape[0], kv_heads, head_dim
+        self.c = Kv(elem, kv_heads, head_dim, page_tokens, pool.shape[0], block_table.shape[0], block_table.shape[1],
+                    _ptr_of(pool), _ptr_of(block_table))
+        self.ref = C.byref(self.c)
+        self.page_bytes = _check(self._lib.skd_kv_page_bytes(self.ref), "skd_kv_page_bytes")
+        if pool.numel() * pool.element_size() != self.page_bytes * pool.shape[0]:
+            raise ValueError(f"a page of the pool needs {self.page_bytes} bytes")
+
+    def _rows_of(self, chunk: KvChunk, heads: int, t, *types):
+        """Pointer and stride of [tokens][heads][head_dim] or [tokens][heads * head_dim]."""
+        if chunk.rows != self.rows:
+            raise ValueError("chunk and block table differ in rows")
+        shape, stride = t.shape, t.stride()
+        if shape[0] != chunk.tokens or tuple(shape[1:]) not in ((heads, self.dh), (heads * self.dh,)) or stride[-1] != 1 or (len(shape) == 3 and stride[1] != self.dh):
+            raise ValueError(f"expected [{chunk.tokens}][{heads}][{self.dh}] with dense tokens")
+        if str(t.dtype) not in types:
+            raise ValueError(f"expected {' or '.join(types)}")
+        return t.data_ptr(), max(stride[0], heads * self.dh) if shape[0] < 2 else stride[0]
+
+    def append(self, chunk: KvChunk, k, v, stream: int = 0):
+        _check(self._lib.skd_kv_append(self.ref, chunk.ref, *self._rows_of(chunk, self.heads, k, "torch.bfloat16"),
+                                       *self._rows_of(chunk, self.heads, v, "torch.bfloat16"), stream), "skd_kv_append")
+
+    def read(self, chunk: KvChunk, k_out, v_out, stream: int = 0):
+        """k_out, v_out: both float32 or both bfloat16."""
+        elem = W_FP32 if str(k_out.dtype) == "torch.float32" else W_BF16
+        types = ("torch.float32",) if elem == W_FP32 else ("torch.bfloat16",)
+        _check(self._lib.skd_kv_read(self.ref, chunk.ref, elem, *self._rows_of(chunk, self.heads, k_out, *types),
+                                     *self._rows_of(chunk, self.heads, v_out, *types), stream), "skd_kv_read")
+
+    def attend_workspace(self, chunk: KvChunk, heads: int) -> int:
+        return _check(self._lib.skd_kv_attend_workspace(self.ref, chunk.ref, heads), "skd_kv_attend_workspace")
+
+    def attend(self, chunk: KvChunk, q, out, scale: float, k=None, v=None, workspace=None, stream: int = 0):
+        """q, out [tokens][heads][head_dim]; workspace: a device tensor of attend_workspace bytes (None where that is 0)."""
+        heads = q.shape[1] if q.dim() == 3 else q.shape[1] // self.dh
+        kk = (0, 0) if k is None else self._rows_of(chunk, self.heads, k, "torch.bfloat16")
+        vv = (0, 0) if v is None else self._rows_of(chunk, self.heads, v, "torch.bfloat16")
+        ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        _check(self._lib.skd_kv_attend(self.ref, chunk.ref, heads, scale, *self._rows_of(chunk, heads, q, "torch.bfloat16"), *kk, *vv,
+                                       *self._rows_of(chunk, heads, out, "torch.bfloat16"), *ws, stream), "skd_kv_attend")
+
+
+def _expect(t, dtype: str, dims: int):
+    if str(t.dtype) != "torch." + dtype or t.dim() != dims or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor of {dims} dimensions")
