@@ -224,6 +224,25 @@ int skd_logits_argmax_noalloc(skd_state *st, int32_t *tokens_out, float *logits_
 int skd_logits_sample(skd_state *st, const float *u, float temperature, float top_p, int32_t *tokens_out,
                       float *logits_out);
 
+/* The parameters of a draw, one of each per row: arrays [rows], NULL = off for
+ * every row (temperature: 1). */
+typedef struct {
+  const float *temperature; /* 0: the most likely token, the lowest index of several */
+  const int32_t *top_k;     /* 0: off */
+  const float *top_p;       /* 1: off */
+  const float *min_p;       /* 0: off */
+} skd_sampling;
+
+/* skd_logits_sample with parameters per row, and top-k and min-p: final LayerNorm +
+ * LM head, then the draw of skd_sample below (vocab <= 262144) from the state's
+ * logits.  u [B], the arrays of params (may be NULL: all off) and the outputs are
+ * host memory, or device memory with io_on_device = 1.  Errors: SKD_ERR_NULL,
+ * SKD_ERR_ORDER, SKD_ERR_SHAPE (vocab), SKD_ERR_RANGE (host values: u outside
+ * [0,1), temperature negative or not finite, top_k < 0, top_p outside (0,1],
+ * min_p outside [0,1]), SKD_ERR_HIP. */
+int skd_logits_sample_rows(skd_state *st, const float *u, const skd_sampling *params, int32_t *tokens_out,
+                           float *logits_out);
+
 /* Move the generation back to position t (P <= t <= current position): the
  * next skd_decode_step must be for column t; cache entries at columns >= t are
  * forgotten (they are overwritten when those columns are processed again).
@@ -397,6 +416,28 @@ int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, fl
                   const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
                   void *workspace, int64_t workspace_bytes, void *hip_stream);
 int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads);
+
+/* One token per row of fp32 logits [rows][vocab] (stride: elements from row to
+ * row).  With m_i = exp((z_i - max z) / temperature): kept are the tokens with
+ * m_i >= min_p that are among the top_k largest logits (those equal to the k-th
+ * too), and of these the smallest set of most likely ones whose mass reaches top_p
+ * of theirs (those equal to the last too).  The token is the first index, in
+ * ascending order, whose running mass over that set exceeds u[row] * its mass.
+ * Masses are formed in 64 bits and summed in units of 2^-45 of the largest (a
+ * token below half a unit has none and is never drawn), so the same call gives
+ * the same tokens.  A NaN is taken for -infinity; where the
+ * largest logit is infinite, or temperature is not above 0, the token is the
+ * lowest index that has it (0 in a row without a finite logit).  Device values
+ * outside their ranges: top_k < 0, top_p >= 1 or NaN, min_p <= 0 or NaN are off,
+ * top_p <= 0 keeps the most likely token and those equal to it, min_p >= 1 likewise,
+ * u is cut to [0,1).  vocab <= 262144.  All memory is the current device's, with
+ * stream and workspace (skd_sample_workspace bytes; NULL where that is 0) as for
+ * the calls above.  Errors: SKD_ERR_NULL; SKD_ERR_SHAPE (vocab, stride, pointers not
+ * aligned to their elements); SKD_ERR_RANGE (rows < 0, memory that is not the
+ * current device's); SKD_ERR_NOMEM (workspace_bytes); SKD_ERR_HIP. */
+int skd_sample(const float *logits, int64_t stride, int32_t rows, int32_t vocab, const skd_sampling *params, const float *u,
+               int32_t *tokens_out, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t skd_sample_workspace(int32_t rows, int32_t vocab);
 
 void skd_destroy(skd_state *st);
 const char *skd_strerror(int err);

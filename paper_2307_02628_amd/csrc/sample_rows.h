@@ -1,0 +1,22 @@
+// Draws with parameters per row (sample_rows.hip).  Used by skd_sample and by the engine's sampling head.
+#pragma once
+#include "skd_kernels.h"
+
+namespace skd {
+
+constexpr int SAMPLE_ROWS_VOCAB = 1 << 18;  // masses are counted in units of 2^-45 of the largest, their sum in 63 bits
+
+struct SampleRows {
+  const float *logits;
+  long stride;
+  int rows, vocab;
+  // [rows]; null: 1, off, off, off
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  const float *u;           // [rows]
+  int32_t *tokens, *tokens2;  // tokens2: second destination, or null
+};
+void sample_rows(hipStream_t s, const SampleRows &a);
+
+}  // namespace skd

@@ -12,6 +12,7 @@
 
 #include "../../include/skd.h"
 #include "gave_up.h"
+#include "sample_rows.h"
 #include "skd_kernels.h"
 
 using namespace skd;
@@ -94,6 +95,8 @@ constexpr size_t kPinnedLogits = 1 << 20;  // bytes; larger logits are copied to
 struct Pinned {
   int32_t tok_in[128], tok_out[128];
   float u_in[128];
+  float sampling[3][128];  // temperature, top-p, min-p of each row
+  int32_t top_k[128];
   float logits[kPinnedLogits / sizeof(float)];
 };
 
@@ -127,6 +130,7 @@ struct skd_state {
   int32_t *argmax_dev = nullptr;   // [B]
   float *u_dev = nullptr;          // [B] uniform numbers of the sampling head
   SampleScratch sample{};          // its candidates
+  float *sampling_dev = nullptr;   // fp32 path with host buffers: [u | temperature | top-p | min-p | top-k][B]
   float *x = nullptr;              // residual stream fp32 [B_pad][d]
   float *x2 = nullptr;             // its second buffer (fuse_ln)
   bool fuse_ln = false;            // few rows: the row reducers are prologues of the projections behind them
@@ -862,7 +866,7 @@ static int create_impl(const skd_config *cfg, const skd_weights *w, void *hip_st
   // ---- workspaces
   const int Bp = st->B_pad;
   auto A = [&](auto **p, size_t n) { if (rc == SKD_OK) rc = dev_alloc(st, p, n); };
-  A(&st->tok_dev, B); A(&st->prompt_dev, (size_t)c.prompt_size * B); A(&st->start_dev, B); A(&st->order_dev, B); A(&st->argmax_dev, B); A(&st->u_dev, B);
+  A(&st->tok_dev, B); A(&st->prompt_dev, (size_t)c.prompt_size * B); A(&st->start_dev, B); A(&st->order_dev, B); A(&st->argmax_dev, B); A(&st->u_dev, B); A(&st->sampling_dev, 5 * (size_t)B);
   if (const size_t parts = (size_t)B * sample_chunks(V)) {
     A(&st->sample.z, (size_t)B * SAMPLE_CHUNK_CAND); A(&st->sample.idx, (size_t)B * SAMPLE_CHUNK_CAND);
     A(&st->sample.max_mass, parts * 3); A(&st->sample.count, parts);
@@ -1425,6 +1429,67 @@ extern "C" int skd_logits_sample(skd_state *st, const float *u, float temperatur
   HIPCHECK(hipGetLastError());
   st->have_argmax = true;  // skd_decode_step(.., NULL) continues from the sampled tokens
   if (c.io_on_device) return SKD_OK;  // the sampler has written tokens_out
+  return head_results(st, tokens_out, logits_out, false);
+}
+
+extern "C" int skd_logits_sample_rows(skd_state *st, const float *u, const skd_sampling *params, int32_t *tokens_out, float *logits_out) {
+  if (!st || !u) return SKD_ERR_NULL;
+  if (!st->have_hidden) return SKD_ERR_ORDER;
+  const skd_config &c = st->cfg;
+  const int B = c.batch, V = c.vocab;
+  if (V > SAMPLE_ROWS_VOCAB) return SKD_ERR_SHAPE;
+  const skd_sampling off{};
+  const skd_sampling &p = params ? *params : off;
+  if (!c.io_on_device)
+    for (int b = 0; b < B; ++b) {
+      if (!(u[b] >= 0.f) || u[b] >= 1.f) return SKD_ERR_RANGE;
+      if (p.temperature && (!(p.temperature[b] >= 0.f) || p.temperature[b] > 3.0e38f)) return SKD_ERR_RANGE;
+      if (p.top_k && p.top_k[b] < 0) return SKD_ERR_RANGE;
+      if (p.top_p && (!(p.top_p[b] > 0.f) || p.top_p[b] > 1.f)) return SKD_ERR_RANGE;
+      if (p.min_p && (!(p.min_p[b] >= 0.f) || p.min_p[b] > 1.f)) return SKD_ERR_RANGE;
+    }
+  SKDCHECK(intact(st));
+  hipStream_t s = st->stream;
+  SampleRows a{};
+  a.stride = V;
+  a.rows = B;
+  a.vocab = V;
+  a.u = u;
+  a.temperature = p.temperature;
+  a.top_k = p.top_k;
+  a.top_p = p.top_p;
+  a.min_p = p.min_p;
+  if (!c.io_on_device) {
+    const float *src[] = {u, p.temperature, p.top_p, p.min_p, (const float *)p.top_k};
+    const float *dst[5] = {};
+    float *pin[] = {st->pin ? st->pin->u_in : nullptr, st->pin ? st->pin->sampling[0] : nullptr, st->pin ? st->pin->sampling[1] : nullptr,
+                    st->pin ? st->pin->sampling[2] : nullptr, st->pin ? (float *)st->pin->top_k : nullptr};
+    for (int i = 0; i < 5; ++i) {
+      if (!src[i]) continue;
+      if (st->pin) {
+        memcpy(pin[i], src[i], B * sizeof(float));
+        dst[i] = pin[i];
+      } else {
+        HIPCHECK(hipMemcpyAsync(st->sampling_dev + (size_t)i * B, src[i], B * sizeof(float), hipMemcpyHostToDevice, s));
+        dst[i] = st->sampling_dev + (size_t)i * B;
+      }
+    }
+    if (!st->pin) HIPCHECK(hipStreamSynchronize(s));
+    a.u = dst[0];
+    a.temperature = dst[1];
+    a.top_p = dst[2];
+    a.min_p = dst[3];
+    a.top_k = (const int32_t *)dst[4];
+  }
+  float *lg = (logits_out && c.io_on_device) ? logits_out : st->logits_dev;
+  SKDCHECK(head_logits(st, lg, false, nullptr));
+  a.logits = lg;
+  a.tokens = st->argmax_dev;
+  a.tokens2 = c.io_on_device ? tokens_out : st->pin ? st->pin->tok_out : nullptr;
+  { ProfScope ps_(st, SKD_PROF_ARGMAX); sample_rows(s, a); }
+  HIPCHECK(hipGetLastError());
+  st->have_argmax = true;  // skd_decode_step(.., NULL) continues from the sampled tokens
+  if (c.io_on_device) return SKD_OK;
   return head_results(st, tokens_out, logits_out, false);
 }
 

@@ -5,6 +5,7 @@
 
 #include "../../include/skd.h"
 #include "kv_ops.h"
+#include "sample_rows.h"
 
 using namespace skd;
 
@@ -189,5 +190,39 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
     kv_append((hipStream_t)hip_stream, a.kv, a.tk, rows_of(k, k_stride), rows_of(v, v_stride));
   }
   kv_attend((hipStream_t)hip_stream, a);
+  return launched();
+}
+
+extern "C" int64_t skd_sample_workspace(int32_t rows, int32_t vocab) {
+  if (rows < 0) return SKD_ERR_RANGE;
+  if (vocab < 1 || vocab > SAMPLE_ROWS_VOCAB) return SKD_ERR_SHAPE;
+  return 0;
+}
+
+extern "C" int skd_sample(const float *logits, int64_t stride, int32_t rows, int32_t vocab, const skd_sampling *params, const float *u,
+                          int32_t *tokens_out, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  const int64_t need = skd_sample_workspace(rows, vocab);
+  if (need < 0) return (int)need;
+  if (stride < vocab) return SKD_ERR_SHAPE;
+  if (!rows) return SKD_OK;
+  if (!logits || !u || !tokens_out) return SKD_ERR_NULL;
+  if (((uintptr_t)logits | (uintptr_t)u | (uintptr_t)tokens_out) & 3) return SKD_ERR_SHAPE;
+  SampleRows a{};
+  a.logits = logits;
+  a.stride = (long)stride;
+  a.rows = rows;
+  a.vocab = vocab;
+  if (params) {
+    a.temperature = params->temperature;
+    a.top_k = params->top_k;
+    a.top_p = params->top_p;
+    a.min_p = params->min_p;
+  }
+  a.u = u;
+  a.tokens = tokens_out;
+  CHECK(check_memory({logits, u, tokens_out}));
+  for (const void *p : {(const void *)a.temperature, (const void *)a.top_k, (const void *)a.top_p, (const void *)a.min_p})
+    if (p) CHECK(check_memory({p}));
+  sample_rows((hipStream_t)hip_stream, a);
   return launched();
 }

@@ -25,7 +25,8 @@ KV_BF16, KV_FP8 = 0, 1
 EXPORTS = ["skd_schedule", "skd_active_layers", "skd_create", "skd_create_with_schedule", "skd_state_active_layers", "skd_prefill", "skd_decode_step",
            "skd_logits_argmax", "skd_logits_argmax_noalloc", "skd_logits_sample", "skd_rewind", "skd_profile_enable", "skd_profile_read", "skd_kv_len", "skd_kv_pages_reserved", "skd_kv_pages_dense", "skd_synchronize",
            "skd_debug_read_hidden", "skd_debug_kv_load", "skd_debug_kv_read", "skd_destroy", "skd_strerror",
-           "skd_last_hip_error", "skd_kv_page_bytes", "skd_kv_append", "skd_kv_read", "skd_kv_attend", "skd_kv_attend_workspace"]
+           "skd_last_hip_error", "skd_kv_page_bytes", "skd_kv_append", "skd_kv_read", "skd_kv_attend", "skd_kv_attend_workspace",
+           "skd_logits_sample_rows", "skd_sample", "skd_sample_workspace"]
 
 
 class Config(C.Structure):
@@ -33,6 +34,10 @@ class Config(C.Structure):
         "L", "d_model", "n_heads", "ffn", "vocab", "max_pos",
         "batch", "prompt_size", "sequence_length", "n_min", "n_max", "warmup",
         "page_tokens", "dtype", "io_on_device")]
+
+
+class Sampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
 
 
 _PP = C.POINTER(C.c_void_p)
@@ -93,6 +98,9 @@ def lib() -> C.CDLL:
         l.skd_kv_read.argtypes = [P, P, I32, P, I64, P, I64, P]
         l.skd_kv_attend.argtypes = [P, P, I32, C.c_float, P, I64, P, I64, P, I64, P, I64, P, I64, P]
         l.skd_kv_attend_workspace.argtypes, l.skd_kv_attend_workspace.restype = [P, P, I32], I64
+        l.skd_logits_sample_rows.argtypes = [P] * 5
+        l.skd_sample.argtypes = [P, I64, I32, I32, P, P, P, P, I64, P]
+        l.skd_sample_workspace.argtypes, l.skd_sample_workspace.restype = [I32, I32], I64
         _lib = l
     return _lib
 
@@ -245,6 +253,32 @@ class Decoder:
         _check(self._lib.skd_logits_sample(self._h, _ptr_of(u), temperature, top_p, _ptr_of(tokens_out),
                                            _ptr_of(logits_out)), "skd_logits_sample")
 
+    def logits_sample_rows_rc(self, u, temperature=None, top_k=None, top_p=None, min_p=None, want_logits: bool = True):
+        """Host-I/O form of skd_logits_sample_rows, parameters [B] or None: returns (rc, tokens[B], logits[B,V] or None)."""
+        assert not self.cfg.io_on_device
+        arrays = [None if a is None else np.ascontiguousarray(a, dtype=t) for a, t in
+                  ((temperature, np.float32), (top_k, np.int32), (top_p, np.float32), (min_p, np.float32))]
+        uu = np.ascontiguousarray(u, dtype=np.float32)
+        for a in arrays + [uu]:
+            if a is not None and a.shape != (self.cfg.batch,):
+                raise ValueError("parameters have one entry per row")
+        tok = np.zeros(self.cfg.batch, dtype=np.int32)
+        lg = np.zeros((self.cfg.batch, self.cfg.vocab), dtype=np.float32) if want_logits else None
+        rc = self._lib.skd_logits_sample_rows(self._h, uu.ctypes.data, C.byref(Sampling(*[_ptr_of(a) for a in arrays])), tok.ctypes.data,
+                                              _ptr_of(lg))
+        return rc, tok, lg
+
+    def logits_sample_rows(self, u, temperature=None, top_k=None, top_p=None, min_p=None, want_logits: bool = True):
+        rc, tok, lg = self.logits_sample_rows_rc(u, temperature, top_k, top_p, min_p, want_logits)
+        _check(rc, "skd_logits_sample_rows")
+        return tok, lg
+
+    def logits_sample_rows_device(self, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens_out=None, logits_out=None):
+        """Device-I/O form: device pointers / torch tensors (top_k int32, the others float32); asynchronous."""
+        p = Sampling(*[_ptr_of(a) for a in (temperature, top_k, top_p, min_p)])
+        _check(self._lib.skd_logits_sample_rows(self._h, _ptr_of(u), C.byref(p), _ptr_of(tokens_out), _ptr_of(logits_out)),
+               "skd_logits_sample_rows")
+
     def logits_argmax_device(self, tokens_out=None, logits_out=None):
         """Device-I/O form: pointers / torch tensors on the device; asynchronous."""
         _check(self._lib.skd_logits_argmax(self._h, _ptr_of(tokens_out), _ptr_of(logits_out)), "skd_logits_argmax")
@@ -392,3 +426,23 @@ class KvCache:
 def _expect(t, dtype: str, dims: int):
     if str(t.dtype) != "torch." + dtype or t.dim() != dims or not t.is_contiguous():
         raise ValueError(f"expected a contiguous {dtype} tensor of {dims} dimensions")
+
+
+def sample_workspace(rows: int, vocab: int) -> int:
+    return _check(lib().skd_sample_workspace(rows, vocab), "skd_sample_workspace")
+
+
+def sample(logits, u, tokens_out, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, stream: int = 0):
+    """skd_sample on device tensors: logits [rows][vocab] float32 with dense rows, u and the parameters [rows] (None: off)."""
+    if str(logits.dtype) != "torch.float32" or logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError("expected float32 logits with dense rows")
+    rows, vocab = logits.shape
+    for t, dtype in ((u, "float32"), (tokens_out, "int32"), (temperature, "float32"), (top_k, "int32"), (top_p, "float32"), (min_p, "float32")):
+        if t is not None:
+            _expect(t, dtype, 1)
+            if len(t) != rows:
+                raise ValueError("one entry per row")
+    p = Sampling(*[_ptr_of(a) for a in (temperature, top_k, top_p, min_p)])
+    ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().skd_sample(logits.data_ptr(), max(logits.stride(0), vocab) if rows < 2 else logits.stride(0), rows, vocab, C.byref(p), u.data_ptr(), tokens_out.data_ptr(), *ws,
+                            stream), "skd_sample")

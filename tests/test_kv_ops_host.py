@@ -1,4 +1,4 @@
-"""Refusals of the cache's calls, on the CPU: every one is answered before any device work."""
+"""Refusals of the cache's and the draw's calls, on the CPU: every one is answered before any device work."""
 import ctypes as C
 import os
 
@@ -86,3 +86,17 @@ def test_pointers_and_ranges():
     need = lib.skd_kv_attend_workspace(C.byref(long["c"]), C.byref(long["ch"]), 8)
     assert need > 0 and need % 4 == 0
     assert attend(**long) == skd.ERR_NULL and attend(**long, ws=P + 4, n=need) == skd.ERR_SHAPE and attend(**long, ws=P, n=need - 1) == skd.ERR_NOMEM
+
+
+def test_draws():
+    lib = skd.lib()
+
+    def rc(z=P, stride=1000, rows=3, vocab=1000, u=P, out=P):
+        return lib.skd_sample(z, stride, rows, vocab, None, u, out, None, 0, None)
+
+    assert rc(z=None) == rc(u=None) == rc(out=None) == skd.ERR_NULL
+    assert rc(vocab=0) == rc(vocab=262145, stride=262145) == rc(stride=999) == rc(z=P + 2) == rc(out=P + 1) == skd.ERR_SHAPE
+    assert rc(rows=-1) == skd.ERR_RANGE and rc(rows=0) == skd.OK
+    assert lib.skd_sample_workspace(-1, 10) == skd.ERR_RANGE and lib.skd_sample_workspace(1, 0) == lib.skd_sample_workspace(1, 1 << 19) == skd.ERR_SHAPE
+    assert lib.skd_sample_workspace(128, 262144) >= 0
+    assert lib.skd_logits_sample_rows(None, P, None, None, None) == skd.ERR_NULL
