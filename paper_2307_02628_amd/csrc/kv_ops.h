@@ -48,7 +48,7 @@ struct KvAttend {
   KvTokens tk;
   int heads, group;         // query heads, of them to a kv head
   float c;                  // scores -> log2 of the weights
-  KvRows q, o, k, v;        // bf16; k.p null: the cache holds the new tokens
+  KvRows q, o, k, v;        // bf16; k.p null: the cache holds the new tokens, else they are filed first
   const int32_t *order;     // rows in the order of their dispatch, or null
   int splits;               // of the keys of a query tile
   float *part;              // splits > 1: [splits][tokens * heads][dh + 2]: numerators, maximum, denominator

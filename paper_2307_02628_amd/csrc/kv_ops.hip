@@ -222,196 +222,297 @@ __global__ __launch_bounds__(256) void k_kv_read(KvView kv, KvTokens tk, KvRows 
 
 // ------------------------------------------------------------------ attention
 // A query tile is 16 of the R = new * group queries of a row and kv head, in the order (token, head of the group): the 16
-// columns of the matrix instructions.  A workgroup is NW waves on one tile and one share of its keys; a wave takes every NW-th
-// 32-key block, straight from the page into the operand registers, with a softmax of its own (as k_attention_rows: units of
-// log2, a reference that is raised only by more than 8, denominators from the matrix cores); the waves' states are joined in
-// LDS, the shares of several workgroups by k_kv_merge.
+// columns of the matrix instructions.  The softmax works in units of log2 against a reference that is raised only by more
+// than 8 (weights up to 2^8), denominators come from the matrix cores (a row of ones) and are sums of the rounded weights.
 //
-// Query i of a row sees positions up to past + i.  Blocks that reach beyond what the tile's first query sees are masked:
-// scores by selection, and since 0 * infinity is not 0, values too: beyond the row's last position they are cleared (a page
-// may hold anything there), and an infinity or NaN that only later queries see is kept out of the products and put into the
-// sums of those that see it.  8-bit values are finite, what is not is in their scales, which are selected with the weights.
-template <int DH, bool FP8>
-struct KvBlock {
-  static constexpr int QC = DH / 32, VM = DH / 16;
-  uint32x4 k[FP8 ? QC : 2 * QC], v[FP8 ? VM / 2 : VM];
-  uint32_t ke[2], ve[2];  // exponents: of keys 16 tl + (lane & 15) (K), of keys 16 tl + 4 (lane >> 4) .. + 3 (V)
-};
-// bf16x8 of two words of codes, times a power of two
-__device__ inline bf16x8 widen(uint32_t a, uint32_t b, float scale) {
+// Query i of a row sees positions up to past + i.  Blocks that reach beyond what a tile's first query sees are masked: scores
+// by selection, and since 0 * infinity is not 0, values too: beyond the row's last position they are cleared (a page may hold
+// anything there), and an infinity or NaN that only later queries see is kept out of the products and put into the sums of
+// those that see it.  8-bit values are finite, what is not is in their scales, which are selected with the weights.
+// The powers of two of 8-bit keys are an operand of the conversion to bf16, those of values multiply the weights: both exact.
+
+// bf16x8 of two words of codes, times the power of two whose exponent byte is `e` (255: NaN)
+__device__ inline bf16x8 widen(uint32_t a, uint32_t b, uint32_t e) {
+  const float scale = __uint_as_float(e << 23);
   const bf16x2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true)};
   return bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
 }
+// fp32 of an exponent byte; 2^-127 as 0: a weight times 2^-127 of 448 at most is no value that fp32 sums would notice
+__device__ inline float kv8_factor(uint32_t word, int i) {
+  const uint32_t e = word >> (8 * i) & 255u;
+  return __uint_as_float(e == 255 ? 0x7fc00000u : e << 23);
+}
+__device__ inline bf16x8 pack8(const float (&p)[8]) {
+  return __builtin_bit_cast(bf16x8, (uint32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])}));
+}
+__device__ inline bf16x8 all_ones() {
+  bf16x8 x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (__bf16)1.0f;
+  return x;
+}
+// position (of a block) of element j of a lane's eight
+__device__ inline int block_pos(int j, int grp) { return 16 * (j >> 2) + 4 * grp + (j & 3); }
 
-template <int DH, bool FP8, int NW>
-__global__ __launch_bounds__(NW * 64, 4) void k_kv_attend(KvAttend a, int tiles) {
-  constexpr int QC = DH / 32, VM = DH / 16;
+// SHARES: a lane adds up the weights of its own positions (one_sum joins them) instead of the matrix cores all of them, which
+// takes 7 registers more: at 4 waves a SIMD they are not there.
+template <int DH, bool SHARES>
+struct QueryTile {
+  floatx4 O[DH / 16], L;  // O[m][i]: element 16 m + 4 (lane / 16) + i of the lane's query (lane % 16)
+  float m_ref;
+  __device__ void clear() {
+    m_ref = -3.0e38f;  // below every score: no weight has been taken
+    L = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < DH / 16; ++m) O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  // The weights of a block from its scores S[tl][i] (position 16 tl + 4 grp + i), rounded to bf16 for the products (by 2^-8 of
+  // a weight at most; the denominator adds the rounded ones).  masked: positions from `limit` of the block on have none.
+  template <bool FP8>
+  __device__ bf16x8 weights(bool masked, floatx4 (&S)[2], float c, int limit, int grp, const float (&vs)[8]) {
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (block_pos(j, 0) >= limit - 4 * grp) S[j >> 2][j & 3] = -INFINITY;
+    }
+    float bm = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3]))) * c;
+    if (__any(bm > m_ref + 8.0f)) {
+      bm = fmaxf(bm, __shfl_xor(bm, 16));  // lanes 16 and 32 apart hold the same query
+      bm = fmaxf(bm, __shfl_xor(bm, 32));
+      const float m_new = fmaxf(m_ref, bm), alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+      m_ref = m_new;
+      if constexpr (SHARES) L[0] *= alpha;
+      else L *= alpha;
+#pragma unroll
+      for (int m = 0; m < DH / 16; ++m) O[m] *= alpha;
+    }
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], c, -m_ref));
+    bf16x8 pv = pack8(p);
+    if constexpr (SHARES) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) L[0] += (float)pv[j];
+    } else {
+      L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones(), pv, L, 0, 0, 0);
+    }
+    if constexpr (FP8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] *= vs[j];
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (block_pos(j, 0) >= limit - 4 * grp) p[j] = 0.f;  // (a power of two there may be NaN)
+      }
+      pv = pack8(p);
+    }
+    return pv;
+  }
+  __device__ void one_sum() {
+    if constexpr (SHARES) {
+      L[0] += __shfl_xor(L[0], 16);
+      L[0] += __shfl_xor(L[0], 32);
+    }
+  }
+};
+// 1 at positions below `limit`
+__device__ inline bf16x8 visible(int limit, int grp) {
+  bf16x8 v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (__bf16)(block_pos(j, grp) < limit ? 1.0f : 0.0f);
+  return v;
+}
+// masks of a lane's eight bf16 values: positions below `valid`
+struct Keep {
+  uint32_t w[4];
+  __device__ Keep(int valid, int grp) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (block_pos(2 * i, grp) < valid ? 0xffffu : 0u) | (block_pos(2 * i + 1, grp) < valid ? 0xffff0000u : 0u);
+  }
+  __device__ void bf16(uint32x4 &v) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] &= w[i];
+  }
+  __device__ uint32_t codes(int half) const { return __builtin_amdgcn_perm(w[2 * half + 1], w[2 * half], 0x06040200); }
+};
+// whether one of a lane's bf16 values is an infinity or NaN
+__device__ inline bool not_finite(const uint32x4 &v) {
+  uint32_t odd = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  return odd != 0;
+}
+__device__ inline void drop_odd(uint32x4 &v) {  // infinities and NaNs to 0
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t odd = ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    v[i] &= ~((odd >> 15) * 0xffffu);
+  }
+}
+// Adds to the sums of a tile what the infinities and NaNs of a value fragment are for the queries that see them.
+__device__ inline void add_odd(floatx4 &O, const uint32x4 &v, bf16x8 vis) {
+  uint32x4 up, down;  // 1 where it is +infinity or NaN, -infinity or NaN
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t u = 0, d = 0;
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+      const uint32_t x = v[i] >> s & 0xffffu;
+      if ((x & 0x7f80u) == 0x7f80u) {
+        if (x != 0xff80u) u |= 0x3f80u << s;
+        if (x != 0x7f80u) d |= 0x3f80u << s;
+      }
+    }
+    up[i] = u;
+    down[i] = d;
+  }
+  const floatx4 z = floatx4{0.f, 0.f, 0.f, 0.f};
+  const floatx4 u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, up), vis, z, 0, 0, 0);
+  const floatx4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down), vis, z, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (u[i] > 0.f) O[i] += INFINITY;
+    if (d[i] > 0.f) O[i] -= INFINITY;
+  }
+}
+
+// What a workgroup computes: NQ queries from q0 on of a row and kv head, on one share of their keys.
+struct Share {
+  RowTokens t;
+  int r, h, R, q0;
+  int held;        // positions that the cache holds
+  int lo, hi;      // blocks
+  bool any;
+  template <int NQ>
+  __device__ static Share of(const KvAttend &a, int tiles, bool files) {
+    Share s;
+    const int H = a.kv.g.H, ri = blockIdx.x / tiles / H;
+    s.h = blockIdx.x / tiles % H;
+    s.r = a.order ? a.order[ri] : ri;
+    s.t = row_tokens(a.tk, s.r);
+    s.R = s.t.n * a.group;
+    s.q0 = (int)(tiles - 1 - blockIdx.x % tiles) * NQ;  // the longest first
+    s.any = s.q0 < s.R;
+    s.held = s.t.past + (files ? 0 : s.t.n);
+    const int nblk = (min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held) + 31) >> 5, per = (nblk + a.splits - 1) / a.splits;
+    s.lo = (int)blockIdx.y * per;
+    s.hi = min(s.lo + per, nblk);
+    return s;
+  }
+  __device__ int seen(const KvAttend &a, int q) const { return t.past + q / a.group + 1; }  // positions that query q sees
+  __device__ long token(const KvAttend &a, int q) const { return t.at + (long)(q / a.group) * a.tk.step; }
+  __device__ int head(const KvAttend &a, int q) const { return h * a.group + q % a.group; }
+};
+template <int DH>
+__device__ inline float *part_of(const KvAttend &a, int split, long token, int head) {
+  return a.part + (((long)split * a.tk.tokens + token) * a.heads + head) * (DH + 2);
+}
+template <int DH>
+__device__ inline void load_queries(const KvAttend &a, const Share &s, int q, int grp, bf16x8 (&qf)[DH / 32]) {
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) {
+    qf[c] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    if (q < s.R) qf[c] = *(const bf16x8 *)((const bf16_t *)a.q.p + row_index(a.q, s.token(a, q), s.head(a, q) * DH + 32 * c + 8 * grp));
+  }
+}
+
+// Few queries (one or two tiles): a workgroup is NW waves on NT tiles, and a wave takes every NW-th 32-key block, straight from
+// the page into the operand registers, with a softmax of its own; the waves' states are joined in LDS, the shares of several
+// workgroups by k_kv_merge.  Bound by the bytes of the pages.
+template <int DH, bool FP8>
+struct KvBlock {
+  static constexpr int QC = DH / 32, VM = DH / 16;
+  uint32x4 k[FP8 ? QC : 2 * QC], v[FP8 ? VM / 2 : VM];
+  uint32_t ke[2], ve[2];  // exponents: of key 16 tl + (lane & 15) (K), of keys 16 tl + 4 (lane >> 4) .. + 3 (V)
+};
+template <int DH, bool FP8, int NT, int NW>
+__global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int tiles) {
+  constexpr int QC = DH / 32, VM = DH / 16, NQ = 16 * NT;
   extern __shared__ float lds[];  // [NW][cols][DH + 2]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
-  const int H = a.kv.g.H, qt = blockIdx.x % tiles, h = blockIdx.x / tiles % H;
-  const int ri = blockIdx.x / tiles / H, r = a.order ? a.order[ri] : ri;
-  const RowTokens t = row_tokens(a.tk, r);
-  const int R = t.n * a.group, q0 = qt * 16;
-  if (q0 >= R) return;
-  const bool files = a.k.p != nullptr;               // (t.n is 1: the token is not in the cache yet)
-  const int held = t.past + (files ? 0 : t.n);       // positions that the cache holds
-  const int seen0 = t.past + q0 / a.group + 1;       // positions that the first query of the tile sees
-  const int seen1 = min(t.past + min(q0 + 15, R - 1) / a.group + 1, held);  // that the last one sees
-  const int mine = q0 + col < R ? t.past + (q0 + col) / a.group + 1 : 0;
-  const int nblk = (seen1 + 31) >> 5, per = (nblk + a.splits - 1) / a.splits;
-  const int lo = (int)blockIdx.y * per, hi = min(lo + per, nblk);
-  const int qi = (q0 + col) / a.group, qh = h * a.group + (q0 + col) % a.group;
-  const long q_token = t.at + (long)qi * a.tk.step;
-
-  bf16x8 qf[QC];
+  const bool files = NT == 1 && a.k.p != nullptr;  // (t.n is 1: the token is not in the cache yet)
+  const Share s = Share::of<NQ>(a, tiles, files);
+  if (!s.any) return;
+  const int q0 = s.q0, R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
+  bf16x8 qf[NT][QC];
+  int limit[NT];                  // positions of the cache that the lane's query sees
+  QueryTile<DH, NT == 1> tile[NT];
 #pragma unroll
-  for (int c = 0; c < QC; ++c) {
-    qf[c] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-    if (q0 + col < R) qf[c] = *(const bf16x8 *)((const bf16_t *)a.q.p + row_index(a.q, q_token, qh * DH + 32 * c + 8 * grp));
+  for (int t = 0; t < NT; ++t) {
+    const int q = q0 + 16 * t + col;
+    load_queries<DH>(a, s, q, grp, qf[t]);
+    limit[t] = q < R ? min(s.seen(a, q), s.held) : 0;
+    tile[t].clear();
   }
-  bf16x8 ones;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-  floatx4 O[VM], L = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int m = 0; m < VM; ++m) O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-  float m_ref = -INFINITY;
-
-  auto load = [&](int blk, int page, KvBlock<DH, FP8> &b) {
+  typedef KvBlock<DH, FP8> Block;
+  auto load = [&](int blk, int page, Block &b) {
     const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
-    const int bpp = a.kv.g.page_tokens >> 5, ib = blk % bpp;
+    const long at = (long)h * bpp + blk % bpp;
+    const uint32x4 *src = (const uint32x4 *)(pg + at * ((FP8 ? 64 : 128) * DH)) + lane;
+    constexpr int KF = FP8 ? QC : 2 * QC, VF = FP8 ? VM / 2 : VM;
+#pragma unroll
+    for (int i = 0; i < KF; ++i) b.k[i] = __builtin_nontemporal_load(&src[i * 64]);
+#pragma unroll
+    for (int i = 0; i < VF; ++i) b.v[i] = __builtin_nontemporal_load(&src[(KF + i) * 64]);
     if constexpr (FP8) {
-      const uint32x4 *src = (const uint32x4 *)(pg + ((long)h * bpp + ib) * (64 * DH)) + lane;
-#pragma unroll
-      for (int i = 0; i < QC; ++i) b.k[i] = __builtin_nontemporal_load(&src[i * 64]);
-#pragma unroll
-      for (int i = 0; i < VM / 2; ++i) b.v[i] = __builtin_nontemporal_load(&src[2 * DH + i * 64]);
-      const unsigned char *ex = pg + (long)H * bpp * (64 * DH) + ((long)h * bpp + ib) * 64;
+      const unsigned char *ex = pg + (long)H * bpp * (64 * DH) + at * 64;
 #pragma unroll
       for (int tl = 0; tl < 2; ++tl) {
-        b.ke[tl] = ((const uint32_t *)ex)[4 * tl + grp];
+        b.ke[tl] = ex[16 * tl + col];
         b.ve[tl] = ((const uint32_t *)ex)[8 + 4 * tl + grp];
       }
-    } else {
-      const uint32x4 *src = (const uint32x4 *)(pg + ((long)h * bpp + ib) * (128 * DH)) + lane;
-#pragma unroll
-      for (int i = 0; i < 2 * QC; ++i) b.k[i] = __builtin_nontemporal_load(&src[i * 64]);
-#pragma unroll
-      for (int i = 0; i < VM; ++i) b.v[i] = __builtin_nontemporal_load(&src[4 * DH + i * 64]);
     }
   };
-  // limit: positions of the block from `base` on that the lane's query sees; clear: those that may hold anything
-  auto use = [&](int base, KvBlock<DH, FP8> &b, bool masked, int limit, int valid) {
-    floatx4 S[2];
+  // base: first position of the block; valid: positions that it holds
+  bool odd_seen = false;
+  auto use = [&](auto masked_, int base, Block &b, const int (&lim)[NT], int valid) {
+    constexpr bool masked = decltype(masked_)::value;
+    floatx4 S[NT][2];
 #pragma unroll
     for (int tl = 0; tl < 2; ++tl) {
-      S[tl] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[t][tl] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < QC; ++c) {
         bf16x8 kf;
         if constexpr (FP8) {
           const uint32x4 w = b.k[tl * (QC / 2) + c / 2];
-          kf = widen(w[c % 2 * 2], w[c % 2 * 2 + 1], 1.0f);
+          kf = widen(w[c % 2 * 2], w[c % 2 * 2 + 1], b.ke[tl]);
         } else {
           kf = __builtin_bit_cast(bf16x8, b.k[tl * QC + c]);
         }
-        S[tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c], S[tl], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][c], S[t][tl], 0, 0, 0);
       }
     }
-    // S[tl][i]: position base + 16 tl + 4 grp + i
     float vs[8];
     if constexpr (FP8) {
 #pragma unroll
-      for (int tl = 0; tl < 2; ++tl)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          S[tl][i] *= kv8_scale(b.ke[tl] >> (8 * i) & 255u);
-          vs[tl * 4 + i] = kv8_scale(b.ve[tl] >> (8 * i) & 255u);
-        }
+      for (int j = 0; j < 8; ++j) vs[j] = kv8_factor(b.ve[j >> 2], j & 3);
     }
-    bool ok[8];
+    bf16x8 pv[NT];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      ok[j] = !masked || base + 16 * (j >> 2) + 4 * grp + (j & 3) < limit;
-      if (!ok[j]) S[j >> 2][j & 3] = -INFINITY;
-    }
-    float bm = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3]))) * a.c;
-    if (__any(bm > m_ref + 8.0f)) {
-      bm = fmaxf(bm, __shfl_xor(bm, 16));  // lanes 16 and 32 apart hold the same query
-      bm = fmaxf(bm, __shfl_xor(bm, 32));
-      const float m_new = fmaxf(m_ref, bm);
-      const float alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
-      m_ref = m_new;
-      L *= alpha;
-#pragma unroll
-      for (int m = 0; m < VM; ++m) O[m] *= alpha;
-    }
-    float p[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], a.c, -m_ref));
-      if (!ok[j]) p[j] = 0.f;
-    }
-    auto pack = [&]() { return __builtin_bit_cast(bf16x8, (uint32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])})); };
-    // the weights are rounded to bf16 for the products (2^-9 of a weight on average); so are those that the denominator adds
-    bf16x8 pv = pack();
-    L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pv, L, 0, 0, 0);
-    if constexpr (FP8) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = ok[j] ? p[j] * vs[j] : 0.f;
-      pv = pack();
-    }
-    uint32_t keep[4];  // bf16: values of positions that the row has
+    for (int t = 0; t < NT; ++t) pv[t] = tile[t].template weights<FP8>(masked, S[t], a.c, lim[t] - base, grp, vs);
     if (masked) {
+      const Keep keep(valid - base, grp);
+      bool odd = false;
+      if constexpr (FP8) {  // (codes of positions that the row does not have may be NaN)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int pos = base + 16 * (i >> 1) + 4 * grp + 2 * (i & 1);
-        keep[i] = (pos < valid ? 0xffffu : 0u) | (pos + 1 < valid ? 0xffff0000u : 0u);
-      }
-    }
-    if constexpr (!FP8) {
-      if (masked) {
-        uint32_t odd = 0;
+        for (int m = 0; m < VM / 2; ++m) {
+          b.v[m] &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
+        }
+      } else {
 #pragma unroll
-        for (int m = 0; m < VM; ++m)
+        for (int m = 0; m < VM; ++m) {
+          keep.bf16(b.v[m]);
+          odd |= not_finite(b.v[m]);
+        }
+        if (__any(odd)) {
+          odd_seen = true;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            b.v[m][i] &= keep[i];
-            odd |= ((b.v[m][i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponents that are all ones
-          }
-        if (__any(odd != 0)) {
-          bf16x8 vis;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) vis[j] = (__bf16)(ok[j] ? 1.0f : 0.0f);
-#pragma unroll
-          for (int m = 0; m < VM; ++m) {
-            uint32x4 up, down;  // 1 where the value is +infinity or NaN, -infinity or NaN
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t u = 0, dn = 0, w = b.v[m][i];
-#pragma unroll
-              for (int s = 0; s < 32; s += 16) {
-                const uint32_t x = w >> s & 0xffffu;
-                if ((x & 0x7f80u) == 0x7f80u) {
-                  if (x != 0xff80u) u |= 0x3f80u << s;
-                  if (x != 0x7f80u) dn |= 0x3f80u << s;
-                  w &= ~(0xffffu << s);
-                }
-              }
-              up[i] = u;
-              down[i] = dn;
-              b.v[m][i] = w;
-            }
-            const floatx4 z = floatx4{0.f, 0.f, 0.f, 0.f};
-            const floatx4 nu = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, up), vis, z, 0, 0, 0);
-            const floatx4 nd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down), vis, z, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (nu[i] > 0.f) O[m][i] += INFINITY;
-              if (nd[i] > 0.f) O[m][i] -= INFINITY;
-            }
-          }
+          for (int m = 0; m < VM; ++m) drop_odd(b.v[m]);
         }
       }
     }
@@ -419,149 +520,401 @@ __global__ __launch_bounds__(NW * 64, 4) void k_kv_attend(KvAttend a, int tiles)
     for (int m = 0; m < VM; ++m) {
       bf16x8 vf;
       if constexpr (FP8) {
-        uint32_t w0 = b.v[m / 2][m % 2 * 2], w1 = b.v[m / 2][m % 2 * 2 + 1];
-        if (masked) {  // (codes of positions that the row does not have may be NaN)
-          w0 &= __builtin_amdgcn_perm(keep[1], keep[0], 0x06040200);
-          w1 &= __builtin_amdgcn_perm(keep[3], keep[2], 0x06040200);
-        }
-        vf = widen(w0, w1, 1.0f);
+        vf = widen(b.v[m / 2][m % 2 * 2], b.v[m / 2][m % 2 * 2 + 1], 127);
       } else {
         vf = __builtin_bit_cast(bf16x8, b.v[m]);
       }
-      O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv, O[m], 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv[t], tile[t].O[m], 0, 0, 0);
     }
   };
-  for (int blk = lo + wave; blk < hi; blk += NW) {
-    const int page = page_of(a.kv, r, blk);
-    if (page < 0) continue;
-    KvBlock<DH, FP8> b;
-    load(blk, page, b);
-    const bool masked = blk * 32 + 32 > seen0 || blk * 32 + 32 > held;
-    use(blk * 32, b, masked, min(mine, held), held);
+  const int whole = min(s.seen(a, q0), s.held) >> 5;  // blocks before it are seen whole by every query
+  // (the number of the next page is asked for ahead of the use of a block)
+  int blk = s.lo + wave, page = blk < s.hi ? page_of(a.kv, s.r, blk) : -1;
+  for (; blk < min(whole, s.hi); blk += NW) {
+    Block b;
+    if (page >= 0) load(blk, page, b);
+    const int next = blk + NW < s.hi ? page_of(a.kv, s.r, blk + NW) : -1;
+    if (page >= 0) use(std::false_type(), 0, b, limit, 0);
+    page = next;
   }
-  if (files && blockIdx.y == gridDim.y - 1 && wave == NW - 1) {
-    // The one new token is a block of its own, made from its rows: key 0 of it; and it is filed, by the first tile.  Whoever
-    // reads its place meanwhile, in the block around it, discards what is there.
-    KvBlock<DH, FP8> b;
-    const bool stores = qt == 0;
-    const int page = stores ? page_of(a.kv, r, t.past >> 5) : -1;
-    unsigned char *pg = page < 0 ? nullptr : a.kv.pool + (long)page * a.kv.page_bytes;
-    const int slot = t.past % a.kv.g.page_tokens;
-    uint32x4 kx[QC];
-    bf16_t vx[VM];
+  for (; blk < s.hi; blk += NW) {
+    Block b;
+    if (page >= 0) load(blk, page, b);
+    const int next = blk + NW < s.hi ? page_of(a.kv, s.r, blk + NW) : -1;
+    if (page >= 0) use(std::true_type(), blk * 32, b, limit, s.held);
+    page = next;
+  }
+  if constexpr (!FP8) {
+    // infinities and NaNs among the values of masked blocks: seldom
+    if (odd_seen)
+      for (int at = max(s.lo, whole); at < s.hi; ++at) {
+        const int page = (at - s.lo) % NW == wave ? page_of(a.kv, s.r, at) : -1;
+        if (page < 0) continue;
+        const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)h * bpp + at % bpp) * (128 * DH)) + 4 * DH + lane;
+        const Keep keep(s.held - at * 32, grp);
 #pragma unroll
-    for (int c = 0; c < QC; ++c) {
-      kx[c] = uint32x4{0, 0, 0, 0};
-      if (col == 0) kx[c] = *(const uint32x4 *)((const bf16_t *)a.k.p + row_index(a.k, t.at, h * DH + 32 * c + 8 * grp));
-    }
+        for (int m = 0; m < VM; ++m) {
+          uint32x4 v = src[m * 64];
+          keep.bf16(v);
 #pragma unroll
-    for (int m = 0; m < VM; ++m) vx[m] = grp == 0 ? ((const bf16_t *)a.v.p)[row_index(a.v, t.at, h * DH + 16 * m + col)] : 0;
-    if constexpr (FP8) {
-      uint32_t km = 0, vm = 0;
-#pragma unroll
-      for (int c = 0; c < QC; ++c) km = max(km, max_bits(kx[c]));
-#pragma unroll
-      for (int m = 0; m < VM; ++m) vm = max(vm, (uint32_t)(vx[m] & 0x7fff) << 16);
-      const uint32_t ke = kv8_exponent(max_over<64>(km)), ve = kv8_exponent(max_over<64>(vm));
+          for (int t = 0; t < NT; ++t) add_odd(tile[t].O[m], v, visible(limit[t] - at * 32, grp));
+        }
+      }
+  }
+  if constexpr (NT == 1) {
+    tile[0].one_sum();
+    // The one new token joins the last wave's state: its key as key 0 of a tile, its value by the vector units, four elements of
+    // every 16 in a lane.  The first tile files it.  Whoever reads its place meanwhile, in the block around it, discards what
+    // is there.
+    if (files && blockIdx.y == gridDim.y - 1 && wave == NW - 1) {
+      const int page = q0 == 0 ? page_of(a.kv, s.r, s.held >> 5) : -1, slot = s.held % a.kv.g.page_tokens;
+      unsigned char *pg = page < 0 ? nullptr : a.kv.pool + (long)page * a.kv.page_bytes;
+      uint32x4 kx[QC];
+      uint2 vx[VM];
 #pragma unroll
       for (int c = 0; c < QC; ++c) {
-        const uint2 w = kv8_codes(kx[c], ke);
-        if (c % 2 == 0) b.k[c / 2] = uint32x4{0, 0, 0, 0};
-        b.k[c / 2][c % 2 * 2] = w.x;
-        b.k[c / 2][c % 2 * 2 + 1] = w.y;
-        b.k[QC / 2 + c / 2] = uint32x4{0, 0, 0, 0};
-        if (pg && col == 0) *(uint2 *)(pg + kv8_k_off(h, slot, 32 * c + 8 * grp, a.kv.g)) = w;
+        kx[c] = uint32x4{0, 0, 0, 0};
+        if (col == 0) kx[c] = *(const uint32x4 *)((const bf16_t *)a.k.p + row_index(a.k, s.t.at, h * DH + 32 * c + 8 * grp));
       }
 #pragma unroll
-      for (int m = 0; m < VM; ++m) {
-        const uint32_t w = ve == 255 ? 0u : (kv8_pack(bf2f(vx[m]), 0.f, 0.f, 0.f, ve) & 255u);
-        b.v[m / 2][m % 2 * 2] = w;
-        b.v[m / 2][m % 2 * 2 + 1] = 0;
-        if (pg && grp == 0) pg[kv8_v_off(h, slot, 16 * m + col, a.kv.g)] = (unsigned char)w;
+      for (int m = 0; m < VM; ++m) vx[m] = *(const uint2 *)((const bf16_t *)a.v.p + row_index(a.v, s.t.at, h * DH + 16 * m + 4 * grp));
+      uint32_t ke = 0, ve = 0;
+      if constexpr (FP8) {
+        uint32_t km = 0, vm = 0;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) km = max(km, max_bits(kx[c]));
+#pragma unroll
+        for (int m = 0; m < VM; ++m) vm = max(vm, max_bits(uint32x4{vx[m].x, vx[m].y, 0, 0}));
+        ke = kv8_exponent(max_over<64>(km));
+        ve = kv8_exponent(max_over<64>(vm));
+        if (pg && lane < 2) pg[kv8_exp_off(h, slot, lane, a.kv.g)] = (unsigned char)(lane ? ve : ke);
       }
-      b.ke[0] = ke;
-      b.ve[0] = ve;
-      b.ke[1] = b.ve[1] = 0;
-      if (pg && lane < 2) pg[kv8_exp_off(h, slot, lane, a.kv.g)] = (unsigned char)(lane ? ve : ke);
-    } else {
+      floatx4 S = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < QC; ++c) {
-        b.k[c] = kx[c];
-        b.k[QC + c] = uint32x4{0, 0, 0, 0};
-        if (pg && col == 0) *(uint32x4 *)((bf16_t *)pg + kv_k_off(h, slot, 32 * c + 8 * grp, a.kv.g)) = kx[c];
+        bf16x8 kf;
+        if constexpr (FP8) {
+          const uint2 w = kv8_codes(kx[c], ke);
+          kf = widen(w.x, w.y, ke);
+          if (pg && col == 0) *(uint2 *)(pg + kv8_k_off(h, slot, 32 * c + 8 * grp, a.kv.g)) = w;
+        } else {
+          kf = __builtin_bit_cast(bf16x8, kx[c]);
+          if (pg && col == 0) *(uint32x4 *)((bf16_t *)pg + kv_k_off(h, slot, 32 * c + 8 * grp, a.kv.g)) = kx[c];
+        }
+        S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[0][c], S, 0, 0, 0);
       }
+      auto &x = tile[0];
+      const float score = __shfl(S[0], col) * a.c, m_new = fmaxf(x.m_ref, score);
+      const float alpha = __builtin_amdgcn_exp2f(x.m_ref - m_new), p = __builtin_amdgcn_exp2f(score - m_new);
+      x.m_ref = m_new;
+      x.L[0] = x.L[0] * alpha + p;
 #pragma unroll
       for (int m = 0; m < VM; ++m) {
-        b.v[m] = uint32x4{vx[m], 0, 0, 0};
-        if (pg && grp == 0) ((bf16_t *)pg)[kv_v_off(h, slot, 16 * m + col, a.kv.g)] = vx[m];
+        float v[4] = {bf2f(vx[m].x & 0xffffu), bf2f(vx[m].x >> 16), bf2f(vx[m].y & 0xffffu), bf2f(vx[m].y >> 16)};
+        if constexpr (FP8) {
+          const uint32_t w = ve == 255 ? 0u : kv8_pack(v[0], v[1], v[2], v[3], ve);
+          const float sc = kv8_scale(ve);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[i] = kv8_value(w, i, sc);
+            if (pg && col == m) pg[kv8_v_off(h, slot, 16 * m + 4 * grp + i, a.kv.g)] = (unsigned char)(w >> (8 * i));
+          }
+        } else if (pg && col == m) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ((bf16_t *)pg)[kv_v_off(h, slot, 16 * m + 4 * grp + i, a.kv.g)] = (bf16_t)((i < 2 ? vx[m].x : vx[m].y) >> (16 * (i & 1)));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.O[m][i] = x.O[m][i] * alpha + p * v[i];
       }
     }
-    use(0, b, true, q0 + col < R ? 1 : 0, 1);
   }
-  // O[m][i]: element 16 m + 4 grp + i of query `col`; L, m_ref: its denominator and reference
-  const int cols = min(16, R - q0);
-  float *mine_o = lds + ((long)wave * cols + col) * (DH + 2);
-  if (col < cols) {
+  // the waves' states, a tile at a time
 #pragma unroll
-    for (int m = 0; m < VM; ++m)
+  for (int t = 0; t < NT; ++t) {
+    const int first = q0 + 16 * t, cols = min(16, R - first);
+    if (cols <= 0) break;
+    if (t) __syncthreads();
+    if (col < cols) {
+      float *mine = lds + ((long)wave * cols + col) * (DH + 2);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mine_o[16 * m + 4 * grp + i] = O[m][i];
-    if (grp == 0) {
-      mine_o[DH] = m_ref;
-      mine_o[DH + 1] = L[0];
+      for (int m = 0; m < VM; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[16 * m + 4 * grp + i] = tile[t].O[m][i];
+      if (grp == 0) {
+        mine[DH] = tile[t].m_ref;
+        mine[DH + 1] = tile[t].L[0];
+      }
     }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < cols * DH; i += NW * 64) {
-    const int e = i % DH, cq = i / DH;
-    float M = -INFINITY;
+    __syncthreads();
+    for (int i = threadIdx.x; i < cols * DH; i += NW * 64) {
+      const int e = i % DH, cq = i / DH;
+      float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, lds[((long)w * cols + cq) * (DH + 2) + DH]);
-    float num = 0.f, den = 0.f;
+      for (int w = 0; w < NW; ++w) M = fmaxf(M, lds[((long)w * cols + cq) * (DH + 2) + DH]);
+      float num = 0.f, den = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float *x = lds + ((long)w * cols + cq) * (DH + 2);
-      const float f = x[DH] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[DH] - M);
-      if (f != 0.f || x[DH] != x[DH]) {
+      for (int w = 0; w < NW; ++w) {
+        const float *x = lds + ((long)w * cols + cq) * (DH + 2);
+        const float f = __builtin_amdgcn_exp2f(x[DH] - M);
         num += f * x[e];
         den += f * x[DH + 1];
       }
-    }
-    const int qi2 = (q0 + cq) / a.group, head = h * a.group + (q0 + cq) % a.group;
-    const long token = t.at + (long)qi2 * a.tk.step;
-    if (a.splits == 1) {
-      ((bf16_t *)a.o.p)[row_index(a.o, token, head * DH + e)] = (bf16_t)f2bf(den == 0.f ? 0.f : num / den);
-    } else {
-      float *pp = a.part + (((long)blockIdx.y * a.tk.tokens + token) * a.heads + head) * (DH + 2);
-      pp[e] = num;
-      if (e == 0) {
-        pp[DH] = M;
-        pp[DH + 1] = den;
+      const int q = first + cq, head = s.head(a, q);
+      const long token = s.token(a, q);
+      if (a.splits == 1) {
+        ((bf16_t *)a.o.p)[row_index(a.o, token, head * DH + e)] = (bf16_t)f2bf(den == 0.f ? 0.f : num / den);
+      } else {
+        float *pp = part_of<DH>(a, blockIdx.y, token, head);
+        pp[e] = num;
+        if (e == 0) {
+          pp[DH] = M;
+          pp[DH + 1] = den;
+        }
       }
     }
   }
 }
 
-// Joins the shares of a query's keys, one workgroup per row, query tile of 16 and kv head as above.
-template <int DH>
-__global__ __launch_bounds__(256) void k_kv_merge(KvAttend a, int tiles) {
-  const int H = a.kv.g.H, qt = blockIdx.x % tiles, h = blockIdx.x / tiles % H, r = blockIdx.x / tiles / H;
-  const RowTokens t = row_tokens(a.tk, r);
-  const int R = t.n * a.group, q0 = qt * 16, cols = min(16, R - q0);
-  for (int i = threadIdx.x; i < cols * DH; i += 256) {
-    const int e = i % DH, q = q0 + i / DH, head = h * a.group + q % a.group;
-    const long token = t.at + (long)(q / a.group) * a.tk.step, stride = (long)a.tk.tokens * a.heads * (DH + 2);
-    const float *x = a.part + (token * a.heads + head) * (DH + 2);
-    float M = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, x[s * stride + DH]);
-    float num = 0.f, den = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-      const float m = x[s * stride + DH], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-      if (f != 0.f || m != m) {
-        num += f * x[s * stride + e];
-        den += f * x[s * stride + DH + 1];
+// Many queries: the waves of a workgroup have two tiles each, 128 queries together, and share the blocks, which a ring of
+// stages in LDS holds: filled by LDS-direct loads two stages ahead, one bare barrier a stage (as k_attention_rows does; 8-bit
+// blocks stay codes in LDS, and every wave converts what it reads).  Bound by LDS reads (a block is read by every wave) and by
+// what the softmax takes of the vector units.
+template <int DH, bool FP8>
+__global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int tiles) {
+  constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = 3, NQ = 16 * NT * NW;
+  constexpr int KF = FP8 ? QC : 2 * QC, FR = KF + (FP8 ? VM / 2 : VM), LPW = FR / NW;  // fragments a stage, loads of a wave
+  constexpr int STAGE = FR * 64 + (FP8 ? 16 : 0);  // 16-byte pieces; behind 8-bit blocks 256 bytes for their exponents
+  extern __shared__ uint32x4 ring[];               // [NS][STAGE]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
+  const Share s = Share::of<NQ>(a, tiles, false);
+  if (!s.any) return;
+  const int q0 = s.q0 + wave * (16 * NT), R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
+  // blocks of this wave: whole ones, and up to the last that one of its queries sees
+  const bool busy = q0 < R;
+  const int whole = busy ? s.seen(a, q0) >> 5 : 0;
+  const int last = busy ? min((s.seen(a, min(q0 + 16 * NT, R) - 1) + 31) >> 5, s.hi) : 0;
+  bf16x8 qf[NT][QC];
+  int limit[NT];
+  QueryTile<DH, false> tile[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int q = q0 + 16 * t + col;
+    limit[t] = q < R ? s.seen(a, q) : 0;
+    tile[t].clear();
+  }
+  // Blocks are requested in order.  Lane l holds page 64 w + l of the row, for the window w of 64 pages that the next block is
+  // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked.
+  const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
+  int ip = s.lo / bpp, ib = s.lo % bpp, pages = 0, window = -1, none[NS];
+  auto request = [&](int blk) {
+    if (ip >> 6 != window) {
+      window = ip >> 6;
+      const int at = window * 64 + lane;
+      pages = at < a.kv.g.max_pages ? table[at] : -1;
+      asm volatile("" : "+v"(pages));
+    }
+    int page = __builtin_amdgcn_readlane(pages, ip & 63);
+    const bool is = page >= 0 && page < a.kv.pages;
+    if (!is) page = 0;
+    const int slot = (blk - s.lo) % NS;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (i == slot) none[i] = !is;
+    const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
+    const long at = (long)h * bpp + ib;
+    const uint32x4 *src = (const uint32x4 *)(pg + at * ((FP8 ? 64 : 128) * DH)) + wave * LPW * 64;
+    uint32x4 *dst = ring + slot * STAGE + wave * LPW * 64;
+#pragma unroll
+    for (int i = 0; i < LPW; ++i)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)&(src + i * 64)[lane],
+                                       (__attribute__((address_space(3))) void *)(dst + i * 64), 16, 0, 0);
+    if constexpr (FP8) {  // every wave, so that all wait for the same number of loads; lanes 16 .. 63 repeat
+      const unsigned char *ex = pg + (long)H * bpp * (64 * DH) + at * 64;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(ex + 4 * col),
+                                       (__attribute__((address_space(3))) void *)(ring + slot * STAGE + FR * 64), 4, 0, 0);
+    }
+    if (++ib == bpp) {
+      ib = 0;
+      ++ip;
+    }
+  };
+  constexpr int LOADS = LPW + (FP8 ? 1 : 0);
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (s.lo + i < s.hi) request(s.lo + i);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
+  wait_vmcnt<0>();  // (waited for inside the loop, the queries would make the compiler wait for the ring as well)
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
+
+  bool odd_seen = false;
+  auto use = [&](bool masked, int blk, bool no_page) {
+    const int base = blk * 32;
+    const uint32x4 *kv = ring + (blk - s.lo) % NS * STAGE + lane;
+    const unsigned char *ex = (const unsigned char *)(ring + (blk - s.lo) % NS * STAGE + FR * 64);
+    floatx4 S[NT][2];
+#pragma unroll
+    for (int tl = 0; tl < 2; ++tl) {
+      const uint32_t ke = FP8 ? ex[16 * tl + col] : 0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[t][tl] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < QC; ++c) {
+        bf16x8 kf;
+        if constexpr (FP8) {
+          const uint32x4 w = kv[(tl * (QC / 2) + c / 2) * 64];
+          kf = widen(w[c % 2 * 2], w[c % 2 * 2 + 1], ke);
+        } else {
+          kf = __builtin_bit_cast(bf16x8, kv[(tl * QC + c) * 64]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][c], S[t][tl], 0, 0, 0);
       }
     }
+    float vs[8];
+    if constexpr (FP8) {
+      const uint32_t ve[2] = {((const uint32_t *)ex)[8 + grp], ((const uint32_t *)ex)[12 + grp]};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vs[j] = kv8_factor(ve[j >> 2], j & 3);
+    }
+    bf16x8 pv[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) pv[t] = tile[t].template weights<FP8>(masked, S[t], a.c, no_page ? 0 : limit[t] - base, grp, vs);
+    bool odd = false;
+    Keep keep(32, grp);
+    if (masked) {
+      keep = Keep(no_page ? 0 : s.held - base, grp);
+      if constexpr (!FP8) {
+#pragma unroll
+        for (int m = 0; m < VM; ++m) {
+          uint32x4 v = kv[(KF + m) * 64];
+          keep.bf16(v);
+          odd |= not_finite(v);
+        }
+        odd = __any(odd);
+        odd_seen |= odd;
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < VM; ++m) {
+      bf16x8 vf;
+      if constexpr (FP8) {
+        const uint32x4 w = kv[(KF + m / 2) * 64];
+        uint32_t w0 = w[m % 2 * 2], w1 = w[m % 2 * 2 + 1];
+        if (masked) {
+          w0 &= keep.codes(0);
+          w1 &= keep.codes(1);
+        }
+        vf = widen(w0, w1, 127);
+      } else {
+        uint32x4 w = kv[(KF + m) * 64];
+        if (masked) {
+          keep.bf16(w);
+          if (odd) drop_odd(w);
+        }
+        vf = __builtin_bit_cast(bf16x8, w);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv[t], tile[t].O[m], 0, 0, 0);
+    }
+  };
+  for (int blk = s.lo; blk < s.hi; ++blk) {
+    // this wave's loads of the stage have landed once only those of the next one are outstanding
+    if (blk + 1 < s.hi) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave's reads of the stage before
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    bool no_page = false;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (i == (blk - s.lo) % NS) no_page = none[i];
+    if (blk + NS - 1 < s.hi) request(blk + NS - 1);  // into the place of the stage before
+    if (blk >= last) continue;
+    use(blk >= whole || no_page, blk, no_page);
+  }
+  if constexpr (!FP8) {
+    if (odd_seen)  // seldom
+      for (int at = max(s.lo, whole); at < last; ++at) {
+        const int page = page_of(a.kv, s.r, at);
+        if (page < 0) continue;
+        const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)h * bpp + at % bpp) * (128 * DH)) + 4 * DH + lane;
+        const Keep keep(s.held - at * 32, grp);
+#pragma unroll
+        for (int m = 0; m < VM; ++m) {
+          uint32x4 v = src[m * 64];
+          keep.bf16(v);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) add_odd(tile[t].O[m], v, visible(limit[t] - at * 32, grp));
+        }
+      }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int q = q0 + 16 * t + col;
+    if (q >= R) continue;
+    const auto &x = tile[t];
+    const long token = s.token(a, q);
+    const int head = s.head(a, q);
+    if (a.splits == 1) {
+      const float inv = x.L[0] == 0.f ? 0.f : 1.0f / x.L[0];
+      bf16_t *o = (bf16_t *)a.o.p;
+#pragma unroll
+      for (int m = 0; m < VM; ++m)
+        *(uint2 *)&o[row_index(a.o, token, head * DH + 16 * m + 4 * grp)] =
+            make_uint2(pack2(x.O[m][0] * inv, x.O[m][1] * inv), pack2(x.O[m][2] * inv, x.O[m][3] * inv));
+    } else {
+      float *pp = part_of<DH>(a, blockIdx.y, token, head);
+#pragma unroll
+      for (int m = 0; m < VM; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pp[16 * m + 4 * grp + i] = x.O[m][i];
+      if (grp == 0) {
+        pp[DH] = x.m_ref;
+        pp[DH + 1] = x.L[0];
+      }
+    }
+  }
+}
+
+// Joins the shares of a query's keys: a workgroup per query of a row and head.  Every wave weighs the (at most 64) shares, one a
+// lane, then 256 / DH groups of threads add up the numerators of theirs.  A chain of three round trips whatever their number.
+template <int DH>
+__global__ __launch_bounds__(256) void k_kv_merge(KvAttend a, int queries) {
+  constexpr int GROUPS = 256 / DH;
+  __shared__ float f[64], sum[GROUPS][DH];
+  const int H = a.kv.g.H, q = blockIdx.x % queries, h = blockIdx.x / queries % H, r = blockIdx.x / queries / H;
+  const RowTokens t = row_tokens(a.tk, r);
+  if (q >= t.n * a.group) return;
+  const int head = h * a.group + q % a.group, lane = threadIdx.x & 63;
+  const long token = t.at + (long)(q / a.group) * a.tk.step, stride = (long)a.tk.tokens * a.heads * (DH + 2);
+  const float *x = part_of<DH>(a, 0, token, head);
+  float m = -3.0e38f, l = 0.f;
+  if (lane < a.splits) {
+    m = x[lane * stride + DH];
+    l = x[lane * stride + DH + 1];
+  }
+  float M = m;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
+  const float w = __builtin_amdgcn_exp2f(m - M);
+  const float den = wave_sum_f(lane < a.splits ? w * l : 0.f);
+  if (threadIdx.x < 64) f[lane] = w;
+  __syncthreads();
+  const int e = threadIdx.x % DH, g = threadIdx.x / DH;
+  float num = 0.f;
+#pragma unroll 8
+  for (int s = g; s < a.splits; s += GROUPS) num += f[s] * x[s * stride + e];
+  sum[g][e] = num;
+  __syncthreads();
+  if (g == 0) {
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) num += sum[i][e];
     ((bf16_t *)a.o.p)[row_index(a.o, token, head * DH + e)] = (bf16_t)f2bf(den == 0.f ? 0.f : num / den);
   }
 }
@@ -600,36 +953,72 @@ void kv_read(hipStream_t s, const KvView &kv, const KvTokens &tk, bool bf16, con
 #undef SKD_READ
 }
 
-static long query_tiles(const KvTokens &tk, int group) { return ((long)tk.max_new * group + 15) / 16; }
-// Eight waves a workgroup, and as many shares of the keys as give every CU 16 waves; a share has 8 blocks at least.
-int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads) {
-  const long wgs = query_tiles(tk, heads / kv.g.H) * kv.g.H * kv.rows, blocks = ((long)tk.max_past + tk.max_new + 31) / 32;
-  int splits = 1;
-  while (splits < 64 && wgs * splits < 512 && blocks / (2 * splits) >= 8) splits *= 2;
-  return splits;
+// Which kernel and how many shares of the keys: by the most queries that a row and kv head has.
+struct AttendPlan {
+  int nq;       // queries of a workgroup: 16, 32 or 128
+  int waves;    // 16, 32
+  int splits;
+  long tiles;   // of a row and kv head
+};
+static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
+  AttendPlan p{};
+  const long R = (long)tk.max_new * (heads / kv.g.H), blocks = ((long)tk.max_past + tk.max_new + 31) / 32;
+  p.nq = R <= 16 ? 16 : R <= 64 ? 32 : 128;
+  p.tiles = (R + p.nq - 1) / p.nq;
+  const long wgs = p.tiles * kv.g.H * kv.rows;
+  p.splits = 1;
+  if (p.nq == 128) {
+    p.waves = 4;
+    while (p.splits < 64 && wgs * p.splits < 256 && blocks / (2 * p.splits) >= 8) p.splits *= 2;
+  } else {
+    // 16 waves a CU (8 with two tiles), from workgroups that are wide first
+    const long want = p.nq == 16 ? 4096 : 2048;
+    p.waves = p.nq == 16 && wgs * 4 >= want ? 4 : 8;
+    while (p.splits < 64 && wgs * p.waves * p.splits < want && blocks / (2 * p.splits) >= p.waves) p.splits *= 2;
+  }
+  return p;
 }
+int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads) { return plan_attend(kv, tk, heads).splits; }
 size_t kv_attend_part(const KvView &kv, const KvTokens &tk, int heads, int splits) {
   return splits > 1 ? (size_t)splits * tk.tokens * heads * (kv.g.dh + 2) : 0;
 }
 
-void kv_attend(hipStream_t s, const KvAttend &a) {
-  constexpr int NW = 8;
-  const int tiles = (int)query_tiles(a.tk, a.group);
-  const dim3 grid((unsigned)((long)tiles * a.kv.g.H * a.kv.rows), a.splits);
-  const size_t lds = (size_t)NW * (tiles > 1 ? 16 : a.tk.max_new * a.group) * (a.kv.g.dh + 2) * sizeof(float);
+template <int DH, bool FP8, int NT, int NW>
+static void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int tiles) {
+  const int cols = std::min(16, a.tk.max_new * a.group);
+  const size_t lds = (size_t)NW * cols * (DH + 2) * sizeof(float);
   static std::atomic<uint64_t> done{0};
-  const void *all[] = {(const void *)k_kv_attend<64, false, NW>, (const void *)k_kv_attend<64, true, NW>, (const void *)k_kv_attend<128, false, NW>,
-                       (const void *)k_kv_attend<128, true, NW>};
-  if (lds > 64 * 1024) (void)allow_lds(done, {all[0], all[1], all[2], all[3]}, NW * 16 * 130 * sizeof(float));
-  if (a.kv.g.dh == 64) {
-    if (a.kv.fp8) SKD_LAUNCH((k_kv_attend<64, true, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
-    else SKD_LAUNCH((k_kv_attend<64, false, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
-    if (a.splits > 1) SKD_LAUNCH(k_kv_merge<64>, dim3(grid.x), dim3(256), 0, s, a, tiles);
+  if (lds > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend<DH, FP8, NT, NW>}, NW * 16 * (DH + 2) * sizeof(float));
+  SKD_LAUNCH((k_kv_attend<DH, FP8, NT, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
+}
+template <int DH, bool FP8>
+static void attend(hipStream_t s, const KvAttend &a) {
+  const AttendPlan p = plan_attend(a.kv, a.tk, a.heads);
+  const int tiles = (int)p.tiles;
+  const dim3 grid((unsigned)(p.tiles * a.kv.g.H * a.kv.rows), a.splits);
+  if (p.nq == 128) {
+    const size_t lds = 3 * (32 * DH * (FP8 ? 2 : 4) + (FP8 ? 256 : 0));
+    SKD_LAUNCH((k_kv_attend_rows<DH, FP8>), grid, dim3(256), lds, s, a, tiles);
+  } else if (p.nq == 32) {
+    launch_attend<DH, FP8, 2, 8>(s, a, grid, tiles);
+  } else if (p.waves == 4) {
+    launch_attend<DH, FP8, 1, 4>(s, a, grid, tiles);
   } else {
-    if (a.kv.fp8) SKD_LAUNCH((k_kv_attend<128, true, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
-    else SKD_LAUNCH((k_kv_attend<128, false, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
-    if (a.splits > 1) SKD_LAUNCH(k_kv_merge<128>, dim3(grid.x), dim3(256), 0, s, a, tiles);
+    launch_attend<DH, FP8, 1, 8>(s, a, grid, tiles);
   }
+  if (a.splits > 1) {
+    const int queries = a.tk.max_new * a.group;
+    SKD_LAUNCH(k_kv_merge<DH>, dim3((unsigned)((long)queries * a.kv.g.H * a.kv.rows)), dim3(256), 0, s, a, queries);
+  }
+}
+void kv_attend(hipStream_t s, const KvAttend &call) {
+  KvAttend a = call;
+  if (a.k.p && !(a.tk.max_new == 1 && plan_attend(a.kv, a.tk, a.heads).nq == 16)) {  // (one token of few heads: the same launch)
+    kv_append(s, a.kv, a.tk, a.k, a.v);
+    a.k.p = nullptr;
+  }
+  if (a.kv.g.dh == 64) a.kv.fp8 ? attend<64, true>(s, a) : attend<64, false>(s, a);
+  else a.kv.fp8 ? attend<128, true>(s, a) : attend<128, false>(s, a);
 }
 
 }  // namespace skd

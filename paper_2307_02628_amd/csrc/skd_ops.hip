@@ -137,8 +137,8 @@ static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads)
   if (heads < 1 || heads % kv->kv_heads) return SKD_ERR_SHAPE;
   const KvTokens tk = tokens(kv, ch);
   const int64_t group = heads / kv->kv_heads;
-  if (!fits_grid(((int64_t)tk.max_new * group + 15) / 16 * kv->kv_heads * std::max(kv->rows, 1)) || (int64_t)tk.max_new * group > std::numeric_limits<int32_t>::max() - 16)
-    return SKD_ERR_RANGE;
+  const int64_t queries = tk.max_new * group;
+  if (queries > std::numeric_limits<int32_t>::max() - 128 || !fits_grid((queries + 15) / 16 * kv->kv_heads * std::max(kv->rows, 1))) return SKD_ERR_RANGE;
   return SKD_OK;
 }
 
@@ -183,11 +183,9 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
   CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, q, out}));
   if (k) CHECK(check_memory({k, v}));
   if (a.splits > 1) CHECK(check_memory({workspace}));
-  if (k && a.tk.max_new == 1) {  // one launch
+  if (k) {
     a.k = rows_of(k, k_stride);
     a.v = rows_of(v, v_stride);
-  } else if (k) {
-    kv_append((hipStream_t)hip_stream, a.kv, a.tk, rows_of(k, k_stride), rows_of(v, v_stride));
   }
   kv_attend((hipStream_t)hip_stream, a);
   return launched();
