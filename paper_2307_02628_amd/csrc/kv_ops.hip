@@ -430,12 +430,25 @@ struct KvBlock {
 template <int DH, bool FP8, int NT, int NW>
 __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int tiles) {
   constexpr int QC = DH / 32, VM = DH / 16, NQ = 16 * NT;
-  extern __shared__ float lds[];  // [NW][cols][DH + 2]
+  // One tile of 128-wide heads keeps its queries in LDS: with them in registers the loop did not fit the 128 of 4 waves a SIMD.
+  constexpr bool LDS_Q = NT == 1 && DH == 128;
+  __shared__ bf16x8 sh_q[LDS_Q ? QC * 64 : 1];
+  __shared__ __align__(16) bf16_t sh_k[DH], sh_v[DH];  // the new token
+  extern __shared__ float lds[];                       // [NW][cols][DH + 2]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
   const bool files = NT == 1 && a.k.p != nullptr;  // (t.n is 1: the token is not in the cache yet)
   const Share s = Share::of<NQ>(a, tiles, files);
   if (!s.any) return;
   const int q0 = s.q0, R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
+  const bool fresh = files && blockIdx.y == gridDim.y - 1 && wave == NW - 1;  // this wave takes the new token
+  if constexpr (NT == 1) {
+    constexpr int LPT = DH / 8;
+    if (fresh && lane < 2 * LPT) {
+      const KvRows &x = lane < LPT ? a.k : a.v;
+      const int e = lane % LPT * 8;
+      *(uint32x4 *)&(lane < LPT ? sh_k : sh_v)[e] = *(const uint32x4 *)((const bf16_t *)x.p + row_index(x, s.t.at, h * DH + e));
+    }
+  }
   bf16x8 qf[NT][QC];
   int limit[NT];                  // positions of the cache that the lane's query sees
   QueryTile<DH, NT == 1> tile[NT];
@@ -446,10 +459,17 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     limit[t] = q < R ? min(s.seen(a, q), s.held) : 0;
     tile[t].clear();
   }
+  if constexpr (LDS_Q) {
+    if (wave == 0) {
+#pragma unroll
+      for (int c = 0; c < QC; ++c) sh_q[c * 64 + lane] = qf[0][c];
+    }
+    __syncthreads();
+  }
   typedef KvBlock<DH, FP8> Block;
-  auto load = [&](int blk, int page, Block &b) {
+  auto load = [&](int page, int ib, Block &b) {
     const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
-    const long at = (long)h * bpp + blk % bpp;
+    const long at = (long)h * bpp + ib;
     const uint32x4 *src = (const uint32x4 *)(pg + at * ((FP8 ? 64 : 128) * DH)) + lane;
     constexpr int KF = FP8 ? QC : 2 * QC, VF = FP8 ? VM / 2 : VM;
 #pragma unroll
@@ -471,11 +491,14 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     constexpr bool masked = decltype(masked_)::value;
     floatx4 S[NT][2];
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl) {
+    for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < NT; ++t) S[t][tl] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < QC; ++c) {
+      bf16x8 x[NT];
 #pragma unroll
-      for (int c = 0; c < QC; ++c) {
+      for (int t = 0; t < NT; ++t) x[t] = LDS_Q ? sh_q[c * 64 + lane] : qf[t][c];
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
         bf16x8 kf;
         if constexpr (FP8) {
           const uint32x4 w = b.k[tl * (QC / 2) + c / 2];
@@ -484,7 +507,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
           kf = __builtin_bit_cast(bf16x8, b.k[tl * QC + c]);
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][c], S[t][tl], 0, 0, 0);
+        for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, x[t], S[t][tl], 0, 0, 0);
       }
     }
     float vs[8];
@@ -529,22 +552,27 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     }
   };
   const int whole = min(s.seen(a, q0), s.held) >> 5;  // blocks before it are seen whole by every query
-  // (the number of the next page is asked for ahead of the use of a block)
-  int blk = s.lo + wave, page = blk < s.hi ? page_of(a.kv, s.r, blk) : -1;
-  for (; blk < min(whole, s.hi); blk += NW) {
+  // place of the wave's next block, whose page's number is asked for ahead of the use of the one before
+  const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
+  int blk = s.lo + wave, ip = blk / bpp, ib = blk % bpp;
+  auto entry = [&]() { return table[min(ip, a.kv.g.max_pages - 1)]; };
+  int number = entry();
+  auto step = [&](auto masked_) {
+    const bool is = number >= 0 && number < a.kv.pages && ip < a.kv.g.max_pages;
     Block b;
-    if (page >= 0) load(blk, page, b);
-    const int next = blk + NW < s.hi ? page_of(a.kv, s.r, blk + NW) : -1;
-    if (page >= 0) use(std::false_type(), 0, b, limit, 0);
-    page = next;
-  }
-  for (; blk < s.hi; blk += NW) {
-    Block b;
-    if (page >= 0) load(blk, page, b);
-    const int next = blk + NW < s.hi ? page_of(a.kv, s.r, blk + NW) : -1;
-    if (page >= 0) use(std::true_type(), blk * 32, b, limit, s.held);
-    page = next;
-  }
+    if (is) load(number, ib, b);
+    ip += NW / bpp;
+    ib += NW % bpp;
+    if (ib >= bpp) {
+      ib -= bpp;
+      ++ip;
+    }
+    number = entry();
+    if (is) use(masked_, blk * 32, b, limit, s.held);
+    blk += NW;
+  };
+  while (blk < min(whole, s.hi)) step(std::false_type());
+  while (blk < s.hi) step(std::true_type());
   if constexpr (!FP8) {
     // infinities and NaNs among the values of masked blocks: seldom
     if (odd_seen)
@@ -562,47 +590,33 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
         }
       }
   }
+  uint32_t ke = 0, ve = 0;  // exponents of the new token
   if constexpr (NT == 1) {
     tile[0].one_sum();
     // The one new token joins the last wave's state: its key as key 0 of a tile, its value by the vector units, four elements of
-    // every 16 in a lane.  The first tile files it.  Whoever reads its place meanwhile, in the block around it, discards what
-    // is there.
-    if (files && blockIdx.y == gridDim.y - 1 && wave == NW - 1) {
-      const int page = q0 == 0 ? page_of(a.kv, s.r, s.held >> 5) : -1, slot = s.held % a.kv.g.page_tokens;
-      unsigned char *pg = page < 0 ? nullptr : a.kv.pool + (long)page * a.kv.page_bytes;
-      uint32x4 kx[QC];
-      uint2 vx[VM];
-#pragma unroll
-      for (int c = 0; c < QC; ++c) {
-        kx[c] = uint32x4{0, 0, 0, 0};
-        if (col == 0) kx[c] = *(const uint32x4 *)((const bf16_t *)a.k.p + row_index(a.k, s.t.at, h * DH + 32 * c + 8 * grp));
-      }
-#pragma unroll
-      for (int m = 0; m < VM; ++m) vx[m] = *(const uint2 *)((const bf16_t *)a.v.p + row_index(a.v, s.t.at, h * DH + 16 * m + 4 * grp));
-      uint32_t ke = 0, ve = 0;
+    // every 16 in a lane.
+    if (fresh) {
       if constexpr (FP8) {
         uint32_t km = 0, vm = 0;
 #pragma unroll
-        for (int c = 0; c < QC; ++c) km = max(km, max_bits(kx[c]));
-#pragma unroll
-        for (int m = 0; m < VM; ++m) vm = max(vm, max_bits(uint32x4{vx[m].x, vx[m].y, 0, 0}));
+        for (int i = 0; i < DH / 64; ++i) {
+          km = max(km, (uint32_t)(sh_k[lane + 64 * i] & 0x7fff) << 16);
+          vm = max(vm, (uint32_t)(sh_v[lane + 64 * i] & 0x7fff) << 16);
+        }
         ke = kv8_exponent(max_over<64>(km));
         ve = kv8_exponent(max_over<64>(vm));
-        if (pg && lane < 2) pg[kv8_exp_off(h, slot, lane, a.kv.g)] = (unsigned char)(lane ? ve : ke);
       }
       floatx4 S = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < QC; ++c) {
-        bf16x8 kf;
+        uint32x4 kx = uint32x4{0, 0, 0, 0};
+        if (col == 0) kx = *(const uint32x4 *)&sh_k[32 * c + 8 * grp];
+        bf16x8 kf = __builtin_bit_cast(bf16x8, kx);
         if constexpr (FP8) {
-          const uint2 w = kv8_codes(kx[c], ke);
+          const uint2 w = kv8_codes(kx, ke);
           kf = widen(w.x, w.y, ke);
-          if (pg && col == 0) *(uint2 *)(pg + kv8_k_off(h, slot, 32 * c + 8 * grp, a.kv.g)) = w;
-        } else {
-          kf = __builtin_bit_cast(bf16x8, kx[c]);
-          if (pg && col == 0) *(uint32x4 *)((bf16_t *)pg + kv_k_off(h, slot, 32 * c + 8 * grp, a.kv.g)) = kx[c];
         }
-        S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[0][c], S, 0, 0, 0);
+        S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, LDS_Q ? sh_q[c * 64 + lane] : qf[0][c], S, 0, 0, 0);
       }
       auto &x = tile[0];
       const float score = __shfl(S[0], col) * a.c, m_new = fmaxf(x.m_ref, score);
@@ -611,18 +625,12 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       x.L[0] = x.L[0] * alpha + p;
 #pragma unroll
       for (int m = 0; m < VM; ++m) {
-        float v[4] = {bf2f(vx[m].x & 0xffffu), bf2f(vx[m].x >> 16), bf2f(vx[m].y & 0xffffu), bf2f(vx[m].y >> 16)};
+        const uint2 vx = *(const uint2 *)&sh_v[16 * m + 4 * grp];
+        float v[4] = {bf2f(vx.x & 0xffffu), bf2f(vx.x >> 16), bf2f(vx.y & 0xffffu), bf2f(vx.y >> 16)};
         if constexpr (FP8) {
           const uint32_t w = ve == 255 ? 0u : kv8_pack(v[0], v[1], v[2], v[3], ve);
-          const float sc = kv8_scale(ve);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[i] = kv8_value(w, i, sc);
-            if (pg && col == m) pg[kv8_v_off(h, slot, 16 * m + 4 * grp + i, a.kv.g)] = (unsigned char)(w >> (8 * i));
-          }
-        } else if (pg && col == m) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ((bf16_t *)pg)[kv_v_off(h, slot, 16 * m + 4 * grp + i, a.kv.g)] = (bf16_t)((i < 2 ? vx[m].x : vx[m].y) >> (16 * (i & 1)));
+          for (int i = 0; i < 4; ++i) v[i] = kv8_value(w, i, kv8_scale(ve));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.O[m][i] = x.O[m][i] * alpha + p * v[i];
@@ -672,6 +680,26 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
           pp[DH + 1] = den;
         }
       }
+    }
+  }
+  if constexpr (NT == 1) {
+    // The first tile files the new token.  Whoever reads its place meanwhile, in the block around it, discards what is there.
+    // (Last of all: a barrier behind the stores would wait for them, 4 us of a step of 32 rows.)
+    const int page = fresh && q0 == 0 ? page_of(a.kv, s.r, s.held >> 5) : -1, slot = s.held % a.kv.g.page_tokens;
+    if (page >= 0) {
+      unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
+      if (lane < DH / 8) {
+        const uint32x4 kx = *(const uint32x4 *)&sh_k[8 * lane];
+        if constexpr (FP8) *(uint2 *)(pg + kv8_k_off(h, slot, 8 * lane, a.kv.g)) = kv8_codes(kx, ke);
+        else *(uint32x4 *)((bf16_t *)pg + kv_k_off(h, slot, 8 * lane, a.kv.g)) = kx;
+      }
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) {
+        const int e = lane + 64 * i;
+        if constexpr (FP8) pg[kv8_v_off(h, slot, e, a.kv.g)] = ve == 255 ? 0 : (unsigned char)kv8_pack(bf2f(sh_v[e]), 0.f, 0.f, 0.f, ve);
+        else ((bf16_t *)pg)[kv_v_off(h, slot, e, a.kv.g)] = sh_v[e];
+      }
+      if (FP8 && lane < 2) pg[kv8_exp_off(h, slot, lane, a.kv.g)] = (unsigned char)(lane ? ve : ke);
     }
   }
 }
@@ -988,7 +1016,7 @@ static void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int tiles
   const int cols = std::min(16, a.tk.max_new * a.group);
   const size_t lds = (size_t)NW * cols * (DH + 2) * sizeof(float);
   static std::atomic<uint64_t> done{0};
-  if (lds > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend<DH, FP8, NT, NW>}, NW * 16 * (DH + 2) * sizeof(float));
+  if (lds + 8192 > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend<DH, FP8, NT, NW>}, NW * 16 * (DH + 2) * sizeof(float));
   SKD_LAUNCH((k_kv_attend<DH, FP8, NT, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
 }
 template <int DH, bool FP8>
