@@ -225,10 +225,11 @@ __global__ __launch_bounds__(256) void k_kv_read(KvView kv, KvTokens tk, KvRows 
 // columns of the matrix instructions.  The softmax works in units of log2 against a reference that is raised only by more
 // than 8 (weights up to 2^8), denominators come from the matrix cores (a row of ones) and are sums of the rounded weights.
 //
-// Query i of a row sees positions up to past + i.  Blocks that reach beyond what a tile's first query sees are masked: scores
-// by selection, and since 0 * infinity is not 0, values too: beyond the row's last position they are cleared (a page may hold
-// anything there), and an infinity or NaN that only later queries see is kept out of the products and put into the sums of
-// those that see it.  8-bit values are finite, what is not is in their scales, which are selected with the weights.
+// Query i of a row sees positions up to past + i.  In blocks that reach beyond what a tile's first query sees scores are masked by
+// selection.  Since 0 * infinity is not 0, that leaves values: beyond the row's last position they are cleared (a page may hold
+// anything there); an infinity or NaN that only later queries see makes sums that are not finite, and a wave that ends with such
+// sums forms them once more (sums_again), without such values, which are added for the queries that see them.  8-bit values are
+// finite, what is not is in their scales, which are selected with the weights.
 // The powers of two of 8-bit keys are an operand of the conversion to bf16, those of values multiply the weights: both exact.
 
 // bf16x8 of two words of codes, times the power of two whose exponent byte is `e` (255: NaN)
@@ -337,13 +338,6 @@ struct Keep {
   }
   __device__ uint32_t codes(int half) const { return __builtin_amdgcn_perm(w[2 * half + 1], w[2 * half], 0x06040200); }
 };
-// whether one of a lane's bf16 values is an infinity or NaN
-__device__ inline bool not_finite(const uint32x4 &v) {
-  uint32_t odd = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) odd |= ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-  return odd != 0;
-}
 __device__ inline void drop_odd(uint32x4 &v) {  // infinities and NaNs to 0
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -385,15 +379,16 @@ struct Share {
   int held;        // positions that the cache holds
   int lo, hi;      // blocks
   bool any;
+  // Workgroup: [tile, the longest first][row and kv head], `pairs` places for the latter.
   template <int NQ>
-  __device__ static Share of(const KvAttend &a, int tiles, bool files) {
+  __device__ static Share of(const KvAttend &a, int pairs, bool files) {
     Share s;
-    const int H = a.kv.g.H, ri = blockIdx.x / tiles / H;
-    s.h = blockIdx.x / tiles % H;
+    const int H = a.kv.g.H, tiles = gridDim.x / pairs, pair = blockIdx.x % pairs, ri = min(pair / H, a.kv.rows - 1);
+    s.h = pair % H;
     s.r = a.order ? a.order[ri] : ri;
     s.t = row_tokens(a.tk, s.r);
-    s.R = s.t.n * a.group;
-    s.q0 = (int)(tiles - 1 - blockIdx.x % tiles) * NQ;  // the longest first
+    s.R = pair < H * a.kv.rows ? s.t.n * a.group : 0;
+    s.q0 = (int)(tiles - 1 - blockIdx.x / pairs) * NQ;
     s.any = s.q0 < s.R;
     s.held = s.t.past + (files ? 0 : s.t.n);
     const int nblk = (min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held) + 31) >> 5, per = (nblk + a.splits - 1) / a.splits;
@@ -418,6 +413,65 @@ __device__ inline void load_queries(const KvAttend &a, const Share &s, int q, in
   }
 }
 
+// Whether a wave's sums hold an infinity or NaN.
+template <int DH, int NT, typename Tile>
+__device__ inline bool not_finite_(const Tile (&tile)[NT]) {
+  float x = 0.f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int m = 0; m < DH / 16; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x = __builtin_fmaf(tile[t].O[m][i], 0.f, x);
+  return __any(x != x);
+}
+template <int DH, typename Tile, int NT>
+__device__ inline bool not_finite(const Tile (&tile)[NT]) { return not_finite_<DH, NT, Tile>(tile); }
+// The numerators of a wave's tiles again, over blocks first, first + step, ... below end of bf16 pages, against the references
+// that the wave has arrived at: values without their infinities and NaNs, which are then added.
+template <int DH, typename Tile, int NT>
+__device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, int q0, const int (&limit)[NT], int first, int step, int end, Tile (&tile)[NT]) {
+  constexpr int QC = DH / 32, VM = DH / 16;
+  const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15, bpp = a.kv.g.page_tokens >> 5;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int m = 0; m < VM; ++m) tile[t].O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int blk = first; blk < end; blk += step) {
+    const int page = page_of(a.kv, s.r, blk);
+    if (page < 0) continue;
+    const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)s.h * bpp + blk % bpp) * (128 * DH)) + lane;
+    const Keep keep(s.held - blk * 32, grp);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      bf16x8 qf[QC];
+      load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf);
+      const int lim = limit[t] - blk * 32;
+      floatx4 S[2];
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
+        S[tl] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < QC; ++c) S[tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, src[(tl * QC + c) * 64]), qf[c], S[tl], 0, 0, 0);
+      }
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        p[j] = block_pos(j, grp) < lim ? __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], a.c, -tile[t].m_ref)) : 0.f;
+      const bf16x8 pv = pack8(p), vis = visible(lim, grp);
+#pragma unroll
+      for (int m = 0; m < VM; ++m) {
+        uint32x4 v = src[4 * DH + m * 64], w;
+        keep.bf16(v);
+        w = v;
+        drop_odd(w);
+        tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pv, tile[t].O[m], 0, 0, 0);
+        add_odd(tile[t].O[m], v, vis);
+      }
+    }
+  }
+}
+
 // Few queries (one or two tiles): a workgroup is NW waves on NT tiles, and a wave takes every NW-th 32-key block, straight from
 // the page into the operand registers, with a softmax of its own; the waves' states are joined in LDS, the shares of several
 // workgroups by k_kv_merge.  Bound by the bytes of the pages.
@@ -428,7 +482,7 @@ struct KvBlock {
   uint32_t ke[2], ve[2];  // exponents: of key 16 tl + (lane & 15) (K), of keys 16 tl + 4 (lane >> 4) .. + 3 (V)
 };
 template <int DH, bool FP8, int NT, int NW>
-__global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int tiles) {
+__global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int pairs) {
   constexpr int QC = DH / 32, VM = DH / 16, NQ = 16 * NT;
   // One tile of 128-wide heads keeps its queries in LDS: with them in registers the loop did not fit the 128 of 4 waves a SIMD.
   constexpr bool LDS_Q = NT == 1 && DH == 128;
@@ -437,7 +491,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   extern __shared__ float lds[];                       // [NW][cols][DH + 2]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
   const bool files = NT == 1 && a.k.p != nullptr;  // (t.n is 1: the token is not in the cache yet)
-  const Share s = Share::of<NQ>(a, tiles, files);
+  const Share s = Share::of<NQ>(a, pairs, files);
   if (!s.any) return;
   const int q0 = s.q0, R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
   const bool fresh = files && blockIdx.y == gridDim.y - 1 && wave == NW - 1;  // this wave takes the new token
@@ -485,8 +539,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       }
     }
   };
-  // base: first position of the block; valid: positions that it holds
-  bool odd_seen = false;
+  // base: first position of the block; valid: positions that the row has
   auto use = [&](auto masked_, int base, Block &b, const int (&lim)[NT], int valid) {
     constexpr bool masked = decltype(masked_)::value;
     floatx4 S[NT][2];
@@ -520,23 +573,12 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     for (int t = 0; t < NT; ++t) pv[t] = tile[t].template weights<FP8>(masked, S[t], a.c, lim[t] - base, grp, vs);
     if (masked) {
       const Keep keep(valid - base, grp);
-      bool odd = false;
       if constexpr (FP8) {  // (codes of positions that the row does not have may be NaN)
 #pragma unroll
-        for (int m = 0; m < VM / 2; ++m) {
-          b.v[m] &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
-        }
+        for (int m = 0; m < VM / 2; ++m) b.v[m] &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
       } else {
 #pragma unroll
-        for (int m = 0; m < VM; ++m) {
-          keep.bf16(b.v[m]);
-          odd |= not_finite(b.v[m]);
-        }
-        if (__any(odd)) {
-          odd_seen = true;
-#pragma unroll
-          for (int m = 0; m < VM; ++m) drop_odd(b.v[m]);
-        }
+        for (int m = 0; m < VM; ++m) keep.bf16(b.v[m]);
       }
     }
 #pragma unroll
@@ -574,21 +616,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   while (blk < min(whole, s.hi)) step(std::false_type());
   while (blk < s.hi) step(std::true_type());
   if constexpr (!FP8) {
-    // infinities and NaNs among the values of masked blocks: seldom
-    if (odd_seen)
-      for (int at = max(s.lo, whole); at < s.hi; ++at) {
-        const int page = (at - s.lo) % NW == wave ? page_of(a.kv, s.r, at) : -1;
-        if (page < 0) continue;
-        const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)h * bpp + at % bpp) * (128 * DH)) + 4 * DH + lane;
-        const Keep keep(s.held - at * 32, grp);
-#pragma unroll
-        for (int m = 0; m < VM; ++m) {
-          uint32x4 v = src[m * 64];
-          keep.bf16(v);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) add_odd(tile[t].O[m], v, visible(limit[t] - at * 32, grp));
-        }
-      }
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH>(a, s, q0, limit, s.lo + wave, NW, s.hi, tile);
   }
   uint32_t ke = 0, ve = 0;  // exponents of the new token
   if constexpr (NT == 1) {
@@ -709,18 +737,17 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 // blocks stay codes in LDS, and every wave converts what it reads).  Bound by LDS reads (a block is read by every wave) and by
 // what the softmax takes of the vector units.
 template <int DH, bool FP8>
-__global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int tiles) {
+__global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int pairs) {
   constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = 3, NQ = 16 * NT * NW;
   constexpr int KF = FP8 ? QC : 2 * QC, FR = KF + (FP8 ? VM / 2 : VM), LPW = FR / NW;  // fragments a stage, loads of a wave
   constexpr int STAGE = FR * 64 + (FP8 ? 16 : 0);  // 16-byte pieces; behind 8-bit blocks 256 bytes for their exponents
   extern __shared__ uint32x4 ring[];               // [NS][STAGE]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
-  const Share s = Share::of<NQ>(a, tiles, false);
+  const Share s = Share::of<NQ>(a, pairs, false);
   if (!s.any) return;
   const int q0 = s.q0 + wave * (16 * NT), R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
-  // blocks of this wave: whole ones, and up to the last that one of its queries sees
+  const int whole = s.seen(a, s.q0) >> 5;  // blocks before it are seen whole by every query of the workgroup
   const bool busy = q0 < R;
-  const int whole = busy ? s.seen(a, q0) >> 5 : 0;
   const int last = busy ? min((s.seen(a, min(q0 + 16 * NT, R) - 1) + 31) >> 5, s.hi) : 0;
   bf16x8 qf[NT][QC];
   int limit[NT];
@@ -732,15 +759,19 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int tiles
     tile[t].clear();
   }
   // Blocks are requested in order.  Lane l holds page 64 w + l of the row, for the window w of 64 pages that the next block is
-  // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked.
+  // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked, as is every block from the
+  // moment on at which a window has an entry that is no page.
   const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
   int ip = s.lo / bpp, ib = s.lo % bpp, pages = 0, window = -1, none[NS];
+  bool gaps = false;
+  const int ip_end = (s.hi + bpp - 1) / bpp;
   auto request = [&](int blk) {
     if (ip >> 6 != window) {
       window = ip >> 6;
       const int at = window * 64 + lane;
       pages = at < a.kv.g.max_pages ? table[at] : -1;
       asm volatile("" : "+v"(pages));
+      gaps |= __any(at >= ip && at < ip_end && (pages < 0 || pages >= a.kv.pages));
     }
     int page = __builtin_amdgcn_readlane(pages, ip & 63);
     const bool is = page >= 0 && page < a.kv.pages;
@@ -779,8 +810,8 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int tiles
 #pragma unroll
     for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
 
-  bool odd_seen = false;
-  auto use = [&](bool masked, int blk, bool no_page) {
+  auto use = [&](auto masked_, int blk, bool no_page) {
+    constexpr bool masked = decltype(masked_)::value;
     const int base = blk * 32;
     const uint32x4 *kv = ring + (blk - s.lo) % NS * STAGE + lane;
     const unsigned char *ex = (const unsigned char *)(ring + (blk - s.lo) % NS * STAGE + FR * 64);
@@ -812,45 +843,35 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int tiles
     bf16x8 pv[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) pv[t] = tile[t].template weights<FP8>(masked, S[t], a.c, no_page ? 0 : limit[t] - base, grp, vs);
-    bool odd = false;
-    Keep keep(32, grp);
-    if (masked) {
-      keep = Keep(no_page ? 0 : s.held - base, grp);
-      if constexpr (!FP8) {
-#pragma unroll
-        for (int m = 0; m < VM; ++m) {
-          uint32x4 v = kv[(KF + m) * 64];
-          keep.bf16(v);
-          odd |= not_finite(v);
-        }
-        odd = __any(odd);
-        odd_seen |= odd;
-      }
-    }
 #pragma unroll
     for (int m = 0; m < VM; ++m) {
       bf16x8 vf;
       if constexpr (FP8) {
         const uint32x4 w = kv[(KF + m / 2) * 64];
-        uint32_t w0 = w[m % 2 * 2], w1 = w[m % 2 * 2 + 1];
-        if (masked) {
-          w0 &= keep.codes(0);
-          w1 &= keep.codes(1);
-        }
-        vf = widen(w0, w1, 127);
+        vf = widen(w[m % 2 * 2], w[m % 2 * 2 + 1], 127);
       } else {
-        uint32x4 w = kv[(KF + m) * 64];
-        if (masked) {
-          keep.bf16(w);
-          if (odd) drop_odd(w);
-        }
-        vf = __builtin_bit_cast(bf16x8, w);
+        vf = __builtin_bit_cast(bf16x8, kv[(KF + m) * 64]);
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv[t], tile[t].O[m], 0, 0, 0);
     }
   };
-  for (int blk = s.lo; blk < s.hi; ++blk) {
+  // clears what a stage holds from position `valid` of its block on
+  auto clear = [&](int blk, int valid) {
+    const Keep keep(valid, grp);
+    for (int m = wave; m < FR - KF; m += NW) {
+      uint32x4 &v = ring[(blk - s.lo) % NS * STAGE + (KF + m) * 64 + lane];
+      uint32x4 x = v;
+      if constexpr (FP8) x &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
+      else keep.bf16(x);
+      v = x;
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto open = [&](int blk) {
     // this wave's loads of the stage have landed once only those of the next one are outstanding
     if (blk + 1 < s.hi) wait_vmcnt<LOADS>();
     else wait_vmcnt<0>();
@@ -863,24 +884,20 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int tiles
     for (int i = 0; i < NS; ++i)
       if (i == (blk - s.lo) % NS) no_page = none[i];
     if (blk + NS - 1 < s.hi) request(blk + NS - 1);  // into the place of the stage before
-    if (blk >= last) continue;
-    use(blk >= whole || no_page, blk, no_page);
+    return no_page;
+  };
+  int blk = s.lo;
+  for (; blk < min(whole, s.hi) && !gaps; ++blk) {
+    (void)open(blk);
+    if (busy) use(std::false_type(), blk, false);
+  }
+  for (; blk < s.hi; ++blk) {
+    const bool no_page = open(blk);
+    if (no_page || blk * 32 + 32 > s.held) clear(blk, no_page ? 0 : s.held - blk * 32);
+    if (blk < last) use(std::true_type(), blk, no_page);
   }
   if constexpr (!FP8) {
-    if (odd_seen)  // seldom
-      for (int at = max(s.lo, whole); at < last; ++at) {
-        const int page = page_of(a.kv, s.r, at);
-        if (page < 0) continue;
-        const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)h * bpp + at % bpp) * (128 * DH)) + 4 * DH + lane;
-        const Keep keep(s.held - at * 32, grp);
-#pragma unroll
-        for (int m = 0; m < VM; ++m) {
-          uint32x4 v = src[m * 64];
-          keep.bf16(v);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) add_odd(tile[t].O[m], v, visible(limit[t] - at * 32, grp));
-        }
-      }
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH>(a, s, q0, limit, s.lo, 1, last, tile);
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -987,13 +1004,19 @@ struct AttendPlan {
   int waves;    // 16, 32
   int splits;
   long tiles;   // of a row and kv head
+  int pairs;    // places for a row and kv head
 };
 static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
   AttendPlan p{};
   const long R = (long)tk.max_new * (heads / kv.g.H), blocks = ((long)tk.max_past + tk.max_new + 31) / 32;
   p.nq = R <= 16 ? 16 : R <= 64 ? 32 : 128;
   p.tiles = (R + p.nq - 1) / p.nq;
-  const long wgs = p.tiles * kv.g.H * kv.rows;
+  const long n = (long)kv.g.H * kv.rows, wgs = p.tiles * n;
+  // Workgroups go to the eight XCDs in turn.  With a multiple of eight places all tiles of a row and kv head are on one of them
+  // and find each other's blocks in its L2 (8 prompts of 2048, 32 heads of 128: 586 us with the tiles next to each other, 441
+  // so); a few more places than there are pairs cost less than that gives, many leave XCDs idle.
+  p.pairs = (int)n;
+  if (p.tiles > 1 && n >= 8 && (n + 7) / 8 * 8 * 20 <= n * 23) p.pairs = (int)((n + 7) / 8 * 8);
   p.splits = 1;
   if (p.nq == 128) {
     p.waves = 4;
@@ -1012,27 +1035,26 @@ size_t kv_attend_part(const KvView &kv, const KvTokens &tk, int heads, int split
 }
 
 template <int DH, bool FP8, int NT, int NW>
-static void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int tiles) {
+static void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int pairs) {
   const int cols = std::min(16, a.tk.max_new * a.group);
   const size_t lds = (size_t)NW * cols * (DH + 2) * sizeof(float);
   static std::atomic<uint64_t> done{0};
   if (lds + 8192 > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend<DH, FP8, NT, NW>}, NW * 16 * (DH + 2) * sizeof(float));
-  SKD_LAUNCH((k_kv_attend<DH, FP8, NT, NW>), grid, dim3(NW * 64), lds, s, a, tiles);
+  SKD_LAUNCH((k_kv_attend<DH, FP8, NT, NW>), grid, dim3(NW * 64), lds, s, a, pairs);
 }
 template <int DH, bool FP8>
 static void attend(hipStream_t s, const KvAttend &a) {
   const AttendPlan p = plan_attend(a.kv, a.tk, a.heads);
-  const int tiles = (int)p.tiles;
-  const dim3 grid((unsigned)(p.tiles * a.kv.g.H * a.kv.rows), a.splits);
+  const dim3 grid((unsigned)(p.tiles * p.pairs), a.splits);
   if (p.nq == 128) {
     const size_t lds = 3 * (32 * DH * (FP8 ? 2 : 4) + (FP8 ? 256 : 0));
-    SKD_LAUNCH((k_kv_attend_rows<DH, FP8>), grid, dim3(256), lds, s, a, tiles);
+    SKD_LAUNCH((k_kv_attend_rows<DH, FP8>), grid, dim3(256), lds, s, a, p.pairs);
   } else if (p.nq == 32) {
-    launch_attend<DH, FP8, 2, 8>(s, a, grid, tiles);
+    launch_attend<DH, FP8, 2, 8>(s, a, grid, p.pairs);
   } else if (p.waves == 4) {
-    launch_attend<DH, FP8, 1, 4>(s, a, grid, tiles);
+    launch_attend<DH, FP8, 1, 4>(s, a, grid, p.pairs);
   } else {
-    launch_attend<DH, FP8, 1, 8>(s, a, grid, tiles);
+    launch_attend<DH, FP8, 1, 8>(s, a, grid, p.pairs);
   }
   if (a.splits > 1) {
     const int queries = a.tk.max_new * a.group;

@@ -138,7 +138,7 @@ static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads)
   const KvTokens tk = tokens(kv, ch);
   const int64_t group = heads / kv->kv_heads;
   const int64_t queries = tk.max_new * group;
-  if (queries > std::numeric_limits<int32_t>::max() - 128 || !fits_grid((queries + 15) / 16 * kv->kv_heads * std::max(kv->rows, 1))) return SKD_ERR_RANGE;
+  if (queries > std::numeric_limits<int32_t>::max() - 128 || !fits_grid((queries + 15) / 16 * ((int64_t)kv->kv_heads * std::max(kv->rows, 1) + 8))) return SKD_ERR_RANGE;
   return SKD_OK;
 }
 
