@@ -46,7 +46,7 @@ typedef enum {
   SKD_ERR_HIP = -7       /* a HIP runtime call failed (skd_last_hip_error) */
 } skd_err;
 
-enum { SKD_BF16 = 0, SKD_FP32 = 1 }; /* skd_config.dtype                 */
+enum { SKD_BF16 = 0, SKD_FP32 = 1, SKD_BF16_KV8 = 2 }; /* skd_config.dtype */
 enum { SKD_HOST = 0, SKD_DEVICE = 1 }; /* skd_weights.location            */
 enum { SKD_W_FP32 = 0, SKD_W_BF16 = 1 }; /* skd_weights.elem              */
 
@@ -71,7 +71,10 @@ typedef struct {
   int32_t page_tokens;  /* tokens per KV page, multiple of 32; 0 = 64       */
   int32_t dtype;        /* SKD_BF16: bf16 weights/KV/activations, fp32 residual
                            stream and accumulation (the production path);
-                           SKD_FP32: everything fp32, simple kernels (debug)  */
+                           SKD_FP32: everything fp32, simple kernels (debug);
+                           SKD_BF16_KV8: as SKD_BF16, with the cache in 8 bits
+                           (SKD_KV_FP8 pages: half the bytes and half the pool;
+                           shapes, calls and errors as with SKD_BF16)        */
   int32_t io_on_device; /* 0: token / logit buffers of prefill, decode_step and
                            logits_argmax are host memory and the calls
                            synchronise; 1: they are device memory and the calls
@@ -167,6 +170,18 @@ int skd_prefill(skd_state *st, const int32_t *tokens, const uint8_t *attn_mask);
  * SKD_ERR_HIP. */
 int skd_decode_step(skd_state *st, int32_t t, const int32_t *tokens_in);
 
+/* Several decode steps at once, for tokens that are known: columns t .. t + cols - 1
+ * of all B rows, every one with the layer set of skd_active_layers, as `cols` calls of
+ * skd_decode_step would process them (another order of the sums: the same values
+ * within rounding).  Every weight is read once for up to 4096 rows x columns
+ * instead of once per column.  The next turn of a conversation, drafted tokens to
+ * be verified; skd_rewind takes columns back.  The heads see the last column.
+ * tokens: [B][cols] host memory, or [cols][B] device memory with io_on_device = 1
+ * (clamped into [0, vocab)).  The first call allocates its workspace.  Errors:
+ * SKD_ERR_NULL, SKD_ERR_ORDER (no prefill, wrong t), SKD_ERR_RANGE (cols < 1,
+ * t + cols > N, host token id), SKD_ERR_NOMEM, SKD_ERR_HIP. */
+int skd_decode_chunk(skd_state *st, int32_t t, int32_t cols, const int32_t *tokens);
+
 /* Final LayerNorm + LM head + greedy argmax on the hidden state of the last
  * processed column: every column emits a token for the whole batch, whatever
  * number of layers it ran (Section 2.1: one exit point per batch column; the
@@ -189,7 +204,7 @@ int skd_logits_argmax(skd_state *st, int32_t *tokens_out, float *logits_out);
  * (every GPU the library runs on holds its own copy until the process ends)
  * instead of buffers of the state, and the call itself calls no hipMalloc,
  * hipFree or other allocating routine.  Only for states with dtype SKD_BF16
- * and io_on_device = 1 (SKD_ERR_SHAPE otherwise): tokens_out [B] and
+ * or SKD_BF16_KV8 and io_on_device = 1 (SKD_ERR_SHAPE otherwise): tokens_out [B] and
  * logits_out [B][vocab] (either may be NULL) are device memory and the call
  * only enqueues work on the state's stream.  Limit:
  * ceil(vocab / (16 R)) * B_pad <= 262144 partials, R = LM-head tile rows per

@@ -1059,7 +1059,7 @@ __device__ inline void tile_epilogue(const GemmArgs &a, const floatx4 (&acc)[RT]
 #pragma unroll
       for (int r = 0; r < RT; ++r)
         *(floatx4 *)&a.partial[((long)sp * a.B_pad + row0_of(m) + j) * a.N + n0_of(r)] = acc[r][m];
-  } else if constexpr (EPI == EPI_RELU) {
+  } else if constexpr (EPI == EPI_RELU || EPI == EPI_ACT) {
     floatx4 bias[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) bias[r] = *(const floatx4 *)&a.bias[n0_of(r)];
@@ -1068,7 +1068,8 @@ __device__ inline void tile_epilogue(const GemmArgs &a, const floatx4 (&acc)[RT]
 #pragma unroll
       for (int r = 0; r < RT; r += 2) {
         floatx4 v0 = acc[r][m] + bias[r], v1 = acc[r + 1][m] + bias[r + 1];
-        for (int i = 0; i < 4; ++i) v0[i] = fmaxf(v0[i], 0.f), v1[i] = fmaxf(v1[i], 0.f);
+        if constexpr (EPI == EPI_RELU)
+          for (int i = 0; i < 4; ++i) v0[i] = fmaxf(v0[i], 0.f), v1[i] = fmaxf(v1[i], 0.f);
         *(uint4 *)&a.act_out[d_act_index(row0_of(m) + j, pair_n0_of(r), a.N)] = pack_tile_pair(v0, v1);
       }
   } else if constexpr (EPI == EPI_RESID) {
@@ -1320,13 +1321,15 @@ int bf16_gemm_tile(hipStream_t s, const GemmArgs &a, int epi) {
   if (!allow_lds(done, {(const void *)k_gemm_tile<EPI_QKV_ROWS>,
                         (const void *)k_gemm_tile<EPI_RESID>,
                         (const void *)k_gemm_tile<EPI_PARTIAL>,
-                        (const void *)k_gemm_tile<EPI_RELU>}, lds))
+                        (const void *)k_gemm_tile<EPI_RELU>,
+                        (const void *)k_gemm_tile<EPI_ACT>}, lds))
     return -1;
   switch (epi) {
     case EPI_QKV_ROWS: SKD_LAUNCH(k_gemm_tile<EPI_QKV_ROWS>, grid, blk, lds, s, a); break;
     case EPI_RESID: SKD_LAUNCH(k_gemm_tile<EPI_RESID>, grid, blk, lds, s, a); break;
     case EPI_PARTIAL: SKD_LAUNCH(k_gemm_tile<EPI_PARTIAL>, grid, blk, lds, s, a); break;
     case EPI_RELU: SKD_LAUNCH(k_gemm_tile<EPI_RELU>, grid, blk, lds, s, a); break;
+    case EPI_ACT: SKD_LAUNCH(k_gemm_tile<EPI_ACT>, grid, blk, lds, s, a); break;
     default: return -1;
   }
   return 0;
@@ -1538,7 +1541,8 @@ static int launch_gemm_mid(hipStream_t s, const GemmArgs &a, int epi) {
   if (!allow_lds(done, {(const void *)k_gemm_mid<RT, MT, WN, WM, NS, EPI_QKV_ROWS>,
                         (const void *)k_gemm_mid<RT, MT, WN, WM, NS, EPI_RESID>,
                         (const void *)k_gemm_mid<RT, MT, WN, WM, NS, EPI_PARTIAL>,
-                        (const void *)k_gemm_mid<RT, MT, WN, WM, NS, EPI_RELU>}, lds))
+                        (const void *)k_gemm_mid<RT, MT, WN, WM, NS, EPI_RELU>,
+                        (const void *)k_gemm_mid<RT, MT, WN, WM, NS, EPI_ACT>}, lds))
     return -1;
   const dim3 grid((a.N / BN) * ((a.rows + BM - 1) / BM) * a.split), blk(WN * WM * 64);
   switch (epi) {
@@ -1546,6 +1550,7 @@ static int launch_gemm_mid(hipStream_t s, const GemmArgs &a, int epi) {
     case EPI_RESID: SKD_LAUNCH((k_gemm_mid<RT, MT, WN, WM, NS, EPI_RESID>), grid, blk, lds, s, a); break;
     case EPI_PARTIAL: SKD_LAUNCH((k_gemm_mid<RT, MT, WN, WM, NS, EPI_PARTIAL>), grid, blk, lds, s, a); break;
     case EPI_RELU: SKD_LAUNCH((k_gemm_mid<RT, MT, WN, WM, NS, EPI_RELU>), grid, blk, lds, s, a); break;
+    case EPI_ACT: SKD_LAUNCH((k_gemm_mid<RT, MT, WN, WM, NS, EPI_ACT>), grid, blk, lds, s, a); break;
     default: return -1;
   }
   return 0;
@@ -2204,6 +2209,23 @@ __global__ __launch_bounds__(1024) void k_embed_ln_rows_wide(const int32_t *toke
     }
   }
   ln_finish_row(v, gv, bv, d, row, a_out, sh);
+}
+
+// x[j * B + b] = embeddings of the token of row b in column t + j (tokens [cols][B])
+__global__ __launch_bounds__(256) void k_embed_columns(const int32_t *tokens, const int32_t *start, int t, const bf16_t *tok_emb,
+                                                       const bf16_t *pos_emb, float *x, int B, int d, int V) {
+  const int row = blockIdx.x, d4 = d >> 2;
+  const int tok = min(max(tokens[row], 0), V - 1), pos = max(t + row / B - start[row % B], 0);
+  const uint2 *te = (const uint2 *)(tok_emb + (long)tok * d), *pe = (const uint2 *)(pos_emb + (long)pos * d);
+  for (int c = threadIdx.x; c < d4; c += 256) {
+    const uint2 a = te[c], p = pe[c];
+    ((floatx4 *)x)[(long)row * d4 + c] = floatx4{bf2f(a.x & 0xffffu) + bf2f(p.x & 0xffffu), bf2f(a.x >> 16) + bf2f(p.x >> 16),
+                                                 bf2f(a.y & 0xffffu) + bf2f(p.y & 0xffffu), bf2f(a.y >> 16) + bf2f(p.y >> 16)};
+  }
+}
+void bf16_embed_columns(hipStream_t s, const int32_t *tokens, const int32_t *start, int t, int cols, const bf16_t *tok_emb,
+                        const bf16_t *pos_emb, float *x, int B, int d, int V) {
+  SKD_LAUNCH(k_embed_columns, dim3(cols * B), dim3(256), 0, s, tokens, start, t, tok_emb, pos_emb, x, B, d, V);
 }
 
 __global__ __launch_bounds__(1024) void k_ln_rows_wide(const float *x, const float *g, const float *bt, bf16_t *a_out, int d) {

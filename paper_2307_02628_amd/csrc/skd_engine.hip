@@ -12,6 +12,7 @@
 
 #include "../../include/skd.h"
 #include "gave_up.h"
+#include "kv_ops.h"
 #include "sample_rows.h"
 #include "skd_kernels.h"
 
@@ -106,6 +107,7 @@ struct skd_state {
   hipStream_t stream = nullptr;
   int B_pad = 0, dh = 0;
   bool bf16 = true;
+  bool kv8 = false;                // bf16 path with 8-bit pages (kv_ops.h)
   std::vector<void *> allocs;
   // weights
   std::vector<LayerW> lw;
@@ -162,6 +164,11 @@ struct skd_state {
   bf16_t *pf_a = nullptr, *pf_q = nullptr, *pf_o = nullptr, *pf_u = nullptr;
   CacheTile *pf_tiles = nullptr;  // cache place of each 16-row tile of the prompt pass
   int32_t *pf_seq = nullptr, *pf_first = nullptr;  // row map of the prompt pass (sequence of each row, first row of each sequence)
+  // several columns at once (allocated by the first skd_decode_chunk, or by the first prompt of a state with 8-bit pages)
+  int ck_cols = 0;                 // columns at a time
+  float *ck_x = nullptr, *ck_partial = nullptr, *ck_attn = nullptr;
+  bf16_t *ck_a = nullptr, *ck_qkv = nullptr, *ck_o = nullptr, *ck_u = nullptr;
+  int32_t *ck_tokens = nullptr;    // host buffers: [columns][B]
   int prefill_mode = 1;            // 1 = whole prompt per layer (bf16 path), 0 = column by column
   int prefill_tiles = 1;           // 1 = prompt projections as plan_rows says, 0 = 128-row chunks on the skinny kernel
   int prefill_wr = 0, prefill_ar = 0, prefill_split = 1;  // forced tile of the prompt projections (0 = plan_rows decides)
@@ -205,9 +212,9 @@ int check_config(const skd_config &c) {
   if (c.n_min < 1 || c.n_min > c.n_max || c.n_max > c.L) return SKD_ERR_SHAPE;
   if (c.warmup < 0 || c.warmup > c.n_min) return SKD_ERR_SHAPE;
   if (c.page_tokens < 0 || c.page_tokens % 32) return SKD_ERR_SHAPE;
-  if (c.dtype != SKD_BF16 && c.dtype != SKD_FP32) return SKD_ERR_SHAPE;
+  if (c.dtype != SKD_BF16 && c.dtype != SKD_FP32 && c.dtype != SKD_BF16_KV8) return SKD_ERR_SHAPE;
   if (c.io_on_device != 0 && c.io_on_device != 1) return SKD_ERR_SHAPE;
-  if (c.dtype == SKD_BF16) {
+  if (c.dtype != SKD_FP32) {
     const int dh = c.d_model / c.n_heads;
     if (dh != 64 && dh != 128) return SKD_ERR_SHAPE;
     if (c.d_model % 32 || c.ffn % 32 || c.d_model > 16384) return SKD_ERR_SHAPE;
@@ -390,8 +397,8 @@ int build_kv(skd_state *st) {
   if (next > 0x7fffffffLL) return SKD_ERR_NOMEM;
   st->pages_reserved = next;
   st->pages_dense = (int64_t)c.L * c.batch * g.max_pages;
-  const size_t esz = st->bf16 ? 2 : 4;
-  const size_t bytes = (size_t)next * g.page_elems * esz;
+  const size_t page = st->kv8 ? (size_t)kv8_page_bytes(g.H, g.dh, pt) : (size_t)g.page_elems * (st->bf16 ? 2 : 4);
+  const size_t bytes = (size_t)next * page;
   void *pool = nullptr;
   HIPCHECK(hipMalloc(&pool, std::max<size_t>(bytes, 256)));
   st->allocs.push_back(pool);
@@ -465,6 +472,41 @@ int prof_drain(skd_state *st) {
 
 const int32_t *bt_layer(const skd_state *st, int l) {
   return st->bt_dev + (size_t)l * st->cfg.batch * st->geom.max_pages;
+}
+// A layer's cache as kv_ops.h takes it (bf16 path), and `cols` columns of all rows from column t on.
+KvView layer_cache(const skd_state *st, int l) {
+  KvView v{};
+  v.g = st->geom;
+  v.fp8 = st->kv8;
+  v.pages = (int)st->pages_reserved;
+  v.rows = st->cfg.batch;
+  v.page_bytes = st->kv8 ? kv8_page_bytes(v.g.H, v.g.dh, v.g.page_tokens) : 2 * v.g.page_elems;
+  v.pool = (unsigned char *)st->pool;
+  v.table = bt_layer(st, l);
+  return v;
+}
+KvTokens columns(const skd_state *st, int t, int cols) {
+  KvTokens tk{};
+  tk.kind = KvTokens::COLUMNS;
+  tk.past = st->start_dev;
+  tk.tokens = cols * st->cfg.batch;
+  tk.count = tk.max_new = cols;
+  tk.t = t;
+  tk.step = st->cfg.batch;
+  tk.max_past = std::max(t - st->start_min, 0);
+  tk.room = st->geom.max_pages * st->geom.page_tokens;
+  return tk;
+}
+KvAttend column_attention(const skd_state *st, int l, int t, int cols) {
+  KvAttend a{};
+  a.kv = layer_cache(st, l);
+  a.tk = columns(st, t, cols);
+  a.heads = st->cfg.n_heads;
+  a.group = 1;
+  a.c = 1.4426950408889634f / sqrtf((float)st->dh);
+  a.order = st->ragged ? st->order_dev : nullptr;
+  a.splits = kv_attend_splits(a.kv, a.tk, a.heads);
+  return a;
 }
 
 // a decode projection on the kernel its plan names; returns the row groups launched or -1
@@ -546,7 +588,17 @@ int run_layer(skd_state *st, int l, int t, const LayerW *prev, const LayerW *nex
   ga.attn_part = st->attn_part; ga.attn_splits = aa.splits;
   // one or two rows: the projection merges the attention's splits
   aa.merge = !(st->fuse_ln && bf16_gemm_merge_check(ga, st->p_out.R, st->p_out.waves) > 0);
-  { ProfScope ps_(st, SKD_PROF_ATTENTION); bf16_attention(s, aa); }
+  if (st->kv8) {
+    KvAttend ka = column_attention(st, l, t, 1);
+    ka.q = KvRows{q, d, 0, false}; ka.o = KvRows{o, d, 0, true}; ka.k = KvRows{st->kv_new, 2 * d, 0, false}; ka.v = KvRows{st->kv_new, 2 * d, d, false};
+    ka.part = st->attn_part;
+    aa.splits = 1;  // its shares are joined
+    ProfScope ps_(st, SKD_PROF_ATTENTION);
+    kv_attend(s, ka);
+  } else {
+    ProfScope ps_(st, SKD_PROF_ATTENTION);
+    bf16_attention(s, aa);
+  }
   {
     ProfScope ps_(st, SKD_PROF_GEMM_OUT);
     grc = aa.splits > 1 && !aa.merge ? bf16_gemm_merge(s, ga, st->p_out.R, st->p_out.U, st->p_out.waves) : launch_gemm(s, ga, EPI_PARTIAL, st->p_out);
@@ -741,7 +793,8 @@ static int create_impl(const skd_config *cfg, const skd_weights *w, void *hip_st
   if (n_table) st->n_table.assign(n_table, n_table + cfg->sequence_length);
   if (!st->cfg.page_tokens) st->cfg.page_tokens = 64;
   st->stream = (hipStream_t)hip_stream;
-  st->bf16 = cfg->dtype == SKD_BF16;
+  st->bf16 = cfg->dtype != SKD_FP32;
+  st->kv8 = cfg->dtype == SKD_BF16_KV8;
   st->dh = cfg->d_model / cfg->n_heads;
   const skd_config &c = st->cfg;
   const int B = c.batch, d = c.d_model, f = c.ffn, V = c.vocab, L = c.L;
@@ -906,7 +959,13 @@ static int create_impl(const skd_config *cfg, const skd_weights *w, void *hip_st
     A(&t16, (size_t)Bp * f); st->u = t16;
     A(&st->kv_new, (size_t)B * 2 * d);
     A(&st->partial, std::max((size_t)st->max_split * Bp * d, st->head_parts ? (size_t)st->p_head.split * Bp * ((V + 15) / 16 * 16) : 0));
-    A(&st->attn_part, (size_t)st->attn_splits * B * c.n_heads * (st->dh + 4));
+    size_t attn_part = (size_t)st->attn_splits * B * c.n_heads * (st->dh + 4);
+    if (st->kv8) {
+      const KvView kv = layer_cache(st, 0);
+      const KvTokens tk = columns(st, c.sequence_length - 1, 1);  // (the later the column the more shares)
+      attn_part = kv_attend_part(kv, tk, c.n_heads, kv_attend_splits(kv, tk, c.n_heads));
+    }
+    A(&st->attn_part, attn_part);
     GemmArgs ga{};
     ga.N = V;
     const int groups = std::max(bf16_head_tiles(ga, st->p_head.R, st->p_head.slots), bf16_gemm_groups(V, st->p_head.R));
@@ -921,7 +980,7 @@ static int create_impl(const skd_config *cfg, const skd_weights *w, void *hip_st
     A(&st->attn_part, (size_t)B * c.n_heads * c.sequence_length);
     A(&st->logits_dev, (size_t)B * V);
   }
-  if (rc == SKD_OK && st->bf16 && bf16_team_ok(d, f, B) && env_int("SKD_TEAM", 1) != 0 && !launch_overrides()) rc = prepare_team(st);
+  if (rc == SKD_OK && st->bf16 && !st->kv8 && bf16_team_ok(d, f, B) && env_int("SKD_TEAM", 1) != 0 && !launch_overrides()) rc = prepare_team(st);
   if (rc != SKD_OK) return fail(rc);
   if (st->bf16 && !c.io_on_device) {
     const hipError_t e = hipHostMalloc((void **)&st->pin, sizeof(Pinned), hipHostMallocDefault);
@@ -1063,6 +1122,44 @@ RowsGemm plan_rows(int N, int K, int rows, bool split_ok) {
 // positions): activation rows are the real (sequence, position) pairs (left padding gets no rows), attention is
 // causal over the pages the QKV projection has just filled.  A row depends on rows of its own sequence before it
 // only, so what padding rows hold never matters.
+// Projection of `rows` rows (whole 16-row tiles, or a decode kernel's batch) as its plan says; rows_pad: of the partial sums.
+static int rows_gemm(hipStream_t s, GemmArgs g, int epi, const RowsGemm &p, int rows, int rows_pad) {
+  g.split = p.split;
+  g.B_pad = p.kind == RowsGemm::SKINNY ? p.B_pad : rows_pad;
+  g.rows = rows;
+  if (p.kind == RowsGemm::TILE) return bf16_gemm_tile(s, g, epi);
+  if (p.kind == RowsGemm::MID) return bf16_gemm_mid(s, g, epi, p.wr, p.ar);
+  if (p.kind == RowsGemm::SKINNY) {
+    g.rows = epi == EPI_RELU ? p.B_pad : 0;
+    g.B = rows;
+    return bf16_gemm(s, g, epi, p.R, 1, 8);
+  }
+  g.B_pad = 128;  // 128-row chunks through the skinny kernel
+  g.rows = (rows + 127) / 128 * 128;
+  return bf16_gemm(s, g, epi, g.N % 64 ? 1 : 4, 1, 4);
+}
+// The q | k | v projection into `out` ([rows_pad][3 d]): as activation tiles, or up to 64 rows (the decode kernel) as rows of q and
+// rows of k | v; where they are is put into `a`.
+static int rows_qkv(skd_state *st, GemmArgs g, int rows, int rows_pad, bf16_t *out, const RowsGemm &p, KvAttend &a) {
+  const int d = st->cfg.d_model;
+  if (p.kind == RowsGemm::SKINNY) {
+    bf16_t *kv = out + (size_t)p.B_pad * d;
+    g.q_out = out;
+    g.kv_new = kv;
+    if (rows_gemm(st->stream, g, EPI_QKV, p, rows, rows_pad) < 0) return SKD_ERR_SHAPE;
+    a.q = KvRows{out, d, 0, false};
+    a.k = KvRows{kv, 2 * d, 0, false};
+    a.v = KvRows{kv, 2 * d, d, false};
+    return SKD_OK;
+  }
+  g.act_out = out;
+  if (p.kind == RowsGemm::CHUNKS || rows_gemm(st->stream, g, EPI_ACT, p, rows, rows_pad) < 0) return SKD_ERR_SHAPE;
+  a.q = KvRows{out, 3 * d, 0, true};
+  a.k = KvRows{out, 3 * d, d, true};
+  a.v = KvRows{out, 3 * d, 2 * d, true};
+  return SKD_OK;
+}
+
 static int prefill_batched(skd_state *st, const int32_t *cols) {
   const skd_config &c = st->cfg;
   const int B = c.batch, P = c.prompt_size, d = c.d_model, f = c.ffn, L = c.L;
@@ -1076,7 +1173,7 @@ static int prefill_batched(skd_state *st, const int32_t *cols) {
       return SKD_OK;
     };
     SKDCHECK(rows_alloc(&st->pf_a, (size_t)cap * d));
-    SKDCHECK(rows_alloc(&st->pf_q, (size_t)cap * d));
+    SKDCHECK(rows_alloc(&st->pf_q, (size_t)cap * d * (st->kv8 ? 3 : 1)));  // 8-bit pages: q | k | v
     SKDCHECK(rows_alloc(&st->pf_o, (size_t)cap * d));
     SKDCHECK(rows_alloc(&st->pf_u, (size_t)cap * f));
     SKDCHECK(dev_alloc(st, &st->pf_partial, (size_t)std::min(kRowsPartialMax, 16 * cap * d)));
@@ -1113,7 +1210,7 @@ static int prefill_batched(skd_state *st, const int32_t *cols) {
     }
     return p;
   };
-  const RowsGemm r_qkv = plan(3 * d, d, false), r_out = plan(d, d, true), r_ffn1 = plan(f, d, false), r_ffn2 = plan(d, f, true);
+  const RowsGemm r_qkv = st->kv8 ? plan_rows(3 * d, d, rows, false) : plan(3 * d, d, false), r_out = plan(d, d, true), r_ffn1 = plan(f, d, false), r_ffn2 = plan(d, f, true);
   auto stride = [&](const RowsGemm &p) { return p.kind == RowsGemm::SKINNY ? p.B_pad : rows_pad; };  // of the partial sums
   auto proj = [&](GemmArgs g, int epi, const RowsGemm &p) {
     if (p.partial) epi = EPI_PARTIAL;
@@ -1145,10 +1242,25 @@ static int prefill_batched(skd_state *st, const int32_t *cols) {
     ga.B = B; ga.rm = rm; ga.cache_tiles = st->pf_tiles; ga.kv = st->geom; ga.d = d; ga.partial = st->pf_partial; ga.x = st->pf_x;
     ga.W = (const bf16_t *)w.wqkv; ga.G = st->p_qkv.R; ga.A = st->pf_a; ga.bias = w.bqkv; ga.N = 3 * d; ga.K = d;
     ga.q_out = st->pf_q; ga.kv_pool = (bf16_t *)st->pool; ga.bt_layer = bt_layer(st, l);
+    KvAttend ka{};
+    if (st->kv8) {
+      // k and v are filed by a kernel of their own, which sees a whole head of a token at once
+      ka.kv = layer_cache(st, l);
+      ka.tk.kind = KvTokens::PROMPT; ka.tk.first = st->pf_first; ka.tk.past = st->start_dev; ka.tk.tokens = rows; ka.tk.count = P; ka.tk.step = 1;
+      ka.tk.max_new = max_len; ka.tk.room = st->geom.max_pages * st->geom.page_tokens;
+      SKDCHECK(rows_qkv(st, ga, rows, rows_pad, st->pf_q, r_qkv, ka));
+      if (l < L - 1 || !last_as_column) {
+        ka.heads = c.n_heads; ka.group = 1; ka.c = 1.4426950408889634f / sqrtf((float)st->dh); ka.o = KvRows{st->pf_o, d, 0, true};
+        ka.splits = 1;
+        kv_attend(s, ka);
+      } else {
+        kv_append(s, ka.kv, ka.tk, ka.k, ka.v);
+      }
+    }
     if (l == L - 1 && last_as_column) {
       ga.t0 = d / 16;
       ga.N = 2 * d;
-      if (proj(ga, EPI_QKV_ROWS, r_kv) < 0) return SKD_ERR_SHAPE;
+      if (!st->kv8 && proj(ga, EPI_QKV_ROWS, r_kv) < 0) return SKD_ERR_SHAPE;
       bf16_last_rows_ln(s, st->pf_x, rm, nullptr, 0, 0, nullptr, w.ln1_g, w.ln1_b, st->x, (bf16_t *)st->a, B, d);
       const int profiling = st->profiling;
       st->profiling = 0;  // the timed classes are those of decode steps
@@ -1158,11 +1270,13 @@ static int prefill_batched(skd_state *st, const int32_t *cols) {
       st->kv_len[l] = P;
       break;
     }
-    if (proj(ga, EPI_QKV_ROWS, r_qkv) < 0) return SKD_ERR_SHAPE;
-    AttnRowsArgs aa{};
-    aa.q = st->pf_q; aa.pool = (const bf16_t *)st->pool; aa.bt_layer = bt_layer(st, l); aa.rm = rm;
-    aa.B = B; aa.max_len = max_len; aa.kv = st->geom; aa.o = st->pf_o;
-    bf16_attention_rows(s, aa);
+    if (!st->kv8) {
+      if (proj(ga, EPI_QKV_ROWS, r_qkv) < 0) return SKD_ERR_SHAPE;
+      AttnRowsArgs aa{};
+      aa.q = st->pf_q; aa.pool = (const bf16_t *)st->pool; aa.bt_layer = bt_layer(st, l); aa.rm = rm;
+      aa.B = B; aa.max_len = max_len; aa.kv = st->geom; aa.o = st->pf_o;
+      bf16_attention_rows(s, aa);
+    }
     ga.W = (const bf16_t *)w.wo; ga.G = st->p_out.R; ga.A = st->pf_o; ga.bias = w.bo; ga.N = d; ga.K = d;
     if (proj(ga, EPI_RESID, r_out) < 0) return SKD_ERR_SHAPE;
     if (r_out.partial) bf16_reduce_ln(s, st->pf_partial, r_out.split, stride(r_out), w.bo, st->pf_x, st->pf_x, w.ln2_g, w.ln2_b, st->pf_a, rows, d);
@@ -1186,6 +1300,139 @@ static int prefill_batched(skd_state *st, const int32_t *cols) {
   st->have_hidden = true;
   st->have_argmax = false;
   return SKD_OK;
+}
+
+// Several columns at once: what is between them and a prompt is the depth, which falls from column to column.  A layer's columns
+// are the first ones of the chunk (a layer that has left does not come back), so with rows in the order [column][row of the
+// batch] its rows are the first ones too.
+static int chunk_workspace(skd_state *st) {
+  if (st->ck_cols) return SKD_OK;
+  const skd_config &c = st->cfg;
+  const int B = c.batch, d = c.d_model;
+  // rows at a time: enough to fill the chip, few enough for the partial sums
+  const long most = std::min(4096L, kRowsPartialMax / d - 256);
+  const int cols = (int)std::max(1L, std::min((long)(c.sequence_length - c.prompt_size), most / B));
+  const size_t cap = ((size_t)cols * B + 255) / 256 * 256;
+  auto rows_alloc = [&](auto **p, size_t n) -> int {
+    SKDCHECK(dev_alloc(st, p, n));
+    HIPCHECK(hipMemsetAsync(*p, 0, n * sizeof(**p), st->stream));  // once: padding rows are read by the projections
+    return SKD_OK;
+  };
+  SKDCHECK(rows_alloc(&st->ck_x, cap * d));
+  SKDCHECK(rows_alloc(&st->ck_a, cap * d));
+  SKDCHECK(rows_alloc(&st->ck_qkv, cap * 3 * d));
+  SKDCHECK(rows_alloc(&st->ck_o, cap * d));
+  SKDCHECK(rows_alloc(&st->ck_u, cap * c.ffn));
+  SKDCHECK(dev_alloc(st, &st->ck_partial, std::min((size_t)kRowsPartialMax, 16 * cap * d)));
+  SKDCHECK(dev_alloc(st, &st->ck_tokens, (size_t)cols * B));
+  size_t part = 0;
+  for (int m = 1; m <= cols; ++m) {
+    KvTokens tk = columns(st, c.sequence_length, m);
+    tk.max_past = c.sequence_length;  // (prompts without padding too)
+    const KvView kv = layer_cache(st, 0);
+    part = std::max(part, kv_attend_part(kv, tk, c.n_heads, kv_attend_splits(kv, tk, c.n_heads)));
+  }
+  SKDCHECK(dev_alloc(st, &st->ck_attn, part));
+  st->ck_cols = cols;
+  return SKD_OK;
+}
+// Columns t .. t + m - 1 (m <= ck_cols) with the device tokens [m][B].
+static int run_columns(skd_state *st, int t, int m, const int32_t *tokens) {
+  const skd_config &c = st->cfg;
+  const int B = c.batch, d = c.d_model, f = c.ffn, L = c.L;
+  hipStream_t s = st->stream;
+  std::vector<int> cols(L, 0);  // of each layer
+  for (int j = 0; j < m; ++j) {
+    const int n = state_active_layers(st, t + j, st->layers_tmp.data());
+    if (n < 0) return n;
+    for (int i = 0; i < n; ++i) {
+      const int l = st->layers_tmp[i];
+      if (cols[l] != j) return SKD_ERR_SCHEDULE;
+      cols[l] = j + 1;
+    }
+  }
+  for (int l = 0; l < L; ++l) {
+    if (cols[l] && st->kv_len[l] != t) return SKD_ERR_ORDER;
+    if (cols[l] && t + cols[l] > st->kv_cap[l]) return SKD_ERR_NOMEM;
+  }
+  bf16_embed_columns(s, tokens, st->start_dev, t, m, (const bf16_t *)st->tok_emb, (const bf16_t *)st->pos_emb, st->ck_x, B, d, c.vocab);
+  int normed = 0;  // rows whose LayerNorm 1 of the layer at hand is in ck_a
+  for (int l = 0; l < L; ++l) {
+    if (!cols[l]) continue;
+    int next = l + 1;
+    while (next < L && !cols[next]) ++next;
+    const LayerW &w = st->lw[l];
+    const int rows = cols[l] * B, rows_pad = (rows + 255) / 256 * 256;
+    if (normed < rows) bf16_ln_rows(s, st->ck_x, w.ln1_g, w.ln1_b, st->ck_a, rows, d);
+    GemmArgs ga{};
+    ga.B = B; ga.kv = st->geom; ga.d = d; ga.partial = st->ck_partial;
+    ga.W = (const bf16_t *)w.wqkv; ga.G = st->p_qkv.R; ga.A = st->ck_a; ga.bias = w.bqkv; ga.N = 3 * d; ga.K = d;
+    KvAttend ka = column_attention(st, l, t, cols[l]);
+    SKDCHECK(rows_qkv(st, ga, rows, rows_pad, st->ck_qkv, plan_rows(3 * d, d, rows, false), ka));
+    ka.o = KvRows{st->ck_o, d, 0, true};
+    ka.part = st->ck_attn;
+    kv_attend(s, ka);
+    // the residual rows of later columns pass this layer by: partial sums, which are added to whole rows only
+    auto resid = [&](const void *W, int G, const bf16_t *A, int K, const float *bias, const float *g, const float *b) -> int {
+      const RowsGemm p = plan_rows(d, K, rows, true);
+      ga.W = (const bf16_t *)W; ga.G = G; ga.A = A; ga.bias = nullptr; ga.N = d; ga.K = K;
+      if (p.kind == RowsGemm::CHUNKS || rows_gemm(s, ga, EPI_PARTIAL, p, rows, rows_pad) < 0) return SKD_ERR_SHAPE;
+      bf16_reduce_ln(s, st->ck_partial, p.split, p.kind == RowsGemm::SKINNY ? p.B_pad : rows_pad, bias, st->ck_x, st->ck_x, g, b, st->ck_a, rows, d);
+      return SKD_OK;
+    };
+    SKDCHECK(resid(w.wo, st->p_out.R, st->ck_o, d, w.bo, w.ln2_g, w.ln2_b));
+    ga.W = (const bf16_t *)w.w1; ga.G = st->p_ffn1.R; ga.A = st->ck_a; ga.bias = w.b1; ga.N = f; ga.K = d; ga.act_out = st->ck_u;
+    if (rows_gemm(s, ga, EPI_RELU, plan_rows(f, d, rows, false), rows, rows_pad) < 0) return SKD_ERR_SHAPE;
+    const LayerW &after = st->lw[next < L ? next : l];
+    SKDCHECK(resid(w.w2, st->p_ffn2.R, st->ck_u, f, w.b2, after.ln1_g, after.ln1_b));
+    normed = rows;
+    st->kv_len[l] = t + cols[l];
+  }
+  // hidden state of the last column, and its final LayerNorm, where the heads expect them
+  HIPCHECK(hipMemcpyAsync(st->x, st->ck_x + (size_t)(m - 1) * B * d, (size_t)B * d * sizeof(float), hipMemcpyDeviceToDevice, s));
+  bf16_ln_rows(s, st->x, st->lnf_g, st->lnf_b, (bf16_t *)st->a, B, d);
+  HIPCHECK(hipGetLastError());
+  st->have_hidden = true;
+  st->have_argmax = false;
+  return SKD_OK;
+}
+
+extern "C" int skd_decode_chunk(skd_state *st, int32_t t, int32_t cols, const int32_t *tokens) {
+  if (!st || !tokens) return SKD_ERR_NULL;
+  const skd_config &c = st->cfg;
+  const int B = c.batch;
+  if (!st->prefilled) return SKD_ERR_ORDER;
+  if (t < 0 || cols < 1 || cols > c.sequence_length || t > c.sequence_length - cols) return SKD_ERR_RANGE;
+  if (t != c.prompt_size + st->steps_done) return SKD_ERR_ORDER;
+  if (!c.io_on_device)
+    for (size_t i = 0; i < (size_t)B * cols; ++i)
+      if (tokens[i] < 0 || tokens[i] >= c.vocab) return SKD_ERR_RANGE;
+  SKDCHECK(intact(st));
+  if (st->bf16) SKDCHECK(chunk_workspace(st));
+  const int at_once = st->bf16 ? st->ck_cols : 1;
+  std::vector<int32_t> some;
+  for (int done = 0; done < cols; done += at_once) {
+    const int m = std::min(at_once, cols - done);
+    const int32_t *dev = tokens + (size_t)done * B;
+    if (!c.io_on_device) {
+      some.resize((size_t)m * B);
+      for (int b = 0; b < B; ++b)
+        for (int j = 0; j < m; ++j) some[(size_t)j * B + b] = tokens[(size_t)b * cols + done + j];
+      int32_t *to = st->bf16 ? st->ck_tokens : st->tok_dev;
+      HIPCHECK(hipMemcpyAsync(to, some.data(), some.size() * sizeof(int32_t), hipMemcpyHostToDevice, st->stream));
+      HIPCHECK(hipStreamSynchronize(st->stream));
+      dev = to;
+    }
+    if (st->bf16) {
+      SKDCHECK(run_columns(st, t + done, m, dev));
+    } else {
+      const int n = state_active_layers(st, t + done, st->layers_tmp.data());
+      if (n < 0) return n;
+      SKDCHECK(run_column(st, t + done, dev, st->layers_tmp.data(), n));
+    }
+    st->steps_done += m;
+  }
+  return c.io_on_device ? SKD_OK : wait_stream(st);
 }
 
 extern "C" int skd_prefill(skd_state *st, const int32_t *tokens, const uint8_t *attn_mask) {
@@ -1546,6 +1793,50 @@ extern "C" int skd_debug_read_hidden(skd_state *st, float *x_out) {
   return wait_stream(st);
 }
 
+// Layer l's 8-bit pages from device arrays [B][cols][d] fp32 (rounded to bf16 first), and back.
+static int kv_load_8(skd_state *st, int l, const float *k, const float *v, int cols) {
+  const int B = st->cfg.batch, d = st->cfg.d_model;
+  const size_t n = (size_t)B * cols * d;
+  std::vector<int32_t> first(B);
+  for (int b = 0; b < B; ++b) first[b] = b * cols + st->start_host[b];
+  bf16_t *k16 = nullptr;
+  HIPCHECK(hipMalloc((void **)&k16, 2 * n * sizeof(bf16_t) + B * sizeof(int32_t)));
+  int32_t *first_dev = (int32_t *)(k16 + 2 * n);
+  prep_matrix_rm_bf16(st->stream, k, 0, k16, (long)n);
+  prep_matrix_rm_bf16(st->stream, v, 0, k16 + n, (long)n);
+  hipError_t e = hipMemcpyAsync(first_dev, first.data(), B * sizeof(int32_t), hipMemcpyHostToDevice, st->stream);
+  if (e == hipSuccess) {
+    KvTokens tk{};
+    tk.kind = KvTokens::PROMPT; tk.first = first_dev; tk.past = st->start_dev; tk.tokens = B * cols; tk.count = cols; tk.step = 1;
+    tk.max_new = cols - st->start_min; tk.room = st->geom.max_pages * st->geom.page_tokens;
+    kv_append(st->stream, layer_cache(st, l), tk, KvRows{k16, d, 0, false}, KvRows{k16 + n, d, 0, false});
+    e = hipStreamSynchronize(st->stream);
+  }
+  (void)hipFree(k16);
+  return e == hipSuccess ? SKD_OK : hip_failed(e);
+}
+static int kv_read_8(skd_state *st, int l, int b, int len, float *k, float *v) {
+  const int d = st->cfg.d_model, start = st->start_host.empty() ? 0 : st->start_host[b];
+  int32_t *zero = nullptr;
+  HIPCHECK(hipMalloc((void **)&zero, sizeof(int32_t)));
+  hipError_t e = hipSuccess;
+  for (hipError_t r : {hipMemsetAsync(zero, 0, sizeof(int32_t), st->stream), hipMemsetAsync(k, 0, (size_t)len * d * sizeof(float), st->stream),
+                       hipMemsetAsync(v, 0, (size_t)len * d * sizeof(float), st->stream)})
+    if (e == hipSuccess) e = r;
+  if (e == hipSuccess && len > start) {
+    KvView kv = layer_cache(st, l);
+    kv.table += (size_t)b * kv.g.max_pages;
+    kv.rows = 1;
+    KvTokens tk{};
+    tk.kind = KvTokens::PROMPT; tk.first = tk.past = zero; tk.tokens = tk.count = tk.max_new = len - start; tk.step = 1;
+    tk.room = st->geom.max_pages * st->geom.page_tokens;
+    kv_read(st->stream, kv, tk, false, KvRows{k + (size_t)start * d, d, 0, false}, KvRows{v + (size_t)start * d, d, 0, false});
+  }
+  if (e == hipSuccess) e = hipStreamSynchronize(st->stream);
+  (void)hipFree(zero);
+  return e == hipSuccess ? SKD_OK : hip_failed(e);
+}
+
 extern "C" int skd_debug_kv_load(skd_state *st, int32_t cols, const float *const *Kin, const float *const *Vin,
                                  const int32_t *start_in) {
   if (!st) return SKD_ERR_NULL;
@@ -1578,7 +1869,9 @@ extern "C" int skd_debug_kv_load(skd_state *st, int32_t cols, const float *const
       rc = SKD_ERR_HIP;
       break;
     }
-    if (st->bf16)
+    if (st->kv8) {
+      if (have) rc = kv_load_8(st, l, kd, vd, cols);
+    } else if (st->bf16)
       kv_load_bf16(st->stream, have ? kd : nullptr, have ? vd : nullptr, (bf16_t *)st->pool, bt_layer(st, l), st->start_dev, cols, B, st->geom);
     else
       kv_load_f32(st->stream, have ? kd : nullptr, have ? vd : nullptr, (float *)st->pool, bt_layer(st, l), cols, B, st->geom);
@@ -1605,10 +1898,12 @@ extern "C" int skd_debug_kv_read(skd_state *st, int32_t layer, int32_t b, float 
   HIPCHECK(hipMalloc((void **)&kd, (size_t)len * d * sizeof(float)));
   if (hipMalloc((void **)&vd, (size_t)len * d * sizeof(float)) != hipSuccess) { (void)hipFree(kd); return SKD_ERR_NOMEM; }
   const int32_t *row = bt_layer(st, layer) + (size_t)b * st->geom.max_pages;
-  if (st->bf16) kv_read_bf16(st->stream, (const bf16_t *)st->pool, row, st->start_host.empty() ? 0 : st->start_host[b], len, kd, vd, st->geom);
-  else kv_read_f32(st->stream, (const float *)st->pool, row, len, kd, vd, st->geom);
   int rc = SKD_OK;
-  if (hipMemcpyAsync(k_out, kd, (size_t)len * d * sizeof(float), hipMemcpyDeviceToHost, st->stream) != hipSuccess ||
+  if (st->kv8) rc = kv_read_8(st, layer, b, len, kd, vd);
+  else if (st->bf16) kv_read_bf16(st->stream, (const bf16_t *)st->pool, row, st->start_host.empty() ? 0 : st->start_host[b], len, kd, vd, st->geom);
+  else kv_read_f32(st->stream, (const float *)st->pool, row, len, kd, vd, st->geom);
+  if (rc != SKD_OK) {
+  } else if (hipMemcpyAsync(k_out, kd, (size_t)len * d * sizeof(float), hipMemcpyDeviceToHost, st->stream) != hipSuccess ||
       hipMemcpyAsync(v_out, vd, (size_t)len * d * sizeof(float), hipMemcpyDeviceToHost, st->stream) != hipSuccess ||
       hipStreamSynchronize(st->stream) != hipSuccess)
     rc = SKD_ERR_HIP;

@@ -112,7 +112,8 @@ enum GemmEpilogue {
   EPI_RELU = 2,     // + bias, ReLU -> activation tiles bf16 [B_pad][N]
   EPI_LOGITS = 3,   // optional fp32 logits [B][N] + per-workgroup (max, argmax) partials
   EPI_QKV_ROWS = 4, // batched prompt: + bias; q -> activation tiles [rows][d]; k/v -> KV page slot of (sequence, position)
-  EPI_RESID = 5     // batched prompt: x[row][n] += value + bias (fp32 residual stream)
+  EPI_RESID = 5,    // batched prompt: x[row][n] += value + bias (fp32 residual stream)
+  EPI_ACT = 6       // output tiles of many rows: + bias -> activation tiles bf16 [rows][N]
 };
 
 struct GemmArgs {
@@ -175,7 +176,7 @@ int bf16_head_tiles(GemmArgs &a, int R, int slots);
 // shapes it does not handle; bf16_gemm_ws_check answers the same without launching.
 int bf16_gemm_ws(hipStream_t s, const GemmArgs &a, int epilogue, int R);
 int bf16_gemm_ws_check(const GemmArgs &a, int epilogue, int R);
-// Batched prompt only (a.rows > 0; EPI_QKV_ROWS, EPI_RESID, EPI_RELU or EPI_PARTIAL; a.split > 1 with EPI_PARTIAL
+// Many rows only (a.rows > 0; EPI_QKV_ROWS, EPI_RESID, EPI_RELU, EPI_ACT or EPI_PARTIAL; a.split > 1 with EPI_PARTIAL
 // only): output tiles with LDS-staged operands.  Buffers are padded to whole tiles of 256 rows: the rows past a.rows of
 // the last tile are read and written.  EPI_PARTIAL: fp32 sums [split][B_pad][N], B_pad = rows of that buffer.
 // Both return -1 for shapes that do not tile (nothing launched).
@@ -223,6 +224,9 @@ void bf16_attention_rows(hipStream_t s, const AttnRowsArgs &a);
 void bf16_embed_ln_rows(hipStream_t s, const int32_t *tokens, RowMap rm, int rows, const bf16_t *tok_emb,
                         const bf16_t *pos_emb, const float *g, const float *b, float *x, bf16_t *a_out, int B, int d,
                         int V);
+// x [cols * B][d]: embeddings of columns t .. t + cols - 1, tokens [cols][B]
+void bf16_embed_columns(hipStream_t s, const int32_t *tokens, const int32_t *start, int t, int cols, const bf16_t *tok_emb,
+                        const bf16_t *pos_emb, float *x, int B, int d, int V);
 void bf16_ln_rows(hipStream_t s, float *x, const float *g, const float *b, bf16_t *a_out, int rows, int d);
 // x_out[b][:] = row of sequence b's last prompt position (+ bias + sum of `split` partial sums [split][stride][d] when
 // split > 0); a_out = its LayerNorm

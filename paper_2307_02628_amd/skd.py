@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libskd.so")
 
 OK, ERR_NULL, ERR_SHAPE, ERR_RANGE, ERR_ORDER, ERR_SCHEDULE, ERR_NOMEM, ERR_HIP = 0, -1, -2, -3, -4, -5, -6, -7
-BF16, FP32 = 0, 1
+BF16, FP32, BF16_KV8 = 0, 1, 2
 HOST, DEVICE = 0, 1
 W_FP32, W_BF16 = 0, 1
 KV_BF16, KV_FP8 = 0, 1
@@ -26,7 +26,7 @@ EXPORTS = ["skd_schedule", "skd_active_layers", "skd_create", "skd_create_with_s
            "skd_logits_argmax", "skd_logits_argmax_noalloc", "skd_logits_sample", "skd_rewind", "skd_profile_enable", "skd_profile_read", "skd_kv_len", "skd_kv_pages_reserved", "skd_kv_pages_dense", "skd_synchronize",
            "skd_debug_read_hidden", "skd_debug_kv_load", "skd_debug_kv_read", "skd_destroy", "skd_strerror",
            "skd_last_hip_error", "skd_kv_page_bytes", "skd_kv_append", "skd_kv_read", "skd_kv_attend", "skd_kv_attend_workspace",
-           "skd_logits_sample_rows", "skd_sample", "skd_sample_workspace"]
+           "skd_logits_sample_rows", "skd_sample", "skd_sample_workspace", "skd_decode_chunk"]
 
 
 class Config(C.Structure):
@@ -99,6 +99,7 @@ def lib() -> C.CDLL:
         l.skd_kv_attend.argtypes = [P, P, I32, C.c_float, P, I64, P, I64, P, I64, P, I64, P, I64, P]
         l.skd_kv_attend_workspace.argtypes, l.skd_kv_attend_workspace.restype = [P, P, I32], I64
         l.skd_logits_sample_rows.argtypes = [P] * 5
+        l.skd_decode_chunk.argtypes = [P, I32, I32, P]
         l.skd_sample.argtypes = [P, I64, I32, I32, P, P, P, P, I64, P]
         l.skd_sample_workspace.argtypes, l.skd_sample_workspace.restype = [I32, I32], I64
         _lib = l
@@ -225,6 +226,20 @@ class Decoder:
 
     def decode_step(self, t: int, tokens_in=None):
         _check(self.decode_step_rc(t, tokens_in), "skd_decode_step")
+
+    def decode_chunk_rc(self, t: int, tokens) -> int:
+        """tokens: [B][cols] host array, or [cols][B] int32 device tensor with io_on_device."""
+        if isinstance(tokens, np.ndarray):
+            tokens = np.ascontiguousarray(tokens, dtype=np.int32)
+        elif not tokens.is_contiguous() or str(tokens.dtype) != "torch.int32":
+            raise ValueError("expected contiguous int32 tokens")
+        B, cols = tokens.shape if not self.cfg.io_on_device else tuple(tokens.shape)[::-1]
+        if B != self.cfg.batch:
+            raise ValueError(f"tokens of {self.cfg.batch} rows expected")
+        return self._lib.skd_decode_chunk(self._h, t, cols, _ptr_of(tokens))
+
+    def decode_chunk(self, t: int, tokens):
+        _check(self.decode_chunk_rc(t, tokens), "skd_decode_chunk")
 
     def logits_argmax(self, want_logits: bool = True):
         """Host-I/O form: returns (tokens[B] int32, logits[B,V] float32 or None)."""
