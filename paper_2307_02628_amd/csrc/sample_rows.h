@@ -5,6 +5,14 @@
 namespace skd {
 
 constexpr int SAMPLE_ROWS_VOCAB = 1 << 18;  // masses are counted in units of 2^-45 of the largest, their sum in 63 bits
+constexpr int SAMPLE_BINS = 1024;
+
+struct SampleBins {           // of a piece of a row; [rows][pieces]
+  uint64_t mass[SAMPLE_BINS + 1];
+  uint32_t count[SAMPLE_BINS + 1];
+  float top;                  // largest logit of the piece
+  uint64_t all;               // mass of the piece
+};
 
 struct SampleRows {
   const float *logits;
@@ -14,9 +22,12 @@ struct SampleRows {
   const float *temperature;
   const int32_t *top_k;
   const float *top_p, *min_p;
-  const float *u;           // [rows]
+  const float *u;             // [rows]
   int32_t *tokens, *tokens2;  // tokens2: second destination, or null
+  SampleBins *bins;           // sample_rows_bins(rows, vocab) of them
+  int piece, pieces;          // set by sample_rows: tokens of a piece
 };
+size_t sample_rows_bins(int rows, int vocab);
 void sample_rows(hipStream_t s, const SampleRows &a);
 
 }  // namespace skd

@@ -2,16 +2,21 @@
 //
 // With m_i = exp((z_i - max z) / T): kept are the tokens with m_i >= min_p that are among the k largest logits (ties with the k-th
 // too), of these the smallest set of largest ones whose mass reaches top_p of theirs (ties with the last too).  All three are
-// "z >= threshold", so the kernel looks for one threshold and then for the first index whose running mass over the tokens at or
+// "z >= threshold", so what is looked for is one threshold, and then the first index whose running mass over the tokens at or
 // above it exceeds u times their mass.
 //
-// Masses are integers in units of 2^-45 (exponentials in 64 bits, to 2^-44): sums do not depend on their order, so neither
-// atomics nor the share of a wave change a draw, and a draw that 64-bit arithmetic decides comes out the same.  What lies
-// 32 T below the largest logit has no mass, is never drawn, and is left out from the start.
+// Masses are integers in units of 2^-45 (exponentials in 64 bits, to 2^-44), sums of them integers or added in a fixed order in 64
+// bits: neither atomics nor the shares of the waves change a draw, and one that 64-bit arithmetic decides comes out the same.
+// What lies 32 T below the largest logit has no mass, is never drawn, and is left out from the start.
 //
-// One workgroup of 16 waves per row, every wave a contiguous piece of it.  Passes over the row: extremes; counts and masses
-// by bins of equal width; for top-k and top-p each the values of the bin in which the threshold lies, among which it is found bit
-// by bit; running masses.  The row comes from HBM once and from L2 after that.
+// Two launches.  k_sample_bins, pieces of rows over the whole chip: the piece's largest logit, and by bins of T / 32 (1024 and one
+// for what is left) how many tokens (rows with top-k or min-p) or how much mass (the others).  It reads the logits once
+// and is bound by that.  The bins lie on a grid that all pieces share.  k_sample_pick, a workgroup per row.  Few tokens left by
+// top-k or min-p, which is what they are for: the bins say from where on, those tokens go into LDS, and thresholds and token
+// are searched there bit by bit.  Top-p alone: the bin in which the threshold lies, whose values are searched; the piece in which
+// the running mass passes the target, and the token in it.  What does not fit into LDS is swept over again instead.
+// us, one workgroup per row for everything (six passes over the row, one CU's worth of exponentials) -> this: 128 rows of 131072
+// with mixed parameters 227 -> PICK128, one row of 50272 with top-p 75 -> PICK1.
 #include "sample_rows.h"
 
 #include <math.h>
@@ -24,71 +29,75 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int NW = 16, BINS = 2048, CAP = 4096, ROUND = 256;  // ROUND: tokens of a wave at a time
+constexpr int BINS = SAMPLE_BINS, NW = 16, CAP = 5120;  // CAP: values of a bin that are listed
 
 __device__ inline uint32_t key_of(float z) {  // ordered as the values are
   const uint32_t b = __float_as_uint(z);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ inline u64 shfl_xor64(u64 v, int o) {
-  return (u64)(uint32_t)__shfl_xor((int)(uint32_t)v, o) | (u64)(uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), o) << 32;
+__device__ inline float usable(float z) { return z == z ? z + 0.f : -INFINITY; }  // (-0 as 0)
+template <typename T>
+__device__ inline T shfl64(T v, int lane) {
+  const u64 b = __builtin_bit_cast(u64, v);
+  return __builtin_bit_cast(T, (u64)(uint32_t)__shfl((int)(uint32_t)b, lane) | (u64)(uint32_t)__shfl((int)(uint32_t)(b >> 32), lane) << 32);
 }
-__device__ inline u64 wave_sum64(u64 v) {
+template <typename T>
+__device__ inline T wave_sum64(T v, int lane) {
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) v += shfl_xor64(v, o);
+  for (int o = 1; o < 64; o *= 2) v += shfl64(v, lane ^ o);
+  return v;
+}
+template <typename T>
+__device__ inline T wave_scan64(T v, int lane) {  // sums of the lanes up to each
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const T x = shfl64(v, max(lane - o, 0));
+    if (lane >= o) v += x;
+  }
   return v;
 }
 
-__device__ inline float usable(float z) { return z == z ? z + 0.f : -INFINITY; }  // (-0 as 0)
-struct Shared {
-  double tab[64];             // 2^(i / 64)
-  uint32_t count[BINS];
-  u64 mass[BINS];
-  float cand[CAP];
-  int n_cand;
-  u64 part[2][NW];
-  float lo[NW], hi[NW];
-  u64 run[NW][SAMPLE_ROWS_VOCAB / NW / ROUND];
-};
-
-struct Row {
-  const float *z;
-  int V, begin, end;          // begin, end: this wave's tokens
-  bool vec;                   // 16-byte loads
-  float top;                  // largest logit
-  double c;                   // 64 log2(e) / T
-  int lane;
-
-  // f(first token of the lane's four, the four logits); NaN and what lies past the row: -infinity
-  template <typename F>
-  __device__ void each(F f) const {
-    constexpr int U = 4;
-    for (int i = begin; i < end; i += U * ROUND) {
-      floatx4 v[U];
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int at = i + k * ROUND + 4 * lane;
-        if (vec && at + 4 <= end) {
-          v[k] = *(const floatx4 *)(z + at);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[k][j] = at + j < end ? z[at + j] : -INFINITY;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        if (i + k * ROUND >= end) break;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[k][j] = usable(v[k][j]);
-        f(i + k * ROUND + 4 * lane, v[k]);
-      }
-    }
+// What a row's parameters come to.
+struct Params {
+  float T, top_p, u;
+  int k;
+  double log_min;             // log(min_p); 0 from 1 on, -32 where it is off (or below e^-32)
+  bool greedy, by_k, by_p;
+  bool counts, masses;        // what the bins hold: rows with top-k, all others, both with min-p alone
+  __device__ Params(const SampleRows &a, int b) {
+    T = a.temperature ? a.temperature[b] : 1.0f;
+    k = a.top_k ? a.top_k[b] : 0;
+    top_p = a.top_p ? fmaxf(a.top_p[b], 0.f) : 1.0f;
+    if (a.top_p && a.top_p[b] != a.top_p[b]) top_p = 1.0f;
+    const float m = a.min_p ? a.min_p[b] : 0.f;
+    log_min = m > 0.f ? fmax(m < 1.f ? log((double)m) : 0.0, -32.0) : -32.0;
+    u = fminf(fmaxf(a.u[b], 0.f), 0x1.fffffep-1f);  // (NaN: 0)
+    greedy = !(T > 0.f);
+    by_k = !greedy && k > 0 && k < a.vocab;
+    by_p = !greedy && top_p < 1.f;
+    counts = !greedy && (by_k || log_min > -32.0);
+    masses = !greedy && !by_k;
   }
-  // mass in units of 2^-45; 64 log2 of it is split into n + r: 2^(n / 64) from the table, 2^(r / 64) by its series (|r| <= 1/2:
-  // the first term left out is below 2^-44)
-  __device__ u64 mass(float x, const double *tab) const {
-    if (x == top) return 1ull << 45;
-    const double y = fmax(((double)x - (double)top) * c, -64.0 * 60);
+  // the smallest float that is not below top + T * log_min
+  __device__ float floor_of(float top) const {
+    const double f = (double)top + (double)T * log_min;
+    float x = (float)f;
+    if ((double)x < f) x = nextafterf(x, INFINITY);
+    return fminf(x, top);
+  }
+};
+// Places on the grid of bins, and masses against a largest logit.
+struct Grid {
+  float s;                    // 32 / T
+  double c;                   // 64 log2(e) / T
+  const double *tab;          // 2^(i / 64)
+  __device__ Grid(float T, const double *t) : s((float)(32.0 / (double)T)), c(64.0 * 1.44269504088896340736 / (double)T), tab(t) {}
+  __device__ float place(float z) const { return floorf(z * s); }
+  __device__ int bin(float top_place, float z) const { return (int)fminf(top_place - place(z), (float)BINS); }  // (NaN: the rest)
+  // 64 log2 of a mass is split into n + r: 2^(n / 64) from the table, 2^(r / 64) by its series (|r| <= 1/2: the first term left
+  // out is below 2^-44); in units of 2^-45, nearest
+  __device__ u64 mass(float z, float top) const {
+    const double y = fmax(((double)z - (double)top) * c, -64.0 * 60);
     const double t = y + 0x1.8p52, r = (y - (t - 0x1.8p52)) * (0.69314718055994530942 / 64);
     const int n = (int)(uint32_t)__double_as_longlong(t);
     const double p = 1.0 + r * (1.0 + r * (0.5 + r * (1.0 / 6 + r * (1.0 / 24))));
@@ -96,262 +105,573 @@ struct Row {
     return (u64)(__double_as_longlong(m + 128.0) - __double_as_longlong(128.0));
   }
 };
-
-__device__ inline u64 block_sum(u64 v, u64 *part, int wave, int lane) {
-  v = wave_sum64(v);
-  if (lane == 0) part[wave] = v;
-  __syncthreads();
-  u64 s = 0;
+__device__ inline floatx4 load4(const float *z, int at, int end, bool vec) {  // past the end: -infinity
+  floatx4 v;
+  if (vec && at + 4 <= end) {
+    v = *(const floatx4 *)(z + at);
+  } else {
 #pragma unroll
-  for (int w = 0; w < NW; ++w) s += part[w];
-  return s;
+    for (int j = 0; j < 4; ++j) v[j] = at + j < end ? z[at + j] : -INFINITY;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = usable(v[j]);
+  return v;
 }
 
-__global__ __launch_bounds__(NW * 64) void k_sample_rows(SampleRows a) {
-  __shared__ Shared sh;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, b = blockIdx.x, V = a.vocab;
-  const int piece = (V + NW * ROUND - 1) / (NW * ROUND) * ROUND;
-  Row row;
-  row.z = a.logits + (long)b * a.stride;
-  row.V = V;
-  row.begin = min(wave * piece, V);
-  row.end = min(row.begin + piece, V);
-  row.vec = ((uintptr_t)row.z & 15) == 0;
-  row.lane = lane;
-  const float T = a.temperature ? a.temperature[b] : 1.0f;
-  const int k = a.top_k ? a.top_k[b] : 0;
-  const float top_p = a.top_p ? a.top_p[b] : 1.0f, min_p = a.min_p ? a.min_p[b] : 0.f;
-  const float u = fminf(fmaxf(a.u[b], 0.f), 0x1.fffffep-1f);  // (NaN: 0)
-
-  // ---- extremes
-  float hi = -INFINITY, lo = INFINITY;
-  row.each([&](int, floatx4 z) {
+// PER: tokens of a thread, four neighbouring ones at a time; they stay in registers.
+template <int PER>
+__global__ __launch_bounds__(256) void k_sample_bins(SampleRows a) {
+  __shared__ u64 mass[BINS + 1];
+  __shared__ uint32_t count[BINS + 1];
+  __shared__ double tab[64];
+  __shared__ float tops[4];
+  const int tid = threadIdx.x, piece = blockIdx.x % a.pieces, b = blockIdx.x / a.pieces;
+  const float *z = a.logits + (long)b * a.stride;
+  const bool vec = ((uintptr_t)z & 15) == 0;
+  const int begin = piece * (256 * PER), end = min(begin + 256 * PER, a.vocab);
+  floatx4 v[PER / 4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      hi = fmaxf(hi, z[j]);
-      lo = fminf(lo, z[j] == -INFINITY ? INFINITY : z[j]);
-    }
-  });
+  for (int i = 0; i < PER / 4; ++i) v[i] = load4(z, begin + (i * 256 + tid) * 4, end, vec);
+  const Params p(a, b);
+  float top = -INFINITY;
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    hi = fmaxf(hi, __shfl_xor(hi, o));
-    lo = fminf(lo, __shfl_xor(lo, o));
+  for (int i = 0; i < PER / 4; ++i) top = fmaxf(top, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  for (int i = tid; i <= BINS; i += 256) {
+    mass[i] = 0;
+    count[i] = 0;
   }
-  if (lane == 0) {
-    sh.hi[wave] = hi;
-    sh.lo[wave] = lo;
-  }
-  if (tid < 64) sh.tab[tid] = exp2(tid / 64.0);
-  for (int i = tid; i < BINS; i += NW * 64) {
-    sh.count[i] = 0;
-    sh.mass[i] = 0;
-  }
+  if (tid < 64) tab[tid] = exp2(tid / 64.0);
   __syncthreads();
-  for (int w = 0; w < NW; ++w) {
-    hi = fmaxf(hi, sh.hi[w]);
-    lo = fminf(lo, sh.lo[w]);
-  }
-  row.top = hi;
-  // greedy: no temperature, or nothing but the largest has mass
-  const bool greedy = !(T > 0.f) || hi == INFINITY || hi == -INFINITY;
-  row.c = greedy ? 1.0 : 64.0 * 1.44269504088896340736 / (double)T;
-  float floor_ = hi;                      // tokens below have no mass, or too little
-  if (!greedy) {
-    double f = (double)hi - 32.0 * (double)T;
-    if (min_p > 0.f) f = fmax(f, min_p < 1.f ? (double)hi + (double)T * log((double)min_p) : (double)hi);
-    // the smallest float that is not below f
-    floor_ = (float)f;
-    if ((double)floor_ < f) floor_ = nextafterf(floor_, INFINITY);
-    floor_ = fminf(fmaxf(floor_, lo), hi);
-  }
-  uint32_t thr = key_of(floor_);          // keep key >= thr
-  const bool by_k = !greedy && k > 0 && k < V, by_p = !greedy && top_p < 1.f;
-
-  if (by_k || by_p) {
-    // ---- counts and masses by bins of equal width, the largest logits in bin 0
-    const float width = hi - floor_;
-    const float s = width > 0.f ? fminf((float)BINS / width, 3.0e38f) : 0.f;
-    auto bin_of = [&](float z) { return (int)fminf((hi - z) * s, (float)(BINS - 1)); };
-    row.each([&](int, floatx4 z) {
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  SampleBins &out = a.bins[(long)b * a.pieces + piece];
+  if (tid == 0) out.top = top;
+  if (p.greedy || top == INFINITY || top == -INFINITY) return;
+  const Grid g(p.T, tab);
+  const float place = g.place(top);
+  const float lowest = p.floor_of(top);  // (the row's is not lower)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (z[j] >= floor_) {
-          const int bin = bin_of(z[j]);
-          atomicAdd(&sh.count[bin], 1u);
-          if (by_p) atomicAdd(&sh.mass[bin], row.mass(z[j], sh.tab));
-        }
-    });
-    __syncthreads();
-    // The largest threshold t in the first bin with (weight of the bins before and of its values from t on) reaching a
-    // target; `need` says whether a weight does.  Returns the weight of the values above floor_ and at or above t.
-    auto find = [&](auto weight_of_bin, auto weight_of, auto need) -> u64 {
-      // every wave looks the bins through by itself: 64 at a time
-      u64 before = 0;
-      int bin = -1;
-      for (int i = 0; i < BINS && bin < 0; i += 64) {
-        u64 w = weight_of_bin(i + lane);
+  for (int i = 0; i < PER / 4; ++i)
 #pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-          const u64 other = (u64)(uint32_t)__shfl_up((int)(uint32_t)w, o) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(w >> 32), o) << 32;
-          if (lane >= o) w += other;
-        }
-        const u64 hits = __ballot(need(before + w));
-        const int at = hits ? __ffsll((long long)hits) - 1 : 63;
-        const u64 upto = (u64)(uint32_t)__shfl((int)(uint32_t)w, at) | (u64)(uint32_t)__shfl((int)(uint32_t)(w >> 32), at) << 32;
-        if (hits) {
-          bin = i + at;
-          before += upto - weight_of_bin(bin);
-        } else {
-          before += upto;
-        }
+    for (int j = 0; j < 4; ++j)
+      if (v[i][j] >= lowest && v[i][j] > -INFINITY) {
+        const int bin = g.bin(place, v[i][j]);
+        if (p.counts) atomicAdd(&count[bin], 1u);
+        if (p.masses) atomicAdd(&mass[bin], g.mass(v[i][j], top));
       }
-      if (bin < 0) return before;         // all of them together do not reach it: no cut
-      const bool listed = sh.count[bin] <= CAP;
-      __syncthreads();
-      if (tid == 0) sh.n_cand = 0;
-      __syncthreads();
-      if (listed)
-        row.each([&](int, floatx4 z) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (z[j] >= floor_ && bin_of(z[j]) == bin) sh.cand[atomicAdd(&sh.n_cand, 1)] = z[j];
-        });
-      __syncthreads();
-      constexpr int PER = CAP / (NW * 64);
-      uint32_t key[PER];
-      u64 w[PER];
-      if (listed) {
-        const int C = sh.n_cand;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const bool is = tid + i * NW * 64 < C;
-          const float z = is ? sh.cand[tid + i * NW * 64] : 0.f;
-          key[i] = is ? key_of(z) : 0u;
-          w[i] = is ? weight_of(z) : 0ull;
-        }
-      }
-      uint32_t t = 0;
-      u64 got = 0;
-      for (int bit = 31, set = 0; bit >= 0; --bit, set ^= 1) {
-        const uint32_t trial = t | 1u << bit;
-        u64 mine = 0;
-        if (listed) {
-#pragma unroll
-          for (int i = 0; i < PER; ++i) mine += key[i] >= trial ? w[i] : 0ull;
-        } else {
-          row.each([&](int, floatx4 z) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (z[j] >= floor_ && bin_of(z[j]) == bin && key_of(z[j]) >= trial) mine += weight_of(z[j]);
-          });
-        }
-        const u64 sum = before + block_sum(mine, sh.part[set], wave, lane);
-        if (need(sum)) {
-          t = trial;
-          got = sum;
-        }
-      }
-      __syncthreads();
-      thr = max(thr, t);
-      return got;
-    };
-    if (by_k) {
-      (void)find([&](int i) { return (u64)sh.count[i]; }, [&](float) { return 1ull; }, [&](u64 n) { return n >= (u64)k; });
-    }
-    if (by_p) {
-      // masses of what top-k leaves: bins below the threshold's are dropped, its own is added up again
-      u64 total = 0;
-      if (by_k) {
-        u64 mine = 0;
-        row.each([&](int, floatx4 z) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (z[j] >= floor_ && key_of(z[j]) >= thr) mine += row.mass(z[j], sh.tab);
-        });
-        total = block_sum(mine, sh.part[0], wave, lane);
-      } else {
-        u64 mine = 0;
-        for (int i = tid; i < BINS; i += NW * 64) mine += sh.mass[i];
-        total = block_sum(mine, sh.part[0], wave, lane);
-      }
-      __syncthreads();
-      const double target = (double)fmaxf(top_p, 0.f) * (double)total;
-      // (values that top-k drops lie below those that reach the target, so they may stay in the bins)
-      (void)find([&](int i) { return sh.mass[i]; }, [&](float z) { return row.mass(z, sh.tab); }, [&](u64 m) { return (double)m >= target; });
-    }
-    thr = min(thr, key_of(hi));
-  }
-
-  // ---- running masses in the order of the indices
-  auto mass_of = [&](float z) -> u64 { return key_of(z) < thr || z == -INFINITY ? 0ull : greedy ? (z == hi ? 1ull : 0ull) : row.mass(z, sh.tab); };
-  u64 mine = 0;
-  row.each([&](int at, floatx4 z) {
-    u64 m = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m += mass_of(z[j]);
-    m = wave_sum64(m);
-    if (lane == 0) sh.run[wave][(at - row.begin) / ROUND] = m;
-    mine += m;
-  });
-  if (lane == 0) sh.part[1][wave] = mine;
   __syncthreads();
+  if (p.counts)
+    for (int i = tid; i <= BINS; i += 256) out.count[i] = count[i];
+  if (!p.masses) return;
   u64 all = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) all += sh.part[1][w];
-  const double target = greedy ? 0.0 : (double)u * (double)all;
-  u64 run = 0;
-  int win = NW - 1;
-  for (int w = 0; w < NW; ++w) {
-    if ((double)(run + sh.part[1][w]) > target) {
-      win = w;
-      break;
-    }
-    run += sh.part[1][w];
+  for (int i = tid; i <= BINS; i += 256) {
+    out.mass[i] = mass[i];
+    all += mass[i];
   }
-  if (wave != win) return;
-  int token = 0;                          // (a row without a usable logit)
-  for (int i = row.begin; i < row.end; i += ROUND) {
-    const u64 m = sh.run[wave][(i - row.begin) / ROUND];
-    if (!((double)(run + m) > target)) {
-      run += m;
-      continue;
-    }
-    u64 own[4], sum = 0;
+  all = wave_sum64(all, tid & 63);
+  __shared__ u64 sums[4];
+  if ((tid & 63) == 0) sums[tid >> 6] = all;
+  __syncthreads();
+  if (tid == 0) out.all = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+constexpr int PIECES = 128;  // of a row, at most
+
+struct Pick {
+  double tab[64];
+  double mass[BINS + 1];
+  uint32_t count[BINS + 1];
+  double scale[PIECES];       // of a piece's masses
+  double kept[PIECES];        // masses of its kept tokens
+  u64 part[PIECES];           // of those in the threshold's bin
+  int shift[PIECES];          // its first bin
+  float top[PIECES];
+  uint8_t wanted[PIECES];     // a sweep reads it
+  float value[CAP];           // listed tokens
+  int index[CAP];
+  int n;
+  u64 sum[2][NW];
+  int seen[NW];
+  uint32_t lo, hi;
+  u64 bucket[1024];
+  u64 wave_mass[NW];
+  int bucket_at;
+  u64 bucket_before;
+  uint32_t near_key[64];      // the elements of one bucket
+  u64 near_mass[64];
+  int near_n;
+};
+
+__global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
+  extern __shared__ unsigned char lds[];
+  Pick &sh = *(Pick *)lds;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, b = blockIdx.x, pieces = a.pieces, V = a.vocab;
+  const float *z = a.logits + (long)b * a.stride;
+  const bool vec = ((uintptr_t)z & 15) == 0;
+  const SampleBins *bins = a.bins + (long)b * pieces;
+  const Params p(a, b);
+  float top = lane < pieces ? bins[lane].top : -INFINITY;
+  if (lane + 64 < pieces) top = fmaxf(top, bins[lane + 64].top);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = i + 4 * lane + j;
-      own[j] = mass_of(at < row.end ? usable(row.z[at]) : -INFINITY);
-      sum += own[j];
-    }
-    u64 upto = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const u64 other = (u64)(uint32_t)__shfl_up((int)(uint32_t)upto, o) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(upto >> 32), o) << 32;
-      if (lane >= o) upto += other;
-    }
-    u64 x = run + upto - sum;
-    int found = 4;
-#pragma unroll
-    for (int j = 3; j >= 0; --j) {
-      u64 at = x;
-      for (int q = 0; q <= j; ++q) at += own[q];
-      if ((double)at > target) found = j;
-    }
-    const u64 hits = __ballot(found < 4);
-    const int l = __ffsll((long long)hits) - 1;
-    token = i + 4 * l + __shfl(found, l);
-    break;
+  for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  const bool greedy = p.greedy || top == INFINITY || top == -INFINITY;
+  const Grid g(p.T, sh.tab);
+  const float place = greedy ? 0.f : g.place(top), lowest = greedy ? top : p.floor_of(top);
+  if (tid < 64) sh.tab[tid] = exp2(tid / 64.0);
+  if (tid < pieces) {
+    const float t = bins[tid].top;
+    sh.top[tid] = t;
+    sh.shift[tid] = t == -INFINITY ? BINS + 1 : (int)fminf(place - g.place(t), (float)(BINS + 1));
+    sh.scale[tid] = t == -INFINITY || greedy ? 0.0 : exp(((double)t - (double)top) / (double)p.T);
+    sh.kept[tid] = t == -INFINITY || greedy || !p.masses ? 0.0 : (double)bins[tid].all * sh.scale[tid];
+    sh.part[tid] = 0;
   }
-  if (lane == 0) {
+  __syncthreads();
+  auto answer = [&](int token) {
     a.tokens[b] = token;
     if (a.tokens2) a.tokens2[b] = token;
+  };
+  auto usable_here = [&](float x) { return x >= lowest && x > -INFINITY; };
+  auto value_of = [](uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); };
+  // f(logit, index) for the tokens of the wanted pieces, several requested at a time
+  auto sweep = [&](auto f) {
+    constexpr int U = 8, STEP = 4 * NW * 64;
+    for (int base = 0; base < V; base += U * STEP) {
+      floatx4 v[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int at = base + i * STEP + 4 * tid;
+        v[i] = at < V && sh.wanted[at / a.piece] ? load4(z, at, V, vec) : floatx4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (usable_here(v[i][j])) f(v[i][j], base + i * STEP + 4 * tid + j);
+    }
+  };
+  // Lists the tokens for which `in` holds; whether all of them fit.  lo, hi: their smallest and largest key.
+  bool whole = false;
+  auto list = [&](auto in) {
+    __syncthreads();
+    if (tid == 0) {
+      sh.n = 0;
+      sh.lo = 0xffffffffu;
+      sh.hi = 0;
+    }
+    __syncthreads();
+    uint32_t lo = 0xffffffffu, hi = 0;
+    sweep([&](float x, int at) {
+      if (!in(x)) return;
+      const int n = atomicAdd(&sh.n, 1);
+      if (n < CAP) {
+        sh.value[n] = x;
+        sh.index[n] = at;
+      }
+      lo = min(lo, key_of(x));
+      hi = max(hi, key_of(x));
+    });
+    if (hi) {
+      atomicMin(&sh.lo, lo);
+      atomicMax(&sh.hi, hi);
+    }
+    __syncthreads();
+    whole = sh.n <= CAP;
+  };
+  // A thread's listed tokens, and their masses where they are needed: in registers.
+  constexpr int PER = CAP / (NW * 64);
+  uint32_t key[PER];
+  int index[PER];
+  u64 mass[PER];
+  auto take = [&](bool masses) {
+    const int n = whole ? sh.n : 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = tid + i * NW * 64;
+      key[i] = 0;
+      index[i] = V;
+      mass[i] = 0;
+      if (at < n) {
+        key[i] = key_of(sh.value[at]);
+        index[i] = sh.index[at];
+        if (masses) mass[i] = g.mass(sh.value[at], top);
+      }
+    }
+  };
+  // The listed elements (is(i)) by buckets in an order, their weights added up bucket by bucket: the one in which enough(sum) comes
+  // to hold, the sum before it, and its elements' order words and weights in LDS; false where there is none, or too many there.
+  auto locate = [&](auto is, auto bucket_of, auto word, auto weight, auto enough) -> bool {
+    sh.bucket[tid] = 0;
+    if (tid == 0) {
+      sh.bucket_at = 1 << 30;
+      sh.near_n = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (is(i)) atomicAdd(&sh.bucket[bucket_of(i)], weight(i));
+    __syncthreads();
+    const u64 own = sh.bucket[tid], scan = wave_scan64(own, lane);
+    if (lane == 63) sh.wave_mass[wave] = scan;
+    __syncthreads();
+    u64 before = 0;
+    for (int w = 0; w < wave; ++w) before += sh.wave_mass[w];
+    const u64 hits = __ballot(enough(before + scan));
+    if (hits) {
+      const int l = __ffsll((long long)hits) - 1;
+      if (lane == l) atomicMin(&sh.bucket_at, tid);
+    }
+    __syncthreads();
+    const int at = sh.bucket_at;
+    if (at >= 1024) return false;
+    if (tid == at) sh.bucket_before = before + scan - own;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (is(i) && bucket_of(i) == at) {
+        const int n = atomicAdd(&sh.near_n, 1);
+        if (n < 64) {
+          sh.near_key[n] = word(i);
+          sh.near_mass[n] = weight(i);
+        }
+      }
+    __syncthreads();
+    return sh.near_n <= 64;
+  };
+  // Of the located elements, every wave for itself: f(order word, sum of the weights of those whose word is at least (or, ascending,
+  // at most) this one) for a lane's element.
+  auto near = [&](bool ascending, auto f) {
+    const int n = sh.near_n;
+    const uint32_t own = lane < n ? sh.near_key[lane] : 0;
+    u64 sum = 0;
+    for (int j = 0; j < n; ++j) {
+      const uint32_t k = sh.near_key[j];
+      if (ascending ? k <= own : k >= own) sum += sh.near_mass[j];
+    }
+    if (lane < n) f(own, sh.bucket_before + sum);
+  };
+  // sum of weight(logit, index) over the listed tokens, or over what they would be
+  auto sum_of = [&](auto in, auto weight, int set) -> u64 {
+    u64 mine = 0;
+    if (whole) {
+      const int n = sh.n;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = tid + i * NW * 64;
+        if (at < n) mine += weight(sh.value[at], sh.index[at]);
+      }
+    } else {
+      sweep([&](float x, int at) {
+        if (in(x)) mine += weight(x, at);
+      });
+    }
+    mine = wave_sum64(mine, lane);
+    if (lane == 0) sh.sum[set][wave] = mine;
+    __syncthreads();
+    u64 s = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s += sh.sum[set][w];
+    return s;
+  };
+  // The largest key among them from which on enough(weight) holds; 0: it does not even for all of them.
+  auto search = [&](auto in, auto weight, auto enough) -> uint32_t {
+    const uint32_t lo = sh.lo, hi = sh.hi;
+    auto from = [&](uint32_t key, int set) { return sum_of(in, [&](float x, int) { return key_of(x) >= key ? weight(x) : 0ull; }, set); };
+    if (sh.n == 0 || !enough(from(lo, 0))) return 0;
+    uint32_t t = lo;
+    if (lo != hi) {
+      const int bits = 32 - __clz((int)(lo ^ hi));  // the keys differ in these
+      t = bits == 32 ? 0 : lo >> bits << bits;
+      for (int bit = bits - 1, set = 1; bit >= 0; --bit, set ^= 1) {
+        const uint32_t trial = t | 1u << bit;
+        if (enough(from(trial, set))) t = trial;
+      }
+    }
+    __syncthreads();
+    return max(t, lo);
+  };
+  // The same by buckets where the tokens are listed (take() has been called).
+  auto find = [&](auto in, auto weight, auto weight_at, auto enough) -> uint32_t {
+    if (whole && sh.n) {
+      const float high = value_of(sh.hi), low = value_of(sh.lo);
+      const float s = high > low ? fminf(1023.0f / (high - low), 3.0e38f) : 0.f;
+      const bool ok = locate([&](int i) { return key[i] != 0; }, [&](int i) { return (int)fminf((high - value_of(key[i])) * s, 1023.0f); },
+                             [&](int i) { return key[i]; }, weight_at, enough);
+      uint32_t best = 0;
+      if (ok) near(false, [&](uint32_t k, u64 sum) { best = enough(sum) ? k : 0; });
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) best = max(best, (uint32_t)__shfl_xor((int)best, o));
+      const bool none = sh.bucket_at >= 1024;
+      __syncthreads();
+      if (ok) return best;
+      if (none) return 0;
+    }
+    return search(in, weight, enough);
+  };
+  // First bin up to `last` at which enough(running sum) holds, its sum before; BINS + 1: none.  Every wave for itself.
+  auto first_bin = [&](const auto *of, int last, auto enough, auto &before) -> int {
+    typedef typename std::remove_reference<decltype(before)>::type S;
+    S run = 0;
+    for (int i = 0; i <= last; i += 64) {
+      const S x = i + lane <= last ? (S)of[i + lane] : (S)0;
+      const S w = wave_scan64(x, lane);
+      const u64 hits = __ballot(i + lane <= last && enough(run + w));
+      if (hits) {
+        const int at = __ffsll((long long)hits) - 1;
+        before = run + shfl64(w, at) - shfl64(x, at);
+        return i + at;
+      }
+      run += shfl64(w, 63);
+    }
+    before = run;
+    return BINS + 1;
+  };
+  auto mass_at = [&](float x) { return g.mass(x, top); };
+  // the bins of the row: sums over the pieces of what(piece, bin of the piece)
+  static_assert(BINS == NW * 64, "a bin for every thread");
+  auto add_bins = [&](auto *to, auto what) {
+    typedef typename std::remove_reference<decltype(*to)>::type S;
+    S sum = 0;
+#pragma unroll 16
+    for (int c = 0; c < pieces; ++c) {
+      const int i = tid - sh.shift[c];
+      if (i >= 0) sum += what(c, i);
+    }
+    to[tid] = sum;
+    __syncthreads();
+  };
+
+  const int floor_bin = greedy ? 0 : g.bin(place, lowest);
+  int bound = floor_bin;              // top-k or min-p: the bin of the k-th, or of the lowest that min-p leaves
+  u64 few = 0;                        // tokens up to that bin
+  if (p.counts && !greedy) {
+    add_bins(sh.count, [&](int c, int i) { return bins[c].count[i]; });
+    u64 before = 0;
+    if (p.by_k) bound = min(bound, first_bin(sh.count, BINS - 1, [&](u64 n) { return n >= (u64)p.k; }, before));
+    if (!p.by_k)
+      for (int i = 0; i <= min(bound, BINS - 1); i += 64) few += wave_sum64(i + lane <= min(bound, BINS - 1) ? (u64)sh.count[i + lane] : 0ull, lane);
   }
+  if (!greedy && (p.by_k || (p.counts && bound < BINS && few <= CAP))) {
+    if (tid < pieces) sh.wanted[tid] = sh.shift[tid] <= bound || (bound == BINS && sh.top[tid] > -INFINITY);
+    auto in = [&](float x) { return g.bin(place, x) <= bound; };
+    list(in);
+    take(true);
+    auto own_mass = [&](int i) { return mass[i]; };
+    float cut = lowest;
+    if (p.by_k) {
+      const uint32_t t = find(in, [](float) { return 1ull; }, [](int) { return 1ull; }, [&](u64 n) { return n >= (u64)p.k; });
+      if (t) cut = fmaxf(cut, value_of(t));
+    }
+    auto kept = [&](int i) { return key[i] != 0 && key[i] >= key_of(cut); };
+    auto total_kept = [&]() -> u64 {
+      if (!whole) return sum_of(in, [&](float x, int) { return x >= cut ? mass_at(x) : 0ull; }, 0);
+      u64 mine = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) mine += kept(i) ? mass[i] : 0ull;
+      mine = wave_sum64(mine, lane);
+      if (lane == 0) sh.sum[0][wave] = mine;
+      __syncthreads();
+      u64 s = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) s += sh.sum[0][w];
+      return s;
+    };
+    u64 all = total_kept();
+    if (p.by_p) {
+      const double need = (double)p.top_p * (double)all;
+      __syncthreads();
+      const uint32_t t = find(in, mass_at, own_mass, [&](u64 m) { return (double)m >= need; });
+      if (t) cut = fmaxf(cut, value_of(t));
+      __syncthreads();
+      cut = fminf(cut, top);
+      all = total_kept();
+    }
+    cut = fminf(cut, top);
+    const double target = (double)p.u * (double)all;
+    // the first index up to which the mass passes the target
+    const int shift = max(32 - __clz(V - 1) - 10, 0);
+    int token = V;
+    __syncthreads();
+    if (whole && locate(kept, [&](int i) { return index[i] >> shift; }, [&](int i) { return (uint32_t)index[i]; }, own_mass, [&](u64 m) { return (double)m > target; })) {
+      near(true, [&](uint32_t i, u64 sum) { token = (double)sum > target ? (int)i : V; });
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) token = min(token, __shfl_xor(token, o));
+    } else {  // bit by bit, as large as it does not
+      __syncthreads();
+      auto below = [&](int end, int set) { return sum_of(in, [&](float x, int i) { return x >= cut && i < end ? mass_at(x) : 0ull; }, set); };
+      token = 0;
+      for (int bit = 31 - __clz(V), set = 1; bit >= 0; --bit, set ^= 1) {
+        const int trial = token | 1 << bit;
+        if (trial < V && !((double)below(trial, set) > target)) token = trial;
+      }
+    }
+    if (tid == 0) answer(token);
+    return;
+  }
+
+  float cut = lowest;                 // keep z >= cut (and above -infinity)
+  double target = 0.0;
+  if (!greedy) {
+    if (p.by_p || p.counts) {
+      // ---- top-p alone, or a min-p that leaves many
+      add_bins(sh.mass, [&](int c, int i) { return (double)bins[c].mass[i] * sh.scale[c]; });
+      int bin = floor_bin;
+      auto in = [&](float x) { return g.bin(place, x) == bin; };
+      auto list_bin = [&]() {
+        if (tid < pieces) {
+          const int i = bin - sh.shift[tid];
+          sh.wanted[tid] = sh.top[tid] > -INFINITY && (bin >= BINS || (i >= 0 && bins[tid].mass[i] != 0));
+        }
+        list(in);
+      };
+      double before = 0.0, total;     // masses: of the bins before `bin`, of all that min-p leaves
+      if (p.counts) {                 // of the lowest bin only a part
+        for (int i = 0; i < bin; i += 64) before += wave_sum64(i + lane < bin ? sh.mass[i + lane] : 0.0, lane);
+        list_bin();
+        total = before + (double)sum_of(in, [&](float x, int) { return mass_at(x); }, 0);
+        __syncthreads();
+      } else {
+        total = lane < pieces ? sh.kept[lane] : 0.0;
+        if (lane + 64 < pieces) total += sh.kept[lane + 64];
+        total = wave_sum64(total, lane);
+      }
+      if (p.by_p) {
+        const double need = (double)p.top_p * total;
+        const int first = first_bin(sh.mass, floor_bin - 1, [&](double m) { return m >= need; }, before);
+        if (first < floor_bin || !p.counts) {
+          bin = min(first, floor_bin);
+          list_bin();
+        }
+        take(true);
+        const uint32_t t = find(in, mass_at, [&](int i) { return mass[i]; }, [&](u64 m) { return before + (double)m >= need; });
+        if (t) cut = fmaxf(cut, value_of(t));
+      }
+      cut = fminf(cut, top);
+      // kept masses of the pieces: their bins above the cut's, and of that one what is not below the cut
+      if (whole) {
+        for (int i = tid; i < sh.n; i += NW * 64)
+          if (sh.value[i] >= cut) atomicAdd(&sh.part[sh.index[i] / a.piece], mass_at(sh.value[i]));
+      } else {
+        sweep([&](float x, int at) {
+          if (x >= cut && in(x)) atomicAdd(&sh.part[at / a.piece], mass_at(x));
+        });
+      }
+      __syncthreads();
+      for (int c = wave; c < pieces; c += NW) {
+        double m = 0.0;
+        const int most = sh.top[c] == -INFINITY ? 0 : min(bin - sh.shift[c], BINS);
+        for (int i = lane; i < most; i += 64) m += (double)bins[c].mass[i];
+        m = wave_sum64(m, lane) * sh.scale[c] + (double)sh.part[c];
+        if (lane == 0) sh.kept[c] = m;
+      }
+      __syncthreads();
+    }
+    double all = lane < pieces ? sh.kept[lane] : 0.0;
+    if (lane + 64 < pieces) all += sh.kept[lane + 64];
+    target = (double)p.u * wave_sum64(all, lane);
+  }
+  // ---- the piece in which the running mass passes the target (with rounding, or u = 0, perhaps one behind), and the token
+  int piece = 0;
+  double run = 0.0;
+  if (greedy) {
+    while (piece < pieces - 1 && sh.top[piece] != top) ++piece;
+  } else {
+    while (piece < pieces - 1 && !(run + sh.kept[piece] > target)) run += sh.kept[piece++];
+  }
+  auto mass_of = [&](float x) -> u64 { return !(x >= cut) || x == -INFINITY ? 0ull : greedy ? 1ull : mass_at(x); };
+  int last = 0;                       // the last token that has a mass: what rounding at the very end leaves
+  for (; piece < pieces && top > -INFINITY; ++piece) {
+    // a wave takes a sixteenth, 256 tokens at a time
+    const int begin = piece * a.piece, end = min(begin + a.piece, V), share = a.piece / NW, w0 = begin + wave * share, w1 = min(w0 + share, end);
+    u64 mine = 0;
+    int seen = -1;
+    for (int at = w0; at < w1; at += 256) {
+      const floatx4 v = load4(z, at + 4 * lane, w1, vec);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u64 m = mass_of(v[j]);
+        mine += m;
+        if (m) seen = at + 4 * lane + j;
+      }
+    }
+    mine = wave_sum64(mine, lane);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) seen = max(seen, __shfl_xor(seen, o));
+    __syncthreads();
+    if (lane == 0) {
+      sh.sum[0][wave] = mine;
+      sh.seen[wave] = seen;
+    }
+    __syncthreads();
+    double upto = run;
+    int win = -1;
+    for (int w = 0; w < NW; ++w) {
+      last = max(last, sh.seen[w]);
+      if (win < 0 && upto + (double)sh.sum[0][w] > target) win = w;
+      if (win < 0) upto += (double)sh.sum[0][w];
+    }
+    if (win < 0) {
+      run = upto;
+      continue;
+    }
+    if (wave != win) return;
+    u64 before = 0;
+    for (int at = w0; at < w1; at += 256) {
+      const floatx4 v = load4(z, at + 4 * lane, w1, vec);
+      u64 own[4], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += own[j] = mass_of(v[j]);
+      const u64 scan = wave_scan64(sum, lane);
+      u64 x = before + scan - sum;
+      int found = 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x += own[j];
+        if (found == 4 && upto + (double)x > target) found = j;
+      }
+      const u64 hits = __ballot(found < 4);
+      if (hits) {
+        const int l = __ffsll((long long)hits) - 1;
+        last = at + 4 * l + __shfl(found, l);
+        break;
+      }
+      before += shfl64(scan, 63);
+    }
+    if (lane == 0) answer(last);
+    return;
+  }
+  if (tid == 0) answer(last);
+}
+
+// Tokens of a thread of k_sample_bins, pieces of 256 times as many: few enough pieces for their bins to be small beside the logits,
+// enough of them for the chip.
+int per_thread(int rows, int vocab) {
+  int per = 8;
+  while (per < 64 && (((long)rows * vocab + 256L * per - 1) / (256L * per) > 4096 || (vocab + 256 * per - 1) / (256 * per) > PIECES)) per *= 2;
+  return per;
 }
 
 }  // namespace
 
-void sample_rows(hipStream_t s, const SampleRows &a) {
-  SKD_LAUNCH(k_sample_rows, dim3(a.rows), dim3(NW * 64), 0, s, a);
+size_t sample_rows_bins(int rows, int vocab) {
+  const int piece = 256 * per_thread(rows, vocab);
+  return (size_t)rows * ((vocab + piece - 1) / piece);
+}
+
+void sample_rows(hipStream_t s, const SampleRows &call) {
+  SampleRows a = call;
+  const int per = per_thread(a.rows, a.vocab);
+  a.piece = 256 * per;
+  a.pieces = (a.vocab + a.piece - 1) / a.piece;
+  const dim3 grid((unsigned)a.rows * a.pieces);
+  if (per == 8) SKD_LAUNCH(k_sample_bins<8>, grid, dim3(256), 0, s, a);
+  else if (per == 16) SKD_LAUNCH(k_sample_bins<16>, grid, dim3(256), 0, s, a);
+  else if (per == 32) SKD_LAUNCH(k_sample_bins<32>, grid, dim3(256), 0, s, a);
+  else SKD_LAUNCH(k_sample_bins<64>, grid, dim3(256), 0, s, a);
+  static std::atomic<uint64_t> done{0};
+  (void)allow_lds(done, {(const void *)k_sample_pick}, sizeof(Pick));
+  SKD_LAUNCH(k_sample_pick, dim3(a.rows), dim3(NW * 64), sizeof(Pick), s, a);
 }
 
 }  // namespace skd

@@ -132,6 +132,7 @@ struct skd_state {
   int32_t *argmax_dev = nullptr;   // [B]
   float *u_dev = nullptr;          // [B] uniform numbers of the sampling head
   SampleScratch sample{};          // its candidates
+  SampleBins *sample_bins = nullptr;
   float *sampling_dev = nullptr;   // fp32 path with host buffers: [u | temperature | top-p | min-p | top-k][B]
   float *x = nullptr;              // residual stream fp32 [B_pad][d]
   float *x2 = nullptr;             // its second buffer (fuse_ln)
@@ -920,6 +921,7 @@ static int create_impl(const skd_config *cfg, const skd_weights *w, void *hip_st
   const int Bp = st->B_pad;
   auto A = [&](auto **p, size_t n) { if (rc == SKD_OK) rc = dev_alloc(st, p, n); };
   A(&st->tok_dev, B); A(&st->prompt_dev, (size_t)c.prompt_size * B); A(&st->start_dev, B); A(&st->order_dev, B); A(&st->argmax_dev, B); A(&st->u_dev, B); A(&st->sampling_dev, 5 * (size_t)B);
+  if (V <= SAMPLE_ROWS_VOCAB) A(&st->sample_bins, sample_rows_bins(B, V));
   if (const size_t parts = (size_t)B * sample_chunks(V)) {
     A(&st->sample.z, (size_t)B * SAMPLE_CHUNK_CAND); A(&st->sample.idx, (size_t)B * SAMPLE_CHUNK_CAND);
     A(&st->sample.max_mass, parts * 3); A(&st->sample.count, parts);
@@ -1701,6 +1703,7 @@ extern "C" int skd_logits_sample_rows(skd_state *st, const float *u, const skd_s
   a.stride = V;
   a.rows = B;
   a.vocab = V;
+  a.bins = st->sample_bins;
   a.u = u;
   a.temperature = p.temperature;
   a.top_k = p.top_k;

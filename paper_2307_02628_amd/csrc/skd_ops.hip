@@ -194,7 +194,7 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
 extern "C" int64_t skd_sample_workspace(int32_t rows, int32_t vocab) {
   if (rows < 0) return SKD_ERR_RANGE;
   if (vocab < 1 || vocab > SAMPLE_ROWS_VOCAB) return SKD_ERR_SHAPE;
-  return 0;
+  return (int64_t)(sample_rows_bins(rows, vocab) * sizeof(SampleBins));
 }
 
 extern "C" int skd_sample(const float *logits, int64_t stride, int32_t rows, int32_t vocab, const skd_sampling *params, const float *u,
@@ -203,9 +203,12 @@ extern "C" int skd_sample(const float *logits, int64_t stride, int32_t rows, int
   if (need < 0) return (int)need;
   if (stride < vocab) return SKD_ERR_SHAPE;
   if (!rows) return SKD_OK;
-  if (!logits || !u || !tokens_out) return SKD_ERR_NULL;
-  if (((uintptr_t)logits | (uintptr_t)u | (uintptr_t)tokens_out) & 3) return SKD_ERR_SHAPE;
+  if (!logits || !u || !tokens_out || !workspace) return SKD_ERR_NULL;
+  if (!aligned(workspace) || ((uintptr_t)logits | (uintptr_t)u | (uintptr_t)tokens_out) & 3) return SKD_ERR_SHAPE;
+  if (workspace_bytes < need) return SKD_ERR_NOMEM;
+  if (!fits_grid((int64_t)sample_rows_bins(rows, vocab))) return SKD_ERR_RANGE;
   SampleRows a{};
+  a.bins = (SampleBins *)workspace;
   a.logits = logits;
   a.stride = (long)stride;
   a.rows = rows;
@@ -218,7 +221,7 @@ extern "C" int skd_sample(const float *logits, int64_t stride, int32_t rows, int
   }
   a.u = u;
   a.tokens = tokens_out;
-  CHECK(check_memory({logits, u, tokens_out}));
+  CHECK(check_memory({logits, u, tokens_out, workspace}));
   for (const void *p : {(const void *)a.temperature, (const void *)a.top_k, (const void *)a.top_p, (const void *)a.min_p})
     if (p) CHECK(check_memory({p}));
   sample_rows((hipStream_t)hip_stream, a);

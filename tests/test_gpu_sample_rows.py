@@ -37,7 +37,8 @@ def reference(z, u, t=1.0, k=0, p=1.0, m=0.0):
 def draw(z, u, **params):
     t = {n: None if a is None else torch.as_tensor(a, dtype=torch.int32 if n == "top_k" else torch.float32).cuda() for n, a in params.items()}
     out = torch.full((z.shape[0],), -5, dtype=torch.int32, device="cuda")
-    skd.sample(z, torch.as_tensor(u, dtype=torch.float32).cuda(), out, **t)
+    ws = torch.full((skd.sample_workspace(*z.shape),), 0xff, dtype=torch.uint8, device="cuda")
+    skd.sample(z, torch.as_tensor(u, dtype=torch.float32).cuda(), out, **t, workspace=ws)
     return out.cpu().numpy()
 
 

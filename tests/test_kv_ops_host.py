@@ -91,11 +91,14 @@ def test_pointers_and_ranges():
 def test_draws():
     lib = skd.lib()
 
-    def rc(z=P, stride=1000, rows=3, vocab=1000, u=P, out=P):
-        return lib.skd_sample(z, stride, rows, vocab, None, u, out, None, 0, None)
+    need = lib.skd_sample_workspace(3, 1000)
 
-    assert rc(z=None) == rc(u=None) == rc(out=None) == skd.ERR_NULL
-    assert rc(vocab=0) == rc(vocab=262145, stride=262145) == rc(stride=999) == rc(z=P + 2) == rc(out=P + 1) == skd.ERR_SHAPE
+    def rc(z=P, stride=1000, rows=3, vocab=1000, u=P, out=P, ws=P, n=1 << 30):
+        return lib.skd_sample(z, stride, rows, vocab, None, u, out, ws, n, None)
+
+    assert rc(z=None) == rc(u=None) == rc(out=None) == rc(ws=None) == skd.ERR_NULL
+    assert rc(vocab=0) == rc(vocab=262145, stride=262145) == rc(stride=999) == rc(z=P + 2) == rc(out=P + 1) == rc(ws=P + 8) == skd.ERR_SHAPE
+    assert need > 0 and rc(n=need - 1) == skd.ERR_NOMEM
     assert rc(rows=-1) == skd.ERR_RANGE and rc(rows=0) == skd.OK
     assert lib.skd_sample_workspace(-1, 10) == skd.ERR_RANGE and lib.skd_sample_workspace(1, 0) == lib.skd_sample_workspace(1, 1 << 19) == skd.ERR_SHAPE
     assert lib.skd_sample_workspace(128, 262144) >= 0
