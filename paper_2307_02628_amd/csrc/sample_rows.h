@@ -5,7 +5,7 @@
 namespace skd {
 
 constexpr int SAMPLE_ROWS_VOCAB = 1 << 18;  // masses are counted in units of 2^-45 of the largest, their sum in 63 bits
-constexpr int SAMPLE_BINS = 1024;
+constexpr int SAMPLE_BINS = 512;
 
 struct SampleBins {           // of a piece of a row; [rows][pieces]
   uint64_t mass[SAMPLE_BINS + 1];

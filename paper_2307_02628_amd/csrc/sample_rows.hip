@@ -9,16 +9,21 @@
 // bits: neither atomics nor the shares of the waves change a draw, and one that 64-bit arithmetic decides comes out the same.
 // What lies 32 T below the largest logit has no mass, is never drawn, and is left out from the start.
 //
-// Two launches.  k_sample_bins, pieces of rows over the whole chip: the piece's largest logit, and by bins of T / 32 (1024 and one
+// Two launches.  k_sample_bins, pieces of rows over the whole chip: the piece's largest logit, and by bins of T / 16 (512 and one
 // for what is left) how many tokens (rows with top-k or min-p) or how much mass (the others).  It reads the logits once
 // and is bound by that.  The bins lie on a grid that all pieces share.  k_sample_pick, a workgroup per row.  Few tokens left by
 // top-k or min-p, which is what they are for: the bins say from where on, those tokens go into LDS, and thresholds and token
-// are searched there bit by bit.  Top-p alone: the bin in which the threshold lies, whose values are searched; the piece in which
-// the running mass passes the target, and the token in it.  What does not fit into LDS is swept over again instead.
-// us, one workgroup per row for everything (six passes over the row, one CU's worth of exponentials) -> this: 128 rows of 131072
-// with mixed parameters 227 -> PICK128, one row of 50272 with top-p 75 -> PICK1.
+// are found there by buckets.  Top-p alone: the bin in which the threshold lies, whose values are listed; the piece in which
+// the running mass passes the target, and the token in it.  What does not fit into LDS is looked at again instead, ten bits of
+// the answer each time.  k_sample_pick is bound by what one CU does: an instruction for each of 131072 tokens is 0.9 us, a barrier
+// or a trip to memory 0.3 to 1 us, so four tokens are compared at once, the waves' sums move in registers, and requests go out
+// together.
+// us (bins + pick), one workgroup per row for everything (six passes over the row) -> this: 128 rows of 131072 with mixed
+// parameters 227 -> 62 to 69 (21 + 48), one row of 50272 with top-p 75 -> 21 (5 + 16).  1024 bins of T / 32 cost
+// twice the traffic: one row 33; shuffles through LDS for the sums and one list for all waves: 25 and 95.
 #include "sample_rows.h"
 
+#include <float.h>
 #include <math.h>
 
 #include "bf16_device.h"
@@ -29,33 +34,54 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int BINS = SAMPLE_BINS, NW = 16, CAP = 5120;  // CAP: values of a bin that are listed
+constexpr int BINS = SAMPLE_BINS, NW = 16, CAP = 8192;  // CAP: tokens that are listed, a wave's share of it by each
 
 __device__ inline uint32_t key_of(float z) {  // ordered as the values are
   const uint32_t b = __float_as_uint(z);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ inline float usable(float z) { return z == z ? z + 0.f : -INFINITY; }  // (-0 as 0)
-template <typename T>
-__device__ inline T shfl64(T v, int lane) {
+// Running results of a wave's lanes by moves within the registers (through LDS each of the six steps takes its latency): lanes that
+// a step has no other lane for combine with `none`.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t moved32(uint32_t v, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS, typename T>
+__device__ inline T moved64(T v) {
   const u64 b = __builtin_bit_cast(u64, v);
-  return __builtin_bit_cast(T, (u64)(uint32_t)__shfl((int)(uint32_t)b, lane) | (u64)(uint32_t)__shfl((int)(uint32_t)(b >> 32), lane) << 32);
+  return __builtin_bit_cast(T, (u64)moved32<CTRL, ROWS>((uint32_t)b, 0) | (u64)moved32<CTRL, ROWS>((uint32_t)(b >> 32), 0) << 32);
 }
 template <typename T>
-__device__ inline T wave_sum64(T v, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v += shfl64(v, lane ^ o);
+__device__ inline T lane64(T v, int lane) {
+  const u64 b = __builtin_bit_cast(u64, v);
+  return __builtin_bit_cast(T, (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane) | (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane) << 32);
+}
+template <typename T>
+__device__ inline T wave_scan64(T v) {  // sums of the lanes up to each
+  v += moved64<0x111, 0xf>(v);  // 1, 2, 4 and 8 lanes on within each 16; the last of 16 to the next 16, of 32 to the next 32
+  v += moved64<0x112, 0xf>(v);
+  v += moved64<0x114, 0xf>(v);
+  v += moved64<0x118, 0xf>(v);
+  v += moved64<0x142, 0xa>(v);
+  v += moved64<0x143, 0xc>(v);
   return v;
 }
 template <typename T>
-__device__ inline T wave_scan64(T v, int lane) {  // sums of the lanes up to each
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const T x = shfl64(v, max(lane - o, 0));
-    if (lane >= o) v += x;
-  }
-  return v;
+__device__ inline T wave_sum64(T v) {
+  return lane64(wave_scan64(v), 63);
 }
+__device__ inline uint32_t wave_max(uint32_t v) {
+  v = max(v, moved32<0x111, 0xf>(v, 0));
+  v = max(v, moved32<0x112, 0xf>(v, 0));
+  v = max(v, moved32<0x114, 0xf>(v, 0));
+  v = max(v, moved32<0x118, 0xf>(v, 0));
+  v = max(v, moved32<0x142, 0xa>(v, 0));
+  v = max(v, moved32<0x143, 0xc>(v, 0));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ inline float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+__device__ inline float wave_top(float v) { return value_of(wave_max(key_of(v))); }
 
 // What a row's parameters come to.
 struct Params {
@@ -88,10 +114,10 @@ struct Params {
 };
 // Places on the grid of bins, and masses against a largest logit.
 struct Grid {
-  float s;                    // 32 / T
+  float s;                    // 16 / T
   double c;                   // 64 log2(e) / T
   const double *tab;          // 2^(i / 64)
-  __device__ Grid(float T, const double *t) : s((float)(32.0 / (double)T)), c(64.0 * 1.44269504088896340736 / (double)T), tab(t) {}
+  __device__ Grid(float T, const double *t) : s((float)(16.0 / (double)T)), c(64.0 * 1.44269504088896340736 / (double)T), tab(t) {}
   __device__ float place(float z) const { return floorf(z * s); }
   __device__ int bin(float top_place, float z) const { return (int)fminf(top_place - place(z), (float)BINS); }  // (NaN: the rest)
   // 64 log2 of a mass is split into n + r: 2^(n / 64) from the table, 2^(r / 64) by its series (|r| <= 1/2: the first term left
@@ -136,8 +162,7 @@ __global__ __launch_bounds__(256) void k_sample_bins(SampleRows a) {
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < PER / 4; ++i) top = fmaxf(top, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  top = wave_top(top);
   if ((tid & 63) == 0) tops[tid >> 6] = top;
   for (int i = tid; i <= BINS; i += 256) {
     mass[i] = 0;
@@ -170,7 +195,7 @@ __global__ __launch_bounds__(256) void k_sample_bins(SampleRows a) {
     out.mass[i] = mass[i];
     all += mass[i];
   }
-  all = wave_sum64(all, tid & 63);
+  all = wave_sum64(all);
   __shared__ u64 sums[4];
   if ((tid & 63) == 0) sums[tid >> 6] = all;
   __syncthreads();
@@ -191,6 +216,7 @@ struct Pick {
   uint8_t wanted[PIECES];     // a sweep reads it
   float value[CAP];           // listed tokens
   int index[CAP];
+  u64 weight[CAP];            // their masses
   int n;
   u64 sum[2][NW];
   int seen[NW];
@@ -211,11 +237,11 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   const float *z = a.logits + (long)b * a.stride;
   const bool vec = ((uintptr_t)z & 15) == 0;
   const SampleBins *bins = a.bins + (long)b * pieces;
+  const int piece_bits = __builtin_ctz((unsigned)a.piece);  // (a power of two)
   const Params p(a, b);
   float top = lane < pieces ? bins[lane].top : -INFINITY;
   if (lane + 64 < pieces) top = fmaxf(top, bins[lane + 64].top);
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  top = wave_top(top);
   const bool greedy = p.greedy || top == INFINITY || top == -INFINITY;
   const Grid g(p.T, sh.tab);
   const float place = greedy ? 0.f : g.place(top), lowest = greedy ? top : p.floor_of(top);
@@ -233,9 +259,9 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     a.tokens[b] = token;
     if (a.tokens2) a.tokens2[b] = token;
   };
-  auto usable_here = [&](float x) { return x >= lowest && x > -INFINITY; };
-  auto value_of = [](uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); };
-  // f(logit, index) for the tokens of the wanted pieces, several requested at a time
+  // f(logit, index, whether it is one), by whole waves, for the tokens of the wanted pieces from `low` to `high`, several requested at a time.  An instruction for every
+  // token is 0.9 us at 131072 of them: four are compared at once.
+  float low = fmaxf(lowest, -FLT_MAX), high = INFINITY;
   auto sweep = [&](auto f) {
     constexpr int U = 8, STEP = 4 * NW * 64;
     for (int base = 0; base < V; base += U * STEP) {
@@ -243,17 +269,44 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int at = base + i * STEP + 4 * tid;
-        v[i] = at < V && sh.wanted[at / a.piece] ? load4(z, at, V, vec) : floatx4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        v[i] = floatx4{NAN, NAN, NAN, NAN};
+        if (at < V && sh.wanted[at >> piece_bits]) {
+          if (vec && at + 4 <= V) {
+            v[i] = *(const floatx4 *)(z + at);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = at + j < V ? z[at + j] : NAN;
+          }
+        }
       }
 #pragma unroll
       for (int i = 0; i < U; ++i)
+        if (__any(fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])) >= low))
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (usable_here(v[i][j])) f(v[i][j], base + i * STEP + 4 * tid + j);
+          for (int j = 0; j < 4; ++j) {
+            const bool hit = v[i][j] >= low && v[i][j] <= high;
+            if (__any(hit)) f(v[i][j] + 0.f, base + i * STEP + 4 * tid + j, hit);
+          }
     }
   };
-  // Lists the tokens for which `in` holds; whether all of them fit.  lo, hi: their smallest and largest key.
+  // low and high for the bins from `first` to `last`: a little wider than they are, in() decides
+  auto bounds = [&](int first, int last) {
+    const double w = 1.0 / (double)g.s, m = (fabs((double)place) + BINS) * 0x1p-22;
+    const double lo = ((double)place - last - m) * w, hi = ((double)place - first + 1 + m) * w;
+    const bool sound = g.s < INFINITY && w < INFINITY;
+    low = sound && last < BINS ? fmaxf(lowest, nextafterf((float)lo, -INFINITY)) : lowest;
+    low = fmaxf(low, -FLT_MAX);
+    high = sound && first > 0 ? nextafterf((float)hi, INFINITY) : INFINITY;
+  };
+  // Lists the tokens for which `in` holds, a wave's in its own part of the list, their masses beside them, and takes them into registers;
+  // whether all of them fit.  lo, hi: their smallest and largest key.
   bool whole = false;
+  constexpr int PER = CAP / (NW * 64);
+  uint32_t key[PER];
+  float *const value_list = sh.value + wave * (64 * PER);
+  int *const index_list = sh.index + wave * (64 * PER);
+  auto mass_in = [&](int i) { return sh.weight[wave * (64 * PER) + lane + 64 * i]; };
+  auto index_of = [&](int i) { return index_list[lane + 64 * i]; };
   auto list = [&](auto in) {
     __syncthreads();
     if (tid == 0) {
@@ -262,58 +315,71 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
       sh.hi = 0;
     }
     __syncthreads();
-    uint32_t lo = 0xffffffffu, hi = 0;
-    sweep([&](float x, int at) {
-      if (!in(x)) return;
-      const int n = atomicAdd(&sh.n, 1);
-      if (n < CAP) {
-        sh.value[n] = x;
-        sh.index[n] = at;
+    uint32_t most = 0, least = 0;     // of key and of ~key
+    int n = 0;
+    sweep([&](float x, int at, bool hit) {
+      hit = hit && in(x);
+      const u64 hits = __ballot(hit);
+      if (!hits) return;
+      const int to = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0));
+      if (hit) {
+        if (to < 64 * PER) {
+          value_list[to] = x;
+          index_list[to] = at;
+        }
+        most = max(most, key_of(x));
+        least = max(least, ~key_of(x));
       }
-      lo = min(lo, key_of(x));
-      hi = max(hi, key_of(x));
+      n += __popcll(hits);
     });
-    if (hi) {
-      atomicMin(&sh.lo, lo);
-      atomicMax(&sh.hi, hi);
+    if (n) {
+      most = wave_max(most);
+      least = wave_max(least);
+      if (lane == 0) {
+        atomicAdd(&sh.n, n <= 64 * PER ? n : CAP + 1);
+        atomicMin(&sh.lo, ~least);
+        atomicMax(&sh.hi, most);
+      }
     }
     __syncthreads();
     whole = sh.n <= CAP;
-  };
-  // A thread's listed tokens, and their masses where they are needed: in registers.
-  constexpr int PER = CAP / (NW * 64);
-  uint32_t key[PER];
-  int index[PER];
-  u64 mass[PER];
-  auto take = [&](bool masses) {
-    const int n = whole ? sh.n : 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = tid + i * NW * 64;
+      const int at = lane + 64 * i;
       key[i] = 0;
-      index[i] = V;
-      mass[i] = 0;
-      if (at < n) {
-        key[i] = key_of(sh.value[at]);
-        index[i] = sh.index[at];
-        if (masses) mass[i] = g.mass(sh.value[at], top);
+      if (whole && at < n) {
+        key[i] = key_of(value_list[at]);
+        sh.weight[wave * (64 * PER) + at] = g.mass(value_list[at], top);
       }
     }
   };
   // The listed elements (is(i)) by buckets in an order, their weights added up bucket by bucket: the one in which enough(sum) comes
   // to hold, the sum before it, and its elements' order words and weights in LDS; false where there is none, or too many there.
   auto locate = [&](auto is, auto bucket_of, auto word, auto weight, auto enough) -> bool {
+    const bool few = sh.n <= 64;
     sh.bucket[tid] = 0;
     if (tid == 0) {
-      sh.bucket_at = 1 << 30;
+      sh.bucket_at = few ? 0 : 1 << 30;
+      sh.bucket_before = 0;
       sh.near_n = 0;
     }
     __syncthreads();
+    if (few) {  // one bucket
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (is(i)) {
+          const int n = atomicAdd(&sh.near_n, 1);
+          sh.near_key[n] = word(i);
+          sh.near_mass[n] = weight(i);
+        }
+      __syncthreads();
+      return true;
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       if (is(i)) atomicAdd(&sh.bucket[bucket_of(i)], weight(i));
     __syncthreads();
-    const u64 own = sh.bucket[tid], scan = wave_scan64(own, lane);
+    const u64 own = sh.bucket[tid], scan = wave_scan64(own);
     if (lane == 63) sh.wave_mass[wave] = scan;
     __syncthreads();
     u64 before = 0;
@@ -344,29 +410,28 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   auto near = [&](bool ascending, auto f) {
     const int n = sh.near_n;
     const uint32_t own = lane < n ? sh.near_key[lane] : 0;
+    const u64 w = lane < n ? sh.near_mass[lane] : 0;
     u64 sum = 0;
     for (int j = 0; j < n; ++j) {
-      const uint32_t k = sh.near_key[j];
-      if (ascending ? k <= own : k >= own) sum += sh.near_mass[j];
+      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)own, j);
+      const u64 wj = lane64(w, j);
+      sum += (ascending ? k <= own : k >= own) ? wj : 0ull;
     }
     if (lane < n) f(own, sh.bucket_before + sum);
   };
-  // sum of weight(logit, index) over the listed tokens, or over what they would be
+  // sum of weight(logit) over the listed tokens, or over what they would be
   auto sum_of = [&](auto in, auto weight, int set) -> u64 {
     u64 mine = 0;
     if (whole) {
-      const int n = sh.n;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int at = tid + i * NW * 64;
-        if (at < n) mine += weight(sh.value[at], sh.index[at]);
-      }
+      for (int i = 0; i < PER; ++i)
+        if (key[i]) mine += weight(value_of(key[i]));
     } else {
-      sweep([&](float x, int at) {
-        if (in(x)) mine += weight(x, at);
+      sweep([&](float x, int at, bool hit) {
+        if (hit && in(x)) mine += weight(x);
       });
     }
-    mine = wave_sum64(mine, lane);
+    mine = wave_sum64(mine);
     if (lane == 0) sh.sum[set][wave] = mine;
     __syncthreads();
     u64 s = 0;
@@ -374,71 +439,114 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     for (int w = 0; w < NW; ++w) s += sh.sum[set][w];
     return s;
   };
-  // The largest key among them from which on enough(weight) holds; 0: it does not even for all of them.
-  auto search = [&](auto in, auto weight, auto enough) -> uint32_t {
-    const uint32_t lo = sh.lo, hi = sh.hi;
-    auto from = [&](uint32_t key, int set) { return sum_of(in, [&](float x, int) { return key_of(x) >= key ? weight(x) : 0ull; }, set); };
-    if (sh.n == 0 || !enough(from(lo, 0))) return 0;
-    uint32_t t = lo;
-    if (lo != hi) {
-      const int bits = 32 - __clz((int)(lo ^ hi));  // the keys differ in these
-      t = bits == 32 ? 0 : lo >> bits << bits;
-      for (int bit = bits - 1, set = 1; bit >= 0; --bit, set ^= 1) {
-        const uint32_t trial = t | 1u << bit;
-        if (enough(from(trial, set))) t = trial;
+  // Where there are too many: of the order words word(logit, index) from `first` to `last` the one at which enough(sum of the weights
+  // up to it) comes to hold, ten bits of it with every look at the tokens; false: nowhere.
+  auto narrow = [&](auto in, auto word, auto weight, auto enough, uint32_t first, uint32_t last, uint32_t &at) -> bool {
+    u64 before = 0;
+    while (true) {
+      const int shift = max(22 - __clz((int)((last - first) | 1)), 0);
+      __syncthreads();
+      sh.bucket[tid] = 0;
+      if (tid == 0) sh.bucket_at = 1 << 30;
+      __syncthreads();
+      auto add = [&](float x, int i) {
+        const uint32_t w = word(x, i);
+        if (w >= first && w <= last) atomicAdd(&sh.bucket[(w - first) >> shift], weight(x));
+      };
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (key[i]) add(value_of(key[i]), index_of(i));
+      } else {
+        sweep([&](float x, int i, bool hit) {
+          if (hit && in(x)) add(x, i);
+        });
       }
+      __syncthreads();
+      const u64 own = sh.bucket[tid], scan = wave_scan64(own);
+      if (lane == 63) sh.wave_mass[wave] = scan;
+      __syncthreads();
+      u64 run = before;
+      for (int w = 0; w < wave; ++w) run += sh.wave_mass[w];
+      const u64 hits = __ballot(enough(run + scan));
+      if (hits && lane == __ffsll((long long)hits) - 1) atomicMin(&sh.bucket_at, tid);
+      __syncthreads();
+      const int bucket = sh.bucket_at;
+      if (bucket >= 1024) return false;
+      if (tid == bucket) sh.bucket_before = run + (scan - own);
+      __syncthreads();
+      before = sh.bucket_before;
+      first += (uint32_t)bucket << shift;
+      if (shift == 0) {
+        at = first;
+        return true;
+      }
+      last = min(last, first + ((1u << shift) - 1));
     }
-    __syncthreads();
-    return max(t, lo);
   };
-  // The same by buckets where the tokens are listed (take() has been called).
+  // The largest key among the listed tokens, or what they would be, from which on enough(weight) holds; 0: it does not even for all.
   auto find = [&](auto in, auto weight, auto weight_at, auto enough) -> uint32_t {
-    if (whole && sh.n) {
+    if (sh.n == 0) return 0;
+    if (whole) {
       const float high = value_of(sh.hi), low = value_of(sh.lo);
       const float s = high > low ? fminf(1023.0f / (high - low), 3.0e38f) : 0.f;
       const bool ok = locate([&](int i) { return key[i] != 0; }, [&](int i) { return (int)fminf((high - value_of(key[i])) * s, 1023.0f); },
                              [&](int i) { return key[i]; }, weight_at, enough);
       uint32_t best = 0;
       if (ok) near(false, [&](uint32_t k, u64 sum) { best = enough(sum) ? k : 0; });
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) best = max(best, (uint32_t)__shfl_xor((int)best, o));
+      best = wave_max(best);
       const bool none = sh.bucket_at >= 1024;
       __syncthreads();
       if (ok) return best;
       if (none) return 0;
     }
-    return search(in, weight, enough);
+    uint32_t at;
+    return narrow(in, [&](float x, int) { return ~key_of(x); }, weight, enough, ~sh.hi, ~sh.lo, at) ? ~at : 0;
   };
-  // First bin up to `last` at which enough(running sum) holds, its sum before; BINS + 1: none.  Every wave for itself.
+  // First bin up to `last` at which enough(running sum) holds, the sum before it; BINS + 1: none, the sum of them all.
   auto first_bin = [&](const auto *of, int last, auto enough, auto &before) -> int {
     typedef typename std::remove_reference<decltype(before)>::type S;
-    S run = 0;
-    for (int i = 0; i <= last; i += 64) {
-      const S x = i + lane <= last ? (S)of[i + lane] : (S)0;
-      const S w = wave_scan64(x, lane);
-      const u64 hits = __ballot(i + lane <= last && enough(run + w));
-      if (hits) {
-        const int at = __ffsll((long long)hits) - 1;
-        before = run + shfl64(w, at) - shfl64(x, at);
-        return i + at;
-      }
-      run += shfl64(w, 63);
+    const S x = tid <= last ? (S)of[tid] : (S)0, scan = wave_scan64(x);
+    if (lane == 63) sh.wave_mass[wave] = __builtin_bit_cast(u64, scan);
+    if (tid == 0) sh.bucket_at = BINS + 1;
+    __syncthreads();
+    S run = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      if (w == wave) run = all;
+      all += __builtin_bit_cast(S, sh.wave_mass[w]);
     }
-    before = run;
-    return BINS + 1;
+    const u64 hits = __ballot(tid <= last && enough(run + scan));
+    if (hits && lane == __ffsll((long long)hits) - 1) atomicMin(&sh.bucket_at, tid);
+    __syncthreads();
+    const int at = sh.bucket_at;
+    if (tid == at) sh.bucket_before = __builtin_bit_cast(u64, run + (scan - x));
+    __syncthreads();
+    before = at <= BINS ? __builtin_bit_cast(S, sh.bucket_before) : all;
+    __syncthreads();
+    return at;
   };
   auto mass_at = [&](float x) { return g.mass(x, top); };
   // the bins of the row: sums over the pieces of what(piece, bin of the piece)
-  static_assert(BINS == NW * 64, "a bin for every thread");
+  static_assert(2 * BINS == NW * 64, "two threads for every bin, each with half of the pieces");
   auto add_bins = [&](auto *to, auto what) {
     typedef typename std::remove_reference<decltype(*to)>::type S;
+    const int bin = tid % BINS, half = wave / (NW / 2);
     S sum = 0;
-#pragma unroll 16
-    for (int c = 0; c < pieces; ++c) {
-      const int i = tid - sh.shift[c];
-      if (i >= 0) sum += what(c, i);
+    for (int c0 = half; c0 < pieces; c0 += 32) {  // (all requested before the first is used)
+      S x[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int c = min(c0 + 2 * j, pieces - 1);
+        x[j] = what(c, max(bin - sh.shift[c], 0));
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (c0 + 2 * j < pieces && bin >= sh.shift[c0 + 2 * j]) sum += x[j];
     }
-    to[tid] = sum;
+    if (half) ((S *)sh.bucket)[bin] = sum;
+    __syncthreads();
+    if (!half) to[bin] = sum + ((S *)sh.bucket)[bin];
     __syncthreads();
   };
 
@@ -450,14 +558,14 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     u64 before = 0;
     if (p.by_k) bound = min(bound, first_bin(sh.count, BINS - 1, [&](u64 n) { return n >= (u64)p.k; }, before));
     if (!p.by_k)
-      for (int i = 0; i <= min(bound, BINS - 1); i += 64) few += wave_sum64(i + lane <= min(bound, BINS - 1) ? (u64)sh.count[i + lane] : 0ull, lane);
+      for (int i = 0; i <= min(bound, BINS - 1); i += 64) few += wave_sum64(i + lane <= min(bound, BINS - 1) ? (u64)sh.count[i + lane] : 0ull);
   }
   if (!greedy && (p.by_k || (p.counts && bound < BINS && few <= CAP))) {
     if (tid < pieces) sh.wanted[tid] = sh.shift[tid] <= bound || (bound == BINS && sh.top[tid] > -INFINITY);
     auto in = [&](float x) { return g.bin(place, x) <= bound; };
+    bounds(0, bound);
     list(in);
-    take(true);
-    auto own_mass = [&](int i) { return mass[i]; };
+    auto own_mass = mass_in;
     float cut = lowest;
     if (p.by_k) {
       const uint32_t t = find(in, [](float) { return 1ull; }, [](int) { return 1ull; }, [&](u64 n) { return n >= (u64)p.k; });
@@ -465,11 +573,11 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     }
     auto kept = [&](int i) { return key[i] != 0 && key[i] >= key_of(cut); };
     auto total_kept = [&]() -> u64 {
-      if (!whole) return sum_of(in, [&](float x, int) { return x >= cut ? mass_at(x) : 0ull; }, 0);
+      if (!whole) return sum_of(in, [&](float x) { return x >= cut ? mass_at(x) : 0ull; }, 0);
       u64 mine = 0;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) mine += kept(i) ? mass[i] : 0ull;
-      mine = wave_sum64(mine, lane);
+      for (int i = 0; i < PER; ++i) mine += kept(i) ? mass_in(i) : 0ull;
+      mine = wave_sum64(mine);
       if (lane == 0) sh.sum[0][wave] = mine;
       __syncthreads();
       u64 s = 0;
@@ -493,18 +601,13 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     const int shift = max(32 - __clz(V - 1) - 10, 0);
     int token = V;
     __syncthreads();
-    if (whole && locate(kept, [&](int i) { return index[i] >> shift; }, [&](int i) { return (uint32_t)index[i]; }, own_mass, [&](u64 m) { return (double)m > target; })) {
+    if (whole && locate(kept, [&](int i) { return index_of(i) >> shift; }, [&](int i) { return (uint32_t)index_of(i); }, own_mass, [&](u64 m) { return (double)m > target; })) {
       near(true, [&](uint32_t i, u64 sum) { token = (double)sum > target ? (int)i : V; });
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) token = min(token, __shfl_xor(token, o));
-    } else {  // bit by bit, as large as it does not
-      __syncthreads();
-      auto below = [&](int end, int set) { return sum_of(in, [&](float x, int i) { return x >= cut && i < end ? mass_at(x) : 0ull; }, set); };
-      token = 0;
-      for (int bit = 31 - __clz(V), set = 1; bit >= 0; --bit, set ^= 1) {
-        const int trial = token | 1 << bit;
-        if (trial < V && !((double)below(trial, set) > target)) token = trial;
-      }
+      token = V - (int)wave_max((uint32_t)(V - token));
+    } else {
+      uint32_t at;
+      if (narrow(in, [&](float, int i) { return (uint32_t)i; }, [&](float x) { return x >= cut ? mass_at(x) : 0ull; }, [&](u64 m) { return (double)m > target; }, 0, V - 1, at))
+        token = (int)at;
     }
     if (tid == 0) answer(token);
     return;
@@ -523,18 +626,19 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
           const int i = bin - sh.shift[tid];
           sh.wanted[tid] = sh.top[tid] > -INFINITY && (bin >= BINS || (i >= 0 && bins[tid].mass[i] != 0));
         }
+        bounds(bin, bin);
         list(in);
       };
       double before = 0.0, total;     // masses: of the bins before `bin`, of all that min-p leaves
       if (p.counts) {                 // of the lowest bin only a part
-        for (int i = 0; i < bin; i += 64) before += wave_sum64(i + lane < bin ? sh.mass[i + lane] : 0.0, lane);
+        for (int i = 0; i < bin; i += 64) before += wave_sum64(i + lane < bin ? sh.mass[i + lane] : 0.0);
         list_bin();
-        total = before + (double)sum_of(in, [&](float x, int) { return mass_at(x); }, 0);
+        total = before + (double)sum_of(in, mass_at, 0);
         __syncthreads();
       } else {
         total = lane < pieces ? sh.kept[lane] : 0.0;
         if (lane + 64 < pieces) total += sh.kept[lane + 64];
-        total = wave_sum64(total, lane);
+        total = wave_sum64(total);
       }
       if (p.by_p) {
         const double need = (double)p.top_p * total;
@@ -543,33 +647,34 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
           bin = min(first, floor_bin);
           list_bin();
         }
-        take(true);
-        const uint32_t t = find(in, mass_at, [&](int i) { return mass[i]; }, [&](u64 m) { return before + (double)m >= need; });
+        const uint32_t t = find(in, mass_at, mass_in, [&](u64 m) { return before + (double)m >= need; });
         if (t) cut = fmaxf(cut, value_of(t));
       }
       cut = fminf(cut, top);
       // kept masses of the pieces: their bins above the cut's, and of that one what is not below the cut
       if (whole) {
-        for (int i = tid; i < sh.n; i += NW * 64)
-          if (sh.value[i] >= cut) atomicAdd(&sh.part[sh.index[i] / a.piece], mass_at(sh.value[i]));
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (key[i] && value_of(key[i]) >= cut) atomicAdd(&sh.part[index_of(i) >> piece_bits], mass_in(i));
       } else {
-        sweep([&](float x, int at) {
-          if (x >= cut && in(x)) atomicAdd(&sh.part[at / a.piece], mass_at(x));
+        sweep([&](float x, int at, bool hit) {
+          if (hit && x >= cut && in(x)) atomicAdd(&sh.part[at >> piece_bits], mass_at(x));
         });
       }
       __syncthreads();
       for (int c = wave; c < pieces; c += NW) {
         double m = 0.0;
         const int most = sh.top[c] == -INFINITY ? 0 : min(bin - sh.shift[c], BINS);
-        for (int i = lane; i < most; i += 64) m += (double)bins[c].mass[i];
-        m = wave_sum64(m, lane) * sh.scale[c] + (double)sh.part[c];
+  #pragma unroll 8
+      for (int i = lane; i < BINS; i += 64) m += i < most ? (double)bins[c].mass[i] : 0.0;
+        m = wave_sum64(m) * sh.scale[c] + (double)sh.part[c];
         if (lane == 0) sh.kept[c] = m;
       }
       __syncthreads();
     }
     double all = lane < pieces ? sh.kept[lane] : 0.0;
     if (lane + 64 < pieces) all += sh.kept[lane + 64];
-    target = (double)p.u * wave_sum64(all, lane);
+    target = (double)p.u * wave_sum64(all);
   }
   // ---- the piece in which the running mass passes the target (with rounding, or u = 0, perhaps one behind), and the token
   int piece = 0;
@@ -577,27 +682,34 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   if (greedy) {
     while (piece < pieces - 1 && sh.top[piece] != top) ++piece;
   } else {
-    while (piece < pieces - 1 && !(run + sh.kept[piece] > target)) run += sh.kept[piece++];
+    for (int c0 = 0; c0 < pieces; c0 += 64) {
+      const double m = c0 + lane < pieces ? sh.kept[c0 + lane] : 0.0, scan = wave_scan64(m);
+      const u64 hits = __ballot(c0 + lane < pieces && run + scan > target);
+      const int at = hits ? __ffsll((long long)hits) - 1 : 63;
+      piece = min(c0 + at, pieces - 1);
+      run += lane64(scan, at) - lane64(m, at);
+      if (hits) break;
+      if (piece < pieces - 1) run += lane64(m, at);
+    }
   }
   auto mass_of = [&](float x) -> u64 { return !(x >= cut) || x == -INFINITY ? 0ull : greedy ? 1ull : mass_at(x); };
   int last = 0;                       // the last token that has a mass: what rounding at the very end leaves
   for (; piece < pieces && top > -INFINITY; ++piece) {
     // a wave takes a sixteenth, 256 tokens at a time
     const int begin = piece * a.piece, end = min(begin + a.piece, V), share = a.piece / NW, w0 = begin + wave * share, w1 = min(w0 + share, end);
-    u64 mine = 0;
+    u64 mine = 0, own[4];
     int seen = -1;
     for (int at = w0; at < w1; at += 256) {
       const floatx4 v = load4(z, at + 4 * lane, w1, vec);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const u64 m = mass_of(v[j]);
-        mine += m;
-        if (m) seen = at + 4 * lane + j;
+        own[j] = mass_of(v[j]);
+        mine += own[j];
+        if (own[j]) seen = at + 4 * lane + j;
       }
     }
-    mine = wave_sum64(mine, lane);
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) seen = max(seen, __shfl_xor(seen, o));
+    mine = wave_sum64(mine);
+    seen = (int)wave_max((uint32_t)(seen + 1)) - 1;
     __syncthreads();
     if (lane == 0) {
       sh.sum[0][wave] = mine;
@@ -618,11 +730,12 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     if (wave != win) return;
     u64 before = 0;
     for (int at = w0; at < w1; at += 256) {
-      const floatx4 v = load4(z, at + 4 * lane, w1, vec);
-      u64 own[4], sum = 0;
+      if (share > 256) {  // (a share of 256 is there already)
+        const floatx4 v = load4(z, at + 4 * lane, w1, vec);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum += own[j] = mass_of(v[j]);
-      const u64 scan = wave_scan64(sum, lane);
+        for (int j = 0; j < 4; ++j) own[j] = mass_of(v[j]);
+      }
+      const u64 sum = own[0] + own[1] + own[2] + own[3], scan = wave_scan64(sum);
       u64 x = before + scan - sum;
       int found = 4;
 #pragma unroll
@@ -636,7 +749,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
         last = at + 4 * l + __shfl(found, l);
         break;
       }
-      before += shfl64(scan, 63);
+      before += lane64(scan, 63);
     }
     if (lane == 0) answer(last);
     return;
