@@ -363,6 +363,23 @@ struct QueryTile {
 #pragma unroll
     for (int m = 0; m < DH / 16; ++m) O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
+  __device__ void relative(const floatx4 (&S)[2], float c, float (&p)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_fmaf(S[j >> 2][j & 3], c, -m_ref);
+  }
+  __device__ static float most(const float (&x)[8]) {
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  }
+  __device__ void raise(float bm) {  // the reference to bm, this lane's largest score, if that is above it
+    bm = fmaxf(bm, __shfl_xor(bm, 16));  // lanes 16 and 32 apart hold the same query
+    bm = fmaxf(bm, __shfl_xor(bm, 32));
+    const float m_new = fmaxf(m_ref, bm), alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+    m_ref = m_new;
+    if constexpr (SHARES) L[0] *= alpha;
+    else L *= alpha;
+#pragma unroll
+    for (int m = 0; m < DH / 16; ++m) O[m] *= alpha;
+  }
   // The weights of a block from its scores S[tl][i] (position 16 tl + 4 grp + i), rounded to bf16 for the products (by 2^-8 of
   // a weight at most; the denominator adds the rounded ones).  masked: positions from `limit` of the block on have none.
   template <bool FP8>
@@ -372,20 +389,15 @@ struct QueryTile {
       for (int j = 0; j < 8; ++j)
         if (block_pos(j, 0) >= limit - 4 * grp) S[j >> 2][j & 3] = -INFINITY;
     }
-    float bm = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3]))) * c;
-    if (__any(bm > m_ref + 8.0f)) {
-      bm = fmaxf(bm, __shfl_xor(bm, 16));  // lanes 16 and 32 apart hold the same query
-      bm = fmaxf(bm, __shfl_xor(bm, 32));
-      const float m_new = fmaxf(m_ref, bm), alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
-      m_ref = m_new;
-      if constexpr (SHARES) L[0] *= alpha;
-      else L *= alpha;
-#pragma unroll
-      for (int m = 0; m < DH / 16; ++m) O[m] *= alpha;
-    }
     float p[8];
+    relative(S, c, p);
+    if (__any(most(p) > 8.0f)) {
+      const float x[8] = {S[0][0], S[0][1], S[0][2], S[0][3], S[1][0], S[1][1], S[1][2], S[1][3]};
+      raise(most(x) * c);
+      relative(S, c, p);
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], c, -m_ref));
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(p[j]);
     bf16x8 pv = pack8(p);
     if constexpr (SHARES) {
 #pragma unroll
@@ -828,12 +840,17 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 }
 
 // Many queries: the waves of a workgroup have two tiles each, 128 queries together, and share the blocks, which a ring of
-// stages in LDS holds: filled by LDS-direct loads two stages ahead, one bare barrier a stage (as k_attention_rows does; 8-bit
-// blocks stay codes in LDS, and every wave converts what it reads).  Bound by LDS reads (a block is read by every wave) and by
-// what the softmax takes of the vector units.
+// stages in LDS holds: filled by LDS-direct loads, one bare barrier for two blocks (8-bit blocks stay codes in LDS, and every wave
+// converts what it reads).  Blocks that all queries see whole are taken two at a time with one branch for all weights, the values
+// requested before it.  80 KB of stages and up to 256 registers: two workgroups a CU.  Three (168 registers, three stages, a
+// block at a time, fragments requested as they are needed): us, 8 rows of 512 new tokens behind 2048, 32 heads of 128, bf16
+// 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 340.  Bound by the vector units (softmax;
+// conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.
+constexpr int rows_stages(int dh, bool fp8) { return dh == 128 && !fp8 ? 5 : 8; }
+constexpr size_t rows_lds(int dh, bool fp8) { return (size_t)rows_stages(dh, fp8) * (32 * dh * (fp8 ? 2 : 4) + (fp8 ? 256 : 0)); }
 template <int DH, bool FP8>
-__global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int pairs) {
-  constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = 3, NQ = 16 * NT * NW;
+__global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs) {
+  constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = rows_stages(DH, FP8), NQ = 16 * NT * NW;
   constexpr int KF = FP8 ? QC : 2 * QC, FR = KF + (FP8 ? VM / 2 : VM), LPW = FR / NW;  // fragments a stage, loads of a wave
   constexpr int STAGE = FR * 64 + (FP8 ? 16 : 0);  // 16-byte pieces; behind 8-bit blocks 256 bytes for their exponents
   extern __shared__ uint32x4 ring[];               // [NS][STAGE]
@@ -857,10 +874,16 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int pairs
   // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked, as is every block from the
   // moment on at which a window has an entry that is no page.
   const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
-  int ip = s.lo / bpp, ib = s.lo % bpp, pages = 0, window = -1, none[NS];
+  int ip = s.lo / bpp, ib = s.lo % bpp, pages = 0, window = -1;
+  uint32_t none = 0;                               // a bit for each stage: its block has no page
+  int into = 0, from = 0, asked = s.lo;            // stages of the next block requested and used; blocks requested
   bool gaps = false;
   const int ip_end = (s.hi + bpp - 1) / bpp;
-  auto request = [&](int blk) {
+  const uint32x4 *src = nullptr;                   // this wave's part of the next block
+  const unsigned char *ex_src = nullptr;
+  bool is = false;
+  auto next = [](int stage) { return stage == NS - 1 ? 0 : stage + 1; };
+  auto new_page = [&]() {
     if (ip >> 6 != window) {
       window = ip >> 6;
       const int at = window * 64 + lane;
@@ -869,34 +892,36 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int pairs
       gaps |= __any(at >= ip && at < ip_end && (pages < 0 || pages >= a.kv.pages));
     }
     int page = __builtin_amdgcn_readlane(pages, ip & 63);
-    const bool is = page >= 0 && page < a.kv.pages;
+    is = page >= 0 && page < a.kv.pages;
     if (!is) page = 0;
-    const int slot = (blk - s.lo) % NS;
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-      if (i == slot) none[i] = !is;
     const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
     const long at = (long)h * bpp + ib;
-    const uint32x4 *src = (const uint32x4 *)(pg + at * ((FP8 ? 64 : 128) * DH)) + wave * LPW * 64;
-    uint32x4 *dst = ring + slot * STAGE + wave * LPW * 64;
+    src = (const uint32x4 *)(pg + at * ((FP8 ? 64 : 128) * DH)) + wave * LPW * 64;
+    ex_src = pg + (long)H * bpp * (64 * DH) + at * 64;
+  };
+  if (s.lo < s.hi) new_page();
+  auto request = [&]() {
+    none = (none & ~(1u << into)) | (uint32_t)!is << into;
+    uint32x4 *dst = ring + into * STAGE + wave * LPW * 64;
 #pragma unroll
     for (int i = 0; i < LPW; ++i)
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)&(src + i * 64)[lane],
                                        (__attribute__((address_space(3))) void *)(dst + i * 64), 16, 0, 0);
-    if constexpr (FP8) {  // every wave, so that all wait for the same number of loads; lanes 16 .. 63 repeat
-      const unsigned char *ex = pg + (long)H * bpp * (64 * DH) + at * 64;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(ex + 4 * col),
-                                       (__attribute__((address_space(3))) void *)(ring + slot * STAGE + FR * 64), 4, 0, 0);
-    }
+    if constexpr (FP8)  // every wave, so that all wait for the same number of loads; lanes 16 .. 63 repeat
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(ex_src + 4 * col),
+                                       (__attribute__((address_space(3))) void *)(ring + into * STAGE + FR * 64), 4, 0, 0);
+    into = next(into);
+    ++asked;
+    src += FR * 64;
+    ex_src += 64;
     if (++ib == bpp) {
       ib = 0;
-      ++ip;
+      if (++ip < ip_end) new_page();
     }
   };
   constexpr int LOADS = LPW + (FP8 ? 1 : 0);
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (s.lo + i < s.hi) request(s.lo + i);
+  for (int i = 0; i < NS - 2; ++i)
+    if (asked < s.hi) request();
 #pragma unroll
   for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
   wait_vmcnt<0>();  // (waited for inside the loop, the queries would make the compiler wait for the ring as well)
@@ -905,57 +930,145 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int pairs
 #pragma unroll
     for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
 
-  auto use = [&](auto masked_, int blk, bool no_page) {
-    constexpr bool masked = decltype(masked_)::value;
-    const int base = blk * 32;
-    const uint32x4 *kv = ring + (blk - s.lo) % NS * STAGE + lane;
-    const unsigned char *ex = (const unsigned char *)(ring + (blk - s.lo) % NS * STAGE + FR * 64);
-    floatx4 S[NT][2];
+  // scores of a block: S[t][tl][i] of position 16 tl + 4 grp + i
+  auto scores = [&](int stage, floatx4 (&S)[NT][2]) {
+    const uint32x4 *kv = ring + stage * STAGE + lane;
+    const unsigned char *ex = (const unsigned char *)(ring + stage * STAGE + FR * 64);
+    uint32x4 kw[KF];
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl) {
-      const uint32_t ke = FP8 ? ex[16 * tl + col] : 0;
+    for (int i = 0; i < KF; ++i) kw[i] = kv[i * 64];
+    const uint32_t ke[2] = {FP8 ? ex[col] : 0u, FP8 ? ex[16 + col] : 0u};
 #pragma unroll
-      for (int t = 0; t < NT; ++t) S[t][tl] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < QC; ++c) {
+    for (int c = 0; c < QC; ++c)
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
         bf16x8 kf;
         if constexpr (FP8) {
-          const uint32x4 w = kv[(tl * (QC / 2) + c / 2) * 64];
-          kf = widen(w[c % 2 * 2], w[c % 2 * 2 + 1], ke);
+          const uint32x4 w = kw[tl * (QC / 2) + c / 2];
+          kf = widen(w[c % 2 * 2], w[c % 2 * 2 + 1], ke[tl]);
         } else {
-          kf = __builtin_bit_cast(bf16x8, kv[(tl * QC + c) * 64]);
+          kf = __builtin_bit_cast(bf16x8, kw[tl * QC + c]);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][c], S[t][tl], 0, 0, 0);
       }
-    }
-    float vs[8];
-    if constexpr (FP8) {
-      const uint32_t ve[2] = {((const uint32_t *)ex)[8 + grp], ((const uint32_t *)ex)[12 + grp]};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) vs[j] = kv8_factor(ve[j >> 2], j & 3);
-    }
-    bf16x8 pv[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) pv[t] = tile[t].template weights<FP8>(masked, S[t], a.c, no_page ? 0 : limit[t] - base, grp, vs);
+  };
+  auto factor_words = [&](int stage, uint32_t (&ve)[2]) {
+    const uint32_t *ex = (const uint32_t *)(ring + stage * STAGE + FR * 64);
+    ve[0] = ex[8 + grp];
+    ve[1] = ex[12 + grp];
+  };
+  auto add_values = [&](const uint32x4 (&vw)[FR - KF], const bf16x8 (&pv)[NT]) {
 #pragma unroll
     for (int m = 0; m < VM; ++m) {
       bf16x8 vf;
       if constexpr (FP8) {
-        const uint32x4 w = kv[(KF + m / 2) * 64];
+        const uint32x4 w = vw[m / 2];
         vf = widen(w[m % 2 * 2], w[m % 2 * 2 + 1], 127);
       } else {
-        vf = __builtin_bit_cast(bf16x8, kv[(KF + m) * 64]);
+        vf = __builtin_bit_cast(bf16x8, vw[m]);
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv[t], tile[t].O[m], 0, 0, 0);
     }
   };
+  auto values_of = [&](int stage, uint32x4 (&vw)[FR - KF]) {
+#pragma unroll
+    for (int i = 0; i < FR - KF; ++i) vw[i] = ring[stage * STAGE + (KF + i) * 64 + lane];
+  };
+  auto use = [&](int blk, bool no_page) {
+    const int base = blk * 32;
+    floatx4 S[NT][2];
+    scores(from, S);
+    float vs[8];
+    if constexpr (FP8) {
+      uint32_t ve[2];
+      factor_words(from, ve);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vs[j] = kv8_factor(ve[j >> 2], j & 3);
+    }
+    bf16x8 pv[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) pv[t] = tile[t].template weights<FP8>(true, S[t], a.c, no_page ? 0 : limit[t] - base, grp, vs);
+    uint32x4 vw[FR - KF];
+    values_of(from, vw);
+    add_values(vw, pv);
+  };
+  // Two blocks that every query sees whole: one branch for all of their weights, so that from there on exponentials and products
+  // are formed side by side, and the values are on their way before.
+  auto use_two = [&](int one, int two) {
+    const int stage[2] = {one, two};
+    floatx4 S[2][NT][2];
+    uint32_t ve[2][2];
+    float vs[2][8];
+    uint32x4 vw[FR - KF];
+    bool raise = false;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      __builtin_amdgcn_s_setprio(1);  // (before the other waves' exponentials: 140 -> 136 us)
+      scores(stage[u], S[u]);
+      __builtin_amdgcn_s_setprio(0);
+      if constexpr (FP8) {
+        factor_words(stage[u], ve[u]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vs[u][j] = __uint_as_float((j & 3) == 3 ? ve[u][j >> 2] >> 1 & 0x7f800000u : ve[u][j >> 2] << (23 - 8 * (j & 3)) & 0x7f800000u);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raise |= (((ve[u][i] & 0x7f7f7f7fu) + 0x01010101u) & ve[u][i] & 0x80808080u) != 0;
+      }
+    }
+    values_of(stage[0], vw);
+    float p[2][NT][8];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        tile[t].relative(S[u][t], a.c, p[u][t]);
+        raise |= tile[t].most(p[u][t]) > 8.0f;
+      }
+    if (__any(raise)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) most = fmaxf(most, S[u][t][j >> 2][j & 3]);
+        tile[t].raise(most * a.c);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) tile[t].relative(S[u][t], a.c, p[u][t]);
+      }
+      if constexpr (FP8)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) vs[u][j] = kv8_factor(ve[u][j >> 2], j & 3);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8 pv[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[u][t][j] = __builtin_amdgcn_exp2f(p[u][t][j]);
+        pv[t] = pack8(p[u][t]);
+        tile[t].L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones(), pv[t], tile[t].L, 0, 0, 0);
+        if constexpr (FP8) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[u][t][j] *= vs[u][j];
+          pv[t] = pack8(p[u][t]);
+        }
+      }
+      add_values(vw, pv);
+      if (u == 0) values_of(stage[1], vw);
+    }
+  };
   // clears what a stage holds from position `valid` of its block on
-  auto clear = [&](int blk, int valid) {
+  auto clear = [&](int valid) {
     const Keep keep(valid, grp);
     for (int m = wave; m < FR - KF; m += NW) {
-      uint32x4 &v = ring[(blk - s.lo) % NS * STAGE + (KF + m) * 64 + lane];
+      uint32x4 &v = ring[from * STAGE + (KF + m) * 64 + lane];
       uint32x4 x = v;
       if constexpr (FP8) x &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
       else keep.bf16(x);
@@ -966,30 +1079,32 @@ __global__ __launch_bounds__(256, 3) void k_kv_attend_rows(KvAttend a, int pairs
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  auto open = [&](int blk) {
-    // this wave's loads of the stage have landed once only those of the next one are outstanding
-    if (blk + 1 < s.hi) wait_vmcnt<LOADS>();
+  // waits until the next `n` blocks are there for all waves, and requests others into the stages of those before
+  auto open = [&](int blk, int n) {
+    const int ahead = asked - blk - n;  // requested behind them
+    if (ahead >= 3) wait_vmcnt<3 * LOADS>();
+    else if (ahead == 2) wait_vmcnt<2 * LOADS>();
+    else if (ahead == 1) wait_vmcnt<LOADS>();
     else wait_vmcnt<0>();
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave's reads of the stage before
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave's reads of the stages before
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    bool no_page = false;
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-      if (i == (blk - s.lo) % NS) no_page = none[i];
-    if (blk + NS - 1 < s.hi) request(blk + NS - 1);  // into the place of the stage before
-    return no_page;
+    while (asked < min(s.hi, blk + NS)) request();
   };
   int blk = s.lo;
-  for (; blk < min(whole, s.hi) && !gaps; ++blk) {
-    (void)open(blk);
-    if (busy) use(std::false_type(), blk, false);
+  for (; blk + 2 <= min(whole, s.hi) && !gaps; blk += 2) {
+    open(blk, 2);
+    const int second = next(from);
+    if (busy) use_two(from, second);
+    from = next(second);
   }
   for (; blk < s.hi; ++blk) {
-    const bool no_page = open(blk);
-    if (no_page || blk * 32 + 32 > s.held) clear(blk, no_page ? 0 : s.held - blk * 32);
-    if (blk < last) use(std::true_type(), blk, no_page);
+    open(blk, 1);
+    const bool no_page = none >> from & 1;
+    if (no_page || blk * 32 + 32 > s.held) clear(no_page ? 0 : s.held - blk * 32);
+    if (blk < last) use(blk, no_page);
+    from = next(from);
   }
   if constexpr (!FP8) {
     if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH>(a, s, q0, limit, s.lo, 1, last, tile);
@@ -1160,8 +1275,9 @@ static void attend(hipStream_t s, const KvAttend &a) {
   const AttendPlan p = plan_attend(a.kv, a.tk, a.heads);
   const dim3 grid((unsigned)(p.tiles * p.pairs), a.splits);
   if (p.nq == 128) {
-    const size_t lds = 3 * (32 * DH * (FP8 ? 2 : 4) + (FP8 ? 256 : 0));
-    SKD_LAUNCH((k_kv_attend_rows<DH, FP8>), grid, dim3(256), lds, s, a, p.pairs);
+    static std::atomic<uint64_t> done{0};
+    if (rows_lds(DH, FP8) > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend_rows<DH, FP8>}, rows_lds(DH, FP8));
+    SKD_LAUNCH((k_kv_attend_rows<DH, FP8>), grid, dim3(256), rows_lds(DH, FP8), s, a, p.pairs);
   } else if (p.nq == 32) {
     launch_attend<DH, FP8, 2, 8>(s, a, grid, p.pairs);
   } else if (p.waves == 4) {
