@@ -119,7 +119,8 @@ struct Grid {
   const double *tab;          // 2^(i / 64)
   __device__ Grid(float T, const double *t) : s((float)(16.0 / (double)T)), c(64.0 * 1.44269504088896340736 / (double)T), tab(t) {}
   __device__ float place(float z) const { return floorf(z * s); }
-  __device__ int bin(float top_place, float z) const { return (int)fminf(top_place - place(z), (float)BINS); }  // (NaN: the rest)
+  // (where places overflow, what differs from the largest logit is far below it: NaN is the rest)
+  __device__ int bin(float top, float top_place, float z) const { return z == top ? 0 : (int)fminf(top_place - place(z), (float)BINS); }
   // 64 log2 of a mass is split into n + r: 2^(n / 64) from the table, 2^(r / 64) by its series (|r| <= 1/2: the first term left
   // out is below 2^-44); in units of 2^-45, nearest
   __device__ u64 mass(float z, float top) const {
@@ -182,7 +183,7 @@ __global__ __launch_bounds__(256) void k_sample_bins(SampleRows a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (v[i][j] >= lowest && v[i][j] > -INFINITY) {
-        const int bin = g.bin(place, v[i][j]);
+        const int bin = g.bin(top, place, v[i][j]);
         if (p.counts) atomicAdd(&count[bin], 1u);
         if (p.masses) atomicAdd(&mass[bin], g.mass(v[i][j], top));
       }
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   if (tid < pieces) {
     const float t = bins[tid].top;
     sh.top[tid] = t;
-    sh.shift[tid] = t == -INFINITY ? BINS + 1 : (int)fminf(place - g.place(t), (float)(BINS + 1));
+    sh.shift[tid] = t == -INFINITY ? BINS + 1 : t == top ? 0 : (int)fminf(place - g.place(t), (float)(BINS + 1));
     sh.scale[tid] = t == -INFINITY || greedy ? 0.0 : exp(((double)t - (double)top) / (double)p.T);
     sh.kept[tid] = t == -INFINITY || greedy || !p.masses ? 0.0 : (double)bins[tid].all * sh.scale[tid];
     sh.part[tid] = 0;
@@ -296,7 +297,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     const bool sound = g.s < INFINITY && w < INFINITY;
     low = sound && last < BINS ? fmaxf(lowest, nextafterf((float)lo, -INFINITY)) : lowest;
     low = fmaxf(low, -FLT_MAX);
-    high = sound && first > 0 ? nextafterf((float)hi, INFINITY) : INFINITY;
+    high = sound && first > 0 && hi == hi ? nextafterf((float)hi, INFINITY) : INFINITY;  // (places that overflowed)
   };
   // Lists the tokens for which `in` holds, a wave's in its own part of the list, their masses beside them, and takes them into registers;
   // whether all of them fit.  lo, hi: their smallest and largest key.
@@ -550,7 +551,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     __syncthreads();
   };
 
-  const int floor_bin = greedy ? 0 : g.bin(place, lowest);
+  const int floor_bin = greedy ? 0 : g.bin(top, place, lowest);
   int bound = floor_bin;              // top-k or min-p: the bin of the k-th, or of the lowest that min-p leaves
   u64 few = 0;                        // tokens up to that bin
   if (p.counts && !greedy) {
@@ -562,7 +563,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   }
   if (!greedy && (p.by_k || (p.counts && bound < BINS && few <= CAP))) {
     if (tid < pieces) sh.wanted[tid] = sh.shift[tid] <= bound || (bound == BINS && sh.top[tid] > -INFINITY);
-    auto in = [&](float x) { return g.bin(place, x) <= bound; };
+    auto in = [&](float x) { return g.bin(top, place, x) <= bound; };
     bounds(0, bound);
     list(in);
     auto own_mass = mass_in;
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
       // ---- top-p alone, or a min-p that leaves many
       add_bins(sh.mass, [&](int c, int i) { return (double)bins[c].mass[i] * sh.scale[c]; });
       int bin = floor_bin;
-      auto in = [&](float x) { return g.bin(place, x) == bin; };
+      auto in = [&](float x) { return g.bin(top, place, x) == bin; };
       auto list_bin = [&]() {
         if (tid < pieces) {
           const int i = bin - sh.shift[tid];
@@ -685,11 +686,11 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     for (int c0 = 0; c0 < pieces; c0 += 64) {
       const double m = c0 + lane < pieces ? sh.kept[c0 + lane] : 0.0, scan = wave_scan64(m);
       const u64 hits = __ballot(c0 + lane < pieces && run + scan > target);
-      const int at = hits ? __ffsll((long long)hits) - 1 : 63;
-      piece = min(c0 + at, pieces - 1);
-      run += lane64(scan, at) - lane64(m, at);
+      const int at = hits ? __ffsll((long long)hits) - 1 : min(63, pieces - 1 - c0);
+      piece = c0 + at;
+      if (!hits && piece < pieces - 1) run += lane64(scan, 63);
+      else if (at) run += lane64(scan, at - 1);  // (not above the target)
       if (hits) break;
-      if (piece < pieces - 1) run += lane64(m, at);
     }
   }
   auto mass_of = [&](float x) -> u64 { return !(x >= cut) || x == -INFINITY ? 0ull : greedy ? 1ull : mass_at(x); };
@@ -741,7 +742,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         x += own[j];
-        if (found == 4 && upto + (double)x > target) found = j;
+        if (found == 4 && own[j] && upto + (double)x > target) found = j;
       }
       const u64 hits = __ballot(found < 4);
       if (hits) {

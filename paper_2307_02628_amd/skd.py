@@ -114,6 +114,16 @@ class SkdError(RuntimeError):
         self.code = code
 
 
+_DTYPES: dict = {}
+
+
+def _dtype_of(t) -> str:
+    name = _DTYPES.get(t.dtype)
+    if name is None:
+        name = _DTYPES[t.dtype] = str(t.dtype)
+    return name
+
+
 def _check(rc: int, where: str) -> int:
     if rc < 0:
         raise SkdError(rc, where)
@@ -407,10 +417,10 @@ class KvCache:
         """Pointer and stride of [tokens][heads][head_dim] or [tokens][heads * head_dim]."""
         if chunk.rows != self.rows:
             raise ValueError("chunk and block table differ in rows")
-        shape, stride = t.shape, t.stride()
-        if shape[0] != chunk.tokens or tuple(shape[1:]) not in ((heads, self.dh), (heads * self.dh,)) or stride[-1] != 1 or (len(shape) == 3 and stride[1] != self.dh):
+        shape, stride = tuple(t.shape), t.stride()
+        if shape not in ((chunk.tokens, heads, self.dh), (chunk.tokens, heads * self.dh)) or stride[-1] != 1 or (len(shape) == 3 and stride[1] != self.dh):
             raise ValueError(f"expected [{chunk.tokens}][{heads}][{self.dh}] with dense tokens")
-        if str(t.dtype) not in types:
+        if _dtype_of(t) not in types:
             raise ValueError(f"expected {' or '.join(types)}")
         return t.data_ptr(), max(stride[0], heads * self.dh) if shape[0] < 2 else stride[0]
 
@@ -420,7 +430,7 @@ class KvCache:
 
     def read(self, chunk: KvChunk, k_out, v_out, stream: int = 0):
         """k_out, v_out: both float32 or both bfloat16."""
-        elem = W_FP32 if str(k_out.dtype) == "torch.float32" else W_BF16
+        elem = W_FP32 if _dtype_of(k_out) == "torch.float32" else W_BF16
         types = ("torch.float32",) if elem == W_FP32 else ("torch.bfloat16",)
         _check(self._lib.skd_kv_read(self.ref, chunk.ref, elem, *self._rows_of(chunk, self.heads, k_out, *types),
                                      *self._rows_of(chunk, self.heads, v_out, *types), stream), "skd_kv_read")
@@ -439,7 +449,7 @@ class KvCache:
 
 
 def _expect(t, dtype: str, dims: int):
-    if str(t.dtype) != "torch." + dtype or t.dim() != dims or not t.is_contiguous():
+    if _dtype_of(t) != "torch." + dtype or t.dim() != dims or not t.is_contiguous():
         raise ValueError(f"expected a contiguous {dtype} tensor of {dims} dimensions")
 
 
@@ -449,7 +459,7 @@ def sample_workspace(rows: int, vocab: int) -> int:
 
 def sample(logits, u, tokens_out, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, stream: int = 0):
     """skd_sample on device tensors: logits [rows][vocab] float32 with dense rows, u and the parameters [rows] (None: off)."""
-    if str(logits.dtype) != "torch.float32" or logits.dim() != 2 or logits.stride(1) != 1:
+    if _dtype_of(logits) != "torch.float32" or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("expected float32 logits with dense rows")
     rows, vocab = logits.shape
     for t, dtype in ((u, "float32"), (tokens_out, "int32"), (temperature, "float32"), (top_k, "int32"), (top_p, "float32"), (min_p, "float32")):

@@ -122,6 +122,35 @@ def test_temperatures(t):
     check(z, r[0], temperature=[t] * 7, top_k=[20] * 7, min_p=[0.001] * 7)
 
 
+@pytest.mark.parametrize("t", [1e-37, 1e-30, 1e-3, 1.0, 3e38, math.inf])
+@pytest.mark.parametrize("offset", [-3e38, -1e10, -700.0, 1e4, 1e10])
+def test_logits_far_from_zero(offset, t):
+    """Places on the grid of bins that overflow, that are not distinct, or that are all the same."""
+    z, r = some(4, 5003, 2.0, 15)
+    z = z + offset
+    check(z, r[0], temperature=[t] * 4)
+    check(z, r[0], temperature=[t] * 4, top_p=[0.8, 0.3, 0.99, 0.0])
+    check(z, r[0], temperature=[t] * 4, top_k=[20, 1, 3000, 5003], min_p=[0.001] * 4)
+    check(z, r[0], temperature=[t] * 4, top_p=[0.8] * 4, min_p=[0.5] * 4)
+
+
+@pytest.mark.parametrize("levels", [2, 40, 4000])
+def test_long_lists_of_few_values(levels):
+    """Thresholds among more tokens than are listed, and buckets with many equal ones."""
+    B, V = 8, 100003
+    g = torch.Generator().manual_seed(levels)
+    z = (torch.randint(0, levels, (B, V), generator=g).float() / levels * 0.5).cuda()
+    u = torch.rand(B, generator=g).numpy()
+    k = np.array([0, 1, 9000, 50000, 99999, 8192, 8193, 3])
+    p = np.array([0.5, 1.0, 0.9, 0.99, 0.05, 1.0, 0.3, 0.7])
+    m = np.array([0.0, 0.0, 0.0, 0.5, 0.8, 0.9, 0.7, 0.99])
+    check(z, u, top_k=k)
+    check(z, u, top_p=p)
+    check(z, u, min_p=m)
+    check(z, u, top_k=k, top_p=p, min_p=m)
+    check(z, u, temperature=[0.01] * B, top_k=k, top_p=p, min_p=m)
+
+
 def test_values_outside_their_ranges():
     z, _ = some(6, 500, 2.0, 6)
     nan = math.nan
