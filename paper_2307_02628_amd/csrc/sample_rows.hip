@@ -19,8 +19,9 @@
 // or a trip to memory 0.3 to 1 us, so four tokens are compared at once, the waves' sums move in registers, and requests go out
 // together.
 // us (bins + pick), one workgroup per row for everything (six passes over the row) -> this: 128 rows of 131072 with mixed
-// parameters 227 -> 62 to 69 (21 + 48), one row of 50272 with top-p 75 -> 21 (5 + 16).  1024 bins of T / 32 cost
-// twice the traffic: one row 33; shuffles through LDS for the sums and one list for all waves: 25 and 95.
+// parameters 227 -> 60 (21 + 39), one row of 50272 with top-p 75 -> 22 (5 + 17).  1024 bins of T / 32 cost twice the traffic: one
+// row 33; shuffles through LDS for the sums and one list for all waves: 25 and 95; the bin of every token computed instead of
+// compared with its edges, and the last 64 searched by every wave: 128 rows 70.
 #include "sample_rows.h"
 
 #include <float.h>
@@ -81,6 +82,11 @@ __device__ inline uint32_t wave_max(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 __device__ inline float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+__device__ inline float uniform(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v))); }
+__device__ inline double uniform(double v) {
+  const u64 b = __builtin_bit_cast(u64, v);
+  return __builtin_bit_cast(double, (u64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b) | (u64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) << 32);
+}
 __device__ inline float wave_top(float v) { return value_of(wave_max(key_of(v))); }
 
 // What a row's parameters come to.
@@ -90,13 +96,13 @@ struct Params {
   double log_min;             // log(min_p); 0 from 1 on, -32 where it is off (or below e^-32)
   bool greedy, by_k, by_p;
   bool counts, masses;        // what the bins hold: rows with top-k, all others, both with min-p alone
-  __device__ Params(const SampleRows &a, int b) {
+  __device__ __forceinline__ Params(const SampleRows &a, int b) {
     T = a.temperature ? a.temperature[b] : 1.0f;
     k = a.top_k ? a.top_k[b] : 0;
     top_p = a.top_p ? fmaxf(a.top_p[b], 0.f) : 1.0f;
     if (a.top_p && a.top_p[b] != a.top_p[b]) top_p = 1.0f;
     const float m = a.min_p ? a.min_p[b] : 0.f;
-    log_min = m > 0.f ? fmax(m < 1.f ? log((double)m) : 0.0, -32.0) : -32.0;
+    log_min = uniform(m > 0.f ? fmax(m < 1.f ? log((double)m) : 0.0, -32.0) : -32.0);
     u = fminf(fmaxf(a.u[b], 0.f), 0x1.fffffep-1f);  // (NaN: 0)
     greedy = !(T > 0.f);
     by_k = !greedy && k > 0 && k < a.vocab;
@@ -105,7 +111,7 @@ struct Params {
     masses = !greedy && !by_k;
   }
   // the smallest float that is not below top + T * log_min
-  __device__ float floor_of(float top) const {
+  __device__ __forceinline__ float floor_of(float top) const {
     const double f = (double)top + (double)T * log_min;
     float x = (float)f;
     if ((double)x < f) x = nextafterf(x, INFINITY);
@@ -117,13 +123,13 @@ struct Grid {
   float s;                    // 16 / T
   double c;                   // 64 log2(e) / T
   const double *tab;          // 2^(i / 64)
-  __device__ Grid(float T, const double *t) : s((float)(16.0 / (double)T)), c(64.0 * 1.44269504088896340736 / (double)T), tab(t) {}
+  __device__ __forceinline__ Grid(float T, const double *t) : s(uniform((float)(16.0 / (double)T))), c(uniform(64.0 * 1.44269504088896340736 / (double)T)), tab(t) {}
   __device__ float place(float z) const { return floorf(z * s); }
   // (where places overflow, what differs from the largest logit is far below it: NaN is the rest)
   __device__ int bin(float top, float top_place, float z) const { return z == top ? 0 : (int)fminf(top_place - place(z), (float)BINS); }
   // 64 log2 of a mass is split into n + r: 2^(n / 64) from the table, 2^(r / 64) by its series (|r| <= 1/2: the first term left
   // out is below 2^-44); in units of 2^-45, nearest
-  __device__ u64 mass(float z, float top) const {
+  __device__ __forceinline__ u64 mass(float z, float top) const {
     const double y = fmax(((double)z - (double)top) * c, -64.0 * 60);
     const double t = y + 0x1.8p52, r = (y - (t - 0x1.8p52)) * (0.69314718055994530942 / 64);
     const int n = (int)(uint32_t)__double_as_longlong(t);
@@ -229,8 +235,12 @@ struct Pick {
   uint32_t near_key[64];      // the elements of one bucket
   u64 near_mass[64];
   int near_n;
+  uint32_t found;
+  u64 found_sum;
 };
 
+// (With a call left to any of the steps all that they share would live in memory: 139 us.)
+#define SKD_INLINE __attribute__((always_inline))
 __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   extern __shared__ unsigned char lds[];
   Pick &sh = *(Pick *)lds;
@@ -245,7 +255,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   top = wave_top(top);
   const bool greedy = p.greedy || top == INFINITY || top == -INFINITY;
   const Grid g(p.T, sh.tab);
-  const float place = greedy ? 0.f : g.place(top), lowest = greedy ? top : p.floor_of(top);
+  const float place = uniform(greedy ? 0.f : g.place(top)), lowest = uniform(greedy ? top : p.floor_of(top));
   if (tid < 64) sh.tab[tid] = exp2(tid / 64.0);
   if (tid < pieces) {
     const float t = bins[tid].top;
@@ -260,11 +270,13 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     a.tokens[b] = token;
     if (a.tokens2) a.tokens2[b] = token;
   };
-  // f(logit, index, whether it is one), by whole waves, for the tokens of the wanted pieces from `low` to `high`, several requested at a time.  An instruction for every
-  // token is 0.9 us at 131072 of them: four are compared at once.
+  // f(logit, index, whether it is one), by whole waves, for the tokens of the wanted pieces from `low` on and below `high`, several
+  // requested at a time.  An instruction for every token is 0.9 us at 131072 of them: four are compared at once.
   float low = fmaxf(lowest, -FLT_MAX), high = INFINITY;
-  auto sweep = [&](auto f) {
-    constexpr int U = 8, STEP = 4 * NW * 64;
+  constexpr std::integral_constant<int, 8> at_once{};  // requests in flight; looking again: 2
+  constexpr std::integral_constant<int, 2> again{};
+  auto sweep = [&](auto f, auto u) SKD_INLINE {
+    constexpr int U = decltype(u)::value, STEP = 4 * NW * 64;
     for (int base = 0; base < V; base += U * STEP) {
       floatx4 v[U];
 #pragma unroll
@@ -285,78 +297,93 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
         if (__any(fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])) >= low))
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const bool hit = v[i][j] >= low && v[i][j] <= high;
+            const bool hit = v[i][j] >= low && v[i][j] < high;
             if (__any(hit)) f(v[i][j] + 0.f, base + i * STEP + 4 * tid + j, hit);
           }
     }
   };
-  // low and high for the bins from `first` to `last`: a little wider than they are, in() decides
-  auto bounds = [&](int first, int last) {
-    const double w = 1.0 / (double)g.s, m = (fabs((double)place) + BINS) * 0x1p-22;
-    const double lo = ((double)place - last - m) * w, hi = ((double)place - first + 1 + m) * w;
-    const bool sound = g.s < INFINITY && w < INFINITY;
-    low = sound && last < BINS ? fmaxf(lowest, nextafterf((float)lo, -INFINITY)) : lowest;
-    low = fmaxf(low, -FLT_MAX);
-    high = sound && first > 0 && hi == hi ? nextafterf((float)hi, INFINITY) : INFINITY;  // (places that overflowed)
+  // The smallest value whose bin is not behind `last`: from where it lies by arithmetic, give or take the roundings of place(), 64
+  // candidates at a time.
+  auto edge = [&](int last) SKD_INLINE -> float {
+    const double w = 1.0 / (double)g.s, z0 = ((double)place - last) * w, m = (fabs((double)place) + BINS) * 0x1p-22 * w;
+    const float from = (float)(z0 - m), to = (float)(z0 + m);  // (NaN, infinite: all values)
+    uint32_t lo = key_of(from >= -FLT_MAX && from <= top ? from : -FLT_MAX), hi = key_of(to >= -FLT_MAX && to <= top ? to : top);
+    while (lo < hi) {
+      const uint32_t step = (hi - lo + 63) / 64, k = lo + min(lane * step, hi - lo);
+      const u64 hits = __ballot(g.bin(top, place, value_of(k)) <= last);
+      if (!hits) {
+        lo = min(lo + 63 * step, hi - 1) + 1;
+        continue;
+      }
+      const int l = __ffsll((long long)hits) - 1;
+      hi = lo + min(l * step, hi - lo);
+      if (l) lo = min(lo + (l - 1) * step + 1, hi);
+      else lo = hi;
+    }
+    return value_of((uint32_t)__builtin_amdgcn_readfirstlane((int)hi)) + 0.f;
   };
-  // Lists the tokens for which `in` holds, a wave's in its own part of the list, their masses beside them, and takes them into registers;
-  // whether all of them fit.  lo, hi: their smallest and largest key.
+  auto bounds = [&](int first, int last) SKD_INLINE {  // low and high for the bins from `first` to `last`
+    low = uniform(fmaxf(lowest, last < BINS ? edge(last) : -FLT_MAX));
+    high = uniform(first > 0 ? edge(first - 1) : INFINITY);
+  };
+  // Lists the tokens of the bounds, a wave's in its own part of the list, their masses beside them, and takes their keys into
+  // registers; whether all of them fit.  lo, hi: their smallest and largest key.
   bool whole = false;
   constexpr int PER = CAP / (NW * 64);
   uint32_t key[PER];
-  float *const value_list = sh.value + wave * (64 * PER);
-  int *const index_list = sh.index + wave * (64 * PER);
-  auto mass_in = [&](int i) { return sh.weight[wave * (64 * PER) + lane + 64 * i]; };
-  auto index_of = [&](int i) { return index_list[lane + 64 * i]; };
-  auto list = [&](auto in) {
+  const int own_list = wave * (64 * PER);
+  auto mass_in = [&](int i) { return sh.weight[own_list + lane + 64 * i]; };
+  auto index_of = [&](int i) { return sh.index[own_list + lane + 64 * i]; };
+  auto list = [&]() SKD_INLINE {
     __syncthreads();
     if (tid == 0) {
       sh.n = 0;
       sh.lo = 0xffffffffu;
       sh.hi = 0;
     }
-    __syncthreads();
-    uint32_t most = 0, least = 0;     // of key and of ~key
     int n = 0;
+    __syncthreads();
     sweep([&](float x, int at, bool hit) {
-      hit = hit && in(x);
       const u64 hits = __ballot(hit);
-      if (!hits) return;
       const int to = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0));
-      if (hit) {
-        if (to < 64 * PER) {
-          value_list[to] = x;
-          index_list[to] = at;
-        }
-        most = max(most, key_of(x));
-        least = max(least, ~key_of(x));
+      if (hit && to < 64 * PER) {
+        sh.value[own_list + to] = x;
+        sh.index[own_list + to] = at;
       }
       n += __popcll(hits);
-    });
-    if (n) {
-      most = wave_max(most);
-      least = wave_max(least);
-      if (lane == 0) {
-        atomicAdd(&sh.n, n <= 64 * PER ? n : CAP + 1);
-        atomicMin(&sh.lo, ~least);
-        atomicMax(&sh.hi, most);
-      }
-    }
+    }, at_once);
+    if (n && lane == 0) atomicAdd(&sh.n, n <= 64 * PER ? n : CAP + 1);
     __syncthreads();
     whole = sh.n <= CAP;
+    uint32_t most = 0, least = 0;     // of key and of ~key
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int at = lane + 64 * i;
       key[i] = 0;
       if (whole && at < n) {
-        key[i] = key_of(value_list[at]);
-        sh.weight[wave * (64 * PER) + at] = g.mass(value_list[at], top);
+        key[i] = key_of(sh.value[own_list + at]);
+        sh.weight[own_list + at] = g.mass(sh.value[own_list + at], top);
+        most = max(most, key[i]);
+        least = max(least, ~key[i]);
       }
     }
+    if (!whole) {
+      most = key_of(high < top ? high : top);
+      least = ~key_of(low);
+    }
+    if (n || !whole) {
+      most = wave_max(most);
+      least = wave_max(least);
+      if (lane == 0) {
+        atomicMin(&sh.lo, ~least);
+        atomicMax(&sh.hi, most);
+      }
+    }
+    __syncthreads();
   };
   // The listed elements (is(i)) by buckets in an order, their weights added up bucket by bucket: the one in which enough(sum) comes
   // to hold, the sum before it, and its elements' order words and weights in LDS; false where there is none, or too many there.
-  auto locate = [&](auto is, auto bucket_of, auto word, auto weight, auto enough) -> bool {
+  auto locate = [&](auto is, auto bucket_of, auto word, auto weight, auto enough) SKD_INLINE -> bool {
     const bool few = sh.n <= 64;
     sh.bucket[tid] = 0;
     if (tid == 0) {
@@ -406,22 +433,36 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     __syncthreads();
     return sh.near_n <= 64;
   };
-  // Of the located elements, every wave for itself: f(order word, sum of the weights of those whose word is at least (or, ascending,
-  // at most) this one) for a lane's element.
-  auto near = [&](bool ascending, auto f) {
-    const int n = sh.near_n;
-    const uint32_t own = lane < n ? sh.near_key[lane] : 0;
-    const u64 w = lane < n ? sh.near_mass[lane] : 0;
-    u64 sum = 0;
-    for (int j = 0; j < n; ++j) {
-      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)own, j);
-      const u64 wj = lane64(w, j);
-      sum += (ascending ? k <= own : k >= own) ? wj : 0ull;
+  // Of the located elements the largest order word (ascending: the smallest) with enough(sum of the weights of those whose word is at
+  // least, or at most, as large), and that sum; false: none.  (By one wave: a loop of 64 by all of them takes 5 us.)
+  u64 found_sum = 0;
+  auto near = [&](bool ascending, auto enough, uint32_t &at) SKD_INLINE -> bool {
+    if (wave == 0) {
+      const int n = sh.near_n;
+      const uint32_t own = lane < n ? sh.near_key[lane] : 0;
+      const u64 w = lane < n ? sh.near_mass[lane] : 0;
+      u64 sum = sh.bucket_before;
+      for (int j = 0; j < n; ++j) {
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)own, j);
+        const u64 wj = lane64(w, j);
+        sum += (ascending ? k <= own : k >= own) ? wj : 0ull;
+      }
+      const bool ok = lane < n && enough(sum);
+      const uint32_t best = wave_max(ok ? ascending ? ~own : own : 0u), word = ascending ? ~best : best;
+      const u64 at_word = __ballot(ok && own == word);
+      if (lane == 0) {
+        sh.found = word;
+        sh.near_n = at_word ? 1 : 0;
+      }
+      if (at_word && lane == __ffsll((long long)at_word) - 1) sh.found_sum = sum;
     }
-    if (lane < n) f(own, sh.bucket_before + sum);
+    __syncthreads();
+    at = sh.found;
+    found_sum = sh.found_sum;
+    return sh.near_n != 0;
   };
   // sum of weight(logit) over the listed tokens, or over what they would be
-  auto sum_of = [&](auto in, auto weight, int set) -> u64 {
+  auto sum_of = [&](auto weight, int set) SKD_INLINE -> u64 {
     u64 mine = 0;
     if (whole) {
 #pragma unroll
@@ -429,8 +470,8 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
         if (key[i]) mine += weight(value_of(key[i]));
     } else {
       sweep([&](float x, int at, bool hit) {
-        if (hit && in(x)) mine += weight(x);
-      });
+        if (hit) mine += weight(x);
+      }, again);
     }
     mine = wave_sum64(mine);
     if (lane == 0) sh.sum[set][wave] = mine;
@@ -442,7 +483,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   };
   // Where there are too many: of the order words word(logit, index) from `first` to `last` the one at which enough(sum of the weights
   // up to it) comes to hold, ten bits of it with every look at the tokens; false: nowhere.
-  auto narrow = [&](auto in, auto word, auto weight, auto enough, uint32_t first, uint32_t last, uint32_t &at) -> bool {
+  auto narrow = [&](auto word, auto weight, auto enough, uint32_t first, uint32_t last, uint32_t &at) SKD_INLINE -> bool {
     u64 before = 0;
     while (true) {
       const int shift = max(22 - __clz((int)((last - first) | 1)), 0);
@@ -460,8 +501,8 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
           if (key[i]) add(value_of(key[i]), index_of(i));
       } else {
         sweep([&](float x, int i, bool hit) {
-          if (hit && in(x)) add(x, i);
-        });
+          if (hit) add(x, i);
+        }, again);
       }
       __syncthreads();
       const u64 own = sh.bucket[tid], scan = wave_scan64(own);
@@ -486,26 +527,26 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     }
   };
   // The largest key among the listed tokens, or what they would be, from which on enough(weight) holds; 0: it does not even for all.
-  auto find = [&](auto in, auto weight, auto weight_at, auto enough) -> uint32_t {
+  // summed: found_sum is that weight.
+  bool summed = false;
+  auto find = [&](auto weight, auto weight_at, auto enough) SKD_INLINE -> uint32_t {
+    summed = false;
     if (sh.n == 0) return 0;
+    uint32_t at;
     if (whole) {
-      const float high = value_of(sh.hi), low = value_of(sh.lo);
-      const float s = high > low ? fminf(1023.0f / (high - low), 3.0e38f) : 0.f;
-      const bool ok = locate([&](int i) { return key[i] != 0; }, [&](int i) { return (int)fminf((high - value_of(key[i])) * s, 1023.0f); },
-                             [&](int i) { return key[i]; }, weight_at, enough);
-      uint32_t best = 0;
-      if (ok) near(false, [&](uint32_t k, u64 sum) { best = enough(sum) ? k : 0; });
-      best = wave_max(best);
+      const float most = value_of(sh.hi), least = value_of(sh.lo);
+      const float s = most > least ? fminf(1023.0f / (most - least), 3.0e38f) : 0.f;
+      if (locate([&](int i) { return key[i] != 0; }, [&](int i) { return (int)fminf((most - value_of(key[i])) * s, 1023.0f); }, [&](int i) { return key[i]; },
+                 weight_at, enough))
+        return (summed = near(false, enough, at)) ? at : 0;
       const bool none = sh.bucket_at >= 1024;
       __syncthreads();
-      if (ok) return best;
       if (none) return 0;
     }
-    uint32_t at;
-    return narrow(in, [&](float x, int) { return ~key_of(x); }, weight, enough, ~sh.hi, ~sh.lo, at) ? ~at : 0;
+    return narrow([&](float x, int) { return ~key_of(x); }, weight, enough, ~sh.hi, ~sh.lo, at) ? ~at : 0;
   };
   // First bin up to `last` at which enough(running sum) holds, the sum before it; BINS + 1: none, the sum of them all.
-  auto first_bin = [&](const auto *of, int last, auto enough, auto &before) -> int {
+  auto first_bin = [&](const auto *of, int last, auto enough, auto &before) SKD_INLINE -> int {
     typedef typename std::remove_reference<decltype(before)>::type S;
     const S x = tid <= last ? (S)of[tid] : (S)0, scan = wave_scan64(x);
     if (lane == 63) sh.wave_mass[wave] = __builtin_bit_cast(u64, scan);
@@ -530,7 +571,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   auto mass_at = [&](float x) { return g.mass(x, top); };
   // the bins of the row: sums over the pieces of what(piece, bin of the piece)
   static_assert(2 * BINS == NW * 64, "two threads for every bin, each with half of the pieces");
-  auto add_bins = [&](auto *to, auto what) {
+  auto add_bins = [&](auto *to, auto what) SKD_INLINE {
     typedef typename std::remove_reference<decltype(*to)>::type S;
     const int bin = tid % BINS, half = wave / (NW / 2);
     S sum = 0;
@@ -563,18 +604,16 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   }
   if (!greedy && (p.by_k || (p.counts && bound < BINS && few <= CAP))) {
     if (tid < pieces) sh.wanted[tid] = sh.shift[tid] <= bound || (bound == BINS && sh.top[tid] > -INFINITY);
-    auto in = [&](float x) { return g.bin(top, place, x) <= bound; };
     bounds(0, bound);
-    list(in);
-    auto own_mass = mass_in;
+    list();
     float cut = lowest;
     if (p.by_k) {
-      const uint32_t t = find(in, [](float) { return 1ull; }, [](int) { return 1ull; }, [&](u64 n) { return n >= (u64)p.k; });
+      const uint32_t t = find([](float) { return 1ull; }, [](int) { return 1ull; }, [&](u64 n) { return n >= (u64)p.k; });
       if (t) cut = fmaxf(cut, value_of(t));
     }
     auto kept = [&](int i) { return key[i] != 0 && key[i] >= key_of(cut); };
-    auto total_kept = [&]() -> u64 {
-      if (!whole) return sum_of(in, [&](float x) { return x >= cut ? mass_at(x) : 0ull; }, 0);
+    auto total_kept = [&]() SKD_INLINE -> u64 {
+      if (!whole) return sum_of([&](float x) { return x >= cut ? mass_at(x) : 0ull; }, 0);
       u64 mine = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) mine += kept(i) ? mass_in(i) : 0ull;
@@ -590,26 +629,31 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     if (p.by_p) {
       const double need = (double)p.top_p * (double)all;
       __syncthreads();
-      const uint32_t t = find(in, mass_at, own_mass, [&](u64 m) { return (double)m >= need; });
-      if (t) cut = fmaxf(cut, value_of(t));
-      __syncthreads();
-      cut = fminf(cut, top);
-      all = total_kept();
+      const uint32_t t = find(mass_at, mass_in, [&](u64 m) { return (double)m >= need; });
+      if (t && value_of(t) >= cut) {
+        cut = fminf(value_of(t), top);
+        if (summed) {
+          all = found_sum;
+        } else {
+          __syncthreads();
+          all = total_kept();
+        }
+      }
     }
     cut = fminf(cut, top);
     const double target = (double)p.u * (double)all;
     // the first index up to which the mass passes the target
     const int shift = max(32 - __clz(V - 1) - 10, 0);
-    int token = V;
+    int token = V - 1;                // (always replaced: the target is below the mass)
     __syncthreads();
-    if (whole && locate(kept, [&](int i) { return index_of(i) >> shift; }, [&](int i) { return (uint32_t)index_of(i); }, own_mass, [&](u64 m) { return (double)m > target; })) {
-      near(true, [&](uint32_t i, u64 sum) { token = (double)sum > target ? (int)i : V; });
-      token = V - (int)wave_max((uint32_t)(V - token));
-    } else {
-      uint32_t at;
-      if (narrow(in, [&](float, int i) { return (uint32_t)i; }, [&](float x) { return x >= cut ? mass_at(x) : 0ull; }, [&](u64 m) { return (double)m > target; }, 0, V - 1, at))
-        token = (int)at;
-    }
+    const auto passed = [&](u64 m) { return (double)m > target; };
+    uint32_t at;
+    bool is;
+    if (whole && locate(kept, [&](int i) { return index_of(i) >> shift; }, [&](int i) { return (uint32_t)index_of(i); }, mass_in, passed))
+      is = near(true, passed, at);
+    else
+      is = narrow([&](float, int i) { return (uint32_t)i; }, [&](float x) { return x >= cut ? mass_at(x) : 0ull; }, passed, 0, V - 1, at);
+    if (is) token = (int)at;
     if (tid == 0) answer(token);
     return;
   }
@@ -621,20 +665,19 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
       // ---- top-p alone, or a min-p that leaves many
       add_bins(sh.mass, [&](int c, int i) { return (double)bins[c].mass[i] * sh.scale[c]; });
       int bin = floor_bin;
-      auto in = [&](float x) { return g.bin(top, place, x) == bin; };
-      auto list_bin = [&]() {
+      auto list_bin = [&]() SKD_INLINE {
         if (tid < pieces) {
           const int i = bin - sh.shift[tid];
           sh.wanted[tid] = sh.top[tid] > -INFINITY && (bin >= BINS || (i >= 0 && bins[tid].mass[i] != 0));
         }
         bounds(bin, bin);
-        list(in);
+        list();
       };
       double before = 0.0, total;     // masses: of the bins before `bin`, of all that min-p leaves
       if (p.counts) {                 // of the lowest bin only a part
         for (int i = 0; i < bin; i += 64) before += wave_sum64(i + lane < bin ? sh.mass[i + lane] : 0.0);
         list_bin();
-        total = before + (double)sum_of(in, mass_at, 0);
+        total = before + (double)sum_of(mass_at, 0);
         __syncthreads();
       } else {
         total = lane < pieces ? sh.kept[lane] : 0.0;
@@ -648,7 +691,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
           bin = min(first, floor_bin);
           list_bin();
         }
-        const uint32_t t = find(in, mass_at, mass_in, [&](u64 m) { return before + (double)m >= need; });
+        const uint32_t t = find(mass_at, mass_in, [&](u64 m) { return before + (double)m >= need; });
         if (t) cut = fmaxf(cut, value_of(t));
       }
       cut = fminf(cut, top);
@@ -659,8 +702,8 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
           if (key[i] && value_of(key[i]) >= cut) atomicAdd(&sh.part[index_of(i) >> piece_bits], mass_in(i));
       } else {
         sweep([&](float x, int at, bool hit) {
-          if (hit && x >= cut && in(x)) atomicAdd(&sh.part[at >> piece_bits], mass_at(x));
-        });
+          if (hit && x >= cut) atomicAdd(&sh.part[at >> piece_bits], mass_at(x));
+        }, again);
       }
       __syncthreads();
       for (int c = wave; c < pieces; c += NW) {
@@ -757,6 +800,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   }
   if (tid == 0) answer(last);
 }
+#undef SKD_INLINE
 
 // Tokens of a thread of k_sample_bins, pieces of 256 times as many: few enough pieces for their bins to be small beside the logits,
 // enough of them for the chip.
