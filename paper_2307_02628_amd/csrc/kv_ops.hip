@@ -486,16 +486,27 @@ struct Share {
   int held;        // positions that the cache holds
   int lo, hi;      // blocks
   bool any;
-  // Workgroup: [tile, the longest first][row and kv head], `pairs` places for the latter.
+  // Workgroup: [tile, the longest first][row and kv head], `pairs` places for the latter.  Tiles of many queries: of 16 rows and
+  // heads of an XCD at a time, so that fewer pages pass through its L2 at once, and the next ones fill the gaps (all of them, 16,
+  // 1 at a time, us: 8 prompts of 2048, 32 heads of 128, bf16 428, 411, 440; 512 tokens behind 2048 203, 192, 194; 8 bits 386,
+  // 380, 440 and 196, 192, 206; 32 prompts of 512, heads of 64, 8 bits 88, 93, 122).
+  static constexpr int TOGETHER = 16;
   template <int NQ>
   __device__ static Share of(const KvAttend &a, int pairs, bool files) {
     Share s;
-    const int H = a.kv.g.H, tiles = gridDim.x / pairs, pair = blockIdx.x % pairs, ri = min(pair / H, a.kv.rows - 1);
+    const int H = a.kv.g.H, tiles = gridDim.x / pairs, id = blockIdx.x;
+    int pair = id % pairs, tile = id / pairs;
+    if (NQ == 128 && pairs % 8 == 0) {
+      const int at = id / 8, g = at / (tiles * TOGETHER), in = at - g * tiles * TOGETHER, n = min(TOGETHER, pairs / 8 - g * TOGETHER);
+      pair = (g * TOGETHER + in % n) * 8 + id % 8;
+      tile = in / n;
+    }
+    const int ri = min(pair / H, a.kv.rows - 1);
     s.h = pair % H;
     s.r = a.order ? a.order[ri] : ri;
     s.t = row_tokens(a.tk, s.r);
     s.R = pair < H * a.kv.rows ? s.t.n * a.group : 0;
-    s.q0 = (int)(tiles - 1 - blockIdx.x / pairs) * NQ;
+    s.q0 = (tiles - 1 - tile) * NQ;
     s.any = s.q0 < s.R;
     s.held = s.t.past + (files ? 0 : s.t.n);
     const int nblk = (min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held) + 31) >> 5, per = (nblk + a.splits - 1) / a.splits;
