@@ -153,36 +153,44 @@ __global__ __launch_bounds__(256) void k_kv_append(KvView kv, KvTokens tk, KvRow
 
 // A few tokens a row (decode steps, drafts): DH / 8 lanes take the key or the value of one token and head.  Hardly any bytes: a
 // chain of three round trips (the row's place, its page, the values), so every token has lanes of its own and nothing is shared.
-// The tokens of a step for 128 rows of 32 heads of 128, 8 bits: 5 us instead of 14.5 by blocks.
+// The tokens of a step for 128 rows of 32 heads of 128, 8 bits: 6.4 us instead of 14.5 by blocks (7.7 with every lane storing the
+// eight values that it has read: eight lines of the page for each store of a token and head, now two).
 template <int DH, bool FP8>
 __global__ __launch_bounds__(256) void k_kv_append_few(KvView kv, KvTokens tk, KvRows k, KvRows v) {
   constexpr int LPT = DH / 8, PER = 256 / LPT;
   const int H = kv.g.H, e = threadIdx.x % LPT * 8;
-  const long unit = (long)blockIdx.x * PER + threadIdx.x / LPT;  // [row][token][k | v][head]
-  const int h = (int)(unit % H), is_v = (int)(unit / H % 2), i = (int)(unit / H / 2 % tk.max_new);
-  const long r = unit / H / 2 / tk.max_new;
+  const uint32_t unit = blockIdx.x * PER + threadIdx.x / LPT, side = unit / H, token = side / 2;  // [row][token][k | v][head]
+  const int h = (int)(unit - side * H), is_v = (int)(side & 1), i = (int)(token % tk.max_new), r = (int)(token / tk.max_new);
   if (r >= kv.rows) return;
-  const RowTokens t = row_tokens(tk, (int)r);
+  const RowTokens t = row_tokens(tk, r);
   if (i >= t.n) return;
-  const int pos = t.past + i, page = page_of(kv, (int)r, pos >> 5);
+  const KvRows &from = is_v ? v : k;
+  const uint32x4 x = *(const uint32x4 *)((const bf16_t *)from.p + row_index(from, t.at + (long)i * tk.step, h * DH + e));
+  const int pos = t.past + i, page = page_of(kv, r, pos >> 5);
   if (page < 0) return;
   unsigned char *pg = kv.pool + (long)page * kv.page_bytes;
   const int slot = pos % kv.g.page_tokens;
-  const KvRows &from = is_v ? v : k;
-  const uint32x4 x = *(const uint32x4 *)((const bf16_t *)from.p + row_index(from, t.at + (long)i * tk.step, h * DH + e));
+  // A value's elements lie 16 bytes apart: in one store the lanes take neighbouring ones, through their own wave's part of LDS.
+  __shared__ uint32x4 line[256];
+  unsigned char *own = (unsigned char *)(line + threadIdx.x / LPT * LPT);
+  const int l = threadIdx.x % LPT;
   if constexpr (FP8) {
     const uint32_t ex = kv8_exponent(max_over<LPT>(max_bits(x)));
     const uint2 c = kv8_codes(x, ex);
     if (e == 0) pg[kv8_exp_off(h, slot, is_v, kv.g)] = (unsigned char)ex;
     if (is_v) {
+      *(uint2 *)(own + 8 * l) = c;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int j = 0; j < 8; ++j) pg[kv8_v_off(h, slot, e + j, kv.g)] = (unsigned char)((j < 4 ? c.x : c.y) >> (8 * (j & 3)));
+      for (int j = 0; j < 8; ++j) pg[kv8_v_off(h, slot, l + LPT * j, kv.g)] = own[l + LPT * j];
     } else {
       *(uint2 *)(pg + kv8_k_off(h, slot, e, kv.g)) = c;
     }
   } else if (is_v) {
+    *(uint32x4 *)(own + 16 * l) = x;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ((bf16_t *)pg)[kv_v_off(h, slot, e + j, kv.g)] = (bf16_t)(x[j / 2] >> (16 * (j & 1)));
+    for (int j = 0; j < 8; ++j) ((bf16_t *)pg)[kv_v_off(h, slot, l + LPT * j, kv.g)] = ((bf16_t *)own)[l + LPT * j];
   } else {
     *(uint32x4 *)((bf16_t *)pg + kv_k_off(h, slot, e, kv.g)) = x;
   }
@@ -219,13 +227,12 @@ template <int DH, bool FP8, typename OUT>
 __global__ __launch_bounds__(256) void k_kv_read_few(KvView kv, KvTokens tk, KvRows k, KvRows v) {
   constexpr int LPT = DH / 8, PER = 256 / LPT;
   const int H = kv.g.H, l = threadIdx.x % LPT;
-  const long unit = (long)blockIdx.x * PER + threadIdx.x / LPT;
-  const int h = (int)(unit % H), is_v = (int)(unit / H % 2), i = (int)(unit / H / 2 % tk.max_new);
-  const long r = unit / H / 2 / tk.max_new;
+  const uint32_t unit = blockIdx.x * PER + threadIdx.x / LPT, side = unit / H, token = side / 2;
+  const int h = (int)(unit - side * H), is_v = (int)(side & 1), i = (int)(token % tk.max_new), r = (int)(token / tk.max_new);
   if (r >= kv.rows) return;
-  const RowTokens t = row_tokens(tk, (int)r);
+  const RowTokens t = row_tokens(tk, r);
   if (i >= t.n) return;
-  const int pos = t.past + i, page = page_of(kv, (int)r, pos >> 5);
+  const int pos = t.past + i, page = page_of(kv, r, pos >> 5);
   if (page < 0) return;
   const unsigned char *pg = kv.pool + (long)page * kv.page_bytes;
   const int slot = pos % kv.g.page_tokens;
@@ -857,7 +864,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 // block at a time, fragments requested as they are needed): us, 8 rows of 512 new tokens behind 2048, 32 heads of 128, bf16
 // 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 340.  Bound by the vector units (softmax;
 // conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.
-constexpr int rows_stages(int dh, bool fp8) { return dh == 128 && !fp8 ? 5 : 8; }
+constexpr int rows_stages(int dh, bool fp8) { return fp8 ? 8 : dh == 128 ? 5 : 6; }  // (64: three workgroups, 97 -> 77 us for 32 prompts of 512)
 constexpr size_t rows_lds(int dh, bool fp8) { return (size_t)rows_stages(dh, fp8) * (32 * dh * (fp8 ? 2 : 4) + (fp8 ? 256 : 0)); }
 template <int DH, bool FP8>
 __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs) {
@@ -1192,7 +1199,7 @@ int blocks_of(const KvTokens &tk) { return (tk.max_new + 31 + 31) / 32; }  // of
 // Workgroups of the kernels for a few tokens, or 0: up to 8 of a row (k_kv_append_few), and a grid that fits.
 static unsigned few_groups(const KvView &kv, const KvTokens &tk) {
   const long units = 2L * kv.g.H * tk.max_new * kv.rows, groups = (units * (kv.g.dh / 8) + 255) / 256;
-  return tk.max_new <= 8 && groups < (1L << 31) ? (unsigned)groups : 0;
+  return tk.max_new <= 8 && units < (1L << 31) ? (unsigned)groups : 0;  // (units are counted in 32 bits)
 }
 void kv_append(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows &k, const KvRows &v) {
   if (const unsigned few = few_groups(kv, tk)) {
