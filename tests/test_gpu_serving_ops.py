@@ -220,3 +220,92 @@ def test_infinities_among_many_queries(elem, past, new):
             assert torch.isnan(col).all()
         else:                                                         # 8 bits: the head's whole token reads as NaN
             assert torch.isnan(out[torch.arange(past, past + new) >= p].float()).all()
+
+
+@pytest.mark.parametrize("elem", [R.BF16, R.FP8])
+@pytest.mark.parametrize("group,dh,new", [(40, 128, 1), (70, 64, 1), (130, 128, 1), (33, 64, 4)])
+def test_many_query_heads_of_a_kv_head(elem, group, dh, new):
+    c = Case(elem, 2, dh, 64, [130, 0, 63], [new, 1, new], seed=group)
+    q = torch.randn(2 * new + 1, 2 * group, dh, generator=torch.Generator().manual_seed(15)).bfloat16().cuda()
+    c.append([0] * 3, c.past)
+    c.check(q, c.attend(q, files=True))
+
+
+@pytest.mark.parametrize("elem", [R.BF16, R.FP8])
+@pytest.mark.parametrize("past,new", [([70, 5], [1, 1]), ([40, 0], [20, 3]), ([300, 20], [140, 70])])
+def test_queries_and_outputs_with_strides(elem, past, new):
+    """q, k and v side by side in one array, outputs in another with room between the tokens, which stays as it was."""
+    H, group, dh = 2, 2, 64
+    c = Case(elem, H, dh, 32, past, new, seed=new[0])
+    T, W = sum(new), H * dh
+    packed = torch.full((T, (group + 2) * W + 24), 9.0, dtype=torch.bfloat16, device="cuda")
+    q = torch.randn(T, group * W, generator=torch.Generator().manual_seed(16)).bfloat16().cuda()
+    packed[:, :group * W], packed[:, group * W:(group + 1) * W], packed[:, (group + 1) * W:(group + 2) * W] = q, c.tokens(c.k, past, new).flatten(1), c.tokens(c.v, past, new).flatten(1)
+    c.append([0, 0], past)
+    out = torch.full((T, group * W + 40), 5.0, dtype=torch.bfloat16, device="cuda")
+    ch = c.chunk(past, new)
+    c.cache.attend(ch, packed[:, :group * W], out[:, 8:8 + group * W], 0.125, packed[:, group * W:(group + 1) * W], packed[:, (group + 1) * W:(group + 2) * W],
+                   workspace=torch.empty(c.cache.attend_workspace(ch, H * group), dtype=torch.uint8, device="cuda"))
+    c.check(q.view(T, H * group, dh), out[:, 8:8 + group * W].reshape(T, H * group, dh).cpu())
+    assert (out[:, :8] == 5).all() and (out[:, 8 + group * W:] == 5).all()
+
+
+@pytest.mark.parametrize("elem", [R.BF16, R.FP8])
+@pytest.mark.parametrize("new", [1, 6, 150])
+def test_queries_that_are_not_finite(elem, new):
+    """They are NaN by themselves: the queries beside them are what they are without."""
+    c = Case(elem, 1, 128, 64, [200], [new], seed=new)
+    q = torch.randn(new, 4, 128, generator=torch.Generator().manual_seed(18)).bfloat16().cuda()
+    c.append([0], c.total)
+    bad = q.clone()
+    bad[new // 2, 1, 3], bad[new - 1, 3, 9] = math.nan, math.inf
+    out = c.attend(bad)
+    odd = torch.zeros(new, 4, dtype=torch.bool)
+    odd[new // 2, 1] = odd[new - 1, 3] = True
+    assert torch.isnan(out[odd].float()).all()
+    k, v = (torch.from_numpy(R.as_held(x[0].double().numpy(), elem)) for x in (c.k, c.v))
+    ref, bound = R.attention(q.cpu().double(), k, v, 200, 1 / math.sqrt(128))
+    assert ((out.double() - ref).abs() <= bound)[~odd].all()
+
+
+def test_bounds_that_are_too_small_or_too_large():
+    """max_past only decides how the work is shared out; tokens beyond max_new are left out."""
+    c = Case(R.BF16, 2, 64, 32, [2000, 64], [3, 3], seed=5)
+    c.append([0, 0], c.total)
+    q = torch.randn(6, 2, 64, generator=torch.Generator().manual_seed(19)).bfloat16().cuda()
+    for max_past in (0, 1999, 1 << 29):
+        ch = skd.KvChunk(i32([0, 3, 6]), i32([2000, 64]), 6, 3, max_past)
+        out = torch.full_like(q, 5.0)
+        c.cache.attend(ch, q, out, 0.125, workspace=torch.empty(c.cache.attend_workspace(ch, 2), dtype=torch.uint8, device="cuda"))
+        c.check(q, out.cpu())
+    ch = skd.KvChunk(i32([0, 3, 6]), i32([2000, 64]), 6, 2, 2000)
+    out = torch.full_like(q, 5.0)
+    c.cache.attend(ch, q, out, 0.125, workspace=torch.empty(c.cache.attend_workspace(ch, 2), dtype=torch.uint8, device="cuda"))
+    assert (out[[2, 5]] == 5).all() and (out[[0, 1, 3, 4]] != 5).any(-1).all()
+
+
+def test_two_streams_at_once():
+    """Rows of one pool that share no page, on two streams with workspaces of their own, again and again."""
+    c = Case(R.FP8, 2, 128, 64, [3000, 2500], [1, 1], seed=23)
+    c.append([0, 0], c.total)
+    q = torch.randn(2, 8, 128, generator=torch.Generator().manual_seed(20)).bfloat16().cuda()
+    z, u = torch.randn(2, 60000, generator=torch.Generator().manual_seed(21)).cuda(), torch.tensor([0.3, 0.8]).cuda()
+    parts = []
+    for r in range(2):
+        cache = skd.KvCache(c.pool, c.table[r:r + 1].cuda(), 2, 128, 64, R.FP8)
+        ch = skd.KvChunk(i32([0, 1]), i32([c.past[r]]), 1, 1, 3000)
+        ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (cache.attend_workspace(ch, 8), skd.sample_workspace(1, 60000))]
+        parts.append((torch.cuda.Stream(), cache, ch, q[r:r + 1], torch.zeros(20, 8, 128, dtype=torch.bfloat16, device="cuda"), z[r:r + 1], u[r:r + 1],
+                      torch.zeros(20, dtype=torch.int32, device="cuda"), torch.full((1,), 0.9, device="cuda"), *ws))
+    kv = [(c.tokens(c.k, c.past, c.new)[r:r + 1].contiguous(), c.tokens(c.v, c.past, c.new)[r:r + 1].contiguous()) for r in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for r, (s, cache, ch, qr, out, zr, ur, tok, top_p, ws, draw_ws) in enumerate(parts):
+            cache.attend(ch, qr, out[i:i + 1], 1 / math.sqrt(128), *kv[r], workspace=ws, stream=s.cuda_stream)
+            skd.sample(zr, ur, tok[i:i + 1], top_p=top_p, workspace=draw_ws, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for r in range(2):
+        out, tok = parts[r][4], parts[r][7]
+        assert (out == out[0]).all() and (tok == tok[0]).all()
+        assert int(tok[0]) == reference(z[r].cpu().numpy(), float(u[r]), p=float(np.float32(0.9)))
+    c.check(q, torch.cat([parts[0][4][:1], parts[1][4][:1]]).cpu())
