@@ -12,6 +12,12 @@ using namespace skd;
 namespace {
 
 bool aligned(const void *p) { return ((uintptr_t)p & 15) == 0; }
+// 4-byte elements
+bool aligned4(std::initializer_list<const void *> ps) {
+  for (const void *p : ps)
+    if ((uintptr_t)p & 3) return false;
+  return true;
+}
 
 int check_kv(const skd_kv *kv) {
   if (!kv) return SKD_ERR_NULL;
@@ -28,8 +34,8 @@ int check_call(const skd_kv *kv, const skd_kv_chunk *ch) {
   if (ch->tokens < 0 || ch->max_new < 0 || ch->max_past < 0) return SKD_ERR_RANGE;
   return SKD_OK;
 }
-// The device memory of a call, which is the current device's: a pointer that is not, or is no device memory, is refused
-// before it reaches a kernel.
+// The device memory of a call, which is the current device's: a pointer of another one, or of memory that no device knows, is
+// refused before it reaches a kernel.
 int check_memory(std::initializer_list<const void *> ps) {
   int device = 0;
   if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return hip_failed(e);
@@ -108,7 +114,7 @@ extern "C" int skd_kv_append(const skd_kv *kv, const skd_kv_chunk *ch, const voi
   const int64_t width = (int64_t)kv->kv_heads * kv->head_dim;
   CHECK(check_rows(k, k_stride, width));
   CHECK(check_rows(v, v_stride, width));
-  if (!aligned(kv->pool)) return SKD_ERR_SHAPE;
+  if (!aligned(kv->pool) || !aligned4({kv->block_table, ch->first, ch->past})) return SKD_ERR_SHAPE;
   if (!fits_grid(((int64_t)tk.max_new + 62) / 32 * kv->kv_heads * kv->rows)) return SKD_ERR_RANGE;
   CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, k, v}));
   kv_append((hipStream_t)hip_stream, view(kv), tk, rows_of(k, k_stride), rows_of(v, v_stride));
@@ -125,7 +131,7 @@ extern "C" int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *ch, int32_t ele
   const int64_t width = (int64_t)kv->kv_heads * kv->head_dim;
   CHECK(check_rows(k_out, k_stride, width));
   CHECK(check_rows(v_out, v_stride, width));
-  if (!aligned(kv->pool)) return SKD_ERR_SHAPE;
+  if (!aligned(kv->pool) || !aligned4({kv->block_table, ch->first, ch->past})) return SKD_ERR_SHAPE;
   if (!fits_grid(((int64_t)tk.max_new + 62) / 32 * kv->kv_heads * kv->rows)) return SKD_ERR_RANGE;
   CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, k_out, v_out}));
   kv_read((hipStream_t)hip_stream, view(kv), tk, elem == SKD_W_BF16, rows_of(k_out, k_stride), rows_of(v_out, v_stride));
@@ -167,7 +173,7 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
     CHECK(check_rows(k, k_stride, width));
     CHECK(check_rows(v, v_stride, width));
   }
-  if (!aligned(kv->pool)) return SKD_ERR_SHAPE;
+  if (!aligned(kv->pool) || !aligned4({kv->block_table, ch->first, ch->past})) return SKD_ERR_SHAPE;
   a.heads = heads;
   a.group = heads / kv->kv_heads;
   a.c = scale * 1.4426950408889634f;
@@ -204,7 +210,8 @@ extern "C" int skd_sample(const float *logits, int64_t stride, int32_t rows, int
   if (stride < vocab) return SKD_ERR_SHAPE;
   if (!rows) return SKD_OK;
   if (!logits || !u || !tokens_out || !workspace) return SKD_ERR_NULL;
-  if (!aligned(workspace) || ((uintptr_t)logits | (uintptr_t)u | (uintptr_t)tokens_out) & 3) return SKD_ERR_SHAPE;
+  if (!aligned(workspace) || !aligned4({logits, u, tokens_out})) return SKD_ERR_SHAPE;
+  if (params && !aligned4({params->temperature, params->top_k, params->top_p, params->min_p})) return SKD_ERR_SHAPE;
   if (workspace_bytes < need) return SKD_ERR_NOMEM;
   if (!fits_grid((int64_t)sample_rows_bins(rows, vocab))) return SKD_ERR_RANGE;
   SampleRows a{};

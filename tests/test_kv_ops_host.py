@@ -65,7 +65,7 @@ def test_pointers_and_ranges():
     assert lib.skd_kv_append(C.byref(kv()), None, P, 512, P, 512, None) == skd.ERR_NULL
     for call in (append, read, attend):
         assert call(kv(pool=None)) == call(kv(block_table=None)) == call(None, chunk(first=None)) == call(None, chunk(past=None)) == skd.ERR_NULL
-        assert call(kv(pool=P + 8)) == skd.ERR_SHAPE
+        assert call(kv(pool=P + 8)) == call(kv(block_table=P + 2)) == call(None, chunk(first=P + 1)) == call(None, chunk(past=P + 3)) == skd.ERR_SHAPE
         assert call(None, chunk(tokens=-1)) == call(None, chunk(max_new=-1)) == call(None, chunk(max_past=-1)) == skd.ERR_RANGE
         assert call(kv(max_pages=1 << 26)) == skd.ERR_RANGE           # positions beyond 32 bits
         assert call(None, chunk(max_new=0)) == call(None, chunk(tokens=0)) == call(kv(rows=0)) == skd.OK
@@ -99,6 +99,9 @@ def test_draws():
     assert rc(z=None) == rc(u=None) == rc(out=None) == rc(ws=None) == skd.ERR_NULL
     assert rc(vocab=0) == rc(vocab=262145, stride=262145) == rc(stride=999) == rc(z=P + 2) == rc(out=P + 1) == rc(ws=P + 8) == skd.ERR_SHAPE
     assert need > 0 and rc(n=need - 1) == skd.ERR_NOMEM
+    for name in ("temperature", "top_k", "top_p", "min_p"):
+        bad = skd.Sampling(**{name: P + 2})
+        assert lib.skd_sample(P, 1000, 3, 1000, C.byref(bad), P, P, P, need, None) == skd.ERR_SHAPE
     assert rc(rows=-1) == skd.ERR_RANGE and rc(rows=0) == skd.OK
     assert lib.skd_sample_workspace(-1, 10) == skd.ERR_RANGE and lib.skd_sample_workspace(1, 0) == lib.skd_sample_workspace(1, 1 << 19) == skd.ERR_SHAPE
     assert lib.skd_sample_workspace(128, 262144) >= 0
