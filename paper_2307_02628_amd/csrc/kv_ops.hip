@@ -1268,10 +1268,13 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
     p.waves = 4;
     while (p.splits < 64 && wgs * p.splits < 256 && blocks / (2 * p.splits) >= 8) p.splits *= 2;
   } else {
-    // 16 waves a CU (8 with two tiles), from workgroups that are wide first
-    const long want = p.nq == 16 ? 4096 : 2048;
-    p.waves = p.nq == 16 && wgs * 4 >= want ? 4 : 8;
-    while (p.splits < 64 && wgs * p.waves * p.splits < want && blocks / (2 * p.splits) >= p.waves) p.splits *= 2;
+    // 8 waves a CU, and 16 from 1024 workgroups on, which are narrower then.  (Shares up to 16 waves a CU against this, us: 8 rows of
+    // 2000, 32 heads of 128, bf16 44.5, 40.5, 8 bits 26.5, 22.6; one of 32766, 8 kv heads, 8 bits 18.5, 17.4; up to 4: 20.5.)
+    // Joining takes 5 us: two tiles that are on half of the CUs already are shared out only if every wave keeps six blocks
+    // (4 rows of 1000 with 20 new tokens, 32 heads: 22.3, 18.7; 16 of 2000 with 5, 8 kv heads: 31.5, 30.3).
+    p.waves = p.nq == 16 && wgs >= 1024 ? 4 : 8;
+    const int least = p.waves * (p.nq == 32 && wgs >= 128 ? 6 : 1);
+    while (p.splits < 64 && wgs * p.waves * p.splits < 2048 && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
   }
   return p;
 }
