@@ -1255,7 +1255,12 @@ struct AttendPlan {
 static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
   AttendPlan p{};
   const long R = (long)tk.max_new * (heads / kv.g.H), blocks = ((long)tk.max_past + tk.max_new + 31) / 32;
-  p.nq = R <= 16 ? 16 : R <= 64 ? 32 : 128;
+  // Up to 16 queries one tile, up to 32 two; beyond, the blocks go through LDS once for all, which 8 bits gain from only with five
+  // tiles and more (inputs not in the last-level cache, us.  Two tiles of 16 for 17 .. 32 queries: 16 rows of 2000, 8 kv heads of
+  // 128, bf16 31.3, 30.9; 40 rows 70.7, 104.9.  33 .. 64 as two of 32 or through LDS: 8 rows of 1000, 32 heads of 128, bf16 58.7,
+  // 35.2, 8 bits 38.7, 38.2; 32 rows of 700, 8 kv heads of 64, bf16 23.4, 19.7, 8 bits 15.2, 22.1; one of 20000, 8 of 128, 8 bits
+  // 23.3, 30.5.  65 .. 128: 8 rows of 1000 bf16 107, 38, 8 bits 70, 41.)
+  p.nq = R <= 16 ? 16 : R <= (kv.fp8 ? 64 : 32) ? 32 : 128;
   p.tiles = (R + p.nq - 1) / p.nq;
   const long n = (long)kv.g.H * kv.rows, wgs = p.tiles * n;
   // Workgroups go to the eight XCDs in turn.  With a multiple of eight places all tiles of a row and kv head are on one of them
