@@ -1192,6 +1192,47 @@ __global__ __launch_bounds__(256) void k_kv_merge(KvAttend a, int queries) {
   }
 }
 
+// The same for up to 8 shares, of which there are many queries: a wave each, all shares requested at once (two shares of 16384
+// queries, 2 rows of 256 tokens behind 500: 44 -> 32 us with the attention, 12 of them a workgroup for each query).
+template <int DH>
+__global__ __launch_bounds__(256) void k_kv_merge_few(KvAttend a, int queries) {
+  constexpr int S = 8, E = DH / 64;
+  const int H = a.kv.g.H, lane = threadIdx.x & 63;
+  const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int q = (int)(id % queries), h = (int)(id / queries % H), r = (int)(id / queries / H);
+  if (r >= a.kv.rows) return;
+  const RowTokens t = row_tokens(a.tk, r);
+  if (q >= t.n * a.group) return;
+  const int head = h * a.group + q % a.group;
+  const long token = t.at + (long)(q / a.group) * a.tk.step, stride = (long)a.tk.tokens * a.heads * (DH + 2);
+  const float *x = part_of<DH>(a, 0, token, head);
+  float m[S], l[S], v[S][E], M = -3.0e38f, den = 0.f, num[E] = {};
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const float *y = x + min(s, a.splits - 1) * stride;
+    m[s] = s < a.splits ? y[DH] : -3.0e38f;
+    l[s] = s < a.splits ? y[DH + 1] : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[s][e] = y[E * lane + e];
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) M = fmaxf(M, m[s]);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const float w = s < a.splits ? __builtin_amdgcn_exp2f(m[s] - M) : 0.f;
+    den += w * l[s];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (s < a.splits) num[e] += w * v[s][e];
+  }
+  uint32_t o = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o |= (uint32_t)f2bf(den == 0.f ? 0.f : num[e] / den) << (16 * e);
+  bf16_t *to = (bf16_t *)a.o.p + row_index(a.o, token, head * DH + E * lane);
+  if constexpr (E == 2) *(uint32_t *)to = o;
+  else *to = (bf16_t)o;
+}
+
 int blocks_of(const KvTokens &tk) { return (tk.max_new + 31 + 31) / 32; }  // of a row, wherever in a block it begins
 
 }  // namespace
@@ -1270,8 +1311,13 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
   if (p.tiles > 1 && n >= 8 && (n + 7) / 8 * 8 * 20 <= n * 23) p.pairs = (int)((n + 7) / 8 * 8);
   p.splits = 1;
   if (p.nq == 128) {
+    // A workgroup for each CU, in shares of 8 blocks at least, of 16 where half of the CUs have one already, and two where shares
+    // keep 24 (that rule, without the 16, without the second workgroup, us: one row of 512 behind 8000, 32 heads, 8 kv heads
+    // 95, 95, 116; four of 100 behind 3000 47, 47, 54; 512 tokens from nothing, 32 heads of 64 17, 23, 17; one row of 1000 behind
+    // 100, 32 heads 36, two workgroups for shares of 16: 48).
     p.waves = 4;
-    while (p.splits < 64 && wgs * p.splits < 256 && blocks / (2 * p.splits) >= 8) p.splits *= 2;
+    auto least = [&]() { return wgs * p.splits >= 256 ? 24 : p.splits == 1 && wgs >= 128 ? 16 : 8; };
+    while (p.splits < 64 && wgs * p.splits <= 384 && blocks / (2 * p.splits) >= least()) p.splits *= 2;  // (456: the same either way)
   } else {
     // 8 waves a CU, and 16 from 1024 workgroups on, which are narrower then.  (Shares up to 16 waves a CU against this, us: 8 rows of
     // 2000, 32 heads of 128, bf16 44.5, 40.5, 8 bits 26.5, 22.6; one of 32766, 8 kv heads, 8 bits 18.5, 17.4; up to 4: 20.5.)
@@ -1313,7 +1359,9 @@ static void attend(hipStream_t s, const KvAttend &a) {
   }
   if (a.splits > 1) {
     const int queries = a.tk.max_new * a.group;
-    SKD_LAUNCH(k_kv_merge<DH>, dim3((unsigned)((long)queries * a.kv.g.H * a.kv.rows)), dim3(256), 0, s, a, queries);
+    const long all = (long)queries * a.kv.g.H * a.kv.rows;
+    if (a.splits <= 8) SKD_LAUNCH(k_kv_merge_few<DH>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, queries);
+    else SKD_LAUNCH(k_kv_merge<DH>, dim3((unsigned)all), dim3(256), 0, s, a, queries);
   }
 }
 void kv_attend(hipStream_t s, const KvAttend &call) {
