@@ -619,7 +619,9 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   const Share s = Share::of<NQ>(a, pairs, files);
   if (!s.any) return;
   const int q0 = s.q0, R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
-  const bool fresh = files && blockIdx.y == gridDim.y - 1 && wave == NW - 1;  // this wave takes the new token
+  // The page that takes the new token, known to the wave that attends to it: without one it is dropped, and nobody sees it.
+  const int new_page = files && blockIdx.y == gridDim.y - 1 && wave == NW - 1 ? page_of(a.kv, s.r, s.held >> 5) : -1;
+  const bool fresh = new_page >= 0;
   if constexpr (NT == 1) {
     constexpr int LPT = DH / 8;
     if (fresh && lane < 2 * LPT) {
@@ -838,9 +840,9 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   if constexpr (NT == 1) {
     // The first tile files the new token.  Whoever reads its place meanwhile, in the block around it, discards what is there.
     // (Last of all: a barrier behind the stores would wait for them, 4 us of a step of 32 rows.)
-    const int page = fresh && q0 == 0 ? page_of(a.kv, s.r, s.held >> 5) : -1, slot = s.held % a.kv.g.page_tokens;
-    if (page >= 0) {
-      unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
+    if (fresh && q0 == 0) {
+      const int slot = s.held % a.kv.g.page_tokens;
+      unsigned char *pg = a.kv.pool + (long)new_page * a.kv.page_bytes;
       if (lane < DH / 8) {
         const uint32x4 kx = *(const uint32x4 *)&sh_k[8 * lane];
         if constexpr (FP8) *(uint2 *)(pg + kv8_k_off(h, slot, 8 * lane, a.kv.g)) = kv8_codes(kx, ke);

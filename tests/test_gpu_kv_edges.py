@@ -1,0 +1,63 @@
+"""The paged cache at its edges: new tokens whose positions have no page, values at the small end of the range, rows in many shares,
+workspaces that are refused, layers of a state that are set to nothing."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as R
+from paper_2307_02628_amd import skd
+from test_gpu_decode_chunk import NARROW, Run
+from test_gpu_kv_ops import Case
+
+pytestmark = pytest.mark.gpu
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def attended(c, cache, ch, q, out, scale, kv=()):
+    ws = torch.empty(cache.attend_workspace(ch, q.shape[1]), dtype=torch.uint8, device="cuda")
+    cache.attend(ch, q, out, scale, *kv, workspace=ws)
+    return out.cpu()
+
+
+@pytest.mark.parametrize("elem", [R.BF16, R.FP8])
+@pytest.mark.parametrize("H,group,dh", [(2, 1, 64), (1, 4, 128), (2, 16, 128), (1, 20, 64)])
+@pytest.mark.parametrize("long", [0, 4000])
+def test_a_new_token_without_a_page(elem, H, group, dh, long):
+    """One token a row, filed by the call that attends to it: without a page it is dropped and nobody sees it, as if it had been
+    filed by a call of its own."""
+    page, scale = 32, 0.2
+    past = [64 + long, 0, 96 + long, 40, 70]
+    c = Case(elem, H, dh, page, past, [1] * 5, seed=dh + group)
+    c.append([0] * 5, past)
+    width = (96 + long) // page
+    table = c.table[:, :width].clone()                                # row 2 is full: its new position is behind its pages
+    table[0, past[0] // page] = -1
+    table[1, 0] = -5                                                  # row 1 holds nothing at all
+    table[3, 1] = c.pool.shape[0]
+    cache = skd.KvCache(c.pool, table.cuda(), H, dh, page, elem)
+    ch = c.chunk(past, [1] * 5)
+    q = torch.randn(5, H * group, dh, generator=torch.Generator().manual_seed(31)).bfloat16().cuda()
+    kv = c.tokens(c.k, past, [1] * 5), c.tokens(c.v, past, [1] * 5)
+    before = c.pool.clone()
+    out = attended(c, cache, ch, q, torch.full_like(q, 5.0), scale, kv)
+    after = c.pool.clone()
+    c.pool.copy_(before)
+    cache.append(ch, *kv)
+    assert torch.equal(after.view(torch.uint8), c.pool.view(torch.uint8))
+    apart = attended(c, cache, ch, q, torch.full_like(q, 5.0), scale)
+    for r in range(5):
+        has = torch.tensor([i // page < width and 0 <= table[r, i // page] < c.pool.shape[0] for i in range(past[r] + 1)])
+        assert bool(has[-1]) == (r == 4)
+        at = has.nonzero()[:, 0]
+        for got in (out[r], apart[r]):
+            if len(at) == 0:
+                assert (got == 0).all()
+                continue
+            k, v = (torch.from_numpy(R.as_held(x[r][at].double().numpy(), elem)) for x in (c.k, c.v))
+            ref, bound = R.attention(q[r:r + 1].cpu().double(), k, v, len(at) - 1, scale)
+            assert ((got.double() - ref[0]).abs() <= bound[0]).all(), r
