@@ -1796,7 +1796,7 @@ extern "C" int skd_debug_read_hidden(skd_state *st, float *x_out) {
   return wait_stream(st);
 }
 
-// Layer l's 8-bit pages from device arrays [B][cols][d] fp32 (rounded to bf16 first), and back.
+// Layer l's 8-bit pages from device arrays [B][cols][d] fp32 (rounded to bf16 first; null: zeros), and back.
 static int kv_load_8(skd_state *st, int l, const float *k, const float *v, int cols) {
   const int B = st->cfg.batch, d = st->cfg.d_model;
   const size_t n = (size_t)B * cols * d;
@@ -1805,9 +1805,14 @@ static int kv_load_8(skd_state *st, int l, const float *k, const float *v, int c
   bf16_t *k16 = nullptr;
   HIPCHECK(hipMalloc((void **)&k16, 2 * n * sizeof(bf16_t) + B * sizeof(int32_t)));
   int32_t *first_dev = (int32_t *)(k16 + 2 * n);
-  prep_matrix_rm_bf16(st->stream, k, 0, k16, (long)n);
-  prep_matrix_rm_bf16(st->stream, v, 0, k16 + n, (long)n);
-  hipError_t e = hipMemcpyAsync(first_dev, first.data(), B * sizeof(int32_t), hipMemcpyHostToDevice, st->stream);
+  hipError_t e = hipSuccess;
+  if (k) {
+    prep_matrix_rm_bf16(st->stream, k, 0, k16, (long)n);
+    prep_matrix_rm_bf16(st->stream, v, 0, k16 + n, (long)n);
+  } else {
+    e = hipMemsetAsync(k16, 0, 2 * n * sizeof(bf16_t), st->stream);
+  }
+  if (e == hipSuccess) e = hipMemcpyAsync(first_dev, first.data(), B * sizeof(int32_t), hipMemcpyHostToDevice, st->stream);
   if (e == hipSuccess) {
     KvTokens tk{};
     tk.kind = KvTokens::PROMPT; tk.first = first_dev; tk.past = st->start_dev; tk.tokens = B * cols; tk.count = cols; tk.step = 1;
@@ -1873,7 +1878,7 @@ extern "C" int skd_debug_kv_load(skd_state *st, int32_t cols, const float *const
       break;
     }
     if (st->kv8) {
-      if (have) rc = kv_load_8(st, l, kd, vd, cols);
+      rc = kv_load_8(st, l, have ? kd : nullptr, have ? vd : nullptr, cols);
     } else if (st->bf16)
       kv_load_bf16(st->stream, have ? kd : nullptr, have ? vd : nullptr, (bf16_t *)st->pool, bt_layer(st, l), st->start_dev, cols, B, st->geom);
     else

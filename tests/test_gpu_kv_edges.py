@@ -61,3 +61,24 @@ def test_a_new_token_without_a_page(elem, H, group, dh, long):
             k, v = (torch.from_numpy(R.as_held(x[r][at].double().numpy(), elem)) for x in (c.k, c.v))
             ref, bound = R.attention(q[r:r + 1].cpu().double(), k, v, len(at) - 1, scale)
             assert ((got.double() - ref[0]).abs() <= bound[0]).all(), r
+
+
+@pytest.mark.parametrize("dtype", [skd.BF16, skd.FP32, skd.BF16_KV8])
+def test_layers_that_are_set_to_nothing(dtype):
+    """Layers without arrays hold zeros, whatever the generation before has left there."""
+    r = Run(NARROW, 3, 20, 60, NARROW.L, NARROW.L, 0, dtype, ragged=True)
+    for t in range(20, 40):
+        r.step(t)
+    g = np.random.default_rng(5)
+    K, V = ([g.standard_normal((3, 37, NARROW.d)).astype(np.float32) for _ in range(NARROW.L)] for _ in range(2))
+    K[1] = V[1] = K[2] = V[3] = None
+    r.dec.kv_load(37, K, V, r.start)
+    for b in range(3):
+        s = r.start[b]
+        for l in range(NARROW.L):
+            k, v = r.dec.kv_read(l, b)
+            assert len(k) == 37
+            assert ((k[s:] == 0).all() and (v[s:] == 0).all()) == (l > 0)
+    r.step(37)
+    assert np.isfinite(r.logits()).all()
+    r.dec.close()
