@@ -341,10 +341,11 @@ __device__ inline bf16x8 widen(uint32_t a, uint32_t b, uint32_t e) {
                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true)};
   return bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
 }
-// fp32 of an exponent byte; 2^-127 as 0: a weight times 2^-127 of 448 at most is no value that fp32 sums would notice
+// fp32 of an exponent byte: byte 0, 2^-127, is a subnormal.  (Weights times such a factor are rounded to multiples of 2^-133, the
+// smallest bf16: a value of exponent 0 is off by 2^-134 * 448 = 2^-125 for each key, beside a sum of weights of at least 1.)
 __device__ inline float kv8_factor(uint32_t word, int i) {
   const uint32_t e = word >> (8 * i) & 255u;
-  return __uint_as_float(e == 255 ? 0x7fc00000u : e << 23);
+  return __uint_as_float(e == 255 ? 0x7fc00000u : max(e << 23, 0x00400000u));
 }
 __device__ inline bf16x8 pack8(const float (&p)[8]) {
   return __builtin_bit_cast(bf16x8, (uint32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])}));
@@ -1022,7 +1023,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
     const int stage[2] = {one, two};
     floatx4 S[2][NT][2];
     uint32_t ve[2][2];
-    float vs[2][8];
+    int power[2][8];  // of the values; 2 rows of 1023 behind 8193, 8 bits, us: by ldexp 338, as factors, 0 for byte 0, 341, as they are 358
     uint32x4 vw[FR - KF];
     bool raise = false;
 #pragma unroll
@@ -1033,7 +1034,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
       if constexpr (FP8) {
         factor_words(stage[u], ve[u]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) vs[u][j] = __uint_as_float((j & 3) == 3 ? ve[u][j >> 2] >> 1 & 0x7f800000u : ve[u][j >> 2] << (23 - 8 * (j & 3)) & 0x7f800000u);
+        for (int j = 0; j < 8; ++j) power[u][j] = (int)(ve[u][j >> 2] >> (8 * (j & 3)) & 255u) - 127;
 #pragma unroll
         for (int i = 0; i < 2; ++i) raise |= (((ve[u][i] & 0x7f7f7f7fu) + 0x01010101u) & ve[u][i] & 0x80808080u) != 0;
       }
@@ -1063,7 +1064,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) vs[u][j] = kv8_factor(ve[u][j >> 2], j & 3);
+          for (int j = 0; j < 8; ++j)
+            if (power[u][j] == 128) {  // a NaN that all queries see: so are their sums of weights
+#pragma unroll
+              for (int t = 0; t < NT; ++t) p[u][t][j] = __uint_as_float(0x7fc00000u);
+            }
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -1076,7 +1081,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
         tile[t].L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones(), pv[t], tile[t].L, 0, 0, 0);
         if constexpr (FP8) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p[u][t][j] *= vs[u][j];
+          for (int j = 0; j < 8; ++j) p[u][t][j] = __builtin_ldexpf(p[u][t][j], power[u][j]);
           pv[t] = pack8(p[u][t]);
         }
       }

@@ -63,6 +63,41 @@ def test_a_new_token_without_a_page(elem, H, group, dh, long):
             assert ((got.double() - ref[0]).abs() <= bound[0]).all(), r
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("past,new", [(4, 1), (300, 1), (70, 20), (500, 150)])
+@pytest.mark.parametrize("files", [True, False])
+def test_values_of_the_smallest_exponent(dh, past, new, files):
+    """8-bit values whose exponent byte is 0 (2^-127) count for what they are, in the call that files them and afterwards."""
+    c = Case(R.FP8, 1, dh, 64, [past], [new], seed=past)
+    g = torch.Generator().manual_seed(33)
+    c.v[0][:] = (torch.randint(8, 16, c.v[0].shape, generator=g) * 2.0 ** -123).bfloat16()  # 128 .. 240 units of 2^-127: exact
+    c.k[0][:] = torch.rand(c.k[0].shape, generator=g).bfloat16() - 0.5
+    q = ((torch.rand(new, 2, dh, generator=g) - 0.5) / 8).bfloat16().cuda()
+    c.append([0], [past])
+    if not files:
+        c.append([past], [new])
+    out = c.attend(q, files=files, scale=0.125).double()
+    k = torch.from_numpy(R.as_held(c.k[0].double().numpy(), R.FP8))
+    ref, bound = R.attention(q.cpu().double(), k, c.v[0].double(), past, 0.125)
+    # Beside the bound of attention(): a weight times 2^-127 is rounded to a multiple of 2^-133, by 2^-134 at most, and a code is 240 at
+    # most: each key adds 2^-126, over a sum of the weights that is 1/2 at least for each (scores are below 0.125 * dh / 2 / 16 <= 1/2
+    # in magnitude: weights lie within a factor of e of each other, and one of them is at least 1).
+    allowed = bound + 2.0 ** -126 * math.e
+    assert allowed.max() < ref.min() / 2
+    assert ((out - ref).abs() <= allowed).all()
+
+
+@pytest.mark.parametrize("past,new", [(40, 1), (70, 20), (500, 150)])
+def test_keys_of_the_smallest_exponent(past, new):
+    """Tiny keys against huge queries: scores of ordinary size."""
+    c = Case(R.FP8, 1, 128, 64, [past], [new], seed=past)
+    g = torch.Generator().manual_seed(34)
+    c.k[0][:] = ((torch.randint(0, 9, c.k[0].shape, generator=g) - 4) * 2.0 ** -122).bfloat16()
+    q = (torch.randn(new, 2, 128, generator=g) * 2.0 ** 120).bfloat16().cuda()
+    c.append([0], c.total)
+    c.check(q, c.attend(q, scale=0.125), 0.125)
+
+
 @pytest.mark.parametrize("dtype", [skd.BF16, skd.FP32, skd.BF16_KV8])
 def test_layers_that_are_set_to_nothing(dtype):
     """Layers without arrays hold zeros, whatever the generation before has left there."""
