@@ -401,9 +401,9 @@ int64_t skd_kv_page_bytes(const skd_kv *kv);
  * strides in elements from token to token (multiples of 8, pointers 16-byte
  * aligned).  What the pages hold at other positions stays.  Errors:
  * SKD_ERR_NULL; SKD_ERR_SHAPE (unknown elem, head_dim, page_tokens, counts below
- * 1, strides, alignment); SKD_ERR_RANGE (negative counts, sizes beyond 32 bits of
- * positions or workgroups, memory that is not the current device's);
- * SKD_ERR_HIP. */
+ * 1, strides, alignment); SKD_ERR_RANGE (negative counts; 2^30 positions of a row,
+ * or 2^31 blocks of 32 positions, max_new of every row and kv head, or more; memory
+ * that is not the current device's); SKD_ERR_HIP. */
 int skd_kv_append(const skd_kv *kv, const skd_kv_chunk *chunk, const void *k, int64_t k_stride, const void *v,
                   int64_t v_stride, void *hip_stream);
 
@@ -425,8 +425,9 @@ int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t elem, void 
  * instructions.  workspace: skd_kv_attend_workspace bytes for this kv, chunk and
  * heads (16-byte aligned; NULL where that is 0), nothing in it is kept from call
  * to call.  The same call gives the same bits.  Errors as skd_kv_append, and
- * SKD_ERR_SHAPE (heads), SKD_ERR_RANGE (scale not above 0), SKD_ERR_NOMEM
- * (workspace_bytes). */
+ * SKD_ERR_SHAPE (heads), SKD_ERR_RANGE (scale not above 0; 2^32 threads or more,
+ * of which 16, 32 or 128 queries of a row and kv head take 256 or 512),
+ * SKD_ERR_NOMEM (workspace_bytes). */
 int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, float scale, const void *q, int64_t q_stride,
                   const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
                   void *workspace, int64_t workspace_bytes, void *hip_stream);
@@ -448,8 +449,8 @@ int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *chunk, int
  * u is cut to [0,1).  vocab <= 262144.  All memory is the current device's, with
  * stream and workspace (skd_sample_workspace bytes; NULL where that is 0) as for
  * the calls above.  Errors: SKD_ERR_NULL; SKD_ERR_SHAPE (vocab, stride, pointers not
- * aligned to their elements); SKD_ERR_RANGE (rows < 0, memory that is not the
- * current device's); SKD_ERR_NOMEM (workspace_bytes); SKD_ERR_HIP. */
+ * aligned to their elements); SKD_ERR_RANGE (rows < 0 or from 2^22 on, 2^20 of
+ * the largest vocab, memory that is not the current device's); SKD_ERR_NOMEM (workspace_bytes); SKD_ERR_HIP. */
 int skd_sample(const float *logits, int64_t stride, int32_t rows, int32_t vocab, const skd_sampling *params, const float *u,
                int32_t *tokens_out, void *workspace, int64_t workspace_bytes, void *hip_stream);
 int64_t skd_sample_workspace(int32_t rows, int32_t vocab);

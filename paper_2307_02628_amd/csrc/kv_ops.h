@@ -38,6 +38,9 @@ struct KvRows {
   bool tiles;
 };
 
+// Blocks of 32 positions that filing and reading back look at (a call's must be below 2^31): of every row and kv head as many as a
+// row's new tokens may lie in.
+long kv_blocks(const KvView &kv, const KvTokens &tk);
 // k, v (bf16) of the tokens into their pages
 void kv_append(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows &k, const KvRows &v);
 // the pages' values of the tokens, fp32 or bf16 rows
@@ -53,6 +56,7 @@ struct KvAttend {
   int splits;               // of the keys of a query tile
   float *part;              // splits > 1: [splits][tokens * heads][dh + 2]: numerators, maximum, denominator
 };
+bool kv_attend_fits(const KvView &kv, const KvTokens &tk, int heads);  // in a launch; rows x kv heads must be below 2^31 before
 int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads);
 size_t kv_attend_part(const KvView &kv, const KvTokens &tk, int heads, int splits);  // floats
 void kv_attend(hipStream_t s, const KvAttend &a);

@@ -100,11 +100,12 @@ __device__ inline float kv8_scale(uint32_t e) { return e == 255 ? __uint_as_floa
 // are neighbours in the page are gathered.  Bound by the bytes of large calls; a block's codes leave as whole words where the
 // row fills them, and element by element at the ends of its tokens, so that what other tokens hold there stays.
 template <int DH, bool FP8>
-__global__ __launch_bounds__(256) void k_kv_append(KvView kv, KvTokens tk, KvRows k, KvRows v, int blocks) {
+__global__ __launch_bounds__(256) void k_kv_append(KvView kv, KvTokens tk, KvRows k, KvRows v, int blocks, uint32_t from) {
   constexpr int LPT = DH / 8, TPP = 256 / LPT;  // lanes a token, tokens a pass
   typedef typename std::conditional<FP8, uint8_t, uint16_t>::type code_t;
   __shared__ __align__(16) code_t sv[32][DH + 8];
-  const int blk_i = blockIdx.x % blocks, h = blockIdx.x / blocks % kv.g.H, r = blockIdx.x / blocks / kv.g.H;
+  const uint32_t id = from + blockIdx.x;
+  const int blk_i = id % blocks, h = id / blocks % kv.g.H, r = id / blocks / kv.g.H;
   const RowTokens t = row_tokens(tk, r);
   const int blk = (t.past >> 5) + blk_i, lo = max(t.past, blk * 32), hi = min(t.past + t.n, blk * 32 + 32);
   if (t.n <= 0 || lo >= hi) return;
@@ -263,10 +264,11 @@ __global__ __launch_bounds__(256) void k_kv_read_few(KvView kv, KvTokens tk, KvR
 // As above, the other way: a workgroup reads the tokens of a row and kv head that lie in one block.  Bound by the fp32 rows
 // that it writes.
 template <int DH, bool FP8, typename OUT>
-__global__ __launch_bounds__(256) void k_kv_read(KvView kv, KvTokens tk, KvRows k, KvRows v, int blocks) {
+__global__ __launch_bounds__(256) void k_kv_read(KvView kv, KvTokens tk, KvRows k, KvRows v, int blocks, uint32_t from) {
   constexpr int LPT = DH / 8, TPP = 256 / LPT;
   __shared__ float sv[32][DH + 1];
-  const int blk_i = blockIdx.x % blocks, h = blockIdx.x / blocks % kv.g.H, r = blockIdx.x / blocks / kv.g.H;
+  const uint32_t id = from + blockIdx.x;
+  const int blk_i = id % blocks, h = id / blocks % kv.g.H, r = id / blocks / kv.g.H;
   const RowTokens t = row_tokens(tk, r);
   const int blk = (t.past >> 5) + blk_i, lo = max(t.past, blk * 32), hi = min(t.past + t.n, blk * 32 + 32);
   if (t.n <= 0 || lo >= hi) return;
@@ -1247,7 +1249,15 @@ int blocks_of(const KvTokens &tk) { return (tk.max_new + 31 + 31) / 32; }  // of
 // Workgroups of the kernels for a few tokens, or 0: up to 8 of a row (k_kv_append_few), and a grid that fits.
 static unsigned few_groups(const KvView &kv, const KvTokens &tk) {
   const long units = 2L * kv.g.H * tk.max_new * kv.rows, groups = (units * (kv.g.dh / 8) + 255) / 256;
-  return tk.max_new <= 8 && units < (1L << 31) ? (unsigned)groups : 0;  // (units are counted in 32 bits)
+  return tk.max_new <= 8 && launch_fits(groups, 256) ? (unsigned)groups : 0;  // (units, of 8 lanes or more, are in 32 bits then)
+}
+long kv_blocks(const KvView &kv, const KvTokens &tk) { return (long)blocks_of(tk) * kv.g.H * kv.rows; }
+// The kernels for many tokens, a workgroup for each block: f(grid, first block) for as many as a launch has, which is all of them
+// but for a row of 100000 tokens among more than a hundred.
+template <typename F>
+static void each_launch(const KvView &kv, const KvTokens &tk, F f) {
+  const long all = kv_blocks(kv, tk);
+  for (long from = 0; from < all; from += launch_most(256)) f(dim3((unsigned)std::min(all - from, launch_most(256))), (uint32_t)from);
 }
 void kv_append(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows &k, const KvRows &v) {
   if (const unsigned few = few_groups(kv, tk)) {
@@ -1261,26 +1271,28 @@ void kv_append(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows
     return;
   }
   const int blocks = blocks_of(tk);
-  const dim3 grid((unsigned)((long)blocks * kv.g.H * kv.rows));
-  if (kv.g.dh == 64) {
-    if (kv.fp8) SKD_LAUNCH((k_kv_append<64, true>), grid, dim3(256), 0, s, kv, tk, k, v, blocks);
-    else SKD_LAUNCH((k_kv_append<64, false>), grid, dim3(256), 0, s, kv, tk, k, v, blocks);
-  } else {
-    if (kv.fp8) SKD_LAUNCH((k_kv_append<128, true>), grid, dim3(256), 0, s, kv, tk, k, v, blocks);
-    else SKD_LAUNCH((k_kv_append<128, false>), grid, dim3(256), 0, s, kv, tk, k, v, blocks);
-  }
+  each_launch(kv, tk, [&](dim3 grid, uint32_t from) {
+    if (kv.g.dh == 64) {
+      if (kv.fp8) SKD_LAUNCH((k_kv_append<64, true>), grid, dim3(256), 0, s, kv, tk, k, v, blocks, from);
+      else SKD_LAUNCH((k_kv_append<64, false>), grid, dim3(256), 0, s, kv, tk, k, v, blocks, from);
+    } else {
+      if (kv.fp8) SKD_LAUNCH((k_kv_append<128, true>), grid, dim3(256), 0, s, kv, tk, k, v, blocks, from);
+      else SKD_LAUNCH((k_kv_append<128, false>), grid, dim3(256), 0, s, kv, tk, k, v, blocks, from);
+    }
+  });
 }
 
 void kv_read(hipStream_t s, const KvView &kv, const KvTokens &tk, bool bf16, const KvRows &k, const KvRows &v) {
   const int blocks = blocks_of(tk);
-  const dim3 grid((unsigned)((long)blocks * kv.g.H * kv.rows));
   const unsigned few = few_groups(kv, tk);
-#define SKD_READ(DH, FP8)                                                                                  \
-  do {                                                                                                     \
-    if (few && bf16) SKD_LAUNCH((k_kv_read_few<DH, FP8, bf16_t>), dim3(few), dim3(256), 0, s, kv, tk, k, v); \
-    else if (few) SKD_LAUNCH((k_kv_read_few<DH, FP8, float>), dim3(few), dim3(256), 0, s, kv, tk, k, v);     \
-    else if (bf16) SKD_LAUNCH((k_kv_read<DH, FP8, bf16_t>), grid, dim3(256), 0, s, kv, tk, k, v, blocks);       \
-    else SKD_LAUNCH((k_kv_read<DH, FP8, float>), grid, dim3(256), 0, s, kv, tk, k, v, blocks);             \
+#define SKD_READ(DH, FP8)                                                                                                     \
+  do {                                                                                                                        \
+    if (few && bf16) SKD_LAUNCH((k_kv_read_few<DH, FP8, bf16_t>), dim3(few), dim3(256), 0, s, kv, tk, k, v);                    \
+    else if (few) SKD_LAUNCH((k_kv_read_few<DH, FP8, float>), dim3(few), dim3(256), 0, s, kv, tk, k, v);                        \
+    else each_launch(kv, tk, [&](dim3 grid, uint32_t from) {                                                                  \
+      if (bf16) SKD_LAUNCH((k_kv_read<DH, FP8, bf16_t>), grid, dim3(256), 0, s, kv, tk, k, v, blocks, from);                   \
+      else SKD_LAUNCH((k_kv_read<DH, FP8, float>), grid, dim3(256), 0, s, kv, tk, k, v, blocks, from);                         \
+    });                                                                                                                       \
   } while (0)
   if (kv.g.dh == 64) {
     if (kv.fp8) SKD_READ(64, true);
@@ -1335,6 +1347,10 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
     while (p.splits < 64 && wgs * p.waves * p.splits < 2048 && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
   }
   return p;
+}
+bool kv_attend_fits(const KvView &kv, const KvTokens &tk, int heads) {
+  const AttendPlan p = plan_attend(kv, tk, heads);
+  return launch_fits(p.tiles * p.pairs, 64 * p.waves);
 }
 int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads) { return plan_attend(kv, tk, heads).splits; }
 size_t kv_attend_part(const KvView &kv, const KvTokens &tk, int heads, int splits) {

@@ -28,6 +28,7 @@ struct SampleRows {
   int piece, pieces;          // set by sample_rows: tokens of a piece
 };
 size_t sample_rows_bins(int rows, int vocab);
+bool sample_rows_fit(int rows, int vocab);  // in a launch each
 void sample_rows(hipStream_t s, const SampleRows &a);
 
 }  // namespace skd

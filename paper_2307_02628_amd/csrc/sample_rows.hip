@@ -818,6 +818,8 @@ size_t sample_rows_bins(int rows, int vocab) {
   return (size_t)rows * ((vocab + piece - 1) / piece);
 }
 
+bool sample_rows_fit(int rows, int vocab) { return launch_fits((long)sample_rows_bins(rows, vocab), 256) && launch_fits(rows, NW * 64); }
+
 void sample_rows(hipStream_t s, const SampleRows &call) {
   SampleRows a = call;
   const int per = per_thread(a.rows, a.vocab);

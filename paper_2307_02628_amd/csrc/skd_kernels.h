@@ -9,6 +9,10 @@
 
 namespace skd {
 
+// Workgroups that a launch may have: its threads are counted in 32 bits.
+constexpr long launch_most(int threads) { return ((1L << 32) - 1) / threads; }
+constexpr bool launch_fits(long workgroups, int threads) { return workgroups <= launch_most(threads); }
+
 typedef uint16_t bf16_t;  // raw bfloat16 bit pattern in host-visible signatures
 
 // Per-launch timing.  While a thread has a LaunchTimer installed, every kernel launch it makes through

@@ -89,7 +89,7 @@ int launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SKD_OK : hip_failed(e);
 }
-bool fits_grid(int64_t wgs) { return wgs <= std::numeric_limits<int32_t>::max(); }
+bool fits_int(__int128 n) { return n <= std::numeric_limits<int32_t>::max(); }
 
 #define CHECK(expr)          \
   do {                       \
@@ -115,7 +115,7 @@ extern "C" int skd_kv_append(const skd_kv *kv, const skd_kv_chunk *ch, const voi
   CHECK(check_rows(k, k_stride, width));
   CHECK(check_rows(v, v_stride, width));
   if (!aligned(kv->pool) || !aligned4({kv->block_table, ch->first, ch->past})) return SKD_ERR_SHAPE;
-  if (!fits_grid(((int64_t)tk.max_new + 62) / 32 * kv->kv_heads * kv->rows)) return SKD_ERR_RANGE;
+  if (!fits_int((__int128)kv->kv_heads * kv->rows * ((tk.max_new + 62LL) / 32))) return SKD_ERR_RANGE;
   CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, k, v}));
   kv_append((hipStream_t)hip_stream, view(kv), tk, rows_of(k, k_stride), rows_of(v, v_stride));
   return launched();
@@ -132,7 +132,7 @@ extern "C" int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *ch, int32_t ele
   CHECK(check_rows(k_out, k_stride, width));
   CHECK(check_rows(v_out, v_stride, width));
   if (!aligned(kv->pool) || !aligned4({kv->block_table, ch->first, ch->past})) return SKD_ERR_SHAPE;
-  if (!fits_grid(((int64_t)tk.max_new + 62) / 32 * kv->kv_heads * kv->rows)) return SKD_ERR_RANGE;
+  if (!fits_int((__int128)kv->kv_heads * kv->rows * ((tk.max_new + 62LL) / 32))) return SKD_ERR_RANGE;
   CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, k_out, v_out}));
   kv_read((hipStream_t)hip_stream, view(kv), tk, elem == SKD_W_BF16, rows_of(k_out, k_stride), rows_of(v_out, v_stride));
   return launched();
@@ -144,8 +144,8 @@ static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads)
   const KvTokens tk = tokens(kv, ch);
   const int64_t group = heads / kv->kv_heads;
   const int64_t queries = tk.max_new * group;
-  if (queries > std::numeric_limits<int32_t>::max() - 128 || !fits_grid((queries + 15) / 16 * ((int64_t)kv->kv_heads * std::max(kv->rows, 1) + 8))) return SKD_ERR_RANGE;
-  return SKD_OK;
+  if (!fits_int(queries + 128) || !fits_int((int64_t)kv->kv_heads * kv->rows + 8)) return SKD_ERR_RANGE;
+  return kv_attend_fits(view(kv), tk, heads) ? SKD_OK : SKD_ERR_RANGE;
 }
 
 extern "C" int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads) {
@@ -200,6 +200,7 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
 extern "C" int64_t skd_sample_workspace(int32_t rows, int32_t vocab) {
   if (rows < 0) return SKD_ERR_RANGE;
   if (vocab < 1 || vocab > SAMPLE_ROWS_VOCAB) return SKD_ERR_SHAPE;
+  if (!sample_rows_fit(rows, vocab)) return SKD_ERR_RANGE;
   return (int64_t)(sample_rows_bins(rows, vocab) * sizeof(SampleBins));
 }
 
@@ -213,7 +214,6 @@ extern "C" int skd_sample(const float *logits, int64_t stride, int32_t rows, int
   if (!aligned(workspace) || !aligned4({logits, u, tokens_out})) return SKD_ERR_SHAPE;
   if (params && !aligned4({params->temperature, params->top_k, params->top_p, params->min_p})) return SKD_ERR_SHAPE;
   if (workspace_bytes < need) return SKD_ERR_NOMEM;
-  if (!fits_grid((int64_t)sample_rows_bins(rows, vocab))) return SKD_ERR_RANGE;
   SampleRows a{};
   a.bins = (SampleBins *)workspace;
   a.logits = logits;

@@ -117,3 +117,28 @@ def test_layers_that_are_set_to_nothing(dtype):
     r.step(37)
     assert np.isfinite(r.logits()).all()
     r.dec.close()
+
+
+@pytest.mark.parametrize("elem", [R.BF16, R.FP8])
+def test_one_long_row_among_many(elem):
+    """More blocks, max_new of every row, than a launch has workgroups: the tokens of all rows are filed and read back."""
+    rows, n, few, page, dh = 4110, 131000, 72, 64, 64
+    assert (n + 62) // 32 * rows >= 2 ** 24
+    table = torch.full((rows, -(-n // page)), -1, dtype=torch.int32)
+    order = torch.randperm(table.shape[1] + 4, generator=torch.Generator().manual_seed(35)).int()
+    table[7] = order[:table.shape[1]]
+    table[rows - 1, :4] = order[table.shape[1]:]
+    size = page * (4 * dh if elem == R.BF16 else 2 * dh + 2)
+    pool = torch.zeros(len(order), size, dtype=torch.uint8, device="cuda")
+    cache = skd.KvCache(pool, table.cuda(), 1, dh, page, elem)
+    first = torch.zeros(rows + 1, dtype=torch.int32)
+    first[8:], first[rows] = n, n + few
+    past = torch.zeros(rows, dtype=torch.int32)
+    past[rows - 1] = 150
+    ch = skd.KvChunk(first.cuda(), past.cuda(), n + few, n, 150)
+    k, v = (torch.randn(n + few, 1, dh, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda").bfloat16() for i in range(2))
+    cache.append(ch, k, v)
+    ko, vo = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    cache.read(ch, ko, vo)
+    for x, y in ((k, ko), (v, vo)):
+        assert torch.equal(torch.from_numpy(R.as_held(x.cpu().double().numpy(), elem)), y.cpu().double())

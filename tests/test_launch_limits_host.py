@@ -1,0 +1,48 @@
+"""Sizes at the end of what a launch can have (its threads are counted in 32 bits), on the CPU: the largest are accepted by the calls
+that size a workspace, one more is refused before any device work."""
+import ctypes as C
+import os
+
+import pytest
+
+from paper_2307_02628_amd import _build, skd
+from test_kv_ops_host import append, attend, chunk, kv, read
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(skd.LIB_PATH):
+        _build.build(force=True)
+
+
+@pytest.mark.parametrize("heads,new,most", [
+    (1, 1, 2 ** 24 - 1),        # a tile of 16 queries, 4 waves
+    (20, 1, 2 ** 23 - 1),       # of 32, 8 waves
+    (200, 1, 2 ** 23 - 8),      # two of 128 each, on places for a multiple of 8 rows
+])
+def test_rows_of_an_attention(heads, new, most):
+    def space(rows):
+        return skd.lib().skd_kv_attend_workspace(C.byref(kv(kv_heads=1, rows=rows)), C.byref(chunk(tokens=1, max_new=new)), heads)
+
+    assert space(most) == 0 and space(most + 1) == skd.ERR_RANGE and space(2 ** 31 - 1) == skd.ERR_RANGE
+    bad = kv(kv_heads=1, rows=most + 1)
+    assert attend(bad, chunk(tokens=1, max_new=new), heads, qs=heads * 128, os_=heads * 128) == skd.ERR_RANGE
+
+
+def test_blocks_of_a_cache():
+    """Rows x kv heads x blocks of the longest row: products beyond 64 bits too."""
+    huge = dict(kv_heads=65536, rows=2 ** 31 - 1, page_tokens=32, max_pages=2 ** 25 - 1)
+    width = 65536 * 128
+    for new in (1, 2 ** 30):
+        ch = chunk(tokens=2 ** 30, max_new=new)
+        for call in (append, read):
+            assert call(kv(**huge), ch, ks=width, vs=width) == skd.ERR_RANGE
+        assert attend(kv(**huge), ch, 65536, qs=width, os_=width) == skd.ERR_RANGE
+
+
+@pytest.mark.parametrize("vocab,most", [(1000, 2 ** 22 - 1), (262144, 2 ** 20 - 1)])
+def test_rows_of_a_draw(vocab, most):
+    lib, P = skd.lib(), 1 << 20
+    assert lib.skd_sample_workspace(most, vocab) > 0
+    assert lib.skd_sample_workspace(most + 1, vocab) == skd.ERR_RANGE
+    assert lib.skd_sample(P, vocab, most + 1, vocab, None, P, P, P, 1 << 62, None) == skd.ERR_RANGE
