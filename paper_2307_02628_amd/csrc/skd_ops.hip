@@ -142,6 +142,7 @@ static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads)
   CHECK(check_call(kv, ch));
   if (heads < 1 || heads % kv->kv_heads) return SKD_ERR_SHAPE;
   const KvTokens tk = tokens(kv, ch);
+  if (!fits_int((int64_t)heads * kv->head_dim)) return SKD_ERR_RANGE;  // columns of a token
   const int64_t group = heads / kv->kv_heads;
   const int64_t queries = tk.max_new * group;
   if (!fits_int(queries + 128) || !fits_int((int64_t)kv->kv_heads * kv->rows + 8)) return SKD_ERR_RANGE;

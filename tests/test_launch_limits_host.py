@@ -40,6 +40,18 @@ def test_blocks_of_a_cache():
         assert attend(kv(**huge), ch, 65536, qs=width, os_=width) == skd.ERR_RANGE
 
 
+def test_columns_of_a_token():
+    """Query heads are elements of a token in 32 bits."""
+    one = dict(c=kv(kv_heads=1, rows=1), ch=chunk(tokens=1, max_new=1, max_past=31))
+    for dh in (64, 128):
+        one["c"].head_dim = dh
+        most = 2 ** 31 // dh - 1
+        assert skd.lib().skd_kv_attend_workspace(C.byref(one["c"]), C.byref(one["ch"]), most) >= 0
+        for heads in (most + 1, 2 ** 31 - 129):
+            assert skd.lib().skd_kv_attend_workspace(C.byref(one["c"]), C.byref(one["ch"]), heads) == skd.ERR_RANGE
+            assert attend(**one, heads=heads, qs=heads * dh, os_=heads * dh) == skd.ERR_RANGE
+
+
 @pytest.mark.parametrize("vocab,most", [(1000, 2 ** 22 - 1), (262144, 2 ** 20 - 1)])
 def test_rows_of_a_draw(vocab, most):
     lib, P = skd.lib(), 1 << 20
