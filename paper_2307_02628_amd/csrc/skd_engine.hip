@@ -1692,7 +1692,7 @@ extern "C" int skd_logits_sample_rows(skd_state *st, const float *u, const skd_s
   if (!c.io_on_device)
     for (int b = 0; b < B; ++b) {
       if (!(u[b] >= 0.f) || u[b] >= 1.f) return SKD_ERR_RANGE;
-      if (p.temperature && (!(p.temperature[b] >= 0.f) || p.temperature[b] > 3.0e38f)) return SKD_ERR_RANGE;
+      if (p.temperature && (!(p.temperature[b] >= 0.f) || !std::isfinite(p.temperature[b]))) return SKD_ERR_RANGE;
       if (p.top_k && p.top_k[b] < 0) return SKD_ERR_RANGE;
       if (p.top_p && (!(p.top_p[b] > 0.f) || p.top_p[b] > 1.f)) return SKD_ERR_RANGE;
       if (p.min_p && (!(p.min_p[b] >= 0.f) || p.min_p[b] > 1.f)) return SKD_ERR_RANGE;

@@ -119,6 +119,17 @@ def test_layers_that_are_set_to_nothing(dtype):
     r.dec.close()
 
 
+def test_temperatures_up_to_the_largest():
+    r = Run(NARROW, 3, 5, 20, 1, 2)
+    u = [0.1, 0.5, 0.9]
+    for t, rc in ((np.finfo(np.float32).max, skd.OK), (3.2e38, skd.OK), (np.inf, skd.ERR_RANGE), (np.nan, skd.ERR_RANGE), (-1.0, skd.ERR_RANGE)):
+        got, tok, _ = r.dec.logits_sample_rows_rc(u, temperature=[1.0, t, 1.0])
+        assert got == rc
+        if rc == skd.OK:
+            assert tok[1] == NARROW.V // 2                            # every token alike: the one at which the running mass passes a half
+    r.dec.close()
+
+
 @pytest.mark.parametrize("elem", [R.BF16, R.FP8])
 def test_one_long_row_among_many(elem):
     """More blocks, max_new of every row, than a launch has workgroups: the tokens of all rows are filed and read back."""
