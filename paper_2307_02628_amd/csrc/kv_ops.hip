@@ -595,6 +595,7 @@ __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, in
         drop_odd(w);
         tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pv, tile[t].O[m], 0, 0, 0);
         add_odd(tile[t].O[m], v, vis);
+        __builtin_amdgcn_sched_barrier(0);  // (one fragment after the other: side by side they take more registers than there are)
       }
     }
   }

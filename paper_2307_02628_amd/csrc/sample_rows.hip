@@ -239,6 +239,13 @@ struct Pick {
   u64 found_sum;
 };
 
+// `v`, so that what is computed from it is computed here: which lanes a step is for takes one comparison, but two scalar registers
+// from one step to the next, and together with the rest more than there are.
+__device__ inline int now(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // (With a call left to any of the steps all that they share would live in memory: 139 us.)
 #define SKD_INLINE __attribute__((always_inline))
 __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
@@ -255,7 +262,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   top = wave_top(top);
   const bool greedy = p.greedy || top == INFINITY || top == -INFINITY;
   const Grid g(p.T, sh.tab);
-  const float place = uniform(greedy ? 0.f : g.place(top)), lowest = uniform(greedy ? top : p.floor_of(top));
+  const float place = greedy ? 0.f : g.place(top), lowest = greedy ? top : p.floor_of(top);
   if (tid < 64) sh.tab[tid] = exp2(tid / 64.0);
   if (tid < pieces) {
     const float t = bins[tid].top;
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   auto index_of = [&](int i) { return sh.index[own_list + lane + 64 * i]; };
   auto list = [&]() SKD_INLINE {
     __syncthreads();
-    if (tid == 0) {
+    if (now(tid) == 0) {
       sh.n = 0;
       sh.lo = 0xffffffffu;
       sh.hi = 0;
@@ -386,7 +393,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
   auto locate = [&](auto is, auto bucket_of, auto word, auto weight, auto enough) SKD_INLINE -> bool {
     const bool few = sh.n <= 64;
     sh.bucket[tid] = 0;
-    if (tid == 0) {
+    if (now(tid) == 0) {
       sh.bucket_at = few ? 0 : 1 << 30;
       sh.bucket_before = 0;
       sh.near_n = 0;
@@ -489,7 +496,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
       const int shift = max(22 - __clz((int)((last - first) | 1)), 0);
       __syncthreads();
       sh.bucket[tid] = 0;
-      if (tid == 0) sh.bucket_at = 1 << 30;
+      if (now(tid) == 0) sh.bucket_at = 1 << 30;
       __syncthreads();
       auto add = [&](float x, int i) {
         const uint32_t w = word(x, i);
@@ -498,7 +505,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
       if (whole) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-          if (key[i]) add(value_of(key[i]), index_of(i));
+          if (const uint32_t x = (uint32_t)now((int)key[i])) add(value_of(x), index_of(i));
       } else {
         sweep([&](float x, int i, bool hit) {
           if (hit) add(x, i);
@@ -550,7 +557,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     typedef typename std::remove_reference<decltype(before)>::type S;
     const S x = tid <= last ? (S)of[tid] : (S)0, scan = wave_scan64(x);
     if (lane == 63) sh.wave_mass[wave] = __builtin_bit_cast(u64, scan);
-    if (tid == 0) sh.bucket_at = BINS + 1;
+    if (now(tid) == 0) sh.bucket_at = BINS + 1;
     __syncthreads();
     S run = 0, all = 0;
 #pragma unroll
@@ -654,7 +661,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     else
       is = narrow([&](float, int i) { return (uint32_t)i; }, [&](float x) { return x >= cut ? mass_at(x) : 0ull; }, passed, 0, V - 1, at);
     if (is) token = (int)at;
-    if (tid == 0) answer(token);
+    if (now(tid) == 0) answer(token);
     return;
   }
 
@@ -798,7 +805,7 @@ __global__ __launch_bounds__(NW * 64) void k_sample_pick(SampleRows a) {
     if (lane == 0) answer(last);
     return;
   }
-  if (tid == 0) answer(last);
+  if (now(tid) == 0) answer(last);
 }
 #undef SKD_INLINE
 
