@@ -63,6 +63,18 @@ def test_a_new_token_without_a_page(elem, H, group, dh, long):
             assert ((got.double() - ref[0]).abs() <= bound[0]).all(), r
 
 
+@pytest.mark.parametrize("elem", [R.BF16, R.FP8])
+@pytest.mark.parametrize("H,group,new", [(1, 1, 1), (1, 8, 1), (2, 3, 5), (1, 2, 14)])
+def test_64_wide_heads_in_many_shares(elem, H, group, new):
+    c = Case(elem, H, 64, 32, [9000], [new], seed=group + new)
+    q = torch.randn(new, H * group, 64, generator=torch.Generator().manual_seed(32)).bfloat16().cuda()
+    shares = c.cache.attend_workspace(c.chunk(c.past, c.new), H * group) / (4 * 66 * new * H * group)
+    assert shares > 8
+    c.append([0], c.past)
+    c.check(q, c.attend(q, files=True))
+    c.check(q, c.attend(q))
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("past,new", [(4, 1), (300, 1), (70, 20), (500, 150)])
 @pytest.mark.parametrize("files", [True, False])
@@ -96,6 +108,23 @@ def test_keys_of_the_smallest_exponent(past, new):
     q = (torch.randn(new, 2, 128, generator=g) * 2.0 ** 120).bfloat16().cuda()
     c.append([0], c.total)
     c.check(q, c.attend(q, scale=0.125), 0.125)
+
+
+def test_workspaces_that_are_refused():
+    c = Case(R.BF16, 2, 64, 32, [3], [1], seed=71, spare=3999)
+    ch, lib = c.chunk([100000], [1]), skd.lib()
+    need = c.cache.attend_workspace(ch, 2)
+    assert need > 0
+    dev, host = torch.zeros(1, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(need, dtype=torch.uint8)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def rc(p, n):
+        return lib.skd_kv_attend(c.cache.ref, ch.ref, 2, 0.1, dev.data_ptr(), 128, None, 0, None, 0, dev.data_ptr(), 128, p, n, None)
+
+    assert rc(None, need) == rc(None, 0) == skd.ERR_NULL
+    assert rc(ws.data_ptr(), need - 1) == skd.ERR_NOMEM
+    at = -host.data_ptr() % 16                                        # (an aligned place in ordinary host memory)
+    assert rc(host.data_ptr() + at, need) == skd.ERR_RANGE
 
 
 @pytest.mark.parametrize("dtype", [skd.BF16, skd.FP32, skd.BF16_KV8])
