@@ -241,8 +241,12 @@ class Decoder:
         """tokens: [B][cols] host array, or [cols][B] int32 device tensor with io_on_device."""
         if isinstance(tokens, np.ndarray):
             tokens = np.ascontiguousarray(tokens, dtype=np.int32)
-        elif not tokens.is_contiguous() or str(tokens.dtype) != "torch.int32":
-            raise ValueError("expected contiguous int32 tokens")
+            if tokens.ndim != 2:
+                raise ValueError("expected tokens of two dimensions")
+        else:
+            _expect(tokens, "int32", 2)
+        if bool(self.cfg.io_on_device) != bool(getattr(tokens, "is_cuda", False)):
+            raise ValueError("expected tokens in " + ("device" if self.cfg.io_on_device else "host") + " memory")
         B, cols = tokens.shape if not self.cfg.io_on_device else tuple(tokens.shape)[::-1]
         if B != self.cfg.batch:
             raise ValueError(f"tokens of {self.cfg.batch} rows expected")
@@ -299,7 +303,17 @@ class Decoder:
         return tok, lg
 
     def logits_sample_rows_device(self, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens_out=None, logits_out=None):
-        """Device-I/O form: device pointers / torch tensors (top_k int32, the others float32); asynchronous."""
+        """Device-I/O form: device pointers / torch tensors (top_k and tokens_out int32, the others float32); asynchronous."""
+        assert self.cfg.io_on_device
+        B = self.cfg.batch
+        for t, dtype, shape in ((u, "float32", (B,)), (temperature, "float32", (B,)), (top_k, "int32", (B,)), (top_p, "float32", (B,)),
+                                (min_p, "float32", (B,)), (tokens_out, "int32", (B,)), (logits_out, "float32", (B, self.cfg.vocab))):
+            if hasattr(t, "data_ptr"):
+                _expect(t, dtype, len(shape))
+                if tuple(t.shape) != shape or not t.is_cuda:
+                    raise ValueError(f"expected device memory of shape {shape}")
+            elif isinstance(t, np.ndarray):
+                raise ValueError("expected device memory")
         p = Sampling(*[_ptr_of(a) for a in (temperature, top_k, top_p, min_p)])
         _check(self._lib.skd_logits_sample_rows(self._h, _ptr_of(u), C.byref(p), _ptr_of(tokens_out), _ptr_of(logits_out)),
                "skd_logits_sample_rows")
