@@ -432,11 +432,11 @@ class KvCache:
         if chunk.rows != self.rows:
             raise ValueError("chunk and block table differ in rows")
         shape, stride = tuple(t.shape), t.stride()
-        if shape not in ((chunk.tokens, heads, self.dh), (chunk.tokens, heads * self.dh)) or stride[-1] != 1 or (len(shape) == 3 and stride[1] != self.dh):
+        if shape not in ((chunk.tokens, heads, self.dh), (chunk.tokens, heads * self.dh)) or stride[-1] != 1 or (len(shape) == 3 and heads > 1 and stride[1] != self.dh):
             raise ValueError(f"expected [{chunk.tokens}][{heads}][{self.dh}] with dense tokens")
         if _dtype_of(t) not in types:
             raise ValueError(f"expected {' or '.join(types)}")
-        return t.data_ptr(), max(stride[0], heads * self.dh) if shape[0] < 2 else stride[0]
+        return t.data_ptr(), heads * self.dh if shape[0] < 2 else stride[0]  # (one token: whatever its stride says)
 
     def append(self, chunk: KvChunk, k, v, stream: int = 0):
         _check(self._lib.skd_kv_append(self.ref, chunk.ref, *self._rows_of(chunk, self.heads, k, "torch.bfloat16"),

@@ -56,3 +56,19 @@ def test_draws_in_the_wrong_memory():
         for bad in (torch.zeros(t.shape, dtype=t.dtype), np.zeros(t.shape), device(*t.shape, dtype=other), device(4, *t.shape[1:], dtype=t.dtype)):
             with pytest.raises(ValueError):
                 decoder(1).logits_sample_rows_device(**{**good, name: bad})
+
+
+def test_strides_of_dense_tokens():
+    """Dimensions of one element may have any stride."""
+    cache = skd.KvCache(torch.zeros(2, 32 * 256, dtype=torch.bfloat16), torch.zeros(1, 2, dtype=torch.int32), 1, 128, 32)
+    place = lambda t, heads: cache._rows_of(skd.KvChunk(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), len(t), len(t), 0), heads, t, "torch.bfloat16")  # noqa: E731
+    x = torch.zeros(1, 5, 128, dtype=torch.bfloat16)
+    assert place(x.transpose(0, 1), 1) == (x.data_ptr(), 128)
+    wide = torch.zeros(7, 1001, dtype=torch.bfloat16)
+    assert place(wide[3:4, 16:144], 1) == (wide[3:4, 16:].data_ptr(), 128)
+    assert place(wide[3:4, 16:528].view(1, 4, 128), 4)[1] == 512
+    assert place(wide[:, 16:144], 1)[1] == 1001                       # (refused by the library: not a multiple of 8)
+    two = torch.zeros(2, 5, 128, dtype=torch.bfloat16)
+    for bad, heads in ((two.transpose(0, 1), 2), (wide[:, 16:272:2], 1), (two, 3), (wide[:5, :640].view(5, 5, 128).transpose(1, 0), 5)):
+        with pytest.raises(ValueError):
+            place(bad, heads)
