@@ -425,8 +425,8 @@ int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t elem, void 
  * instructions.  workspace: skd_kv_attend_workspace bytes for this kv, chunk and
  * heads (16-byte aligned; NULL where that is 0), nothing in it is kept from call
  * to call.  The same call gives the same bits.  Errors as skd_kv_append, and
- * SKD_ERR_SHAPE (heads), SKD_ERR_RANGE (scale not above 0; heads * head_dim of
- * 2^31 or more; 2^32 threads or more, of which 16, 32 or 128 queries of a row and kv
+ * SKD_ERR_SHAPE (heads), SKD_ERR_RANGE (scale not above 0, or above 2.3e38;
+ * heads * head_dim of 2^31 or more; 2^32 threads or more, of which 16, 32 or 128 queries of a row and kv
  * head take 256 or 512), SKD_ERR_NOMEM (workspace_bytes). */
 int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, float scale, const void *q, int64_t q_stride,
                   const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,

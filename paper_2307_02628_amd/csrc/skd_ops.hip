@@ -161,7 +161,8 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
                              const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
                              void *workspace, int64_t workspace_bytes, void *hip_stream) {
   CHECK(check_attend(kv, ch, heads));
-  if (!(scale > 0.f) || !std::isfinite(scale)) return SKD_ERR_RANGE;
+  const float c = scale * 1.4426950408889634f;
+  if (!(scale > 0.f) || !std::isfinite(c)) return SKD_ERR_RANGE;
   KvAttend a{};
   a.kv = view(kv);
   a.tk = tokens(kv, ch);
@@ -177,7 +178,7 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
   if (!aligned(kv->pool) || !aligned4({kv->block_table, ch->first, ch->past})) return SKD_ERR_SHAPE;
   a.heads = heads;
   a.group = heads / kv->kv_heads;
-  a.c = scale * 1.4426950408889634f;
+  a.c = c;
   a.q = rows_of(q, q_stride);
   a.o = rows_of(out, out_stride);
   a.splits = kv_attend_splits(a.kv, a.tk, heads);

@@ -52,6 +52,15 @@ def test_columns_of_a_token():
             assert attend(**one, heads=heads, qs=heads * dh, os_=heads * dh) == skd.ERR_RANGE
 
 
+def test_scales_at_the_ends():
+    """Scores are scaled to units of log 2, which has to be finite: what passes is then refused for its workspace."""
+    few = dict(c=kv(max_pages=2000, rows=1), ch=chunk(max_past=100000))
+    for scale in (1e-45, 1e-38, 2.0 ** 126):
+        assert attend(**few, scale=scale) == skd.ERR_NULL
+    for scale in (2.5e38, 3.4e38):
+        assert attend(**few, scale=scale) == skd.ERR_RANGE
+
+
 @pytest.mark.parametrize("vocab,most", [(1000, 2 ** 22 - 1), (262144, 2 ** 20 - 1)])
 def test_rows_of_a_draw(vocab, most):
     lib, P = skd.lib(), 1 << 20
