@@ -383,10 +383,13 @@ typedef struct {
 /* The tokens of a call: those of row r are tokens first[r] .. first[r + 1] - 1 of
  * the call's arrays and have the positions past[r], past[r] + 1, ... of the row.
  * Rows may have none.  max_new and max_past are upper bounds of the counts and of
- * past[], known to the host: tokens of a row beyond max_new are left out, and
- * max_past only decides how the work is shared out.  Counts that do not fit into
- * [0, tokens) are cut; a row whose past is negative, or more than its pages
- * hold, is left out.  max_pages * page_tokens is below 2^30. */
+ * past[], known to the host: tokens of a row beyond max_new, or beyond max_pages *
+ * page_tokens of them, are left out, and max_past only decides how the work is shared
+ * out.  Counts that do not fit into [0, tokens) are cut; a row whose past is negative,
+ * or more than its pages hold, is left out.  max_pages * page_tokens is below 2^30.
+ * Work is shared out as if every row had max_new tokens: one row of hundreds among
+ * rows of one token each is better served by two calls, with block tables of the long
+ * rows and of the others. */
 typedef struct {
   int32_t tokens;             /* rows of the call's arrays */
   int32_t max_new, max_past;
@@ -420,14 +423,18 @@ int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t elem, void 
  * kv_heads.  k and v (both or neither): the new tokens' keys and values, filed by
  * this call as by skd_kv_append before they are attended to (as they are held, so
  * in 8 bits as rounded); NULL: the cache holds them already.  A query that sees
- * no position gets zeros.  Positions behind a row's last one may hold anything.
- * Sums and softmax are in fp32, weights are rounded to bf16 for the matrix
- * instructions.  workspace: skd_kv_attend_workspace bytes for this kv, chunk and
- * heads (16-byte aligned; NULL where that is 0), nothing in it is kept from call
- * to call.  The same call gives the same bits.  Errors as skd_kv_append, and
- * SKD_ERR_SHAPE (heads), SKD_ERR_RANGE (scale not above 0, or above 2.3e38;
- * heads * head_dim of 2^31 or more; 2^32 threads or more, of which 16, 32 or 128 queries of a row and kv
- * head take 256 or 512), SKD_ERR_NOMEM (workspace_bytes). */
+ * no position, or only such with a score of -infinity, gets zeros.  Positions behind
+ * a row's last one may hold anything.  Sums and softmax are in fp32, weights (relative
+ * to the largest score met so far, up to 2^8) are rounded to bf16 for the matrix
+ * instructions: by 2^-8 of a weight, and times an 8-bit exponent to no less than
+ * 2^-133.  The sum of weights times values has to fit fp32: it does for values up to
+ * 2^119 over the number of positions, larger ones may give infinity.
+ * workspace: skd_kv_attend_workspace bytes for this kv, chunk and heads (16-byte
+ * aligned; NULL where that is 0), nothing in it is kept from call to call.  The same
+ * call gives the same bits.  Errors as skd_kv_append, and SKD_ERR_SHAPE (heads),
+ * SKD_ERR_RANGE (scale not above 0, or above 2.3e38; heads * head_dim of 2^31 or more;
+ * 2^32 threads or more, of which 16, 32 or 128 queries of a row and kv head take 256
+ * or 512), SKD_ERR_NOMEM (workspace_bytes). */
 int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, float scale, const void *q, int64_t q_stride,
                   const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
                   void *workspace, int64_t workspace_bytes, void *hip_stream);
