@@ -182,3 +182,23 @@ def test_one_long_row_among_many(elem):
     cache.read(ch, ko, vo)
     for x, y in ((k, ko), (v, vo)):
         assert torch.equal(torch.from_numpy(R.as_held(x.cpu().double().numpy(), elem)), y.cpu().double())
+
+
+@pytest.mark.parametrize("new", [1, 20, 150])
+def test_scores_of_minus_infinity(new):
+    """Keys at -infinity of a query have no weight; a query that sees no others gets zeros."""
+    past, H, dh = [40, 100], 2, 64
+    c = Case(R.BF16, H, dh, 32, past, [new, new], seed=36)
+    q = torch.randn(2 * new, 4, dh, generator=torch.Generator().manual_seed(37)).bfloat16()
+    q[..., 0] = 1.0
+    q = q.cuda()
+    c.k[0][:, :, 0] = -math.inf                                       # row 0: all of them
+    c.k[1][::3, :, 0] = -math.inf
+    c.append([0, 0], past)
+    for files in (True, False):
+        out = c.attend(q, files=files)
+        assert (out[:new] == 0).all()
+        for i in sorted({0, new // 2, new - 1}):
+            at = torch.tensor([p for p in range(past[1] + i + 1) if p % 3])
+            ref, bound = R.attention(q[new + i].cpu().double()[None], c.k[1][at].double(), c.v[1][at].double(), len(at) - 1, 1 / math.sqrt(dh))
+            assert ((out[new + i].double() - ref[0]).abs() <= bound[0]).all(), i
