@@ -132,7 +132,7 @@ struct skd_state {
   int32_t *argmax_dev = nullptr;   // [B]
   float *u_dev = nullptr;          // [B] uniform numbers of the sampling head
   SampleScratch sample{};          // its candidates
-  SampleBins *sample_bins = nullptr;
+  SampleBins *sample_bins = nullptr;  // of skd_logits_sample_rows, which may be captured: allocated with the state (128 rows of 50272: 20 MB)
   float *sampling_dev = nullptr;   // fp32 path with host buffers: [u | temperature | top-p | min-p | top-k][B]
   float *x = nullptr;              // residual stream fp32 [B_pad][d]
   float *x2 = nullptr;             // its second buffer (fuse_ln)
@@ -165,7 +165,7 @@ struct skd_state {
   bf16_t *pf_a = nullptr, *pf_q = nullptr, *pf_o = nullptr, *pf_u = nullptr;
   CacheTile *pf_tiles = nullptr;  // cache place of each 16-row tile of the prompt pass
   int32_t *pf_seq = nullptr, *pf_first = nullptr;  // row map of the prompt pass (sequence of each row, first row of each sequence)
-  // several columns at once (allocated by the first skd_decode_chunk, or by the first prompt of a state with 8-bit pages)
+  // several columns at once (allocated by the first skd_decode_chunk)
   int ck_cols = 0;                 // columns at a time
   float *ck_x = nullptr, *ck_partial = nullptr, *ck_attn = nullptr;
   bf16_t *ck_a = nullptr, *ck_qkv = nullptr, *ck_o = nullptr, *ck_u = nullptr;
@@ -1120,10 +1120,6 @@ RowsGemm plan_rows(int N, int K, int rows, bool split_ok) {
   return best;  // CHUNKS when no tile divides N
 }
 
-// Whole prompt at once, layer by layer (Section 2.3: the prompt needs no generation, so it can be batched over
-// positions): activation rows are the real (sequence, position) pairs (left padding gets no rows), attention is
-// causal over the pages the QKV projection has just filled.  A row depends on rows of its own sequence before it
-// only, so what padding rows hold never matters.
 // Projection of `rows` rows (whole 16-row tiles, or a decode kernel's batch) as its plan says; rows_pad: of the partial sums.
 static int rows_gemm(hipStream_t s, GemmArgs g, int epi, const RowsGemm &p, int rows, int rows_pad) {
   g.split = p.split;
@@ -1162,6 +1158,10 @@ static int rows_qkv(skd_state *st, GemmArgs g, int rows, int rows_pad, bf16_t *o
   return SKD_OK;
 }
 
+// Whole prompt at once, layer by layer (Section 2.3: the prompt needs no generation, so it can be batched over
+// positions): activation rows are the real (sequence, position) pairs (left padding gets no rows), attention is
+// causal over the pages the QKV projection has just filled.  A row depends on rows of its own sequence before it
+// only, so what padding rows hold never matters.
 static int prefill_batched(skd_state *st, const int32_t *cols) {
   const skd_config &c = st->cfg;
   const int B = c.batch, P = c.prompt_size, d = c.d_model, f = c.ffn, L = c.L;
@@ -1216,18 +1216,10 @@ static int prefill_batched(skd_state *st, const int32_t *cols) {
   auto stride = [&](const RowsGemm &p) { return p.kind == RowsGemm::SKINNY ? p.B_pad : rows_pad; };  // of the partial sums
   auto proj = [&](GemmArgs g, int epi, const RowsGemm &p) {
     if (p.partial) epi = EPI_PARTIAL;
+    if (p.kind != RowsGemm::SKINNY) return rows_gemm(s, g, epi, p, rows, rows_pad);
     g.split = p.split;
-    g.B_pad = stride(p);
-    g.rows = rows;
-    if (p.kind == RowsGemm::TILE) return bf16_gemm_tile(s, g, epi);
-    if (p.kind == RowsGemm::MID) return bf16_gemm_mid(s, g, epi, p.wr, p.ar);
-    if (p.kind == RowsGemm::SKINNY) {
-      g.rows = p.B_pad;
-      return bf16_gemm(s, g, epi, p.R, 1, 8);
-    }
-    g.B_pad = 128;  // 128-row chunks through the skinny kernel
-    g.rows = (rows + 127) / 128 * 128;
-    return bf16_gemm(s, g, epi, g.N % 64 ? 1 : 4, 1, 4);
+    g.B_pad = g.rows = p.B_pad;  // (rows of a prompt, with places in the cache of their own, not of a decode column)
+    return bf16_gemm(s, g, epi, p.R, 1, 8);
   };
   // What leaves the prompt pass is the cache of every layer and the hidden state of each sequence's last position, so
   // of the top layer's rows only the last positions are needed beyond their keys and values: its q | k | v projection
