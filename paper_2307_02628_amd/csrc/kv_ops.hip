@@ -868,7 +868,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 // converts what it reads).  Blocks that all queries see whole are taken two at a time with one branch for all weights, the values
 // requested before it.  80 KB of stages and up to 256 registers: two workgroups a CU.  Three (168 registers, three stages, a
 // block at a time, fragments requested as they are needed): us, 8 rows of 512 new tokens behind 2048, 32 heads of 128, bf16
-// 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 340.  Bound by the vector units (softmax;
+// 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 339.  Bound by the vector units (softmax;
 // conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.
 constexpr int rows_stages(int dh, bool fp8) { return fp8 ? 8 : dh == 128 ? 5 : 6; }  // (64: three workgroups, 97 -> 77 us for 32 prompts of 512)
 constexpr size_t rows_lds(int dh, bool fp8) { return (size_t)rows_stages(dh, fp8) * (32 * dh * (fp8 ? 2 : 4) + (fp8 ? 256 : 0)); }
@@ -1340,9 +1340,10 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads) {
     while (p.splits < 64 && wgs * p.splits <= 384 && blocks / (2 * p.splits) >= least()) p.splits *= 2;  // (456: the same either way)
   } else {
     // 8 waves a CU, and 16 from 1024 workgroups on, which are narrower then.  (Shares up to 16 waves a CU against this, us: 8 rows of
-    // 2000, 32 heads of 128, bf16 44.5, 40.5, 8 bits 26.5, 22.6; one of 32766, 8 kv heads, 8 bits 18.5, 17.4; up to 4: 20.5.)
-    // Joining takes 5 us: two tiles that are on half of the CUs already are shared out only if every wave keeps six blocks
-    // (4 rows of 1000 with 20 new tokens, 32 heads: 22.3, 18.7; 16 of 2000 with 5, 8 kv heads: 31.5, 30.3).
+    // 2000, 32 heads of 128, bf16 45.7, 42.1, 8 bits 28.3, 24.6; one of 32766, 8 kv heads, 8 bits 20.4, 19.6; up to 4: 21.1.)
+    // Two tiles that are on half of the CUs already are shared out only if every wave keeps six blocks (shared out all the same, and
+    // not, us: 4 rows of 1000 with 20 new tokens, 32 heads 23.3, 20.0; 16 of 2000 with 5, 32 queries' and 8 kv heads 31.7, 31.1; 24 of
+    // 3000 with 6 64.9, 50.9; 16 of 500 with 5 17.7, 14.1; against it 16 of 1000 to 2000 with 5, 27.0, 28.5).
     p.waves = p.nq == 16 && wgs >= 1024 ? 4 : 8;
     const int least = p.waves * (p.nq == 32 && wgs >= 128 ? 6 : 1);
     while (p.splits < 64 && wgs * p.waves * p.splits < 2048 && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
