@@ -367,8 +367,19 @@ int skd_profile_read(skd_state *st, double *ms, int64_t *launches);
  * codes are rounded to nearest even (those of exponent 120 end at 240, so that
  * what is finite stays so).  A position and head whose values held an
  * infinity or NaN has byte 255, codes 0, and reads as NaN.
- * The bf16 pages of a state have the same layout. */
-enum { SKD_KV_BF16 = 0, SKD_KV_FP8 = 1 }; /* skd_kv.elem */
+ * The bf16 pages of a state have the same layout.
+ * SKD_KV_FP4 pages hold 4 bits a value (8.5 bits a position and element of keys and values together, 17 / 32 of
+ * SKD_KV_FP8's, 17 / 64 of bf16): e2m1 codes (bits s e e m: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two in a
+ * byte, and for every 32 neighbouring elements of a position one byte that stands for 2^(byte - 127).  The exponent is the smallest
+ * from -124 on with which none of the 32 magnitudes exceeds 6 * 2^exponent; codes are rounded to nearest even (those
+ * of exponent 126 end at 3, so that what is finite stays so).  32 elements among which was an infinity or NaN have byte
+ * 255, codes 0, and read as NaN.  In bytes, per kv head (of page_tokens / 32 * 34 * head_dim) and block of 32 positions
+ * (of 34 * head_dim), with G = head_dim / 32; position 16 x + 4 j + y or 16 half + p:
+ *   keys   [half * G + c over 4][4][16 positions][half * G + c modulo 4][4]: element 32 c + 8 j + 2 i and the one
+ *          behind it (in the upper 4 bits) at [..][j][p][..][i]
+ *   values [G / 2][4][16][2][2][4]: elements 32 (2 i + w) + e and (upper 4 bits) + e + 16 at [i][j][e][w][x][y]
+ *   bytes of the keys' exponents [16 positions][half][G], of the values' [4][G][2][4] at [j][i][x][y] */
+enum { SKD_KV_BF16 = 0, SKD_KV_FP8 = 1, SKD_KV_FP4 = 4 }; /* skd_kv.elem */
 typedef struct {
   int32_t elem;
   int32_t kv_heads, head_dim; /* head_dim 64 or 128 */
@@ -439,6 +450,62 @@ int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, fl
                   const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
                   void *workspace, int64_t workspace_bytes, void *hip_stream);
 int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads);
+
+/* What becomes of the scores of an attention, and which positions a token sees. */
+typedef struct {
+  float cap;            /* scores s = scale * q . k become cap * tanh(s / cap), cap from 2^-20 to 1024; 0: they stay */
+  const float *slopes;  /* [heads]: slopes[h] * |p - j| is then taken from the score of position j at position p; NULL: nothing */
+  int32_t window;       /* a token at position p sees none before p - window + 1; 0: no such bound */
+  const int32_t *begin; /* [tokens]: nor any before begin[token] (its document's first position); NULL: from 0 on */
+  const int32_t *end;   /* [tokens]: it sees positions up to end[token] - 1, which may lie behind its own (a prefix that sees
+                           itself in both directions); NULL: up to its own */
+} skd_kv_scores;
+
+/* skd_kv_attend with changed scores and masks (`scores`, device arrays in it; finite slopes).  Positions seen are cut to those
+ * that the row has once the call's tokens are filed, so tokens of one call see each other in both directions where `end`
+ * says so; a token that sees none gets zeros.  What positions that a token does not see hold, also infinities and NaN,
+ * does not reach it.  A cap's function is off by up to 2^-11.4 of a weight (cap 1024; in proportion to it), a distance above
+ * 2^24 by 2^-24 of itself.  Work, memory, workspace (skd_kv_attend_scores_workspace bytes for these arguments) and
+ * errors as skd_kv_attend, and SKD_ERR_NULL (scores), SKD_ERR_RANGE (cap, also where 3 * scale / cap is no finite
+ * number; window < 0; memory that is not the current device's), SKD_ERR_SHAPE (arrays that are not aligned to their elements). */
+int skd_kv_attend_scores(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, float scale, const skd_kv_scores *scores,
+                         const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                         void *out, int64_t out_stride, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t skd_kv_attend_scores_workspace(const skd_kv *kv, const skd_kv_chunk *chunk, int32_t heads, const skd_kv_scores *scores);
+
+/* The next block table of a batch: rows forked, put into another order, ended, cut and grown.  A page is free if
+ * no entry of a table names it; nothing else is kept.  Row r of table_out [rows][max_pages] goes on from row
+ * source[r] of kv->block_table (outside [0, rows): from none; NULL: every row from itself), which holds len[r] positions, with
+ * more[r] tokens to come (negative: 0; together cut to max_pages * page_tokens).  It has the pages of positions 0 ..
+ * len[r] + more[r] - 1, entries behind are -1, and so are entries before len[r] that were no page.  Entries that tokens
+ * to come go to are its own: one that has no page gets a free one, and so does one whose page other entries of table_out
+ * name too, unless tokens to come go to all of them and it is the first.  Where such a page holds positions below len[r],
+ * the pair (page, new page) is listed in copies [rows][2]: skd_kv_copy_pages, before anything is filed, on the pool of
+ * every cache that goes by this table.  Pages are dealt out from the lowest free one on, by row and position, copies are listed
+ * by row; (-1, -1) follows behind the last.  counts [3]: pages that table_out names; pages that were missing; copies.  If pages
+ * were missing nothing is dealt out: rows have the pages of positions below len[r] only, and no copies are listed.
+ * No pool is read or written (kv->pool may be NULL).  table_out may be kv->block_table if source is NULL.  All of it is
+ * device memory, stream and workspace (skd_kv_assign_workspace bytes) as for the calls above.  Errors: SKD_ERR_NULL;
+ * SKD_ERR_SHAPE (kv as for the calls above; arrays that are not aligned to their elements, workspace to 16 bytes);
+ * SKD_ERR_RANGE (rows * max_pages from 2^31 on; 2^24 rows, or rows and 1024s of pages, or more; table_out that overlaps the table
+ * otherwise; memory that is not the current device's); SKD_ERR_NOMEM (workspace_bytes); SKD_ERR_HIP. */
+int skd_kv_assign(const skd_kv *kv, const int32_t *source, const int32_t *len, const int32_t *more, int32_t *table_out,
+                  int32_t *copies, int32_t *counts, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t skd_kv_assign_workspace(const skd_kv *kv);
+
+/* Moves the pages that a block table names to the lowest places of the pool: with n of them, the k-th one at or
+ * behind place n goes to the k-th free place before it.  table_out [rows][max_pages] is the table with the new places (-1 for
+ * what is no page) and may be kv->block_table; copies [pages / 2][2] lists the moves in ascending order, then (-1, -1);
+ * counts [3]: n, 0, moves.  Pools are moved by skd_kv_copy_pages; memory, workspace and errors as skd_kv_assign. */
+int skd_kv_compact(const skd_kv *kv, int32_t *table_out, int32_t *copies, int32_t *counts, void *workspace, int64_t workspace_bytes,
+                   void *hip_stream);
+int64_t skd_kv_compact_workspace(const skd_kv *kv);
+
+/* Copies whole pages of the pool: page copies[i][0] to page copies[i][1] for i below `most` and, if number is not NULL, below
+ * *number (device memory).  A pair with an entry outside [0, pages), or twice the same, is passed over.  No page may be
+ * written and named in another pair too.  Nothing but elem, the shape, pages and pool is read of kv.  Errors: SKD_ERR_NULL,
+ * SKD_ERR_SHAPE, SKD_ERR_RANGE (most < 0; memory that is not the current device's), SKD_ERR_HIP. */
+int skd_kv_copy_pages(const skd_kv *kv, const int32_t *copies, int32_t most, const int32_t *number, void *hip_stream);
 
 /* One token per row of fp32 logits [rows][vocab] (stride: elements from row to
  * row).  With m_i = exp((z_i - max z) / temperature): kept are the tokens with

@@ -1,0 +1,1199 @@
+// Kernels of the attention over pages, and their launches, for one kind of page (EL) and with or without changed scores (SC).
+#pragma once
+#include "kv_device.h"
+
+namespace skd {
+
+// Which kernel and how many shares of the keys: by the most queries that a row and kv head has.
+struct AttendPlan {
+  int nq;       // queries of a workgroup: 16, 32 or 128
+  int waves;    // 16, 32
+  int splits;
+  long tiles;   // of a row and kv head
+  int pairs;    // places for a row and kv head
+};
+
+namespace {
+
+// ------------------------------------------------------------------ attention
+// A query tile is 16 of the R = new * group queries of a row and kv head, in the order (token, head of the group): the 16
+// columns of the matrix instructions.  The softmax works in units of log2 against a reference that is raised only by more
+// than 8 (weights up to 2^8), denominators come from the matrix cores (a row of ones) and are sums of the rounded weights.
+//
+// Query i of a row sees positions up to past + i.  In blocks that reach beyond what a tile's first query sees scores are masked by
+// selection.  Since 0 * infinity is not 0, that leaves values: beyond the row's last position they are cleared (a page may hold
+// anything there); an infinity or NaN that only later queries see makes sums that are not finite, and a wave that ends with such
+// sums forms them once more (sums_again), without such values, which are added for the queries that see them.  8-bit values are
+// finite, what is not is in their scales, which are selected with the weights.
+// The powers of two of 8-bit keys are an operand of the conversion to bf16, those of values multiply the weights: both exact.
+// Those of 4-bit keys and values are operands of the conversion (32 elements of a value have one each, so that the weights would
+// have to be multiplied for every 32); a value that is not finite is in them, and is added for the queries that see it.
+//
+// Scores that are capped, or fall with the distance, are changed in place into units of log2 (SC kernels); a cap's constant part
+// is the same for every position and left out.  A query of theirs sees positions low .. limit - 1 of its own.
+
+// bf16x8 of two words of codes, times the power of two whose exponent byte is `e` (255: NaN)
+__device__ inline bf16x8 widen(uint32_t a, uint32_t b, uint32_t e) {
+  const float scale = __uint_as_float(e << 23);
+  const bf16x2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true)};
+  return bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+}
+// fp32 of an exponent byte: byte 0, 2^-127, is a subnormal.  (Weights times such a factor are rounded to multiples of 2^-133, the
+// smallest bf16: a value of exponent 0 is off by 2^-134 * 448 = 2^-125 for each key, beside a sum of weights of at least 1.)
+__device__ inline float kv8_factor(uint32_t word, int i) {
+  const uint32_t e = word >> (8 * i) & 255u;
+  return __uint_as_float(e == 255 ? 0x7fc00000u : max(e << 23, 0x00400000u));
+}
+// bf16x8 of a word of eight 4-bit codes, times the power of two whose exponent byte is `e` (255: NaN)
+__device__ inline bf16x8 widen4(uint32_t w, uint32_t e) {
+  const float scale = __uint_as_float(e << 23);
+  const bf16x2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)};
+  return bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+}
+// The two value fragments of 32 elements: byte y of word x is the lane's key 4 x + y, its two codes are of elements 16 apart.
+__device__ inline void widen4_values(const uint32_t (&w)[2], const uint32_t (&e)[2], bf16x8 (&f)[2]) {
+  uint32_t x[8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    x[4 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float((e[i] & 255u) << 23), 0));
+    x[4 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float((e[i] >> 8 & 255u) << 23), 1));
+    x[4 * i + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float((e[i] >> 16 & 255u) << 23), 2));
+    x[4 * i + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float(e[i] >> 24 << 23), 3));
+  }
+  uint32x4 lo, hi;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100);
+    hi[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302);
+  }
+  f[0] = __builtin_bit_cast(bf16x8, lo);
+  f[1] = __builtin_bit_cast(bf16x8, hi);
+}
+// 16-byte pieces of a block that a lane takes: keys, values; bytes of a block's codes, and to the next block
+constexpr int key_pieces(int dh, int el) { return el == EL_BF16 ? dh / 16 : el == EL_FP8 ? dh / 32 : dh / 64; }
+constexpr int value_pieces(int dh, int el) { return key_pieces(dh, el); }
+constexpr int block_bytes(int dh, int el) { return el == EL_BF16 ? 128 * dh : el == EL_FP8 ? 64 * dh : 34 * dh; }
+// the key fragment of tile tl, elements 32 c .. + 31, of a lane's pieces; e: its exponents
+template <int DH, int EL>
+__device__ inline bf16x8 key_fragment(const uint32x4 *k, const uint32_t *e, int tl, int c) {
+  constexpr int QC = DH / 32;
+  if constexpr (EL == EL_FP4) {
+    const int f = tl * QC + c;
+    return widen4(k[f / 4][f % 4], e[f / 4] >> (8 * (f % 4)) & 255u);
+  } else if constexpr (EL == EL_FP8) {
+    const uint32x4 w = k[tl * (QC / 2) + c / 2];
+    return widen(w[c % 2 * 2], w[c % 2 * 2 + 1], e[tl]);
+  } else {
+    return __builtin_bit_cast(bf16x8, k[tl * QC + c]);
+  }
+}
+
+// ------------------------------------------------------------------ changed scores
+// In units of log2, from q . k.  cap tanh(x) = cap - 2 cap / (1 + exp(2 x)), here without the constant: off by up to 3 * 2^-24 of
+// 2 cap (exponential, sum, reciprocal), which for the largest cap, 1024, is 2^-11.4 of a weight, against the 2^-8 of its rounding.
+__device__ inline float change_one(const KvScoring &sc, bool capped, float s) {
+  return capped ? sc.out * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(sc.in * s)) : s * sc.out;
+}
+// away: of the query from the lane's first position.  (Distances are exact up to 2^24, and beyond to 2^-24.)
+__device__ inline void change(const KvScoring &sc, float slope, int away, floatx4 (&S)[2]) {
+  if (sc.capped) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = change_one(sc, true, S[j >> 2][j & 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = change_one(sc, false, S[j >> 2][j & 3]);
+  }
+  if (sc.slopes) {
+    const float d = (float)away;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = __builtin_fmaf(-slope, __builtin_fabsf(d - (float)(16 * (j >> 2) + (j & 3))), S[j >> 2][j & 3]);
+  }
+}
+
+__device__ inline bf16x8 pack8(const float (&p)[8]) {
+  return __builtin_bit_cast(bf16x8, (uint32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])}));
+}
+__device__ inline bf16x8 all_ones() {
+  bf16x8 x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (__bf16)1.0f;
+  return x;
+}
+// position (of a block) of element j of a lane's eight
+__device__ inline int block_pos(int j, int grp) { return 16 * (j >> 2) + 4 * grp + (j & 3); }
+
+template <bool LOW>
+__device__ inline bool hidden(int j, int low, int limit, int grp) {
+  const bool behind = block_pos(j, 0) >= limit - 4 * grp;
+  return LOW ? behind || block_pos(j, 0) < low - 4 * grp : behind;
+}
+
+// SHARES: a lane adds up the weights of its own positions (one_sum joins them) instead of the matrix cores all of them, which
+// takes 7 registers more: at 4 waves a SIMD they are not there.
+template <int DH, bool SHARES>
+struct QueryTile {
+  floatx4 O[DH / 16], L;  // O[m][i]: element 16 m + 4 (lane / 16) + i of the lane's query (lane % 16)
+  float m_ref;
+  __device__ void clear() {
+    m_ref = -3.0e38f;  // below every score: no weight has been taken
+    L = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < DH / 16; ++m) O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ void relative(const floatx4 (&S)[2], float c, float (&p)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_fmaf(S[j >> 2][j & 3], c, -m_ref);
+  }
+  __device__ static float most(const float (&x)[8]) {
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  }
+  __device__ void raise(float bm) {  // the reference to bm, this lane's largest score, if that is above it
+    bm = fmaxf(bm, __shfl_xor(bm, 16));  // lanes 16 and 32 apart hold the same query
+    bm = fmaxf(bm, __shfl_xor(bm, 32));
+    const float m_new = fmaxf(m_ref, bm), alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+    m_ref = m_new;
+    if constexpr (SHARES) L[0] *= alpha;
+    else L *= alpha;
+#pragma unroll
+    for (int m = 0; m < DH / 16; ++m) O[m] *= alpha;
+  }
+  // The weights of a block from its scores S[tl][i] (position 16 tl + 4 grp + i), rounded to bf16 for the products (by 2^-8 of
+  // a weight at most; the denominator adds the rounded ones).  masked: positions from `limit` of the block on have none, nor (LOW)
+  // those before `low`.
+  template <bool FP8, bool LOW>
+  __device__ bf16x8 weights(bool masked, floatx4 (&S)[2], float c, int low, int limit, int grp, const float (&vs)[8]) {
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (hidden<LOW>(j, low, limit, grp)) S[j >> 2][j & 3] = -INFINITY;
+    }
+    float p[8];
+    relative(S, c, p);
+    if (__any(most(p) > 8.0f)) {
+      const float x[8] = {S[0][0], S[0][1], S[0][2], S[0][3], S[1][0], S[1][1], S[1][2], S[1][3]};
+      raise(most(x) * c);
+      relative(S, c, p);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(p[j]);
+    bf16x8 pv = pack8(p);
+    if constexpr (SHARES) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) L[0] += (float)pv[j];
+    } else {
+      L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones(), pv, L, 0, 0, 0);
+    }
+    if constexpr (FP8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] *= vs[j];
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (hidden<LOW>(j, low, limit, grp)) p[j] = 0.f;  // (a power of two there may be NaN)
+      }
+      pv = pack8(p);
+    }
+    return pv;
+  }
+  __device__ void one_sum() {
+    if constexpr (SHARES) {
+      L[0] += __shfl_xor(L[0], 16);
+      L[0] += __shfl_xor(L[0], 32);
+    }
+  }
+};
+// 1 at positions from `low` to `limit` - 1
+template <bool LOW>
+__device__ inline bf16x8 visible(int low, int limit, int grp) {
+  bf16x8 v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (__bf16)(hidden<LOW>(j, low, limit, grp) ? 0.0f : 1.0f);
+  return v;
+}
+// 4-bit values whose exponents stand for no finite number, or for a page that nobody wrote: the words of a lane's exponents,
+// [group][2], are made harmless, and the sums of the queries that see a NaN become NaN.  Rare: out of the way of everything else.
+template <int DH, bool LOW, int NT, typename Tile>
+__device__ inline void odd_exponents(uint32_t (&e)[DH / 16], Tile (&tile)[NT], const int (&low)[NT], const int (&limit)[NT]) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < DH / 16; ++i) any |= ((e[i] & 0x7f7f7f7fu) + 0x02020202u) & e[i] & 0x80808080u;
+  if (__builtin_expect(!__any(any != 0), 1)) return;
+#pragma unroll
+  for (int i = 0; i < DH / 16; ++i) {
+    const uint32_t odd = ((e[i] & 0x7f7f7f7fu) + 0x02020202u) & e[i] & 0x80808080u;
+    if (!__any(odd != 0)) continue;
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {
+      const uint32_t w = (uint32_t)__shfl((int)e[i], 16 * g);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if ((w >> (8 * y) & 255u) == 255u && !hidden<LOW>(4 * (i & 1) + y, low[t], limit[t], g)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) tile[t].O[i / 2 * 2 + u] += __uint_as_float(0x7fc00000u);
+          }
+    }
+    e[i] &= ~((odd >> 7) * 0xffu);
+  }
+}
+// masks of a lane's eight bf16 values: positions below `valid`
+struct Keep {
+  uint32_t w[4];
+  __device__ Keep(int valid, int grp) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (block_pos(2 * i, grp) < valid ? 0xffffu : 0u) | (block_pos(2 * i + 1, grp) < valid ? 0xffff0000u : 0u);
+  }
+  __device__ void bf16(uint32x4 &v) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] &= w[i];
+  }
+  __device__ uint32_t codes(int half) const { return __builtin_amdgcn_perm(w[2 * half + 1], w[2 * half], 0x06040200); }
+};
+__device__ inline void drop_odd(uint32x4 &v) {  // infinities and NaNs to 0
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t odd = ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    v[i] &= ~((odd >> 15) * 0xffffu);
+  }
+}
+// Adds to the sums of a tile what the infinities and NaNs of a value fragment are for the queries that see them.
+__device__ inline void add_odd(floatx4 &O, const uint32x4 &v, bf16x8 vis) {
+  uint32x4 up, down;  // 1 where it is +infinity or NaN, -infinity or NaN
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t u = 0, d = 0;
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+      const uint32_t x = v[i] >> s & 0xffffu;
+      if ((x & 0x7f80u) == 0x7f80u) {
+        if (x != 0xff80u) u |= 0x3f80u << s;
+        if (x != 0x7f80u) d |= 0x3f80u << s;
+      }
+    }
+    up[i] = u;
+    down[i] = d;
+  }
+  const floatx4 z = floatx4{0.f, 0.f, 0.f, 0.f};
+  const floatx4 u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, up), vis, z, 0, 0, 0);
+  const floatx4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down), vis, z, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (u[i] > 0.f) O[i] += INFINITY;
+    if (d[i] > 0.f) O[i] -= INFINITY;
+  }
+}
+
+// What a workgroup computes: NQ queries from q0 on of a row and kv head, on one share of their keys.
+struct Share {
+  RowTokens t;
+  int r, h, R, q0;
+  int held;        // positions that the cache holds
+  int lo, hi;      // blocks
+  int whole_lo, whole_hi;  // those that every query sees whole
+  bool any;
+  // Workgroup: [tile, the longest first][row and kv head], `pairs` places for the latter.  Tiles of many queries: of 16 rows and
+  // heads of an XCD at a time, so that fewer pages pass through its L2 at once, and the next ones fill the gaps (all of them, 16,
+  // 1 at a time, us: 8 prompts of 2048, 32 heads of 128, bf16 428, 411, 440; 512 tokens behind 2048 203, 192, 194; 8 bits 386,
+  // 380, 440 and 196, 192, 206; 32 prompts of 512, heads of 64, 8 bits 88, 93, 122).
+  static constexpr int TOGETHER = 16;
+  template <int NQ, bool SC>
+  __device__ static Share of(const KvAttend &a, int pairs, bool files) {
+    Share s;
+    const int H = a.kv.g.H, tiles = gridDim.x / pairs, id = blockIdx.x;
+    int pair = id % pairs, tile = id / pairs;
+    if (NQ == 128 && pairs % 8 == 0) {
+      const int at = id / 8, g = at / (tiles * TOGETHER), in = at - g * tiles * TOGETHER, n = min(TOGETHER, pairs / 8 - g * TOGETHER);
+      pair = (g * TOGETHER + in % n) * 8 + id % 8;
+      tile = in / n;
+    }
+    const int ri = min(pair / H, a.kv.rows - 1);
+    s.h = pair % H;
+    s.r = a.order ? a.order[ri] : ri;
+    s.t = row_tokens(a.tk, s.r);
+    s.R = pair < H * a.kv.rows ? s.t.n * a.group : 0;
+    s.q0 = (tiles - 1 - tile) * NQ;
+    s.any = s.q0 < s.R;
+    s.held = s.t.past + (files ? 0 : s.t.n);
+    int first = 0, nblk;
+    if constexpr (SC) {
+      // what the queries see together and each of them, by every wave
+      int from = 1 << 30, upto = 0;
+      s.whole_lo = 0;
+      s.whole_hi = 1 << 30;
+      for (int q = s.q0 + (threadIdx.x & 63); q < min(s.q0 + NQ, s.R); q += 64) {
+        const Range x = s.range<true>(a, q);
+        if (x.lo < x.hi) from = min(from, x.lo);
+        upto = max(upto, x.hi);
+        s.whole_lo = max(s.whole_lo, x.lo < x.hi ? x.lo : 1 << 30);
+        s.whole_hi = min(s.whole_hi, x.hi);
+      }
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) {
+        from = min(from, __shfl_xor(from, o));
+        upto = max(upto, __shfl_xor(upto, o));
+        s.whole_lo = max(s.whole_lo, __shfl_xor(s.whole_lo, o));
+        s.whole_hi = min(s.whole_hi, __shfl_xor(s.whole_hi, o));
+      }
+      auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+      nblk = one((min(upto, s.held) + 31) >> 5);
+      first = min(one(from >> 5), nblk);
+      s.whole_lo = one((s.whole_lo + 31) >> 5);
+      s.whole_hi = one(min(s.whole_hi, s.held) >> 5);
+    } else {
+      nblk = (min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held) + 31) >> 5;
+      s.whole_lo = 0;
+      s.whole_hi = min(s.seen(a, s.q0), s.held) >> 5;
+    }
+    const int per = (nblk - first + a.splits - 1) / a.splits;
+    s.lo = first + (int)blockIdx.y * per;
+    s.hi = min(s.lo + per, nblk);
+    return s;
+  }
+  struct Range {
+    int lo, hi;
+  };
+  // Positions lo .. hi - 1 of those that the row has are seen by query q (lo = hi = 0: none).
+  template <bool SC>
+  __device__ Range range(const KvAttend &a, int q) const {
+    if constexpr (!SC) return Range{0, seen(a, q)};
+    const int p = t.past + q / a.group;
+    const long at = token(a, q);
+    Range x{a.sc.begin ? max(a.sc.begin[at], 0) : 0, min(a.sc.end ? a.sc.end[at] : p + 1, t.past + t.n)};
+    if (a.sc.window) x.lo = max(x.lo, p + 1 - a.sc.window);
+    return x.lo < x.hi ? x : Range{0, 0};
+  }
+  // slope of query q, in units of log2
+  __device__ float slope(const KvAttend &a, int q) const { return a.sc.slopes ? a.sc.slopes[head(a, q)] * 1.4426950408889634f : 0.f; }
+  __device__ int seen(const KvAttend &a, int q) const { return t.past + q / a.group + 1; }  // positions that query q sees
+  __device__ long token(const KvAttend &a, int q) const { return t.at + (long)(q / a.group) * a.tk.step; }
+  __device__ int head(const KvAttend &a, int q) const { return h * a.group + q % a.group; }
+};
+// What a lane needs to know of a query: it sees positions low .. limit - 1 of those that the cache holds.
+struct Seen {
+  int low, limit, pos;
+  float slope;
+  template <bool SC>
+  __device__ static Seen of(const KvAttend &a, const Share &s, int q) {
+    if (q >= s.R) return Seen{0, 0, 0, 0.f};
+    const Share::Range x = s.range<SC>(a, q);
+    return Seen{x.lo, min(x.hi, s.held), s.t.past + q / a.group, SC ? s.slope(a, q) : 0.f};
+  }
+};
+template <int DH>
+__device__ inline float *part_of(const KvAttend &a, int split, long token, int head) {
+  return a.part + (((long)split * a.tk.tokens + token) * a.heads + head) * (DH + 2);
+}
+template <int DH>
+__device__ inline void load_queries(const KvAttend &a, const Share &s, int q, int grp, bf16x8 (&qf)[DH / 32]) {
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) {
+    qf[c] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    if (q < s.R) qf[c] = *(const bf16x8 *)((const bf16_t *)a.q.p + row_index(a.q, s.token(a, q), s.head(a, q) * DH + 32 * c + 8 * grp));
+  }
+}
+
+// Whether a wave's sums hold an infinity or NaN.
+template <int DH, int NT, typename Tile>
+__device__ inline bool not_finite_(const Tile (&tile)[NT]) {
+  float x = 0.f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int m = 0; m < DH / 16; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x = __builtin_fmaf(tile[t].O[m][i], 0.f, x);
+  return __any(x != x);
+}
+template <int DH, typename Tile, int NT>
+__device__ inline bool not_finite(const Tile (&tile)[NT]) { return not_finite_<DH, NT, Tile>(tile); }
+// The numerators of a wave's tiles again, over blocks first, first + step, ... below end of bf16 pages, against the references
+// that the wave has arrived at: values without their infinities and NaNs, which are then added.
+template <int DH, bool SC, typename Tile, int NT>
+__device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, int q0, int first, int step, int end, Tile (&tile)[NT]) {
+  constexpr int QC = DH / 32, VM = DH / 16;
+  const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15, bpp = a.kv.g.page_tokens >> 5;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int m = 0; m < VM; ++m) tile[t].O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int blk = first; blk < end; blk += step) {
+    const int page = page_of(a.kv, s.r, blk);
+    if (page < 0) continue;
+    const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)s.h * bpp + blk % bpp) * (128 * DH)) + lane;
+    const Keep keep(s.held - blk * 32, grp);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      bf16x8 qf[QC];
+      load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf);
+      const Seen x = Seen::of<SC>(a, s, q0 + 16 * t + col);
+      const int lim = x.limit - blk * 32, lo = x.low - blk * 32;
+      floatx4 S[2];
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
+        S[tl] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < QC; ++c) S[tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, src[(tl * QC + c) * 64]), qf[c], S[tl], 0, 0, 0);
+      }
+      if constexpr (SC) change(a.sc, x.slope, x.pos - blk * 32 - 4 * grp, S);
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        p[j] = hidden<SC>(j, lo, lim, grp) ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], SC ? 1.0f : a.c, -tile[t].m_ref));
+      const bf16x8 pv = pack8(p), vis = visible<SC>(lo, lim, grp);
+#pragma unroll
+      for (int m = 0; m < VM; ++m) {
+        uint32x4 v = src[4 * DH + m * 64], w;
+        keep.bf16(v);
+        w = v;
+        drop_odd(w);
+        tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pv, tile[t].O[m], 0, 0, 0);
+        add_odd(tile[t].O[m], v, vis);
+        __builtin_amdgcn_sched_barrier(0);  // (one fragment after the other: side by side they take more registers than there are)
+      }
+    }
+  }
+}
+
+// Few queries (one or two tiles): a workgroup is NW waves on NT tiles, and a wave takes every NW-th 32-key block, straight from
+// the page into the operand registers, with a softmax of its own; the waves' states are joined in LDS, the shares of several
+// workgroups by k_kv_merge.  Bound by the bytes of the pages.
+template <int DH, int EL>
+struct KvBlock {
+  uint32x4 k[key_pieces(DH, EL)], v[value_pieces(DH, EL)];
+  uint32_t ke[2], ve[EL == EL_FP4 ? DH / 16 : 2];  // exponents: of key 16 tl + (lane & 15) (K), of keys 16 tl + 4 (lane >> 4) .. + 3 (V)
+};
+template <int DH, int EL, bool SC, int NT, int NW>
+__global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int pairs) {
+  constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
+  constexpr int QC = DH / 32, VM = DH / 16, NQ = 16 * NT;
+  // One tile of 128-wide heads keeps its queries in LDS: with them in registers the loop did not fit the 128 of 4 waves a SIMD.
+  constexpr bool LDS_Q = NT == 1 && DH == 128;
+  __shared__ bf16x8 sh_q[LDS_Q ? QC * 64 : 1];
+  // (and what else is known of a query, if scores are changed)
+  __shared__ Seen sh_seen[SC && LDS_Q ? 16 : 1];
+  __shared__ __align__(16) bf16_t sh_k[DH], sh_v[DH];  // the new token
+  extern __shared__ float lds[];                       // [NW][cols][DH + 2]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
+  const bool files = NT == 1 && a.k.p != nullptr;  // (t.n is 1: the token is not in the cache yet)
+  const Share s = Share::of<NQ, SC>(a, pairs, files);
+  if (!s.any) return;
+  const int q0 = s.q0, R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
+  // The page that takes the new token, known to the wave that attends to it: without one it is dropped, and nobody sees it.
+  const int new_page = files && blockIdx.y == gridDim.y - 1 && wave == NW - 1 ? page_of(a.kv, s.r, s.held >> 5) : -1;
+  const bool fresh = new_page >= 0;
+  if constexpr (NT == 1) {
+    constexpr int LPT = DH / 8;
+    if (fresh && lane < 2 * LPT) {
+      const KvRows &x = lane < LPT ? a.k : a.v;
+      const int e = lane % LPT * 8;
+      *(uint32x4 *)&(lane < LPT ? sh_k : sh_v)[e] = *(const uint32x4 *)((const bf16_t *)x.p + row_index(x, s.t.at, h * DH + e));
+    }
+  }
+  bf16x8 qf[NT][QC];
+  Seen seen[NT];                  // of the lane's queries, positions of the cache
+  QueryTile<DH, NT == 1> tile[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int q = q0 + 16 * t + col;
+    load_queries<DH>(a, s, q, grp, qf[t]);
+    seen[t] = Seen::of<SC>(a, s, q);
+    tile[t].clear();
+  }
+  if constexpr (LDS_Q) {
+    if (wave == 0) {
+#pragma unroll
+      for (int c = 0; c < QC; ++c) sh_q[c * 64 + lane] = qf[0][c];
+      if (SC && grp == 0) sh_seen[col] = seen[0];
+    }
+    __syncthreads();
+  }
+  typedef KvBlock<DH, EL> Block;
+  auto load = [&](int page, int ib, Block &b) {
+    const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
+    const long at = (long)h * bpp + ib;
+    const uint32x4 *src = (const uint32x4 *)(pg + at * block_bytes(DH, EL)) + lane;
+    constexpr int KF = key_pieces(DH, EL), VF = value_pieces(DH, EL);
+#pragma unroll
+    for (int i = 0; i < KF; ++i) b.k[i] = __builtin_nontemporal_load(&src[i * 64]);
+#pragma unroll
+    for (int i = 0; i < VF; ++i) b.v[i] = __builtin_nontemporal_load(&src[(KF + i) * 64]);
+    if constexpr (FP8) {
+      const unsigned char *ex = pg + (long)H * bpp * (64 * DH) + at * 64;
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
+        b.ke[tl] = ex[16 * tl + col];
+        b.ve[tl] = ((const uint32_t *)ex)[8 + 4 * tl + grp];
+      }
+    }
+    if constexpr (FP4) {
+      const unsigned char *ex = pg + at * block_bytes(DH, EL) + 32 * DH;
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) b.ke[i] = ((const uint32_t *)(ex + col * (DH / 16)))[i];
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) *(uint32x4 *)&b.ve[4 * i] = ((const uint32x4 *)(ex + DH + grp * (DH / 4)))[i];
+    }
+  };
+  auto seen_of = [&](int t) {
+    if constexpr (!SC || !LDS_Q) return seen[t];
+    asm volatile("" ::: "memory");  // (read where it is needed, not kept)
+    return sh_seen[col];
+  };
+  // base: first position of the block; valid: positions that the row has
+  auto use = [&](auto masked_, int base, Block &b, int valid) {
+    constexpr bool masked = decltype(masked_)::value;
+    floatx4 S[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < QC; ++c) {
+      bf16x8 x[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) x[t] = LDS_Q ? sh_q[c * 64 + lane] : qf[t][c];
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
+        const bf16x8 kf = key_fragment<DH, EL>(b.k, b.ke, tl, c);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, x[t], S[t][tl], 0, 0, 0);
+      }
+    }
+    float vs[8];
+    if constexpr (FP8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vs[j] = kv8_factor(b.ve[j >> 2], j & 3);
+    }
+    bf16x8 pv[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const Seen x = seen_of(t);
+      if constexpr (SC) change(a.sc, x.slope, x.pos - base - 4 * grp, S[t]);
+      pv[t] = tile[t].template weights<FP8, SC>(masked, S[t], SC ? 1.0f : a.c, SC ? x.low - base : 0, x.limit - base, grp, vs);
+    }
+    if constexpr (FP4) {
+      if (masked) {
+        int from[NT], to[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const Seen x = seen_of(t);
+          from[t] = x.low - base;
+          to[t] = x.limit - base;
+        }
+        odd_exponents<DH, SC, NT>(b.ve, tile, from, to);
+      }
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) {
+        bf16x8 vf[2];
+        widen4_values({b.v[i / 2][i % 2 * 2], b.v[i / 2][i % 2 * 2 + 1]}, {b.ve[2 * i], b.ve[2 * i + 1]}, vf);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) tile[t].O[2 * i + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[u], pv[t], tile[t].O[2 * i + u], 0, 0, 0);
+      }
+      return;
+    }
+    if (masked) {
+      const Keep keep(valid - base, grp);
+      if constexpr (FP8) {  // (codes of positions that the row does not have may be NaN)
+#pragma unroll
+        for (int m = 0; m < VM / 2; ++m) b.v[m] &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
+      } else if constexpr (EL == EL_BF16) {
+#pragma unroll
+        for (int m = 0; m < VM; ++m) keep.bf16(b.v[m]);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < (FP4 ? 0 : VM); ++m) {
+      bf16x8 vf{};
+      if constexpr (FP8) {
+        vf = widen(b.v[m / 2][m % 2 * 2], b.v[m / 2][m % 2 * 2 + 1], 127);
+      } else {
+        vf = __builtin_bit_cast(bf16x8, b.v[m]);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv[t], tile[t].O[m], 0, 0, 0);
+    }
+  };
+  // place of the wave's next block, whose page's number is asked for ahead of the use of the one before
+  const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
+  int blk = s.lo + wave, ip = blk / bpp, ib = blk % bpp;
+  auto entry = [&]() { return table[min(ip, a.kv.g.max_pages - 1)]; };
+  int number = entry();
+  auto step = [&](auto masked_) {
+    const bool is = number >= 0 && number < a.kv.pages && ip < a.kv.g.max_pages;
+    Block b;
+    if (is) load(number, ib, b);
+    ip += NW / bpp;
+    ib += NW % bpp;
+    if (ib >= bpp) {
+      ib -= bpp;
+      ++ip;
+    }
+    number = entry();
+    if (is) use(masked_, blk * 32, b, s.held);
+    blk += NW;
+  };
+  if constexpr (SC) {
+    while (blk < min(s.whole_lo, s.hi)) step(std::true_type());
+  }
+  while (blk < min(s.whole_hi, s.hi)) step(std::false_type());
+  while (blk < s.hi) step(std::true_type());
+  if constexpr (EL == EL_BF16) {
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, s.lo + wave, NW, s.hi, tile);
+  }
+  uint32_t ke = 0, ve = 0;  // exponents of the new token
+  if constexpr (NT == 1) {
+    tile[0].one_sum();
+    // The one new token joins the last wave's state: its key as key 0 of a tile, its value by the vector units, four elements of
+    // every 16 in a lane.
+    if (fresh) {
+      if constexpr (FP8) {
+        uint32_t km = 0, vm = 0;
+#pragma unroll
+        for (int i = 0; i < DH / 64; ++i) {
+          km = max(km, (uint32_t)(sh_k[lane + 64 * i] & 0x7fff) << 16);
+          vm = max(vm, (uint32_t)(sh_v[lane + 64 * i] & 0x7fff) << 16);
+        }
+        ke = kv8_exponent(max_over<64>(km));
+        ve = kv8_exponent(max_over<64>(vm));
+      }
+      floatx4 S = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < QC; ++c) {
+        uint32x4 kx = uint32x4{0, 0, 0, 0};
+        if (col == 0) kx = *(const uint32x4 *)&sh_k[32 * c + 8 * grp];
+        bf16x8 kf = __builtin_bit_cast(bf16x8, kx);
+        if constexpr (FP8) {
+          const uint2 w = kv8_codes(kx, ke);
+          kf = widen(w.x, w.y, ke);
+        }
+        if constexpr (FP4) {
+          const uint32_t e = kv4_exponent(max_over_quarters(max_bits(kx)));
+          kf = widen4(kv4_codes(kx, e), e);
+        }
+        S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, LDS_Q ? sh_q[c * 64 + lane] : qf[0][c], S, 0, 0, 0);
+      }
+      auto &x = tile[0];
+      float score = __shfl(S[0], col);
+      if constexpr (SC) {  // (at a distance of 0)
+        const Share::Range sees = q0 + col < R ? s.range<true>(a, q0 + col) : Share::Range{0, 0};
+        score = change_one(a.sc, a.sc.capped, score);
+        if (!(sees.lo <= s.held && s.held < sees.hi)) score = -INFINITY;
+      } else {
+        score *= a.c;
+      }
+      const float m_new = fmaxf(x.m_ref, score);
+      const float alpha = __builtin_amdgcn_exp2f(x.m_ref - m_new), p = __builtin_amdgcn_exp2f(score - m_new);
+      x.m_ref = m_new;
+      x.L[0] = x.L[0] * alpha + p;
+      uint32_t e4[DH / 32];
+      if constexpr (FP4) {
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) {
+          const uint2 lo = *(const uint2 *)&sh_v[32 * i + 4 * grp], hi = *(const uint2 *)&sh_v[32 * i + 16 + 4 * grp];
+          e4[i] = kv4_exponent(max_over_quarters(max_bits(uint32x4{lo.x, lo.y, hi.x, hi.y})));
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < VM; ++m) {
+        const uint2 vx = *(const uint2 *)&sh_v[16 * m + 4 * grp];
+        float v[4] = {bf2f(vx.x & 0xffffu), bf2f(vx.x >> 16), bf2f(vx.y & 0xffffu), bf2f(vx.y >> 16)};
+        if constexpr (FP8) {
+          const uint32_t w = ve == 255 ? 0u : kv8_pack(v[0], v[1], v[2], v[3], ve);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = kv8_value(w, i, kv8_scale(ve));
+        }
+        if constexpr (FP4) {
+          const uint32_t e = e4[m / 2], w = e == 255 ? 0u : kv4_pair<1>(kv4_pair<0>(0, v[0], v[1], e), v[2], v[3], e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = kv4_values(w >> (4 * (i & 2)) & 255u, e)[i & 1];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (SC) {
+            if (p == 0.f) v[i] = 0.f;  // (nobody sees it, or its weight is nothing beside the others': no 0 x infinity)
+          }
+          x.O[m][i] = x.O[m][i] * alpha + p * v[i];
+        }
+      }
+    }
+  }
+  // the waves' states, a tile at a time
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int first = q0 + 16 * t, cols = min(16, R - first);
+    if (cols <= 0) break;
+    if (t) __syncthreads();
+    if (col < cols) {
+      float *mine = lds + ((long)wave * cols + col) * (DH + 2);
+#pragma unroll
+      for (int m = 0; m < VM; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[16 * m + 4 * grp + i] = tile[t].O[m][i];
+      if (grp == 0) {
+        mine[DH] = tile[t].m_ref;
+        mine[DH + 1] = tile[t].L[0];
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < cols * DH; i += NW * 64) {
+      const int e = i % DH, cq = i / DH;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) M = fmaxf(M, lds[((long)w * cols + cq) * (DH + 2) + DH]);
+      float num = 0.f, den = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float *x = lds + ((long)w * cols + cq) * (DH + 2);
+        const float f = __builtin_amdgcn_exp2f(x[DH] - M);
+        num += f * x[e];
+        den += f * x[DH + 1];
+      }
+      const int q = first + cq, head = s.head(a, q);
+      const long token = s.token(a, q);
+      if (a.splits == 1) {
+        ((bf16_t *)a.o.p)[row_index(a.o, token, head * DH + e)] = (bf16_t)f2bf(den == 0.f ? 0.f : num / den);
+      } else {
+        float *pp = part_of<DH>(a, blockIdx.y, token, head);
+        pp[e] = num;
+        if (e == 0) {
+          pp[DH] = M;
+          pp[DH + 1] = den;
+        }
+      }
+    }
+  }
+  if constexpr (NT == 1) {
+    // The first tile files the new token.  Whoever reads its place meanwhile, in the block around it, discards what is there.
+    // (Last of all: a barrier behind the stores would wait for them, 4 us of a step of 32 rows.)
+    if (fresh && q0 == 0) {
+      const int slot = s.held % a.kv.g.page_tokens;
+      unsigned char *pg = a.kv.pool + (long)new_page * a.kv.page_bytes;
+      if (lane < DH / 8) {
+        const uint32x4 kx = *(const uint32x4 *)&sh_k[8 * lane];
+        if constexpr (FP8) *(uint2 *)(pg + kv8_k_off(h, slot, 8 * lane, a.kv.g)) = kv8_codes(kx, ke);
+        else if constexpr (FP4) {
+          const uint32_t e = kv4_exponent(max_over<4>(max_bits(kx)));
+          *(uint32_t *)(pg + kv4_k_off(h, slot, 8 * lane, a.kv.g)) = kv4_codes(kx, e);
+          if (lane % 4 == 0) pg[kv4_k_exp_off(h, slot, lane / 4, a.kv.g)] = (unsigned char)e;
+        } else *(uint32x4 *)((bf16_t *)pg + kv_k_off(h, slot, 8 * lane, a.kv.g)) = kx;
+      }
+      if constexpr (FP4) {
+        if (lane < DH / 2) {
+          const int e = lane / 16 * 32 + lane % 16;
+          const uint32_t lo = sh_v[e], hi = sh_v[e + 16], ex = kv4_exponent(max_over<16>(max((lo << 16) & 0x7fffffffu, (hi << 16) & 0x7fffffffu)));
+          pg[kv4_v_off(h, slot, e, a.kv.g)] = ex == 255 ? 0 : (unsigned char)kv4_pair<0>(0, bf2f(lo), bf2f(hi), ex);
+          if (lane % 16 == 0) pg[kv4_v_exp_off(h, slot, lane / 16, a.kv.g)] = (unsigned char)ex;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < (FP4 ? 0 : DH / 64); ++i) {
+        const int e = lane + 64 * i;
+        if constexpr (FP8) pg[kv8_v_off(h, slot, e, a.kv.g)] = ve == 255 ? 0 : (unsigned char)kv8_pack(bf2f(sh_v[e]), 0.f, 0.f, 0.f, ve);
+        else ((bf16_t *)pg)[kv_v_off(h, slot, e, a.kv.g)] = sh_v[e];
+      }
+      if (FP8 && lane < 2) pg[kv8_exp_off(h, slot, lane, a.kv.g)] = (unsigned char)(lane ? ve : ke);
+    }
+  }
+}
+
+// Many queries: the waves of a workgroup have two tiles each, 128 queries together, and share the blocks, which a ring of
+// stages in LDS holds: filled by LDS-direct loads, one bare barrier for two blocks (8-bit blocks stay codes in LDS, and every wave
+// converts what it reads).  Blocks that all queries see whole are taken two at a time with one branch for all weights, the values
+// requested before it.  80 KB of stages and up to 256 registers: two workgroups a CU.  Three (168 registers, three stages, a
+// block at a time, fragments requested as they are needed): us, 8 rows of 512 new tokens behind 2048, 32 heads of 128, bf16
+// 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 339.  Bound by the vector units (softmax;
+// conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.
+constexpr int rows_stages(int dh, int el) { return el != EL_BF16 ? 8 : dh == 128 ? 5 : 6; }  // (64: three workgroups, 97 -> 77 us for 32 prompts of 512)
+constexpr size_t rows_lds(int dh, int el) { return (size_t)rows_stages(dh, el) * ((key_pieces(dh, el) + value_pieces(dh, el)) * 1024 + (el != EL_BF16 ? 256 : 0)); }
+template <int DH, int EL, bool SC>
+__global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs) {
+  constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
+  constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = rows_stages(DH, EL), NQ = 16 * NT * NW;
+  constexpr int KF = key_pieces(DH, EL), FR = KF + value_pieces(DH, EL), LPW = FR < NW ? 1 : FR / NW;  // fragments a stage, loads of a wave
+  constexpr int STAGE = FR * 64 + (FP8 || FP4 ? 16 : 0);  // 16-byte pieces; behind 8- and 4-bit blocks 256 bytes for their exponents
+  extern __shared__ uint32x4 ring[];               // [NS][STAGE]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
+  const Share s = Share::of<NQ, SC>(a, pairs, false);
+  if (!s.any) return;
+  const int q0 = s.q0 + wave * (16 * NT), R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
+  const bool busy = q0 < R;
+  int from_blk = 0, last = busy ? min((s.seen(a, min(q0 + 16 * NT, R) - 1) + 31) >> 5, s.hi) : 0;  // this wave's blocks
+  bf16x8 qf[NT][QC];
+  Seen seen[NT];
+  QueryTile<DH, false> tile[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    seen[t] = Seen::of<SC>(a, s, q0 + 16 * t + col);
+    tile[t].clear();
+  }
+  if constexpr (SC) {
+    int from = 1 << 30, upto = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (seen[t].low < seen[t].limit) from = min(from, seen[t].low);
+      upto = max(upto, seen[t].limit);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) {
+      from = min(from, __shfl_xor(from, o));
+      upto = max(upto, __shfl_xor(upto, o));
+    }
+    from_blk = __builtin_amdgcn_readfirstlane(from >> 5);
+    last = min(__builtin_amdgcn_readfirstlane((upto + 31) >> 5), s.hi);
+  }
+  // Blocks are requested in order.  Lane l holds page 64 w + l of the row, for the window w of 64 pages that the next block is
+  // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked, as is every block from the
+  // moment on at which a window has an entry that is no page.
+  const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
+  int ip = s.lo / bpp, ib = s.lo % bpp, pages = 0, window = -1;
+  uint32_t none = 0;                               // a bit for each stage: its block has no page
+  int into = 0, from = 0, asked = s.lo;            // stages of the next block requested and used; blocks requested
+  bool gaps = false;
+  const int ip_end = (s.hi + bpp - 1) / bpp;
+  const uint32x4 *src = nullptr;                   // this wave's part of the next block
+  const unsigned char *ex_src = nullptr;           // its exponents
+  bool is = false;
+  const int part = FR < NW ? wave % FR : wave * LPW;  // (fewer fragments than waves: two waves load the same one)
+  auto next = [](int stage) { return stage == NS - 1 ? 0 : stage + 1; };
+  auto new_page = [&]() {
+    if (ip >> 6 != window) {
+      window = ip >> 6;
+      const int at = window * 64 + lane;
+      pages = at < a.kv.g.max_pages ? table[at] : -1;
+      asm volatile("" : "+v"(pages));
+      gaps |= __any(at >= ip && at < ip_end && (pages < 0 || pages >= a.kv.pages));
+    }
+    int page = __builtin_amdgcn_readlane(pages, ip & 63);
+    is = page >= 0 && page < a.kv.pages;
+    if (!is) page = 0;
+    const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
+    const long at = (long)h * bpp + ib;
+    src = (const uint32x4 *)(pg + at * block_bytes(DH, EL)) + part * 64;
+    ex_src = FP4 ? pg + at * block_bytes(DH, EL) + 32 * DH : pg + (long)H * bpp * (64 * DH) + at * 64;
+  };
+  if (s.lo < s.hi) new_page();
+  auto request = [&]() {
+    none = (none & ~(1u << into)) | (uint32_t)!is << into;
+    uint32x4 *dst = ring + into * STAGE + part * 64;
+#pragma unroll
+    for (int i = 0; i < LPW; ++i)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)&(src + i * 64)[lane],
+                                       (__attribute__((address_space(3))) void *)(dst + i * 64), 16, 0, 0);
+    if constexpr (FP8)  // every wave, so that all wait for the same number of loads; lanes 16 .. 63 repeat
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(ex_src + 4 * col),
+                                       (__attribute__((address_space(3))) void *)(ring + into * STAGE + FR * 64), 4, 0, 0);
+    if constexpr (FP4)  // (64-wide heads: lanes 32 .. 63 repeat)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(ex_src + 4 * (lane % (DH / 2))),
+                                       (__attribute__((address_space(3))) void *)(ring + into * STAGE + FR * 64), 4, 0, 0);
+    into = next(into);
+    ++asked;
+    src += block_bytes(DH, EL) / 16;
+    ex_src += FP4 ? block_bytes(DH, EL) : 64;
+    if (++ib == bpp) {
+      ib = 0;
+      if (++ip < ip_end) new_page();
+    }
+  };
+  constexpr int LOADS = LPW + (FP8 || FP4 ? 1 : 0);
+  for (int i = 0; i < NS - 2; ++i)
+    if (asked < s.hi) request();
+#pragma unroll
+  for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
+  wait_vmcnt<0>();  // (waited for inside the loop, the queries would make the compiler wait for the ring as well)
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
+
+  // scores of a block: S[t][tl][i] of position 16 tl + 4 grp + i
+  auto scores = [&](int stage, floatx4 (&S)[NT][2]) {
+    const uint32x4 *kv = ring + stage * STAGE + lane;
+    const unsigned char *ex = (const unsigned char *)(ring + stage * STAGE + FR * 64);
+    uint32x4 kw[KF];
+#pragma unroll
+    for (int i = 0; i < KF; ++i) kw[i] = kv[i * 64];
+    uint32_t ke[2] = {FP8 ? ex[col] : 0u, FP8 ? ex[16 + col] : 0u};
+    if constexpr (FP4) {
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) ke[i] = ((const uint32_t *)(ex + col * (DH / 16)))[i];
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < QC; ++c)
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
+        const bf16x8 kf = key_fragment<DH, EL>(kw, ke, tl, c);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][c], S[t][tl], 0, 0, 0);
+      }
+  };
+  auto factor_words = [&](int stage, uint32_t (&ve)[2]) {
+    const uint32_t *ex = (const uint32_t *)(ring + stage * STAGE + FR * 64);
+    ve[0] = ex[8 + grp];
+    ve[1] = ex[12 + grp];
+  };
+  auto exponents4 = [&](int stage, uint32_t (&ve)[DH / 16]) {
+    const uint32x4 *ex = (const uint32x4 *)((const unsigned char *)(ring + stage * STAGE + FR * 64) + DH + grp * (DH / 4));
+#pragma unroll
+    for (int i = 0; i < DH / 64; ++i) *(uint32x4 *)&ve[4 * i] = ex[i];
+  };
+  auto add_values4 = [&](const uint32x4 (&vw)[FR - KF], const uint32_t (&ve)[DH / 16], const bf16x8 (&pv)[NT]) {
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) {
+      bf16x8 vf[2];
+      widen4_values({vw[i / 2][i % 2 * 2], vw[i / 2][i % 2 * 2 + 1]}, {ve[2 * i], ve[2 * i + 1]}, vf);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) tile[t].O[2 * i + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[u], pv[t], tile[t].O[2 * i + u], 0, 0, 0);
+    }
+  };
+  auto add_values = [&](const uint32x4 (&vw)[FR - KF], const bf16x8 (&pv)[NT]) {
+#pragma unroll
+    for (int m = 0; m < (FP4 ? 0 : VM); ++m) {
+      bf16x8 vf{};
+      if constexpr (FP8) {
+        const uint32x4 w = vw[m / 2];
+        vf = widen(w[m % 2 * 2], w[m % 2 * 2 + 1], 127);
+      } else {
+        vf = __builtin_bit_cast(bf16x8, vw[m]);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) tile[t].O[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pv[t], tile[t].O[m], 0, 0, 0);
+    }
+  };
+  auto values_of = [&](int stage, uint32x4 (&vw)[FR - KF]) {
+#pragma unroll
+    for (int i = 0; i < FR - KF; ++i) vw[i] = ring[stage * STAGE + (KF + i) * 64 + lane];
+  };
+  auto use = [&](int blk, bool no_page) {
+    const int base = blk * 32;
+    floatx4 S[NT][2];
+    scores(from, S);
+    float vs[8];
+    if constexpr (FP8) {
+      uint32_t ve[2];
+      factor_words(from, ve);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vs[j] = kv8_factor(ve[j >> 2], j & 3);
+    }
+    bf16x8 pv[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (SC) change(a.sc, seen[t].slope, seen[t].pos - base - 4 * grp, S[t]);
+      pv[t] = tile[t].template weights<FP8, SC>(true, S[t], SC ? 1.0f : a.c, SC ? seen[t].low - base : 0, no_page ? 0 : seen[t].limit - base, grp, vs);
+    }
+    uint32x4 vw[FR - KF];
+    values_of(from, vw);
+    if constexpr (FP4) {
+      uint32_t ve[DH / 16];
+      int lo[NT], to[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        lo[t] = seen[t].low - base;
+        to[t] = no_page ? 0 : seen[t].limit - base;
+      }
+      exponents4(from, ve);
+      odd_exponents<DH, SC, NT>(ve, tile, lo, to);
+      add_values4(vw, ve, pv);
+    } else {
+      add_values(vw, pv);
+    }
+  };
+  // Two blocks that every query sees whole: one branch for all of their weights, so that from there on exponentials and products
+  // are formed side by side, and the values are on their way before.
+  auto use_two = [&](int one, int two, int base) {
+    const int stage[2] = {one, two};
+    const float c = SC ? 1.0f : a.c;
+    floatx4 S[2][NT][2];
+    uint32_t ve[2][2];
+    int power[2][8];  // of the values; 2 rows of 1023 behind 8193, 8 bits, us: by ldexp 338, as factors, 0 for byte 0, 341, as they are 358
+    uint32x4 vw[FR - KF];
+    bool raise = false;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      __builtin_amdgcn_s_setprio(1);  // (before the other waves' exponentials: 140 -> 136 us)
+      scores(stage[u], S[u]);
+      __builtin_amdgcn_s_setprio(0);
+      if constexpr (FP8) {
+        factor_words(stage[u], ve[u]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) power[u][j] = (int)(ve[u][j >> 2] >> (8 * (j & 3)) & 255u) - 127;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raise |= (((ve[u][i] & 0x7f7f7f7fu) + 0x01010101u) & ve[u][i] & 0x80808080u) != 0;
+      }
+      if constexpr (SC) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) change(a.sc, seen[t].slope, seen[t].pos - base - 32 * u - 4 * grp, S[u][t]);
+      }
+    }
+    values_of(stage[0], vw);
+    float p[2][NT][8];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        tile[t].relative(S[u][t], c, p[u][t]);
+        raise |= tile[t].most(p[u][t]) > 8.0f;
+      }
+    if (__any(raise)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) most = fmaxf(most, S[u][t][j >> 2][j & 3]);
+        tile[t].raise(most * c);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) tile[t].relative(S[u][t], c, p[u][t]);
+      }
+      if constexpr (FP8)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (power[u][j] == 128) {  // a NaN that all queries see: so are their sums of weights
+#pragma unroll
+              for (int t = 0; t < NT; ++t) p[u][t][j] = __uint_as_float(0x7fc00000u);
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8 pv[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[u][t][j] = __builtin_amdgcn_exp2f(p[u][t][j]);
+        pv[t] = pack8(p[u][t]);
+        tile[t].L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones(), pv[t], tile[t].L, 0, 0, 0);
+        if constexpr (FP8) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[u][t][j] = __builtin_ldexpf(p[u][t][j], power[u][j]);
+          pv[t] = pack8(p[u][t]);
+        }
+      }
+      if constexpr (FP4) {
+        uint32_t e[DH / 16];
+        exponents4(stage[u], e);
+        add_values4(vw, e, pv);
+      } else {
+        add_values(vw, pv);
+      }
+      if (u == 0) values_of(stage[1], vw);
+    }
+  };
+  // clears what a stage holds from position `valid` of its block on
+  auto clear = [&](int valid) {
+    const Keep keep(valid, grp);
+    for (int m = wave; m < FR - KF; m += NW) {
+      uint32x4 &v = ring[from * STAGE + (KF + m) * 64 + lane];
+      uint32x4 x = v;
+      if constexpr (FP8) x &= uint32x4{keep.codes(0), keep.codes(1), keep.codes(0), keep.codes(1)};
+      else if constexpr (EL == EL_BF16) keep.bf16(x);
+      v = x;
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // waits until the next `n` blocks are there for all waves, and requests others into the stages of those before
+  auto open = [&](int blk, int n) {
+    const int ahead = asked - blk - n;  // requested behind them
+    if (ahead >= 3) wait_vmcnt<3 * LOADS>();
+    else if (ahead == 2) wait_vmcnt<2 * LOADS>();
+    else if (ahead == 1) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave's reads of the stages before
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    while (asked < min(s.hi, blk + NS)) request();
+  };
+  auto single = [&](int blk) {
+    open(blk, 1);
+    const bool no_page = none >> from & 1;
+    if (!FP4 && (no_page || blk * 32 + 32 > s.held)) clear(no_page ? 0 : s.held - blk * 32);  // (4 bits: codes are finite, exponents are looked at)
+    if (blk < last && (!SC || blk >= from_blk)) use(blk, no_page);
+    from = next(from);
+  };
+  auto pair = [&](int blk) {
+    open(blk, 2);
+    const int second = next(from);
+    if (busy) use_two(from, second, blk * 32);
+    from = next(second);
+  };
+  int blk = s.lo;
+  if constexpr (SC) {
+    for (; blk < min(s.whole_lo, s.hi); ++blk) single(blk);
+  }
+  for (; blk + 2 <= min(s.whole_hi, s.hi) && !gaps; blk += 2) pair(blk);
+  for (; blk < s.hi; ++blk) single(blk);
+  if constexpr (EL == EL_BF16) {
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, SC ? max(s.lo, from_blk) : s.lo, 1, last, tile);
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int q = q0 + 16 * t + col;
+    if (q >= R) continue;
+    const auto &x = tile[t];
+    const long token = s.token(a, q);
+    const int head = s.head(a, q);
+    if (a.splits == 1) {
+      const float inv = x.L[0] == 0.f ? 0.f : 1.0f / x.L[0];
+      bf16_t *o = (bf16_t *)a.o.p;
+#pragma unroll
+      for (int m = 0; m < VM; ++m)
+        *(uint2 *)&o[row_index(a.o, token, head * DH + 16 * m + 4 * grp)] =
+            make_uint2(pack2(x.O[m][0] * inv, x.O[m][1] * inv), pack2(x.O[m][2] * inv, x.O[m][3] * inv));
+    } else {
+      float *pp = part_of<DH>(a, blockIdx.y, token, head);
+#pragma unroll
+      for (int m = 0; m < VM; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pp[16 * m + 4 * grp + i] = x.O[m][i];
+      if (grp == 0) {
+        pp[DH] = x.m_ref;
+        pp[DH + 1] = x.L[0];
+      }
+    }
+  }
+}
+
+template <int DH, int EL, bool SC, int NT, int NW>
+void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int pairs) {
+  const int cols = std::min(16, a.tk.max_new * a.group);
+  const size_t lds = (size_t)NW * cols * (DH + 2) * sizeof(float);
+  static std::atomic<uint64_t> done{0};
+  if (lds + 8192 > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend<DH, EL, SC, NT, NW>}, NW * 16 * (DH + 2) * sizeof(float));
+  SKD_LAUNCH((k_kv_attend<DH, EL, SC, NT, NW>), grid, dim3(NW * 64), lds, s, a, pairs);
+}
+template <int DH, int EL, bool SC>
+void attend_pages(hipStream_t s, const KvAttend &a, const AttendPlan &p) {
+  const dim3 grid((unsigned)(p.tiles * p.pairs), a.splits);
+  if (p.nq == 128) {
+    static std::atomic<uint64_t> done{0};
+    if (rows_lds(DH, EL) > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend_rows<DH, EL, SC>}, rows_lds(DH, EL));
+    SKD_LAUNCH((k_kv_attend_rows<DH, EL, SC>), grid, dim3(256), rows_lds(DH, EL), s, a, p.pairs);
+  } else if (p.nq == 32) {
+    launch_attend<DH, EL, SC, 2, 8>(s, a, grid, p.pairs);
+  } else if (p.waves == 4) {
+    launch_attend<DH, EL, SC, 1, 4>(s, a, grid, p.pairs);
+  } else {
+    launch_attend<DH, EL, SC, 1, 8>(s, a, grid, p.pairs);
+  }
+}
+template <int EL, bool SC>
+void attend_elem(hipStream_t s, const KvAttend &a, const AttendPlan &p) {
+  if (a.kv.g.dh == 64) attend_pages<64, EL, SC>(s, a, p);
+  else attend_pages<128, EL, SC>(s, a, p);
+}
+
+}  // namespace
+
+}  // namespace skd

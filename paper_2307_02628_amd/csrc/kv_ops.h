@@ -1,5 +1,5 @@
-// Launch interface of the paged cache as an operator (kv_ops.hip): tokens of any rows filed into bf16 or 8-bit pages, read
-// back and attended to.  Used by the C entry points skd_kv_* and by the engine.
+// Launch interface of the paged cache as an operator (kv_ops.hip): tokens of any rows filed into pages of bf16, 8 or 4
+// bits, read back and attended to.  Used by the C entry points skd_kv_* and by the engine.
 #pragma once
 #include "skd_kernels.h"
 
@@ -9,7 +9,7 @@ int hip_failed(hipError_t e);  // notes the error for skd_last_hip_error; what a
 
 struct KvView {
   KvGeom g;                 // H: kv heads; page_elems unused
-  bool fp8;
+  bool fp8, fp4;            // neither: bf16
   int pages, rows;
   long page_bytes;
   unsigned char *pool;
@@ -46,18 +46,30 @@ void kv_append(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows
 // the pages' values of the tokens, fp32 or bf16 rows
 void kv_read(hipStream_t s, const KvView &kv, const KvTokens &tk, bool bf16, const KvRows &k, const KvRows &v);
 
+// What becomes of a score s = scale * q . k, in units of log 2, and which positions a token sees.
+struct KvScoring {
+  bool capped;
+  float in, out;            // factors of q . k: capped: 2 / (log(2) cap) of scale * q . k, and -2 cap / log(2) of the rest; else out alone
+  const float *slopes;      // [heads] or null
+  int window;               // 0: none
+  const int32_t *begin, *end;  // [tokens] or null
+};
+
 struct KvAttend {
   KvView kv;
   KvTokens tk;
   int heads, group;         // query heads, of them to a kv head
   float c;                  // scores -> log2 of the weights
+  bool scored;              // sc is what it goes by
+  KvScoring sc;
   KvRows q, o, k, v;        // bf16; k.p null: the cache holds the new tokens, else they are filed first
-  const int32_t *order;     // rows in the order of their dispatch, or null
+  const int32_t *order;     // rows in the order of their dispatch, or null (scored: null)
   int splits;               // of the keys of a query tile
   float *part;              // splits > 1: [splits][tokens * heads][dh + 2]: numerators, maximum, denominator
 };
-bool kv_attend_fits(const KvView &kv, const KvTokens &tk, int heads);  // in a launch; rows x kv heads must be below 2^31 before
-int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads);
+// window: of the scores, 0 where there is none
+bool kv_attend_fits(const KvView &kv, const KvTokens &tk, int heads, int window = 0);  // in a launch; rows x kv heads must be below 2^31 before
+int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads, int window = 0);
 size_t kv_attend_part(const KvView &kv, const KvTokens &tk, int heads, int splits);  // floats
 void kv_attend(hipStream_t s, const KvAttend &a);
 

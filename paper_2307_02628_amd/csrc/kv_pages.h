@@ -50,7 +50,30 @@ constexpr long kv8_exp_off(int h, int tt, int v, const KvGeom &g) {
   return (long)g.H * g.page_tokens * 2 * g.dh + ((long)h * (g.page_tokens >> 5) + (tt >> 5)) * 64 + 32 * v + (tt & 31);
 }
 
-// The same in parts, for 16 positions (half `half` of a block) at a time: kv_block_base + kv_k_half + kv_k_at is where the
+// 4-bit page (one row): [head][32-key block][K codes | V codes | K exponents | V exponents], 34 * dh bytes a block.  A byte holds two
+// elements of one key, so that no two tokens share one: neighbours in K, elements 16 apart in V (the same lane's in two
+// fragments of the bf16 layout).  K = pieces of 16 bytes a lane, four fragments (tile, chunk) of 4 bytes each; V = pieces of two
+// groups of 32 elements, a lane's 8 keys of each.  Exponents are in the order in which the lanes that take a piece need them.
+constexpr long kv4_page_bytes(int H, int dh, int page_tokens) { return (long)H * (page_tokens >> 5) * 34 * dh; }
+constexpr long kv4_block_base(int h, int tt, const KvGeom &g) { return ((long)h * (g.page_tokens >> 5) + (tt >> 5)) * 34 * g.dh; }
+constexpr long kv4_k_off(int h, int tt, int e, const KvGeom &g) {  // of the byte with elements e and e + 1 (e even)
+  const int kk = tt & 31, f = (kk >> 4) * (g.dh >> 5) + (e >> 5);
+  return kv4_block_base(h, tt, g) + ((long)(f >> 2) * 64 + (kk & 15) + 16 * ((e & 31) >> 3)) * 16 + (f & 3) * 4 + ((e & 7) >> 1);
+}
+constexpr long kv4_v_off(int h, int tt, int e, const KvGeom &g) {  // of the byte with elements e and e + 16 (e & 16 is 0)
+  const int kk = tt & 31, i = e >> 5;
+  return kv4_block_base(h, tt, g) + 16 * g.dh + ((long)(i >> 1) * 64 + 16 * ((kk & 15) >> 2) + (e & 15)) * 16 + (i & 1) * 8 + 4 * (kk >> 4) + (kk & 3);
+}
+constexpr long kv4_k_exp_off(int h, int tt, int i, const KvGeom &g) {  // of elements 32 i .. + 31
+  const int kk = tt & 31;
+  return kv4_block_base(h, tt, g) + 32 * g.dh + (kk & 15) * (g.dh >> 4) + (kk >> 4) * (g.dh >> 5) + i;
+}
+constexpr long kv4_v_exp_off(int h, int tt, int i, const KvGeom &g) {
+  const int kk = tt & 31;
+  return kv4_block_base(h, tt, g) + 33 * g.dh + ((kk & 15) >> 2) * (g.dh >> 2) + i * 8 + 4 * (kk >> 4) + (kk & 3);
+}
+
+// The bf16 page's places in parts, for 16 positions (half `half` of a block) at a time: kv_block_base + kv_k_half + kv_k_at is where the
 // eight elements from e on (a multiple of 8) of the key at position `key` of the 16 begin, kv_block_base + kv_v_half + kv_v_at
 // where the values of element e at four positions from `key` on (a multiple of 4) do.  Parts inside a block fit 32 bits.
 constexpr int kv_k_half(int half, int dh) { return half * (dh >> 5) * 512; }

@@ -1,0 +1,363 @@
+// Block tables on the device.  A table names pages; a page that no entry names is free, so nothing else has to be kept from call
+// to call.  All of it is integer work on a few hundred KB: what counts is the number of launches that have to follow each other.
+#include "kv_table.h"
+
+#include <algorithm>
+
+namespace skd {
+
+namespace {
+
+// Work of an assignment: what a page is to the entries of the new table, before any page is dealt out.
+struct AssignWork {
+  int32_t *uses;     // [pages]: entries that name it
+  int32_t *writes;   // of them those that new tokens go to
+  int32_t *loose;    // of them those that hold nothing yet
+  int32_t *lowest;   // the first of those that new tokens go to
+  int32_t *free, *soft;  // [chunks]: pages that no entry names, that none names but loose ones
+  int32_t *need, *copy;  // [rows]: pages that the row has to get; 1: one of them as a copy
+  int32_t *list;     // free pages, ascending, as many as there could be entries for
+  __host__ __device__ AssignWork(const KvTable &t, int chunks) {
+    uses = t.work;
+    writes = uses + t.pages;
+    loose = writes + t.pages;
+    lowest = loose + t.pages;
+    free = lowest + t.pages;
+    soft = free + chunks;
+    need = soft + chunks;
+    copy = need + t.rows;
+    list = copy + t.rows;
+  }
+};
+__host__ __device__ inline int chunks_of(int pages) { return (int)(((long)pages + TABLE_CHUNK - 1) / TABLE_CHUNK); }
+__host__ __device__ inline long list_of(const KvTable &t) {
+  const long entries = (long)t.rows * t.width;
+  return entries < t.pages ? entries : t.pages;
+}
+
+struct Span {
+  int held, upto;  // positions that a row holds, and will have been given pages for
+};
+__device__ inline Span span_of(const KvTable &t, int r) {
+  const long room = (long)t.width * t.page_tokens;  // below 2^30
+  Span s;
+  s.held = (int)min((long)max(t.len[r], 0), room);
+  s.upto = (int)min((long)s.held + max(t.more[r], 0), room);
+  return s;
+}
+__device__ inline bool written(const KvTable &t, Span s, int i) {
+  return s.upto > s.held && i * t.page_tokens < s.upto && (i + 1) * t.page_tokens > s.held;
+}
+
+__global__ __launch_bounds__(256) void k_table_fill(int32_t *w, long zero, long top) {
+  for (long i = blockIdx.x * 256L + threadIdx.x; i < zero + top; i += gridDim.x * 256L) w[i] = i < zero ? 0 : 0x7fffffff;
+}
+// The rows in their new order, cut to what they will hold, and what every page is to them.
+__global__ __launch_bounds__(256) void k_table_gather(KvTable t) {
+  const AssignWork w(t, chunks_of(t.pages));
+  const uint32_t at = blockIdx.x * 256u + threadIdx.x, all = (uint32_t)t.rows * (uint32_t)t.width;
+  if (at >= all) return;
+  const int r = (int)(at / t.width), i = (int)(at % t.width);
+  const int src = t.source ? t.source[r] : r;
+  const Span s = span_of(t, r);
+  int page = -1;
+  if (src >= 0 && src < t.rows && i * t.page_tokens < s.upto) page = t.table[(long)src * t.width + i];
+  if (page < 0 || page >= t.pages) page = -1;
+  t.out[at] = page;
+  if (page < 0) return;
+  atomicAdd(&w.uses[page], 1);
+  if (written(t, s, i)) {
+    atomicAdd(&w.writes[page], 1);
+    atomicMin(&w.lowest[page], (int)at);
+    if (i * t.page_tokens >= s.held) atomicAdd(&w.loose[page], 1);
+  }
+}
+// Whether an entry that new tokens go to needs a page of its own: it has none, or one that others name too, unless all of them are
+// to be written and it is the first (the others get copies of what it holds before anything is written).
+__device__ inline bool fresh(const AssignWork &w, int page, int at) {
+  if (page < 0) return true;
+  const int n = w.uses[page];
+  return !(n == 1 || (n == w.writes[page] && w.lowest[page] == at));
+}
+__device__ inline int wave_sum_i(int v) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
+  return v;
+}
+// A wave for each row: the pages that it needs; a workgroup for each chunk of pages: the free ones.
+__global__ __launch_bounds__(256) void k_table_count(KvTable t, int rows4) {
+  const int chunks = chunks_of(t.pages), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const AssignWork w(t, chunks);
+  if ((int)blockIdx.x < rows4) {
+    const int r = blockIdx.x * 4 + wave;
+    if (r >= t.rows) return;
+    const Span s = span_of(t, r);
+    int n = 0, copy = 0;
+    if (s.upto > s.held)
+      for (int i = s.held / t.page_tokens + lane; i * t.page_tokens < s.upto; i += 64) {
+        const int at = r * t.width + i, page = t.out[at];
+        if (!fresh(w, page, at)) continue;
+        ++n;
+        if (page >= 0 && i * t.page_tokens < s.held) copy = 1;
+      }
+    n = wave_sum_i(n);
+    copy = wave_sum_i(copy);
+    if (lane == 0) {
+      w.need[r] = n;
+      w.copy[r] = copy;
+    }
+    return;
+  }
+  __shared__ int sum[2][4];
+  const int c = blockIdx.x - rows4;
+  int n = 0, soft = 0;
+  for (int k = threadIdx.x; k < TABLE_CHUNK; k += 256) {
+    const long p = (long)c * TABLE_CHUNK + k;
+    if (p >= t.pages) break;
+    const int uses = w.uses[p];
+    n += uses == 0;
+    soft += uses == w.loose[p];
+  }
+  n = wave_sum_i(n);
+  soft = wave_sum_i(soft);
+  if (lane == 0) {
+    sum[0][wave] = n;
+    sum[1][wave] = soft;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    w.free[c] = sum[0][0] + sum[0][1] + sum[0][2] + sum[0][3];
+    w.soft[c] = sum[1][0] + sum[1][1] + sum[1][2] + sum[1][3];
+  }
+}
+// Sum of n values over the lanes of a wave.
+__device__ inline long sum_of(const int32_t *x, int n) {
+  long v = 0;
+  for (int i = threadIdx.x & 63; i < n; i += 64) v += x[i];
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
+  return v;
+}
+// Place of each of a chunk's pages for which `is` holds among them, in f(page, place).  256 threads, four pages each.
+template <typename Is, typename F>
+__device__ inline void each_in_chunk(int c, int pages, Is is, F f) {
+  __shared__ int sum[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long p = (long)c * TABLE_CHUNK + threadIdx.x * 4;
+  bool has[4];
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    has[k] = p + k < pages && is(p + k);
+    n += has[k];
+  }
+  int upto = n;  // with this lane
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 63) sum[wave] = upto;
+  __syncthreads();
+  int at = upto - n;
+  for (int i = 0; i < wave; ++i) at += sum[i];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (p + k < pages) {
+      f((int)(p + k), has[k], at);
+      at += has[k];
+    }
+}
+// The free pages in ascending order.
+__global__ __launch_bounds__(256) void k_table_list(KvTable t) {
+  const AssignWork w(t, chunks_of(t.pages));
+  const long before = sum_of(w.free, blockIdx.x), room = list_of(t);
+  if (before >= room) return;
+  each_in_chunk(blockIdx.x, t.pages, [&](long p) { return w.uses[p] == 0; },
+                [&](int p, bool is, int at) {
+                  if (is && before + at < room) w.list[before + at] = p;
+                });
+}
+// A wave for each row deals its pages out: those that come behind the needs of the rows before it.
+__global__ __launch_bounds__(64) void k_table_deal(KvTable t) {
+  const int chunks = chunks_of(t.pages), r = blockIdx.x, lane = threadIdx.x;
+  if (t.rows == 0) {
+    if (lane < 3) t.counts[lane] = 0;
+    return;
+  }
+  const AssignWork w(t, chunks);
+  const long free = sum_of(w.free, chunks), before = sum_of(w.need, r), all = before + sum_of(w.need + r, t.rows - r);
+  const long copies_before = sum_of(w.copy, r);
+  const bool enough = all <= free;
+  const Span s = span_of(t, r);
+  long place = before;
+  if (s.upto > s.held)
+    for (int base = s.held / t.page_tokens; base * t.page_tokens < s.upto; base += 64) {
+      const int i = base + lane, at = r * t.width + i;
+      const bool in = i < t.width && i * t.page_tokens < s.upto;
+      const int page = in ? t.out[at] : -1;
+      const bool get = in && fresh(w, page, at);
+      const uint64_t who = __ballot(get);
+      if (!enough) {
+        if (in && i * t.page_tokens >= s.held) t.out[at] = -1;
+        continue;
+      }
+      if (get) {
+        const int to = w.list[place + __popcll(who & ((1ull << lane) - 1))];
+        t.out[at] = to;
+        if (page >= 0 && i * t.page_tokens < s.held) {
+          t.copies[2 * copies_before] = page;
+          t.copies[2 * copies_before + 1] = to;
+        }
+      }
+      place += __popcll(who);
+    }
+  const long copies = enough ? copies_before + sum_of(w.copy + r, t.rows - r) : 0;
+  if (lane == 0 && r >= copies) t.copies[2 * (long)r] = t.copies[2 * (long)r + 1] = -1;
+  if (r == 0) {
+    const long soft = sum_of(w.soft, chunks);
+    if (lane == 0) {
+      t.counts[0] = (int)(enough ? t.pages - free + all : t.pages - soft);
+      t.counts[1] = (int)(enough ? 0 : min(all - free, 0x7fffffffL));
+      t.counts[2] = (int)copies;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ pages in use moved to the lowest places
+struct CompactWork {
+  int32_t *uses, *rank;     // [pages]: 1 if named; place among the pages that move
+  int32_t *used;            // [chunks]
+  int32_t *source, *target; // [pages / 2]
+  __host__ __device__ CompactWork(const KvTable &t, int chunks) {
+    uses = t.work;
+    rank = uses + t.pages;
+    used = rank + t.pages;
+    source = used + chunks;
+    target = source + t.pages / 2;
+  }
+};
+__global__ __launch_bounds__(256) void k_table_mark(KvTable t) {
+  const CompactWork w(t, chunks_of(t.pages));
+  const uint32_t at = blockIdx.x * 256u + threadIdx.x, all = (uint32_t)t.rows * (uint32_t)t.width;
+  if (at >= all) return;
+  const int page = t.table[at];
+  if (page >= 0 && page < t.pages) w.uses[page] = 1;
+}
+__global__ __launch_bounds__(256) void k_table_used(KvTable t) {
+  const CompactWork w(t, chunks_of(t.pages));
+  __shared__ int sum[4];
+  int n = 0;
+  for (int k = threadIdx.x; k < TABLE_CHUNK; k += 256) {
+    const long p = (long)blockIdx.x * TABLE_CHUNK + k;
+    if (p < t.pages) n += w.uses[p];
+  }
+  n = wave_sum_i(n);
+  if ((threadIdx.x & 63) == 0) sum[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) w.used[blockIdx.x] = sum[0] + sum[1] + sum[2] + sum[3];
+}
+// Pages in use before page `n` (of all of them, where n is their number).
+__device__ inline int used_before(const CompactWork &w, int n) {
+  const int c = n / TABLE_CHUNK;
+  return (int)(sum_of(w.used, c) + sum_of(w.uses + (long)c * TABLE_CHUNK, n - c * TABLE_CHUNK));
+}
+// The k-th page in use at or behind the number of all of them goes to the k-th free one before it.
+__global__ __launch_bounds__(256) void k_table_rank(KvTable t) {
+  const int chunks = chunks_of(t.pages), c = blockIdx.x;
+  const CompactWork w(t, chunks);
+  const int used = (int)sum_of(w.used, chunks), below = used_before(w, used), before = (int)sum_of(w.used, c);
+  each_in_chunk(c, t.pages, [&](long p) { return w.uses[p] != 0; },
+                [&](int p, bool is, int at) {
+                  at += before;  // pages in use before p
+                  if (is && p >= used) {
+                    w.rank[p] = at - below;
+                    w.source[at - below] = p;
+                  }
+                  if (!is && p < used) w.target[p - at] = p;
+                });
+}
+__global__ __launch_bounds__(256) void k_table_move(KvTable t) {
+  const int chunks = chunks_of(t.pages);
+  const CompactWork w(t, chunks);
+  const int used = (int)sum_of(w.used, chunks), moved = used - used_before(w, used);
+  const uint32_t at = blockIdx.x * 256u + threadIdx.x, all = (uint32_t)t.rows * (uint32_t)t.width;
+  if (at < all) {
+    const int page = t.table[at];
+    t.out[at] = page < 0 || page >= t.pages ? -1 : page < used ? page : w.target[w.rank[page]];
+  }
+  if (at < (uint32_t)t.pages / 2) {
+    const bool is = (int)at < moved;
+    t.copies[2 * (long)at] = is ? w.source[at] : -1;
+    t.copies[2 * (long)at + 1] = is ? w.target[at] : -1;
+  }
+  if (at == 0) {
+    t.counts[0] = used;
+    t.counts[1] = 0;
+    t.counts[2] = moved;
+  }
+}
+
+// ------------------------------------------------------------------ copies of pages
+// Workgroups take pieces of 16 KB in turn; a thread has four 16-byte loads on their way.  Bound by the bytes, which are streamed.
+constexpr int COPY_PIECE = 16384;
+__global__ __launch_bounds__(256) void k_copy_pages(unsigned char *pool, long page_bytes, int pages, const int32_t *copies, int most, const int32_t *number) {
+  typedef __attribute__((__vector_size__(16))) uint32_t piece_t;
+  const int n = number ? min(*number, most) : most;
+  const long pieces = (page_bytes + COPY_PIECE - 1) / COPY_PIECE;
+  for (long id = blockIdx.x; id < n * pieces; id += gridDim.x) {
+    const long which = id / pieces, at = (id - which * pieces) * COPY_PIECE;
+    const int from = copies[2 * which], to = copies[2 * which + 1];
+    if (from < 0 || from >= pages || to < 0 || to >= pages || from == to) continue;
+    const piece_t *src = (const piece_t *)(pool + (long)from * page_bytes + at);
+    piece_t *dst = (piece_t *)(pool + (long)to * page_bytes + at);
+    const int left = (int)min((long)COPY_PIECE, page_bytes - at) / 16;
+    piece_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((int)threadIdx.x + 256 * i < left) x[i] = __builtin_nontemporal_load(&src[threadIdx.x + 256 * i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((int)threadIdx.x + 256 * i < left) __builtin_nontemporal_store(x[i], &dst[threadIdx.x + 256 * i]);
+  }
+}
+
+unsigned groups_for(long n) { return (unsigned)std::max(1L, (n + 255) / 256); }
+
+}  // namespace
+
+bool kv_table_fits(const KvTable &t) {
+  const long entries = (long)t.rows * t.width;
+  return entries < 1L << 31 && launch_fits((long)t.rows + chunks_of(t.pages), 256);
+}
+size_t kv_assign_words(const KvTable &t) {
+  const size_t chunks = chunks_of(t.pages);
+  return 4 * (size_t)t.pages + 2 * chunks + 2 * (size_t)t.rows + (size_t)list_of(t);
+}
+size_t kv_compact_words(const KvTable &t) { return 2 * (size_t)t.pages + chunks_of(t.pages) + 2 * (size_t)(t.pages / 2); }
+
+void kv_assign(hipStream_t s, const KvTable &t) {
+  const int chunks = chunks_of(t.pages), rows4 = (t.rows + 3) / 4;
+  const long entries = (long)t.rows * t.width;
+  SKD_LAUNCH(k_table_fill, dim3(std::min(groups_for(4L * t.pages), 1024u)), dim3(256), 0, s, t.work, 3L * t.pages, (long)t.pages);
+  SKD_LAUNCH(k_table_gather, dim3(groups_for(entries)), dim3(256), 0, s, t);
+  SKD_LAUNCH(k_table_count, dim3(rows4 + chunks), dim3(256), 0, s, t, rows4);
+  SKD_LAUNCH(k_table_list, dim3(chunks), dim3(256), 0, s, t);
+  SKD_LAUNCH(k_table_deal, dim3(std::max(t.rows, 1)), dim3(64), 0, s, t);
+}
+void kv_compact(hipStream_t s, const KvTable &t) {
+  const int chunks = chunks_of(t.pages);
+  const long entries = (long)t.rows * t.width;
+  SKD_LAUNCH(k_table_fill, dim3(std::min(groups_for(t.pages), 1024u)), dim3(256), 0, s, t.work, (long)t.pages, 0L);
+  SKD_LAUNCH(k_table_mark, dim3(groups_for(entries)), dim3(256), 0, s, t);
+  SKD_LAUNCH(k_table_used, dim3(chunks), dim3(256), 0, s, t);
+  SKD_LAUNCH(k_table_rank, dim3(chunks), dim3(256), 0, s, t);
+  SKD_LAUNCH(k_table_move, dim3(groups_for(std::max(entries, (long)t.pages / 2))), dim3(256), 0, s, t);
+}
+void kv_copy_pages(hipStream_t s, unsigned char *pool, long page_bytes, int pages, const int32_t *copies, int most, const int32_t *number) {
+  const long pieces = (page_bytes + COPY_PIECE - 1) / COPY_PIECE;
+  const unsigned groups = (unsigned)((__int128)most * pieces < 2048 ? most * pieces : 2048);  // (8 a CU)
+  SKD_LAUNCH(k_copy_pages, dim3(groups), dim3(256), 0, s, pool, page_bytes, pages, copies, most, number);
+}
+
+}  // namespace skd

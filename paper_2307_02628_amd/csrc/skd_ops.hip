@@ -5,6 +5,7 @@
 
 #include "../../include/skd.h"
 #include "kv_ops.h"
+#include "kv_table.h"
 #include "sample_rows.h"
 
 using namespace skd;
@@ -21,7 +22,7 @@ bool aligned4(std::initializer_list<const void *> ps) {
 
 int check_kv(const skd_kv *kv) {
   if (!kv) return SKD_ERR_NULL;
-  if (kv->elem != SKD_KV_BF16 && kv->elem != SKD_KV_FP8) return SKD_ERR_SHAPE;
+  if (kv->elem != SKD_KV_BF16 && kv->elem != SKD_KV_FP8 && kv->elem != SKD_KV_FP4) return SKD_ERR_SHAPE;
   if (kv->head_dim != 64 && kv->head_dim != 128) return SKD_ERR_SHAPE;
   if (kv->kv_heads < 1 || kv->kv_heads > 65536 || kv->page_tokens < 32 || kv->page_tokens % 32 || kv->pages < 1 || kv->rows < 0 || kv->max_pages < 1) return SKD_ERR_SHAPE;
   if ((int64_t)kv->max_pages * kv->page_tokens >= 1 << 30) return SKD_ERR_RANGE;  // positions are counted in 32 bits
@@ -62,6 +63,7 @@ KvView view(const skd_kv *kv) {
   v.g.H = kv->kv_heads;
   v.g.dh = kv->head_dim;
   v.fp8 = kv->elem == SKD_KV_FP8;
+  v.fp4 = kv->elem == SKD_KV_FP4;
   v.pages = kv->pages;
   v.rows = kv->rows;
   v.page_bytes = (long)skd_kv_page_bytes(kv);
@@ -101,8 +103,9 @@ bool fits_int(__int128 n) { return n <= std::numeric_limits<int32_t>::max(); }
 
 extern "C" int64_t skd_kv_page_bytes(const skd_kv *kv) {
   CHECK(check_kv(kv));
-  return kv->elem == SKD_KV_FP8 ? (int64_t)kv8_page_bytes(kv->kv_heads, kv->head_dim, kv->page_tokens)
-                                : (int64_t)kv->kv_heads * kv->page_tokens * 4 * kv->head_dim;
+  if (kv->elem == SKD_KV_FP8) return (int64_t)kv8_page_bytes(kv->kv_heads, kv->head_dim, kv->page_tokens);
+  if (kv->elem == SKD_KV_FP4) return (int64_t)kv4_page_bytes(kv->kv_heads, kv->head_dim, kv->page_tokens);
+  return (int64_t)kv->kv_heads * kv->page_tokens * 4 * kv->head_dim;
 }
 
 extern "C" int skd_kv_append(const skd_kv *kv, const skd_kv_chunk *ch, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
@@ -138,32 +141,52 @@ extern "C" int skd_kv_read(const skd_kv *kv, const skd_kv_chunk *ch, int32_t ele
   return launched();
 }
 
-static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads) {
+// sc null: scores as they are
+static int check_scores(const skd_kv_scores *sc) {
+  if (!sc) return SKD_OK;
+  if (sc->cap != 0.f && !(sc->cap >= 0x1p-20f && sc->cap <= 1024.f)) return SKD_ERR_RANGE;
+  if (sc->window < 0) return SKD_ERR_RANGE;
+  if (!aligned4({sc->slopes, sc->begin, sc->end})) return SKD_ERR_SHAPE;
+  return SKD_OK;
+}
+static int window_of(const skd_kv_scores *sc) { return sc ? std::min(sc->window, 1 << 30) : 0; }  // (no row has as many positions)
+static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, const skd_kv_scores *sc) {
   CHECK(check_call(kv, ch));
   if (heads < 1 || heads % kv->kv_heads) return SKD_ERR_SHAPE;
+  CHECK(check_scores(sc));
   const KvTokens tk = tokens(kv, ch);
   if (!fits_int((int64_t)heads * kv->head_dim)) return SKD_ERR_RANGE;  // columns of a token
   const int64_t group = heads / kv->kv_heads;
   const int64_t queries = tk.max_new * group;
   if (!fits_int(queries + 128) || !fits_int((int64_t)kv->kv_heads * kv->rows + 8)) return SKD_ERR_RANGE;
-  return kv_attend_fits(view(kv), tk, heads) ? SKD_OK : SKD_ERR_RANGE;
+  return kv_attend_fits(view(kv), tk, heads, window_of(sc)) ? SKD_OK : SKD_ERR_RANGE;
 }
-
-extern "C" int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads) {
-  CHECK(check_attend(kv, ch, heads));
+static int64_t attend_workspace(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, const skd_kv_scores *sc) {
+  CHECK(check_attend(kv, ch, heads, sc));
   const KvView v = view(kv);
   const KvTokens tk = tokens(kv, ch);
   if (!tk.max_new || !kv->rows) return 0;
-  return (int64_t)(kv_attend_part(v, tk, heads, kv_attend_splits(v, tk, heads)) * sizeof(float));
+  return (int64_t)(kv_attend_part(v, tk, heads, kv_attend_splits(v, tk, heads, window_of(sc))) * sizeof(float));
 }
-
-extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float scale, const void *q, int64_t q_stride,
-                             const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
-                             void *workspace, int64_t workspace_bytes, void *hip_stream) {
-  CHECK(check_attend(kv, ch, heads));
-  const float c = scale * 1.4426950408889634f;
+static int attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float scale, const skd_kv_scores *sc, const void *q, int64_t q_stride,
+                  const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride, void *workspace,
+                  int64_t workspace_bytes, void *hip_stream) {
+  CHECK(check_attend(kv, ch, heads, sc));
+  constexpr float LOG2E = 1.4426950408889634f;
+  const float c = scale * LOG2E;
   if (!(scale > 0.f) || !std::isfinite(c)) return SKD_ERR_RANGE;
   KvAttend a{};
+  if (sc) {
+    a.scored = true;
+    a.sc.capped = sc->cap != 0.f;
+    a.sc.in = a.sc.capped ? (float)(2.0 * 1.4426950408889634 * (double)scale / (double)sc->cap) : 0.f;
+    if (!std::isfinite(a.sc.in)) return SKD_ERR_RANGE;
+    a.sc.out = a.sc.capped ? -2.0f * LOG2E * sc->cap : c;
+    a.sc.slopes = sc->slopes;
+    a.sc.window = window_of(sc);
+    a.sc.begin = sc->begin;
+    a.sc.end = sc->end;
+  }
   a.kv = view(kv);
   a.tk = tokens(kv, ch);
   if (!a.tk.max_new || !kv->rows) return SKD_OK;
@@ -181,7 +204,7 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
   a.c = c;
   a.q = rows_of(q, q_stride);
   a.o = rows_of(out, out_stride);
-  a.splits = kv_attend_splits(a.kv, a.tk, heads);
+  a.splits = kv_attend_splits(a.kv, a.tk, heads, a.sc.window);
   if (a.splits > 1) {
     if (!workspace) return SKD_ERR_NULL;
     if (!aligned(workspace)) return SKD_ERR_SHAPE;
@@ -191,11 +214,107 @@ extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t h
   CHECK(check_memory({kv->pool, kv->block_table, ch->first, ch->past, q, out}));
   if (k) CHECK(check_memory({k, v}));
   if (a.splits > 1) CHECK(check_memory({workspace}));
+  if (sc)
+    for (const void *p : {(const void *)sc->slopes, (const void *)sc->begin, (const void *)sc->end})
+      if (p) CHECK(check_memory({p}));
   if (k) {
     a.k = rows_of(k, k_stride);
     a.v = rows_of(v, v_stride);
   }
   kv_attend((hipStream_t)hip_stream, a);
+  return launched();
+}
+
+extern "C" int64_t skd_kv_attend_workspace(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads) { return attend_workspace(kv, ch, heads, nullptr); }
+extern "C" int skd_kv_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float scale, const void *q, int64_t q_stride,
+                             const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *out, int64_t out_stride,
+                             void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  return attend(kv, ch, heads, scale, nullptr, q, q_stride, k, k_stride, v, v_stride, out, out_stride, workspace, workspace_bytes, hip_stream);
+}
+extern "C" int64_t skd_kv_attend_scores_workspace(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, const skd_kv_scores *scores) {
+  if (!scores) return SKD_ERR_NULL;
+  return attend_workspace(kv, ch, heads, scores);
+}
+extern "C" int skd_kv_attend_scores(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float scale, const skd_kv_scores *scores,
+                                    const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                    void *out, int64_t out_stride, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  if (!scores) return SKD_ERR_NULL;
+  return attend(kv, ch, heads, scale, scores, q, q_stride, k, k_stride, v, v_stride, out, out_stride, workspace, workspace_bytes, hip_stream);
+}
+
+// ---- block tables
+static int table_of(const skd_kv *kv, KvTable &t) {
+  CHECK(check_kv(kv));
+  t.table = kv->block_table;
+  t.rows = kv->rows;
+  t.width = kv->max_pages;
+  t.page_tokens = kv->page_tokens;
+  t.pages = kv->pages;
+  return kv_table_fits(t) ? SKD_OK : SKD_ERR_RANGE;
+}
+// The arrays of such a call: aligned, the current device's, and table_out apart from the table, or (`same`) the table itself.
+static int check_table(const KvTable &t, bool same, size_t words, void *workspace, int64_t workspace_bytes) {
+  if (!t.out || !t.counts || !t.copies || !workspace || (t.rows && !t.table)) return SKD_ERR_NULL;
+  if (!aligned4({t.table, t.out, t.counts, t.copies}) || !aligned(workspace)) return SKD_ERR_SHAPE;
+  if (workspace_bytes < (int64_t)(words * sizeof(int32_t))) return SKD_ERR_NOMEM;
+  const size_t bytes = (size_t)t.rows * t.width * sizeof(int32_t);
+  const uintptr_t a = (uintptr_t)t.table, b = (uintptr_t)t.out;
+  if (!(same && a == b) && a < b + bytes && b < a + bytes) return SKD_ERR_RANGE;
+  CHECK(check_memory({t.out, t.counts, t.copies, workspace}));
+  if (t.rows) CHECK(check_memory({t.table}));
+  return SKD_OK;
+}
+extern "C" int64_t skd_kv_assign_workspace(const skd_kv *kv) {
+  KvTable t{};
+  CHECK(table_of(kv, t));
+  return (int64_t)(kv_assign_words(t) * sizeof(int32_t));
+}
+extern "C" int skd_kv_assign(const skd_kv *kv, const int32_t *source, const int32_t *len, const int32_t *more, int32_t *table_out,
+                             int32_t *copies, int32_t *counts, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  KvTable t{};
+  CHECK(table_of(kv, t));
+  t.source = source;
+  t.len = len;
+  t.more = more;
+  t.out = table_out;
+  t.copies = copies;
+  t.counts = counts;
+  t.work = (int32_t *)workspace;
+  if (t.rows && (!len || !more)) return SKD_ERR_NULL;
+  if (!aligned4({source, len, more})) return SKD_ERR_SHAPE;
+  CHECK(check_table(t, !source, kv_assign_words(t), workspace, workspace_bytes));
+  if (t.rows) CHECK(check_memory({len, more}));
+  if (source) CHECK(check_memory({source}));
+  kv_assign((hipStream_t)hip_stream, t);
+  return launched();
+}
+extern "C" int64_t skd_kv_compact_workspace(const skd_kv *kv) {
+  KvTable t{};
+  CHECK(table_of(kv, t));
+  return (int64_t)(kv_compact_words(t) * sizeof(int32_t));
+}
+extern "C" int skd_kv_compact(const skd_kv *kv, int32_t *table_out, int32_t *copies, int32_t *counts, void *workspace, int64_t workspace_bytes,
+                              void *hip_stream) {
+  KvTable t{};
+  CHECK(table_of(kv, t));
+  t.out = table_out;
+  t.copies = copies;
+  t.counts = counts;
+  t.work = (int32_t *)workspace;
+  CHECK(check_table(t, true, kv_compact_words(t), workspace, workspace_bytes));
+  kv_compact((hipStream_t)hip_stream, t);
+  return launched();
+}
+extern "C" int skd_kv_copy_pages(const skd_kv *kv, const int32_t *copies, int32_t most, const int32_t *number, void *hip_stream) {
+  CHECK(check_kv(kv));
+  if (most < 0) return SKD_ERR_RANGE;
+  if (!most) return SKD_OK;
+  if (!kv->pool || !copies) return SKD_ERR_NULL;
+  if (!aligned(kv->pool) || !aligned4({copies, number})) return SKD_ERR_SHAPE;
+  CHECK(check_memory({kv->pool, copies}));
+  if (number) CHECK(check_memory({number}));
+  const KvView v = view(kv);
+  kv_copy_pages((hipStream_t)hip_stream, v.pool, v.page_bytes, v.pages, copies, most, number);
   return launched();
 }
 

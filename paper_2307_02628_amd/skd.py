@@ -20,13 +20,14 @@ OK, ERR_NULL, ERR_SHAPE, ERR_RANGE, ERR_ORDER, ERR_SCHEDULE, ERR_NOMEM, ERR_HIP 
 BF16, FP32, BF16_KV8 = 0, 1, 2
 HOST, DEVICE = 0, 1
 W_FP32, W_BF16 = 0, 1
-KV_BF16, KV_FP8 = 0, 1
+KV_BF16, KV_FP8, KV_FP4 = 0, 1, 4
 
 EXPORTS = ["skd_schedule", "skd_active_layers", "skd_create", "skd_create_with_schedule", "skd_state_active_layers", "skd_prefill", "skd_decode_step",
            "skd_logits_argmax", "skd_logits_argmax_noalloc", "skd_logits_sample", "skd_rewind", "skd_profile_enable", "skd_profile_read", "skd_kv_len", "skd_kv_pages_reserved", "skd_kv_pages_dense", "skd_synchronize",
            "skd_debug_read_hidden", "skd_debug_kv_load", "skd_debug_kv_read", "skd_destroy", "skd_strerror",
            "skd_last_hip_error", "skd_kv_page_bytes", "skd_kv_append", "skd_kv_read", "skd_kv_attend", "skd_kv_attend_workspace",
-           "skd_logits_sample_rows", "skd_sample", "skd_sample_workspace", "skd_decode_chunk"]
+           "skd_logits_sample_rows", "skd_sample", "skd_sample_workspace", "skd_decode_chunk", "skd_kv_attend_scores", "skd_kv_attend_scores_workspace",
+           "skd_kv_assign", "skd_kv_assign_workspace", "skd_kv_compact", "skd_kv_compact_workspace", "skd_kv_copy_pages"]
 
 
 class Config(C.Structure):
@@ -98,6 +99,13 @@ def lib() -> C.CDLL:
         l.skd_kv_read.argtypes = [P, P, I32, P, I64, P, I64, P]
         l.skd_kv_attend.argtypes = [P, P, I32, C.c_float, P, I64, P, I64, P, I64, P, I64, P, I64, P]
         l.skd_kv_attend_workspace.argtypes, l.skd_kv_attend_workspace.restype = [P, P, I32], I64
+        l.skd_kv_attend_scores.argtypes = [P, P, I32, C.c_float, P, P, I64, P, I64, P, I64, P, I64, P, I64, P]
+        l.skd_kv_attend_scores_workspace.argtypes, l.skd_kv_attend_scores_workspace.restype = [P, P, I32, P], I64
+        l.skd_kv_assign.argtypes = [P] * 8 + [I64, P]
+        l.skd_kv_assign_workspace.argtypes, l.skd_kv_assign_workspace.restype = [P], I64
+        l.skd_kv_compact.argtypes = [P] * 5 + [I64, P]
+        l.skd_kv_compact_workspace.argtypes, l.skd_kv_compact_workspace.restype = [P], I64
+        l.skd_kv_copy_pages.argtypes = [P, P, I32, P, P]
         l.skd_logits_sample_rows.argtypes = [P] * 5
         l.skd_decode_chunk.argtypes = [P, I32, I32, P]
         l.skd_sample.argtypes = [P, I64, I32, I32, P, P, P, P, I64, P]
@@ -409,6 +417,29 @@ class KvChunk:
         self.ref = C.byref(self.c)
 
 
+class Scores(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("window", C.c_int32), ("begin", C.c_void_p), ("end", C.c_void_p)]
+
+
+class KvScores:
+    """What becomes of an attention's scores and which positions a token sees (skd_kv_scores): slopes [heads] float32, begin and end
+    [tokens] int32 device tensors or None."""
+
+    def __init__(self, cap: float = 0.0, slopes=None, window: int = 0, begin=None, end=None):
+        for t, dtype in ((slopes, "float32"), (begin, "int32"), (end, "int32")):
+            if t is not None:
+                _expect(t, dtype, 1)
+        self._keep = (slopes, begin, end)
+        self.c = Scores(cap, _ptr_of(slopes), window, _ptr_of(begin), _ptr_of(end))
+        self.ref = C.byref(self.c)
+
+    def expect(self, heads: int, tokens: int):
+        """Raises unless the arrays are those of so many heads and tokens."""
+        for t, n in zip(self._keep, (heads, tokens, tokens)):
+            if t is not None and len(t) != n:
+                raise ValueError(f"expected an entry for each of {n} heads or tokens")
+
+
 class KvCache:
     """Keys and values in pages of the caller's memory (skd_kv): pool [pages][..] and block_table [rows][max_pages] (int32) are
     contiguous device tensors, kept alive by this object; calls run on `stream` (0: the default stream)."""
@@ -455,11 +486,66 @@ class KvCache:
     def attend(self, chunk: KvChunk, q, out, scale: float, k=None, v=None, workspace=None, stream: int = 0):
         """q, out [tokens][heads][head_dim]; workspace: a device tensor of attend_workspace bytes (None where that is 0)."""
         heads = q.shape[1] if q.dim() == 3 else q.shape[1] // self.dh
+        _check(self._lib.skd_kv_attend(self.ref, chunk.ref, heads, scale, *self._attend_args(chunk, heads, q, out, k, v, workspace), stream),
+               "skd_kv_attend")
+
+    def _attend_args(self, chunk: KvChunk, heads: int, q, out, k, v, workspace):
         kk = (0, 0) if k is None else self._rows_of(chunk, self.heads, k, "torch.bfloat16")
         vv = (0, 0) if v is None else self._rows_of(chunk, self.heads, v, "torch.bfloat16")
-        ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-        _check(self._lib.skd_kv_attend(self.ref, chunk.ref, heads, scale, *self._rows_of(chunk, heads, q, "torch.bfloat16"), *kk, *vv,
-                                       *self._rows_of(chunk, heads, out, "torch.bfloat16"), *ws, stream), "skd_kv_attend")
+        return (*self._rows_of(chunk, heads, q, "torch.bfloat16"), *kk, *vv, *self._rows_of(chunk, heads, out, "torch.bfloat16"), *_bytes_of(workspace))
+
+    def attend_scores_workspace(self, chunk: KvChunk, heads: int, scores: KvScores) -> int:
+        return _check(self._lib.skd_kv_attend_scores_workspace(self.ref, chunk.ref, heads, scores.ref), "skd_kv_attend_scores_workspace")
+
+    def attend_scores(self, chunk: KvChunk, q, out, scale: float, scores: KvScores, k=None, v=None, workspace=None, stream: int = 0):
+        """attend with changed scores and masks; workspace: attend_scores_workspace bytes."""
+        heads = q.shape[1] if q.dim() == 3 else q.shape[1] // self.dh
+        scores.expect(heads, chunk.tokens)
+        _check(self._lib.skd_kv_attend_scores(self.ref, chunk.ref, heads, scale, scores.ref,
+                                              *self._attend_args(chunk, heads, q, out, k, v, workspace), stream), "skd_kv_attend_scores")
+
+    def _table_args(self, table_out, copies, counts, most: int, workspace):
+        for t, shape in ((table_out, (self.rows, self.c.max_pages)), (copies, (most, 2)), (counts, (3,))):
+            _expect(t, "int32", len(shape))
+            if tuple(t.shape) != shape:
+                raise ValueError(f"expected shape {shape}")
+        return (table_out.data_ptr(), copies.data_ptr(), counts.data_ptr(), *_bytes_of(workspace))
+
+    def assign_workspace(self) -> int:
+        return _check(self._lib.skd_kv_assign_workspace(self.ref), "skd_kv_assign_workspace")
+
+    def assign(self, table_out, copies, counts, len, more, source=None, workspace=None, stream: int = 0):
+        """The next block table (skd_kv_assign), all int32 device tensors: table_out as the block table, copies [rows][2], counts [3], and
+        of each row len, more and source (None: every row goes on from itself); workspace: assign_workspace bytes."""
+        for t in (len, more, source):
+            if t is not None:
+                _expect(t, "int32", 1)
+                if t.shape[0] != self.rows:
+                    raise ValueError("one entry per row")
+        _check(self._lib.skd_kv_assign(self.ref, _ptr_of(source), len.data_ptr(), more.data_ptr(),
+                                       *self._table_args(table_out, copies, counts, self.rows, workspace), stream), "skd_kv_assign")
+
+    def compact_workspace(self) -> int:
+        return _check(self._lib.skd_kv_compact_workspace(self.ref), "skd_kv_compact_workspace")
+
+    def compact(self, table_out, copies, counts, workspace=None, stream: int = 0):
+        """The table with its pages at the lowest places (skd_kv_compact): copies [pages // 2][2]; workspace: compact_workspace bytes."""
+        _check(self._lib.skd_kv_compact(self.ref, *self._table_args(table_out, copies, counts, self.c.pages // 2, workspace), stream), "skd_kv_compact")
+
+    def copy_pages(self, copies, number=None, stream: int = 0):
+        """Copies pages of the pool: copies [n][2] (from, to), of them as many as the device tensor `number` says, or all."""
+        _expect(copies, "int32", 2)
+        if copies.shape[1] != 2:
+            raise ValueError("expected pairs of pages")
+        if number is not None:
+            _expect(number, "int32", 1)
+            if number.shape[0] != 1:
+                raise ValueError("expected one number")
+        _check(self._lib.skd_kv_copy_pages(self.ref, copies.data_ptr(), copies.shape[0], _ptr_of(number), stream), "skd_kv_copy_pages")
+
+
+def _bytes_of(workspace):
+    return (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
 def _expect(t, dtype: str, dims: int):

@@ -1,0 +1,232 @@
+"""Pages of 4 bits, attention with changed scores and masks, and block tables, in 64 bits or whole numbers on the CPU, from the layout and
+the formulas that include/skd.h gives; and rows of a cache on the device to hold against them."""
+import math
+
+import numpy as np
+import torch
+
+import kv_reference as R
+from paper_2307_02628_amd import skd
+
+BF16, FP8, FP4 = skd.KV_BF16, skd.KV_FP8, skd.KV_FP4
+E2M1 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6])
+
+
+def exponent4(x):
+    """Exponent byte of each 32 along the last axis, x [..., dh / 32, 32]."""
+    a = np.abs(x).max(-1)
+    with np.errstate(all="ignore"):
+        e = np.ceil(np.log2(a / 6.0))
+        e = np.where(a > 6.0 * np.exp2(e), e + 1, np.where(a <= 3.0 * np.exp2(e), e - 1, e))
+    e = np.where(np.isfinite(e), np.maximum(e, -124), -124)
+    return np.where(np.isfinite(a), e + 127, 255).astype(np.int64)
+
+
+def as_held(x, elem):
+    """What a page holds of x [..., dh] (float64 of bf16 values), as values."""
+    if elem != FP4:
+        return R.as_held(x, elem)
+    y = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
+    b = exponent4(y)
+    with np.errstate(all="ignore"):
+        s = np.exp2(b - 127.0)[..., None]
+        z = np.abs(y / s)
+        step = np.where(z < 2, 0.5, np.where(z < 4, 1.0, 2.0))
+        z = np.round(z / step) * step
+        z = np.where((b == 253)[..., None], np.minimum(z, 3.0), z)
+        z = np.copysign(z, y) * s
+    return np.where((b == 255)[..., None], np.nan, z).reshape(x.shape)
+
+
+def unpack_page4(page, H, dh, page_tokens):
+    """K, V [page_tokens][H][dh] float64 of a 4-bit page given as uint8."""
+    G = dh // 32
+    K, V = np.zeros((page_tokens, H, dh)), np.zeros((page_tokens, H, dh))
+    p, e = np.arange(page_tokens)[:, None], np.arange(dh)[None, :]
+    x, pos, g = p % 32 // 16, p % 16, e // 32
+    for h in range(H):
+        block = (h * (page_tokens // 32) + p // 32) * 34 * dh
+        f = x * G + g
+        k = block + ((f // 4 * 4 + e % 32 // 8) * 16 + pos) * 16 + f % 4 * 4 + e % 8 // 2
+        v = block + 16 * dh + ((g // 2 * 4 + pos // 4) * 16 + e % 16) * 16 + g % 2 * 8 + x * 4 + pos % 4
+        ke = block + 32 * dh + (pos * 2 + x) * G + g
+        ve = block + 33 * dh + ((pos // 4 * G + g) * 2 + x) * 4 + pos % 4
+        for dst, at, ex, high in ((K, k, ke, e % 2), (V, v, ve, e // 16 % 2)):
+            b = page[ex].astype(np.int64)
+            dst[:, h] = np.where(b == 255, np.nan, E2M1[page[at] >> (4 * high) & 15] * np.exp2(b - 127.0))
+    return K, V
+
+
+def ranges(past, new, window=0, begin=None, end=None):
+    """[new] first position seen and the one behind the last, of one row."""
+    p = past + np.arange(new)
+    lo = np.zeros(new, dtype=np.int64) if begin is None else np.maximum(begin, 0)
+    hi = p + 1 if end is None else np.asarray(end)
+    if window:
+        lo = np.maximum(lo, p + 1 - window)
+    return lo, np.minimum(hi, past + new)
+
+
+def attention(q, k, v, past, scale, cap=0.0, slopes=None, window=0, begin=None, end=None):
+    """One row: q [new][heads][dh], k, v [past + new][kv heads][dh] float64.  Returns (out, bound): what a kernel may be off that rounds
+    weights and output to bf16, in fp32 otherwise.
+
+    As kv_reference.attention: weights are rounded by 2^-8 of themselves (8-bit ones once more: numerators only, by 2^-8 too), a score is off by (dh + 4) * 2^-24 of scale *
+    sum |q||k| and a cap's function hands that on by less than all of it.  What is added here: the cap's function is off by 3 *
+    2^-24 of 2 cap; the distance's share and what it is added to are rounded by 2^-24 of themselves each, the argument of
+    the exponential by 2^-23 of the difference of two scores: together no more than 2^-22 of (|score| + share + 3 cap) for a position and
+    for the one with the largest score, which all weights are relative to."""
+    new, heads, dh = q.shape
+    group = heads // k.shape[1]
+    out, bound = torch.zeros(new, heads, dh, dtype=torch.float64), torch.zeros(new, heads, dh, dtype=torch.float64)
+    lo, hi = (torch.from_numpy(np.asarray(x)) for x in ranges(past, new, window, begin, end))
+    j = torch.arange(k.shape[0])[None]
+    seen = (j >= lo[:, None]) & (j < hi[:, None])
+    away = (past + torch.arange(new)[:, None] - j).abs().double()
+    for h in range(heads):
+        kh, vh = k[:, h // group], v[:, h // group]
+        s = q[:, h] @ torch.nan_to_num(kh).t() * scale
+        size = q[:, h].abs() @ torch.nan_to_num(kh).abs().t() * scale
+        if cap:
+            s = cap * torch.tanh(s / cap)
+        share = away * (float(slopes[h]) if slopes is not None else 0.0)
+        s = torch.where(seen, s - share, -math.inf)
+        w = torch.where(seen.any(-1, keepdim=True), torch.softmax(s, -1), 0.0)
+        values = torch.where(seen[..., None], vh[None], 0.0)
+        o = (w[..., None] * values).sum(1)
+        eps = (dh + 4) * 2.0 ** -23 * size + 2.0 ** -22 * (size + share + 3 * cap)
+        top = torch.where(seen, s, -math.inf).argmax(-1, keepdim=True)
+        eps = 2.0 ** -8 * 2.02 + 2.0 ** -18 + torch.where(seen, eps + eps.gather(1, top), 0.0)
+        off = (w * eps)[..., None] * (values - o[:, None]).abs()
+        out[:, h] = o
+        bound[:, h] = off.sum(1) + 2.0 ** -8 * 1.01 * o.abs() + 2.0 ** -18 * (w[..., None] * values.abs()).sum(1) + 1e-37
+    return out, bound
+
+
+class Rows:
+    """Ragged rows of a cache, on the host in float64 and in pages on the device.  Pages are dealt out in random order; what no token
+    was filed to is garbage (NaN bits, exponents of NaN)."""
+
+    def __init__(self, elem, H, dh, page, past, new, seed=0, spare=0):
+        g = torch.Generator().manual_seed(seed)
+        self.elem, self.H, self.dh, self.page, self.past, self.new = elem, H, dh, page, past, new
+        self.total = [p + n for p, n in zip(past, new)]
+        need = [-(-t // page) for t in self.total]
+        order = torch.randperm(sum(need), generator=g).tolist()
+        self.table = torch.full((len(past), max(max(need), 1) + spare), -1, dtype=torch.int32)
+        for r, n in enumerate(need):
+            for i in range(n):
+                self.table[r, i] = order.pop()
+        self.pool = garbage(elem, sum(need) + 1, H, dh, page)
+        self.cache = skd.KvCache(self.pool, self.table.cuda(), H, dh, page, elem)
+        gain = 0.2 + 3 * torch.rand(H, dh, generator=g)
+        self.k = [(torch.randn(t, H, dh, generator=g) * gain).bfloat16() for t in self.total]
+        self.v = [torch.randn(t, H, dh, generator=g).bfloat16() for t in self.total]
+
+    def chunk(self, past, new):
+        first = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32, device="cuda")
+        return skd.KvChunk(first, torch.tensor(past, dtype=torch.int32, device="cuda"), sum(new), max(new), max(past))
+
+    def tokens(self, x, past, new):
+        return torch.cat([t[p:p + n] for t, p, n in zip(x, past, new)]).cuda()
+
+    def append(self, past, new):
+        self.cache.append(self.chunk(past, new), self.tokens(self.k, past, new), self.tokens(self.v, past, new))
+
+    def read(self, past, new, dtype=torch.float32):
+        k, v = (torch.full((sum(new), self.H, self.dh), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+        self.cache.read(self.chunk(past, new), k, v)
+        return k.cpu(), v.cpu()
+
+    def held(self, x, past, new):
+        return torch.cat([torch.from_numpy(as_held(t[p:p + n].double().numpy(), self.elem)) for t, p, n in zip(x, past, new)])
+
+    def scores(self, heads, cap=0.0, slopes=None, window=0, begin=None, end=None):
+        """slopes, begin, end: of all heads and tokens, lists or None."""
+        return skd.KvScores(cap, None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda"), window,
+                            *(None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda") for x in (begin, end)))
+
+    def attend(self, q, files=False, scale=None, out=None, **changes):
+        """As the call, with skd_kv_attend_scores if anything is changed."""
+        ch, heads = self.chunk(self.past, self.new), q.shape[1]
+        out = torch.full_like(q, 5.0) if out is None else out
+        kv = (self.tokens(self.k, self.past, self.new), self.tokens(self.v, self.past, self.new)) if files else ()
+        scale = scale or 1 / math.sqrt(self.dh)
+        if changes:
+            sc = self.scores(heads, **changes)
+            ws = torch.empty(self.cache.attend_scores_workspace(ch, heads, sc), dtype=torch.uint8, device="cuda")
+            self.cache.attend_scores(ch, q, out, scale, sc, *kv, workspace=ws)
+        else:
+            ws = torch.empty(self.cache.attend_workspace(ch, heads), dtype=torch.uint8, device="cuda")
+            self.cache.attend(ch, q, out, scale, *kv, workspace=ws)
+        torch.cuda.synchronize()
+        return out.cpu()
+
+    def check(self, q, out, scale=None, begin=None, end=None, **changes):
+        at = 0
+        for r, (p, n) in enumerate(zip(self.past, self.new)):
+            k, v = (torch.from_numpy(as_held(x[r].double().numpy(), self.elem)) for x in (self.k, self.v))
+            me = slice(at, at + n)
+            ref, bound = attention(q[me].cpu().double(), k, v, p, scale or 1 / math.sqrt(self.dh), begin=None if begin is None else np.array(begin[me]),
+                                   end=None if end is None else np.array(end[me]), **changes)
+            off = (out[me].double() - ref).abs() / bound
+            assert n == 0 or (off <= 1).all(), f"row {r}: {off.max()} of what is allowed"
+            at += n
+
+
+def garbage(elem, pages, H, dh, page):
+    if elem == BF16:
+        return torch.full((pages, H * page * 2 * dh), float("nan"), dtype=torch.bfloat16, device="cuda")
+    size = H * page * (2 * dh + 2) if elem == FP8 else H * page // 32 * 34 * dh
+    return torch.full((pages, size), 0x7f if elem == FP8 else 0xff, dtype=torch.uint8, device="cuda")
+
+
+# ---------------------------------------------------------------------------------------------- block tables
+def assign(table, pages, page, length, more, source=None):
+    """(table, copies, counts) as include/skd.h has them, entry by entry; table: a list of rows."""
+    R_, W = len(table), len(table[0]) if table else 0
+    room = W * page
+    held = [min(max(n, 0), room) for n in length]
+    upto = [min(h + max(m, 0), room) for h, m in zip(held, more)]
+    rows = []
+    for r in range(R_):
+        s = r if source is None else source[r]
+        old = table[s] if 0 <= s < R_ else [-1] * W
+        rows.append([p if i * page < upto[r] and 0 <= p < pages else -1 for i, p in enumerate(old)])
+
+    def to_write(r, i):
+        return upto[r] > held[r] and i * page < upto[r] and (i + 1) * page > held[r]
+
+    names, writes = {}, {}
+    for r in range(R_):
+        for i in range(W):
+            if rows[r][i] >= 0:
+                names.setdefault(rows[r][i], []).append((r, i))
+                if to_write(r, i):
+                    writes.setdefault(rows[r][i], []).append((r, i))
+    wanted = []
+    for r in range(R_):
+        for i in range(W):
+            p = rows[r][i]
+            if to_write(r, i) and not (p >= 0 and (len(names[p]) == 1 or (names[p] == writes.get(p) and writes[p][0] == (r, i)))):
+                wanted.append((r, i))
+    free = [p for p in range(pages) if p not in names]
+    copies, missing = [], max(len(wanted) - len(free), 0)
+    if missing:
+        rows = [[p if i * page < held[r] else -1 for i, p in enumerate(row)] for r, row in enumerate(rows)]
+    else:
+        for (r, i), p in zip(wanted, free):
+            if rows[r][i] >= 0 and i * page < held[r]:
+                copies.append((rows[r][i], p))
+            rows[r][i] = p
+    named = {p for row in rows for p in row if p >= 0}
+    return rows, copies, [len(named), missing, len(copies)]
+
+
+def compact(table, pages):
+    used = sorted({p for row in table for p in row if 0 <= p < pages})
+    n = len(used)
+    free = [p for p in range(n) if p not in set(used)]
+    copies = list(zip([p for p in used if p >= n], free))
+    place = dict(copies)
+    return [[place.get(p, p) if 0 <= p < pages else -1 for p in row] for row in table], copies, [n, 0, len(copies)]
