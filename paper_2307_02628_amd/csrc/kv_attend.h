@@ -15,6 +15,8 @@ struct AttendPlan {
 
 namespace {
 
+enum { SC_MASK = 1, SC_CAP = 2, SC_SLOPES = 4 };  // what of a call's scoring a kernel is made for (no mask, no other)
+
 // ------------------------------------------------------------------ attention
 // A query tile is 16 of the R = new * group queries of a row and kv head, in the order (token, head of the group): the 16
 // columns of the matrix instructions.  The softmax works in units of log2 against a reference that is raised only by more
@@ -29,8 +31,12 @@ namespace {
 // Those of 4-bit keys and values are operands of the conversion (32 elements of a value have one each, so that the weights would
 // have to be multiplied for every 32); a value that is not finite is in them, and is added for the queries that see it.
 //
-// Scores that are capped, or fall with the distance, are changed in place into units of log2 (SC kernels); a cap's constant part
-// is the same for every position and left out.  A query of theirs sees positions low .. limit - 1 of its own.
+// Changed scores and masks (SC, bits of what a call asks for).  A query sees positions low .. limit - 1 of its own.  The share of
+// the distance, over what scores are multiplied by, is where the matrix instructions' sums begin: one instruction a score.  A cap's
+// function is applied in place, but for its factor, which takes that place, and for its constant part, which is the same for every position.
+// (Its four instructions, two of them of a quarter of the rate, stand in the code as such: with a branch around them, or around
+// the share, products and exponentials of two blocks no longer mixed: 512 tokens of 8 rows behind 2048, 32 heads of 128, bf16, us:
+// slopes 217, so 162; cap 194, 177; masks alone 156, 144, which is what the plain attention takes.)
 
 // bf16x8 of two words of codes, times the power of two whose exponent byte is `e` (255: NaN)
 __device__ inline bf16x8 widen(uint32_t a, uint32_t b, uint32_t e) {
@@ -91,26 +97,10 @@ __device__ inline bf16x8 key_fragment(const uint32x4 *k, const uint32_t *e, int 
 }
 
 // ------------------------------------------------------------------ changed scores
-// In units of log2, from q . k.  cap tanh(x) = cap - 2 cap / (1 + exp(2 x)), here without the constant: off by up to 3 * 2^-24 of
-// 2 cap (exponential, sum, reciprocal), which for the largest cap, 1024, is 2^-11.4 of a weight, against the 2^-8 of its rounding.
-__device__ inline float change_one(const KvScoring &sc, bool capped, float s) {
-  return capped ? sc.out * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(sc.in * s)) : s * sc.out;
-}
-// away: of the query from the lane's first position.  (Distances are exact up to 2^24, and beyond to 2^-24.)
-__device__ inline void change(const KvScoring &sc, float slope, int away, floatx4 (&S)[2]) {
-  if (sc.capped) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = change_one(sc, true, S[j >> 2][j & 3]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = change_one(sc, false, S[j >> 2][j & 3]);
-  }
-  if (sc.slopes) {
-    const float d = (float)away;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = __builtin_fmaf(-slope, __builtin_fabsf(d - (float)(16 * (j >> 2) + (j & 3))), S[j >> 2][j & 3]);
-  }
-}
+// cap tanh(x) = cap - 2 cap / (1 + exp(2 x)), here without the constant and times 1 / (2 cap): off by up to 3 * 2^-24 (exponential,
+// sum, reciprocal), which for the largest cap, 1024, is 2^-11.4 of a weight, against the 2^-8 of its rounding.  (As a fraction of
+// polynomials: 11 instructions and one of a quarter of the rate, instead of 2 and two.)
+__device__ inline float capped(float in, float s) { return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(in * s)); }
 
 __device__ inline bf16x8 pack8(const float (&p)[8]) {
   return __builtin_bit_cast(bf16x8, (uint32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])}));
@@ -287,6 +277,10 @@ __device__ inline void add_odd(floatx4 &O, const uint32x4 &v, bf16x8 vis) {
   }
 }
 
+// what scores are multiplied by, in units of log2
+template <int SC>
+__device__ inline float factor(const KvAttend &a) { return SC & SC_CAP ? a.sc.out : a.c; }
+
 // What a workgroup computes: NQ queries from q0 on of a row and kv head, on one share of their keys.
 struct Share {
   RowTokens t;
@@ -300,7 +294,7 @@ struct Share {
   // 1 at a time, us: 8 prompts of 2048, 32 heads of 128, bf16 428, 411, 440; 512 tokens behind 2048 203, 192, 194; 8 bits 386,
   // 380, 440 and 196, 192, 206; 32 prompts of 512, heads of 64, 8 bits 88, 93, 122).
   static constexpr int TOGETHER = 16;
-  template <int NQ, bool SC>
+  template <int NQ, int SC>
   __device__ static Share of(const KvAttend &a, int pairs, bool files) {
     Share s;
     const int H = a.kv.g.H, tiles = gridDim.x / pairs, id = blockIdx.x;
@@ -325,7 +319,7 @@ struct Share {
       s.whole_lo = 0;
       s.whole_hi = 1 << 30;
       for (int q = s.q0 + (threadIdx.x & 63); q < min(s.q0 + NQ, s.R); q += 64) {
-        const Range x = s.range<true>(a, q);
+        const Range x = s.range<SC>(a, q);
         if (x.lo < x.hi) from = min(from, x.lo);
         upto = max(upto, x.hi);
         s.whole_lo = max(s.whole_lo, x.lo < x.hi ? x.lo : 1 << 30);
@@ -342,6 +336,7 @@ struct Share {
       nblk = one((min(upto, s.held) + 31) >> 5);
       first = min(one(from >> 5), nblk);
       s.whole_lo = one((s.whole_lo + 31) >> 5);
+      if constexpr (SC & SC_SLOPES) s.whole_hi = min(s.whole_hi, s.seen(a, s.q0));  // (where distances have a sign)
       s.whole_hi = one(min(s.whole_hi, s.held) >> 5);
     } else {
       nblk = (min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held) + 31) >> 5;
@@ -351,13 +346,20 @@ struct Share {
     const int per = (nblk - first + a.splits - 1) / a.splits;
     s.lo = first + (int)blockIdx.y * per;
     s.hi = min(s.lo + per, nblk);
+    if constexpr (SC) {
+      s.whole_lo = min(max(s.whole_lo, s.lo), max(s.hi, s.lo));
+      s.whole_hi = max(min(s.whole_hi, s.hi), s.whole_lo);
+    }
     return s;
   }
+  // SC: the blocks that every query sees whole come first, the others, before and behind them, then: masks are in the code once.
+  __device__ int wholes() const { return whole_hi - whole_lo; }
+  __device__ int block(int v) const { return v < wholes() ? whole_lo + v : v < whole_hi - lo ? v - wholes() + lo : v + lo; }
   struct Range {
     int lo, hi;
   };
   // Positions lo .. hi - 1 of those that the row has are seen by query q (lo = hi = 0: none).
-  template <bool SC>
+  template <int SC>
   __device__ Range range(const KvAttend &a, int q) const {
     if constexpr (!SC) return Range{0, seen(a, q)};
     const int p = t.past + q / a.group;
@@ -366,8 +368,8 @@ struct Share {
     if (a.sc.window) x.lo = max(x.lo, p + 1 - a.sc.window);
     return x.lo < x.hi ? x : Range{0, 0};
   }
-  // slope of query q, in units of log2
-  __device__ float slope(const KvAttend &a, int q) const { return a.sc.slopes ? a.sc.slopes[head(a, q)] * 1.4426950408889634f : 0.f; }
+  template <int SC>
+  __device__ float slope(const KvAttend &a, int q) const { return a.sc.slopes[head(a, q)] * 1.4426950408889634f / factor<SC>(a); }
   __device__ int seen(const KvAttend &a, int q) const { return t.past + q / a.group + 1; }  // positions that query q sees
   __device__ long token(const KvAttend &a, int q) const { return t.at + (long)(q / a.group) * a.tk.step; }
   __device__ int head(const KvAttend &a, int q) const { return h * a.group + q % a.group; }
@@ -375,14 +377,52 @@ struct Share {
 // What a lane needs to know of a query: it sees positions low .. limit - 1 of those that the cache holds.
 struct Seen {
   int low, limit, pos;
-  float slope;
-  template <bool SC>
+  float slope;  // over what scores are multiplied by
+  template <int SC>
   __device__ static Seen of(const KvAttend &a, const Share &s, int q) {
     if (q >= s.R) return Seen{0, 0, 0, 0.f};
     const Share::Range x = s.range<SC>(a, q);
-    return Seen{x.lo, min(x.hi, s.held), s.t.past + q / a.group, SC ? s.slope(a, q) : 0.f};
+    return Seen{x.lo, min(x.hi, s.held), s.t.past + q / a.group, SC & SC_SLOPES ? s.slope<SC>(a, q) : 0.f};
   }
 };
+// Where the scores of a block begin; from: distance of the query from the lane's first position; before: no position lies behind it.
+// (A distance is exact up to 2^24, and beyond to 2^-24 of itself.)
+template <int SC>
+__device__ inline void share_of(bool before, float slope, int from, floatx4 (&S)[2]) {
+  if constexpr (SC & SC_SLOPES) {
+    const float d = (float)from;
+    if (before) {
+      const float b = -slope * d;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = __builtin_fmaf(slope, (float)block_pos(j, 0), b);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = -slope * __builtin_fabsf(d - (float)block_pos(j, 0));
+    }
+  } else {
+    S[0] = S[1] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+// LATE: the share is added at the end, as it is to capped scores (one tile of 128-wide heads has no registers for it before).
+template <int SC, bool LATE>
+__device__ inline void begin_scores(bool before, const Seen &x, int base, floatx4 (&S)[2]) {
+  share_of<LATE || SC & SC_CAP ? 0 : SC>(before, x.slope, x.pos - base, S);
+}
+template <int SC, bool LATE>
+__device__ inline void end_scores(const KvScoring &sc, bool before, const Seen &x, int base, floatx4 (&S)[2]) {
+  if constexpr (SC & SC_CAP) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) S[j >> 2][j & 3] = capped(sc.in, S[j >> 2][j & 3]);
+  }
+  if constexpr (SC & SC_SLOPES && (LATE || SC & SC_CAP)) {
+    floatx4 B[2];
+    float slope = x.slope;
+    if constexpr (LATE) asm volatile("" : "+v"(slope), "+v"(S[0]), "+v"(S[1]));  // (not before the products, where registers are few)
+    share_of<SC>(before, slope, x.pos - base, B);
+    S[0] += B[0];
+    S[1] += B[1];
+  }
+}
 template <int DH>
 __device__ inline float *part_of(const KvAttend &a, int split, long token, int head) {
   return a.part + (((long)split * a.tk.tokens + token) * a.heads + head) * (DH + 2);
@@ -410,9 +450,9 @@ __device__ inline bool not_finite_(const Tile (&tile)[NT]) {
 }
 template <int DH, typename Tile, int NT>
 __device__ inline bool not_finite(const Tile (&tile)[NT]) { return not_finite_<DH, NT, Tile>(tile); }
-// The numerators of a wave's tiles again, over blocks first, first + step, ... below end of bf16 pages, against the references
+// The numerators of a wave's tiles again, over blocks first, first + step, ... below end (SC: in their order) of bf16 pages, against the references
 // that the wave has arrived at: values without their infinities and NaNs, which are then added.
-template <int DH, bool SC, typename Tile, int NT>
+template <int DH, int SC, typename Tile, int NT>
 __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, int q0, int first, int step, int end, Tile (&tile)[NT]) {
   constexpr int QC = DH / 32, VM = DH / 16;
   const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15, bpp = a.kv.g.page_tokens >> 5;
@@ -420,8 +460,8 @@ __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, in
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int m = 0; m < VM; ++m) tile[t].O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int blk = first; blk < end; blk += step) {
-    const int page = page_of(a.kv, s.r, blk);
+  for (int at = first; at < end; at += step) {
+    const int blk = SC ? s.block(at) : at, page = page_of(a.kv, s.r, blk);
     if (page < 0) continue;
     const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)s.h * bpp + blk % bpp) * (128 * DH)) + lane;
     const Keep keep(s.held - blk * 32, grp);
@@ -432,18 +472,18 @@ __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, in
       const Seen x = Seen::of<SC>(a, s, q0 + 16 * t + col);
       const int lim = x.limit - blk * 32, lo = x.low - blk * 32;
       floatx4 S[2];
+      begin_scores<SC, true>(false, x, blk * 32 + 4 * grp, S);
 #pragma unroll
       for (int tl = 0; tl < 2; ++tl) {
-        S[tl] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < QC; ++c) S[tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, src[(tl * QC + c) * 64]), qf[c], S[tl], 0, 0, 0);
       }
-      if constexpr (SC) change(a.sc, x.slope, x.pos - blk * 32 - 4 * grp, S);
+      end_scores<SC, true>(a.sc, false, x, blk * 32 + 4 * grp, S);
       float p[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        p[j] = hidden<SC>(j, lo, lim, grp) ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], SC ? 1.0f : a.c, -tile[t].m_ref));
-      const bf16x8 pv = pack8(p), vis = visible<SC>(lo, lim, grp);
+        p[j] = hidden<SC != 0>(j, lo, lim, grp) ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(S[j >> 2][j & 3], factor<SC>(a), -tile[t].m_ref));
+      const bf16x8 pv = pack8(p), vis = visible<SC != 0>(lo, lim, grp);
 #pragma unroll
       for (int m = 0; m < VM; ++m) {
         uint32x4 v = src[4 * DH + m * 64], w;
@@ -466,7 +506,7 @@ struct KvBlock {
   uint32x4 k[key_pieces(DH, EL)], v[value_pieces(DH, EL)];
   uint32_t ke[2], ve[EL == EL_FP4 ? DH / 16 : 2];  // exponents: of key 16 tl + (lane & 15) (K), of keys 16 tl + 4 (lane >> 4) .. + 3 (V)
 };
-template <int DH, int EL, bool SC, int NT, int NW>
+template <int DH, int EL, int SC, int NT, int NW>
 __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int pairs) {
   constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
   constexpr int QC = DH / 32, VM = DH / 16, NQ = 16 * NT;
@@ -539,15 +579,16 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   };
   auto seen_of = [&](int t) {
     if constexpr (!SC || !LDS_Q) return seen[t];
-    asm volatile("" ::: "memory");  // (read where it is needed, not kept)
-    return sh_seen[col];
+    int at = threadIdx.x;
+    asm volatile("" : "+v"(at)::"memory");  // (read where it is needed, not kept, nor its place)
+    return sh_seen[at & 15];
   };
   // base: first position of the block; valid: positions that the row has
   auto use = [&](auto masked_, int base, Block &b, int valid) {
     constexpr bool masked = decltype(masked_)::value;
     floatx4 S[NT][2];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) begin_scores<SC, LDS_Q>(!masked, seen_of(t), base + 4 * grp, S[t]);
 #pragma unroll
     for (int c = 0; c < QC; ++c) {
       bf16x8 x[NT];
@@ -569,8 +610,8 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const Seen x = seen_of(t);
-      if constexpr (SC) change(a.sc, x.slope, x.pos - base - 4 * grp, S[t]);
-      pv[t] = tile[t].template weights<FP8, SC>(masked, S[t], SC ? 1.0f : a.c, SC ? x.low - base : 0, x.limit - base, grp, vs);
+      end_scores<SC, LDS_Q>(a.sc, !masked, x, base + 4 * grp, S[t]);
+      pv[t] = tile[t].template weights<FP8, SC != 0>(masked, S[t], factor<SC>(a), x.low - base, x.limit - base, grp, vs);
     }
     if constexpr (FP4) {
       if (masked) {
@@ -581,7 +622,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
           from[t] = x.low - base;
           to[t] = x.limit - base;
         }
-        odd_exponents<DH, SC, NT>(b.ve, tile, from, to);
+        odd_exponents<DH, SC != 0, NT>(b.ve, tile, from, to);
       }
 #pragma unroll
       for (int i = 0; i < DH / 32; ++i) {
@@ -618,30 +659,43 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   };
   // place of the wave's next block, whose page's number is asked for ahead of the use of the one before
   const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
-  int blk = s.lo + wave, ip = blk / bpp, ib = blk % bpp;
+  int blk = SC ? wave : s.lo + wave, ip, ib;  // (SC: in their order)
+  auto place = [&]() {
+    const int b = SC ? s.block(blk) : blk;
+    ip = b / bpp;
+    ib = b % bpp;
+  };
+  place();
   auto entry = [&]() { return table[min(ip, a.kv.g.max_pages - 1)]; };
   int number = entry();
   auto step = [&](auto masked_) {
     const bool is = number >= 0 && number < a.kv.pages && ip < a.kv.g.max_pages;
     Block b;
     if (is) load(number, ib, b);
-    ip += NW / bpp;
-    ib += NW % bpp;
-    if (ib >= bpp) {
-      ib -= bpp;
-      ++ip;
+    const int now = SC ? s.block(blk) : blk;
+    blk += NW;
+    if constexpr (SC) {
+      place();
+    } else {
+      ip += NW / bpp;
+      ib += NW % bpp;
+      if (ib >= bpp) {
+        ib -= bpp;
+        ++ip;
+      }
     }
     number = entry();
-    if (is) use(masked_, blk * 32, b, s.held);
-    blk += NW;
+    if (is) use(masked_, now * 32, b, s.held);
   };
   if constexpr (SC) {
-    while (blk < min(s.whole_lo, s.hi)) step(std::true_type());
+    while (blk < s.wholes()) step(std::false_type());
+    while (blk < s.hi - s.lo) step(std::true_type());
+  } else {
+    while (blk < min(s.whole_hi, s.hi)) step(std::false_type());
+    while (blk < s.hi) step(std::true_type());
   }
-  while (blk < min(s.whole_hi, s.hi)) step(std::false_type());
-  while (blk < s.hi) step(std::true_type());
   if constexpr (EL == EL_BF16) {
-    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, s.lo + wave, NW, s.hi, tile);
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, SC ? wave : s.lo + wave, NW, SC ? s.hi - s.lo : s.hi, tile);
   }
   uint32_t ke = 0, ve = 0;  // exponents of the new token
   if constexpr (NT == 1) {
@@ -678,8 +732,9 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       auto &x = tile[0];
       float score = __shfl(S[0], col);
       if constexpr (SC) {  // (at a distance of 0)
-        const Share::Range sees = q0 + col < R ? s.range<true>(a, q0 + col) : Share::Range{0, 0};
-        score = change_one(a.sc, a.sc.capped, score);
+        const Share::Range sees = q0 + col < R ? s.range<SC>(a, q0 + col) : Share::Range{0, 0};
+        if constexpr (SC & SC_CAP) score = capped(a.sc.in, score);
+        score *= factor<SC>(a);
         if (!(sees.lo <= s.held && s.held < sees.hi)) score = -INFINITY;
       } else {
         score *= a.c;
@@ -808,13 +863,16 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 // conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.
 constexpr int rows_stages(int dh, int el) { return el != EL_BF16 ? 8 : dh == 128 ? 5 : 6; }  // (64: three workgroups, 97 -> 77 us for 32 prompts of 512)
 constexpr size_t rows_lds(int dh, int el) { return (size_t)rows_stages(dh, el) * ((key_pieces(dh, el) + value_pieces(dh, el)) * 1024 + (el != EL_BF16 ? 256 : 0)); }
-template <int DH, int EL, bool SC>
-__global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs) {
+template <int DH, int EL, int SC>
+__global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(KvAttend a, int pairs) {
   constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
   constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = rows_stages(DH, EL), NQ = 16 * NT * NW;
   constexpr int KF = key_pieces(DH, EL), FR = KF + value_pieces(DH, EL), LPW = FR < NW ? 1 : FR / NW;  // fragments a stage, loads of a wave
   constexpr int STAGE = FR * 64 + (FP8 || FP4 ? 16 : 0);  // 16-byte pieces; behind 8- and 4-bit blocks 256 bytes for their exponents
   extern __shared__ uint32x4 ring[];               // [NS][STAGE]
+  // 64-wide heads: three workgroups a CU, if what is known of the queries is not kept in registers
+  constexpr bool LDS_SEEN = SC && DH == 64;
+  __shared__ Seen sh_seen[LDS_SEEN ? NQ : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
   const Share s = Share::of<NQ, SC>(a, pairs, false);
   if (!s.any) return;
@@ -827,8 +885,15 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     seen[t] = Seen::of<SC>(a, s, q0 + 16 * t + col);
+    if (LDS_SEEN && grp == 0) sh_seen[wave * (16 * NT) + 16 * t + col] = seen[t];  // (read by this wave alone)
     tile[t].clear();
   }
+  auto seen_of = [&](int t) {
+    if constexpr (!LDS_SEEN) return seen[t];
+    int at = threadIdx.x;
+    asm volatile("" : "+v"(at)::"memory");  // (read where it is needed, not kept, nor its place)
+    return sh_seen[wave * (16 * NT) + 16 * t + (at & 15)];
+  };
   if constexpr (SC) {
     int from = 1 << 30, upto = 0;
 #pragma unroll
@@ -848,11 +913,13 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
   // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked, as is every block from the
   // moment on at which a window has an entry that is no page.
   const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
-  int ip = s.lo / bpp, ib = s.lo % bpp, pages = 0, window = -1;
+  const int begin = SC ? s.block(0) : s.lo;
+  int ip = begin / bpp, ib = begin % bpp, pages = 0, window = -1;
   uint32_t none = 0;                               // a bit for each stage: its block has no page
-  int into = 0, from = 0, asked = s.lo;            // stages of the next block requested and used; blocks requested
+  int into = 0, from = 0, asked = SC ? 0 : s.lo;   // stages of the next block requested and used; blocks requested (SC: in their order)
+  int turn = SC ? s.wholes() : 0;                  // SC: the next block that does not follow on the one before
   bool gaps = false;
-  const int ip_end = (s.hi + bpp - 1) / bpp;
+  const int ip_end = (s.hi + bpp - 1) / bpp, asked_end = SC ? s.hi - s.lo : s.hi;
   const uint32x4 *src = nullptr;                   // this wave's part of the next block
   const unsigned char *ex_src = nullptr;           // its exponents
   bool is = false;
@@ -892,14 +959,23 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
     ++asked;
     src += block_bytes(DH, EL) / 16;
     ex_src += FP4 ? block_bytes(DH, EL) : 64;
-    if (++ib == bpp) {
+    bool other = ++ib == bpp;  // page
+    if (other) {
       ib = 0;
-      if (++ip < ip_end) new_page();
+      ++ip;
     }
+    if (SC && asked == turn) {  // (behind the whole ones, and where these were)
+      const int blk = s.block(asked);
+      turn = turn == s.wholes() ? s.whole_hi - s.lo : 0;
+      ip = blk / bpp;
+      ib = blk % bpp;
+      other = true;
+    }
+    if (other && ip < ip_end) new_page();
   };
   constexpr int LOADS = LPW + (FP8 || FP4 ? 1 : 0);
   for (int i = 0; i < NS - 2; ++i)
-    if (asked < s.hi) request();
+    if (asked < asked_end) request();
 #pragma unroll
   for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
   wait_vmcnt<0>();  // (waited for inside the loop, the queries would make the compiler wait for the ring as well)
@@ -909,7 +985,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
     for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
 
   // scores of a block: S[t][tl][i] of position 16 tl + 4 grp + i
-  auto scores = [&](int stage, floatx4 (&S)[NT][2]) {
+  auto scores = [&](int stage, int base, bool before, floatx4 (&S)[NT][2]) {
     const uint32x4 *kv = ring + stage * STAGE + lane;
     const unsigned char *ex = (const unsigned char *)(ring + stage * STAGE + FR * 64);
     uint32x4 kw[KF];
@@ -921,7 +997,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
       for (int i = 0; i < DH / 64; ++i) ke[i] = ((const uint32_t *)(ex + col * (DH / 16)))[i];
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) begin_scores<SC, false>(before, seen_of(t), base + 4 * grp, S[t]);
 #pragma unroll
     for (int c = 0; c < QC; ++c)
 #pragma unroll
@@ -973,7 +1049,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
   auto use = [&](int blk, bool no_page) {
     const int base = blk * 32;
     floatx4 S[NT][2];
-    scores(from, S);
+    scores(from, base, false, S);
     float vs[8];
     if constexpr (FP8) {
       uint32_t ve[2];
@@ -984,8 +1060,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
     bf16x8 pv[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if constexpr (SC) change(a.sc, seen[t].slope, seen[t].pos - base - 4 * grp, S[t]);
-      pv[t] = tile[t].template weights<FP8, SC>(true, S[t], SC ? 1.0f : a.c, SC ? seen[t].low - base : 0, no_page ? 0 : seen[t].limit - base, grp, vs);
+      const Seen x = seen_of(t);
+      end_scores<SC, false>(a.sc, false, x, base + 4 * grp, S[t]);
+      pv[t] = tile[t].template weights<FP8, SC != 0>(true, S[t], factor<SC>(a), x.low - base, no_page ? 0 : x.limit - base, grp, vs);
     }
     uint32x4 vw[FR - KF];
     values_of(from, vw);
@@ -994,11 +1071,12 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
       int lo[NT], to[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        lo[t] = seen[t].low - base;
-        to[t] = no_page ? 0 : seen[t].limit - base;
+        const Seen x = seen_of(t);
+        lo[t] = x.low - base;
+        to[t] = no_page ? 0 : x.limit - base;
       }
       exponents4(from, ve);
-      odd_exponents<DH, SC, NT>(ve, tile, lo, to);
+      odd_exponents<DH, SC != 0, NT>(ve, tile, lo, to);
       add_values4(vw, ve, pv);
     } else {
       add_values(vw, pv);
@@ -1008,7 +1086,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
   // are formed side by side, and the values are on their way before.
   auto use_two = [&](int one, int two, int base) {
     const int stage[2] = {one, two};
-    const float c = SC ? 1.0f : a.c;
+    const float c = factor<SC>(a);
     floatx4 S[2][NT][2];
     uint32_t ve[2][2];
     int power[2][8];  // of the values; 2 rows of 1023 behind 8193, 8 bits, us: by ldexp 338, as factors, 0 for byte 0, 341, as they are 358
@@ -1017,7 +1095,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       __builtin_amdgcn_s_setprio(1);  // (before the other waves' exponentials: 140 -> 136 us)
-      scores(stage[u], S[u]);
+      scores(stage[u], base + 32 * u, true, S[u]);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (FP8) {
         factor_words(stage[u], ve[u]);
@@ -1026,10 +1104,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
 #pragma unroll
         for (int i = 0; i < 2; ++i) raise |= (((ve[u][i] & 0x7f7f7f7fu) + 0x01010101u) & ve[u][i] & 0x80808080u) != 0;
       }
-      if constexpr (SC) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) change(a.sc, seen[t].slope, seen[t].pos - base - 32 * u - 4 * grp, S[u][t]);
-      }
+      for (int t = 0; t < NT; ++t) end_scores<SC, false>(a.sc, true, seen_of(t), base + 32 * u + 4 * grp, S[u][t]);
     }
     values_of(stage[0], vw);
     float p[2][NT][8];
@@ -1113,29 +1189,34 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    while (asked < min(s.hi, blk + NS)) request();
+    while (asked < min(asked_end, blk + NS)) request();
   };
-  auto single = [&](int blk) {
-    open(blk, 1);
+  auto single = [&](int at) {
+    open(at, 1);
+    const int blk = SC ? s.block(at) : at;
     const bool no_page = none >> from & 1;
     if (!FP4 && (no_page || blk * 32 + 32 > s.held)) clear(no_page ? 0 : s.held - blk * 32);  // (4 bits: codes are finite, exponents are looked at)
     if (blk < last && (!SC || blk >= from_blk)) use(blk, no_page);
     from = next(from);
   };
-  auto pair = [&](int blk) {
-    open(blk, 2);
+  auto pair = [&](int at) {
+    open(at, 2);
+    const int blk = SC ? s.whole_lo + at : at;
     const int second = next(from);
     if (busy) use_two(from, second, blk * 32);
     from = next(second);
   };
   int blk = s.lo;
   if constexpr (SC) {
-    for (; blk < min(s.whole_lo, s.hi); ++blk) single(blk);
+    int v = 0;
+    for (; v + 2 <= s.wholes() && !gaps; v += 2) pair(v);
+    for (; v < s.hi - s.lo; ++v) single(v);
+  } else {
+    for (; blk + 2 <= min(s.whole_hi, s.hi) && !gaps; blk += 2) pair(blk);
+    for (; blk < s.hi; ++blk) single(blk);
   }
-  for (; blk + 2 <= min(s.whole_hi, s.hi) && !gaps; blk += 2) pair(blk);
-  for (; blk < s.hi; ++blk) single(blk);
   if constexpr (EL == EL_BF16) {
-    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, SC ? max(s.lo, from_blk) : s.lo, 1, last, tile);
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, SC ? 0 : s.lo, 1, SC ? s.hi - s.lo : last, tile);
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -1165,7 +1246,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttend a, int pairs
   }
 }
 
-template <int DH, int EL, bool SC, int NT, int NW>
+template <int DH, int EL, int SC, int NT, int NW>
 void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int pairs) {
   const int cols = std::min(16, a.tk.max_new * a.group);
   const size_t lds = (size_t)NW * cols * (DH + 2) * sizeof(float);
@@ -1173,7 +1254,7 @@ void launch_attend(hipStream_t s, const KvAttend &a, dim3 grid, int pairs) {
   if (lds + 8192 > 64 * 1024) (void)allow_lds(done, {(const void *)k_kv_attend<DH, EL, SC, NT, NW>}, NW * 16 * (DH + 2) * sizeof(float));
   SKD_LAUNCH((k_kv_attend<DH, EL, SC, NT, NW>), grid, dim3(NW * 64), lds, s, a, pairs);
 }
-template <int DH, int EL, bool SC>
+template <int DH, int EL, int SC>
 void attend_pages(hipStream_t s, const KvAttend &a, const AttendPlan &p) {
   const dim3 grid((unsigned)(p.tiles * p.pairs), a.splits);
   if (p.nq == 128) {
@@ -1188,7 +1269,7 @@ void attend_pages(hipStream_t s, const KvAttend &a, const AttendPlan &p) {
     launch_attend<DH, EL, SC, 1, 8>(s, a, grid, p.pairs);
   }
 }
-template <int EL, bool SC>
+template <int EL, int SC>
 void attend_elem(hipStream_t s, const KvAttend &a, const AttendPlan &p) {
   if (a.kv.g.dh == 64) attend_pages<64, EL, SC>(s, a, p);
   else attend_pages<128, EL, SC>(s, a, p);

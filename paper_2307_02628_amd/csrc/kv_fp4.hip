@@ -1,4 +1,4 @@
-// Pages of 4 bits: filed, read back and attended to, with scores as they are or changed.
+// Pages of 4 bits: filed, read back and attended to.
 #include "kv_attend.h"
 #include "kv_file.h"
 
@@ -6,9 +6,6 @@ namespace skd {
 
 void kv_append_fp4(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows &k, const KvRows &v) { append_elem<EL_FP4>(s, kv, tk, k, v); }
 void kv_read_fp4(hipStream_t s, const KvView &kv, const KvTokens &tk, bool bf16, const KvRows &k, const KvRows &v) { read_elem<EL_FP4>(s, kv, tk, bf16, k, v); }
-void kv_attend_fp4(hipStream_t s, const KvAttend &a, const AttendPlan &p) {
-  if (a.scored) attend_elem<EL_FP4, true>(s, a, p);
-  else attend_elem<EL_FP4, false>(s, a, p);
-}
+void kv_attend_fp4(hipStream_t s, const KvAttend &a, const AttendPlan &p) { attend_elem<EL_FP4, 0>(s, a, p); }
 
 }  // namespace skd

@@ -49,7 +49,7 @@ void kv_read(hipStream_t s, const KvView &kv, const KvTokens &tk, bool bf16, con
 // What becomes of a score s = scale * q . k, in units of log 2, and which positions a token sees.
 struct KvScoring {
   bool capped;
-  float in, out;            // factors of q . k: capped: 2 / (log(2) cap) of scale * q . k, and -2 cap / log(2) of the rest; else out alone
+  float in, out;            // capped: q . k becomes -out / (1 + 2^(in q . k))
   const float *slopes;      // [heads] or null
   int window;               // 0: none
   const int32_t *begin, *end;  // [tokens] or null

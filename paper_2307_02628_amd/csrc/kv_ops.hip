@@ -5,8 +5,10 @@
 
 namespace skd {
 
-// the other kinds: kv_scores.hip, kv_fp4.hip
-void kv_attend_scored(hipStream_t s, const KvAttend &a, const AttendPlan &p);
+// the other kinds: kv_scores*.hip, kv_fp4.hip
+void kv_attend_scored_bf16(hipStream_t s, const KvAttend &a, const AttendPlan &p);
+void kv_attend_scored_fp8(hipStream_t s, const KvAttend &a, const AttendPlan &p);
+void kv_attend_scored_fp4(hipStream_t s, const KvAttend &a, const AttendPlan &p);
 void kv_attend_fp4(hipStream_t s, const KvAttend &a, const AttendPlan &p);
 void kv_append_fp4(hipStream_t s, const KvView &kv, const KvTokens &tk, const KvRows &k, const KvRows &v);
 void kv_read_fp4(hipStream_t s, const KvView &kv, const KvTokens &tk, bool bf16, const KvRows &k, const KvRows &v);
@@ -168,10 +170,10 @@ void kv_attend(hipStream_t s, const KvAttend &call) {
     kv_append(s, a.kv, a.tk, a.k, a.v);
     a.k.p = nullptr;
   }
-  if (a.kv.fp4) kv_attend_fp4(s, a, p);
-  else if (a.scored) kv_attend_scored(s, a, p);
-  else if (a.kv.fp8) attend_elem<EL_FP8, false>(s, a, p);
-  else attend_elem<EL_BF16, false>(s, a, p);
+  if (a.scored) (a.kv.fp4 ? kv_attend_scored_fp4 : a.kv.fp8 ? kv_attend_scored_fp8 : kv_attend_scored_bf16)(s, a, p);
+  else if (a.kv.fp4) kv_attend_fp4(s, a, p);
+  else if (a.kv.fp8) attend_elem<EL_FP8, 0>(s, a, p);
+  else attend_elem<EL_BF16, 0>(s, a, p);
   if (a.splits > 1) a.kv.g.dh == 64 ? merge<64>(s, a) : merge<128>(s, a);
 }
 

@@ -181,7 +181,7 @@ static int attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float
     a.sc.capped = sc->cap != 0.f;
     a.sc.in = a.sc.capped ? (float)(2.0 * 1.4426950408889634 * (double)scale / (double)sc->cap) : 0.f;
     if (!std::isfinite(a.sc.in)) return SKD_ERR_RANGE;
-    a.sc.out = a.sc.capped ? -2.0f * LOG2E * sc->cap : c;
+    a.sc.out = a.sc.capped ? 2.0f * LOG2E * sc->cap : 0.f;
     a.sc.slopes = sc->slopes;
     a.sc.window = window_of(sc);
     a.sc.begin = sc->begin;
