@@ -51,9 +51,12 @@ __device__ inline float kv8_factor(uint32_t word, int i) {
   const uint32_t e = word >> (8 * i) & 255u;
   return __uint_as_float(e == 255 ? 0x7fc00000u : max(e << 23, 0x00400000u));
 }
-// bf16x8 of a word of eight 4-bit codes, times the power of two whose exponent byte is `e` (255: NaN)
-__device__ inline bf16x8 widen4(uint32_t w, uint32_t e) {
-  const float scale = __uint_as_float(e << 23);
+// The power of two of byte i of a word, as the conversions take it: the exponent of an fp32 number whatever its other bits are (255: NaN).
+__device__ inline float scale4(uint32_t word, int i) {
+  return __uint_as_float(i == 0 ? word << 23 : i == 1 ? word << 15 : i == 2 ? word << 7 : word >> 1);
+}
+// bf16x8 of a word of eight 4-bit codes
+__device__ inline bf16x8 widen4(uint32_t w, float scale) {
   const bf16x2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)};
   return bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
@@ -63,10 +66,10 @@ __device__ inline void widen4_values(const uint32_t (&w)[2], const uint32_t (&e)
   uint32_t x[8];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    x[4 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float((e[i] & 255u) << 23), 0));
-    x[4 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float((e[i] >> 8 & 255u) << 23), 1));
-    x[4 * i + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float((e[i] >> 16 & 255u) << 23), 2));
-    x[4 * i + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], __uint_as_float(e[i] >> 24 << 23), 3));
+    x[4 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(e[i], 0), 0));
+    x[4 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(e[i], 1), 1));
+    x[4 * i + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(e[i], 2), 2));
+    x[4 * i + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(e[i], 3), 3));
   }
   uint32x4 lo, hi;
 #pragma unroll
@@ -87,7 +90,7 @@ __device__ inline bf16x8 key_fragment(const uint32x4 *k, const uint32_t *e, int 
   constexpr int QC = DH / 32;
   if constexpr (EL == EL_FP4) {
     const int f = tl * QC + c;
-    return widen4(k[f / 4][f % 4], e[f / 4] >> (8 * (f % 4)) & 255u);
+    return widen4(k[f / 4][f % 4], scale4(e[f / 4], f % 4));
   } else if constexpr (EL == EL_FP8) {
     const uint32x4 w = k[tl * (QC / 2) + c / 2];
     return widen(w[c % 2 * 2], w[c % 2 * 2 + 1], e[tl]);
@@ -725,7 +728,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
         }
         if constexpr (FP4) {
           const uint32_t e = kv4_exponent(max_over_quarters(max_bits(kx)));
-          kf = widen4(kv4_codes(kx, e), e);
+          kf = widen4(kv4_codes(kx, e), scale4(e, 0));
         }
         S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, LDS_Q ? sh_q[c * 64 + lane] : qf[0][c], S, 0, 0, 0);
       }
