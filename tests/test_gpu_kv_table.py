@@ -53,11 +53,13 @@ def random_table(rng, rows, width, pages, named=0.6):
     return [[rng.choice([rng.randrange(pages), rng.randrange(pages), -1, pages, -7]) if rng.random() < named else -1 for _ in range(width)] for _ in range(rows)]
 
 
-@pytest.mark.parametrize("seed", range(40))
+@pytest.mark.parametrize("seed", range(60))
 def test_any_table(seed):
     rng = random.Random(seed)
     rows, width = rng.choice([1, 2, 3, 7, 33]), rng.choice([1, 2, 5, 70, 130])
     pages, page = rng.choice([2, 3, 50, 500, 1024, 2500]), rng.choice([32, 64])
+    if seed >= 40:                                                   # by the whole chip
+        rows, pages = rng.choice([(70, 3000), (130, 300), (7, 5000), (1, 4097), (33, 9000)])
     t = Table(random_table(rng, rows, width, pages, rng.choice([0.1, 0.6, 1.0])), pages, page)
     length = [rng.choice([0, -5, 1, page, rng.randrange(width * page + 1), width * page, 2 ** 31 - 1]) for _ in range(rows)]
     more = [rng.choice([0, 1, 1, -3, page, rng.randrange(4 * page), 2 ** 31 - 1]) for _ in range(rows)]
