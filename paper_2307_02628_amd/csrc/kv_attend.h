@@ -205,18 +205,20 @@ __device__ inline bf16x8 visible(int low, int limit, int grp) {
   for (int j = 0; j < 8; ++j) v[j] = (__bf16)(hidden<LOW>(j, low, limit, grp) ? 0.0f : 1.0f);
   return v;
 }
-// 4-bit values whose exponents stand for no finite number, or for a page that nobody wrote: the words of a lane's exponents,
-// [group][2], are made harmless, and the sums of the queries that see a NaN become NaN.  Rare: out of the way of everything else.
+// 4-bit values that are not finite, or that nobody wrote: of a lane's words of exponents, [group][2], those of positions from `valid` of
+// the block on are cleared where their values might not be finite (exponents from 126 on), and where a byte stands for NaN it is
+// cleared and the sums of the queries that see it become NaN.  Rare: out of the way of everything else.
 template <int DH, bool LOW, int NT, typename Tile>
-__device__ inline void odd_exponents(uint32_t (&e)[DH / 16], Tile (&tile)[NT], const int (&low)[NT], const int (&limit)[NT]) {
+__device__ inline void odd_exponents(uint32_t (&e)[DH / 16], Tile (&tile)[NT], const int (&low)[NT], const int (&limit)[NT], int valid) {
+  auto odd = [&](int i) { return ((e[i] & 0x7f7f7f7fu) + 0x03030303u) & e[i] & 0x80808080u; };  // bytes from 253 on
   uint32_t any = 0;
 #pragma unroll
-  for (int i = 0; i < DH / 16; ++i) any |= ((e[i] & 0x7f7f7f7fu) + 0x02020202u) & e[i] & 0x80808080u;
+  for (int i = 0; i < DH / 16; ++i) any |= odd(i);
   if (__builtin_expect(!__any(any != 0), 1)) return;
+  const int grp = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) {
-    const uint32_t odd = ((e[i] & 0x7f7f7f7fu) + 0x02020202u) & e[i] & 0x80808080u;
-    if (!__any(odd != 0)) continue;
+    if (!__any(odd(i) != 0)) continue;
 #pragma unroll 1
     for (int g = 0; g < 4; ++g) {
       const uint32_t w = (uint32_t)__shfl((int)e[i], 16 * g);
@@ -229,7 +231,9 @@ __device__ inline void odd_exponents(uint32_t (&e)[DH / 16], Tile (&tile)[NT], c
             for (int u = 0; u < 2; ++u) tile[t].O[i / 2 * 2 + u] += __uint_as_float(0x7fc00000u);
           }
     }
-    e[i] &= ~((odd >> 7) * 0xffu);
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      if ((e[i] >> (8 * y) & 255u) == 255u || block_pos(4 * (i & 1) + y, grp) >= valid) e[i] &= ~(255u << (8 * y));
   }
 }
 // masks of a lane's eight bf16 values: positions below `valid`
@@ -625,7 +629,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
           from[t] = x.low - base;
           to[t] = x.limit - base;
         }
-        odd_exponents<DH, SC != 0, NT>(b.ve, tile, from, to);
+        odd_exponents<DH, SC != 0, NT>(b.ve, tile, from, to, valid - base);
       }
 #pragma unroll
       for (int i = 0; i < DH / 32; ++i) {
@@ -1097,7 +1101,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
         to[t] = no_page ? 0 : x.limit - base;
       }
       exponents4(from, ve);
-      odd_exponents<DH, SC != 0, NT>(ve, tile, lo, to);
+      odd_exponents<DH, SC != 0, NT>(ve, tile, lo, to, no_page ? 0 : s.held - base);
       add_values4(vw, ve, pv);
     } else {
       add_values(vw, pv);

@@ -36,18 +36,19 @@ __host__ __device__ inline long list_of(const KvTable &t) {
 }
 
 struct Span {
-  int held, upto;  // positions that a row holds, and will have been given pages for
+  int held, upto;   // positions that a row holds, and will have been given pages for
+  int first, last;  // entries that tokens to come go to: first .. last - 1
 };
 __device__ inline Span span_of(const KvTable &t, int r) {
   const long room = (long)t.width * t.page_tokens;  // below 2^30
   Span s;
   s.held = (int)min((long)max(t.len[r], 0), room);
   s.upto = (int)min((long)s.held + max(t.more[r], 0), room);
+  s.first = s.held / t.page_tokens;
+  s.last = s.upto > s.held ? (s.upto - 1) / t.page_tokens + 1 : s.first;
   return s;
 }
-__device__ inline bool written(const KvTable &t, Span s, int i) {
-  return s.upto > s.held && i * t.page_tokens < s.upto && (i + 1) * t.page_tokens > s.held;
-}
+__device__ inline bool written(Span s, int i) { return i >= s.first && i < s.last; }
 
 __global__ __launch_bounds__(256) void k_table_fill(int32_t *w, long zero, long top) {
   for (long i = blockIdx.x * 256L + threadIdx.x; i < zero + top; i += gridDim.x * 256L) w[i] = i < zero ? 0 : 0x7fffffff;
@@ -66,7 +67,7 @@ __global__ __launch_bounds__(256) void k_table_gather(KvTable t) {
   t.out[at] = page;
   if (page < 0) return;
   atomicAdd(&w.uses[page], 1);
-  if (written(t, s, i)) {
+  if (written(s, i)) {
     atomicAdd(&w.writes[page], 1);
     atomicMin(&w.lowest[page], (int)at);
     if (i * t.page_tokens >= s.held) atomicAdd(&w.loose[page], 1);
@@ -93,13 +94,12 @@ __global__ __launch_bounds__(256) void k_table_count(KvTable t, int rows4) {
     if (r >= t.rows) return;
     const Span s = span_of(t, r);
     int n = 0, copy = 0;
-    if (s.upto > s.held)
-      for (int i = s.held / t.page_tokens + lane; i * t.page_tokens < s.upto; i += 64) {
-        const int at = r * t.width + i, page = t.out[at];
-        if (!fresh(w, page, at)) continue;
-        ++n;
-        if (page >= 0 && i * t.page_tokens < s.held) copy = 1;
-      }
+    for (int i = s.first + lane; i < s.last; i += 64) {
+      const int at = r * t.width + i, page = t.out[at];
+      if (!fresh(w, page, at)) continue;
+      ++n;
+      if (page >= 0 && i * t.page_tokens < s.held) copy = 1;
+    }
     n = wave_sum_i(n);
     copy = wave_sum_i(copy);
     if (lane == 0) {
@@ -191,27 +191,26 @@ __global__ __launch_bounds__(64) void k_table_deal(KvTable t) {
   const bool enough = all <= free;
   const Span s = span_of(t, r);
   long place = before;
-  if (s.upto > s.held)
-    for (int base = s.held / t.page_tokens; base * t.page_tokens < s.upto; base += 64) {
-      const int i = base + lane, at = r * t.width + i;
-      const bool in = i < t.width && i * t.page_tokens < s.upto;
-      const int page = in ? t.out[at] : -1;
-      const bool get = in && fresh(w, page, at);
-      const uint64_t who = __ballot(get);
-      if (!enough) {
-        if (in && i * t.page_tokens >= s.held) t.out[at] = -1;
-        continue;
-      }
-      if (get) {
-        const int to = w.list[place + __popcll(who & ((1ull << lane) - 1))];
-        t.out[at] = to;
-        if (page >= 0 && i * t.page_tokens < s.held) {
-          t.copies[2 * copies_before] = page;
-          t.copies[2 * copies_before + 1] = to;
-        }
-      }
-      place += __popcll(who);
+  for (int base = s.first; base < s.last; base += 64) {
+    const int i = base + lane, at = r * t.width + i;
+    const bool in = i < s.last;
+    const int page = in ? t.out[at] : -1;
+    const bool get = in && fresh(w, page, at), holds = in && i * t.page_tokens < s.held;
+    const uint64_t who = __ballot(get);
+    if (!enough) {
+      if (in && !holds) t.out[at] = -1;
+      continue;
     }
+    if (get) {
+      const int to = w.list[place + __popcll(who & ((1ull << lane) - 1))];
+      t.out[at] = to;
+      if (page >= 0 && holds) {
+        t.copies[2 * copies_before] = page;
+        t.copies[2 * copies_before + 1] = to;
+      }
+    }
+    place += __popcll(who);
+  }
   const long copies = enough ? copies_before + sum_of(w.copy + r, t.rows - r) : 0;
   if (lane == 0 && r >= copies) t.copies[2 * (long)r] = t.copies[2 * (long)r + 1] = -1;
   if (r == 0) {
@@ -270,7 +269,7 @@ __global__ __launch_bounds__(1024) void k_table_assign_one(KvTable t) {
     const Span s = span_of(t, r);
     if (src >= 0 && src < t.rows && i * t.page_tokens < s.upto) page[k] = t.table[src * t.width + i];
     if (page[k] < 0 || page[k] >= t.pages) page[k] = -1;
-    write[k] = written(t, s, i);
+    write[k] = written(s, i);
     holds[k] = i * t.page_tokens < s.held;
   }
   __syncthreads();

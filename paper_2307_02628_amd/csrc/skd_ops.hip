@@ -252,16 +252,18 @@ static int table_of(const skd_kv *kv, KvTable &t) {
   t.pages = kv->pages;
   return kv_table_fits(t) ? SKD_OK : SKD_ERR_RANGE;
 }
-// The arrays of such a call: aligned, the current device's, and table_out apart from the table, or (`same`) the table itself.
-static int check_table(const KvTable &t, bool same, size_t words, void *workspace, int64_t workspace_bytes) {
-  if (!t.out || !t.counts || !t.copies || !workspace || (t.rows && !t.table)) return SKD_ERR_NULL;
+// The arrays of such a call (up to `most` copies): aligned, the current device's, and table_out apart from the table, or (`same`) the
+// table itself.  Those without elements may be missing.
+static int check_table(const KvTable &t, bool same, int most, size_t words, void *workspace, int64_t workspace_bytes) {
+  if (!t.counts || !workspace || (most && !t.copies) || (t.rows && (!t.table || !t.out))) return SKD_ERR_NULL;
   if (!aligned4({t.table, t.out, t.counts, t.copies}) || !aligned(workspace)) return SKD_ERR_SHAPE;
   if (workspace_bytes < (int64_t)(words * sizeof(int32_t))) return SKD_ERR_NOMEM;
   const size_t bytes = (size_t)t.rows * t.width * sizeof(int32_t);
   const uintptr_t a = (uintptr_t)t.table, b = (uintptr_t)t.out;
   if (!(same && a == b) && a < b + bytes && b < a + bytes) return SKD_ERR_RANGE;
-  CHECK(check_memory({t.out, t.counts, t.copies, workspace}));
-  if (t.rows) CHECK(check_memory({t.table}));
+  CHECK(check_memory({t.counts, workspace}));
+  if (most) CHECK(check_memory({t.copies}));
+  if (t.rows) CHECK(check_memory({t.table, t.out}));
   return SKD_OK;
 }
 extern "C" int64_t skd_kv_assign_workspace(const skd_kv *kv) {
@@ -282,7 +284,7 @@ extern "C" int skd_kv_assign(const skd_kv *kv, const int32_t *source, const int3
   t.work = (int32_t *)workspace;
   if (t.rows && (!len || !more)) return SKD_ERR_NULL;
   if (!aligned4({source, len, more})) return SKD_ERR_SHAPE;
-  CHECK(check_table(t, !source, kv_assign_words(t), workspace, workspace_bytes));
+  CHECK(check_table(t, !source, t.rows, kv_assign_words(t), workspace, workspace_bytes));
   if (t.rows) CHECK(check_memory({len, more}));
   if (source) CHECK(check_memory({source}));
   kv_assign((hipStream_t)hip_stream, t);
@@ -301,7 +303,7 @@ extern "C" int skd_kv_compact(const skd_kv *kv, int32_t *table_out, int32_t *cop
   t.copies = copies;
   t.counts = counts;
   t.work = (int32_t *)workspace;
-  CHECK(check_table(t, true, kv_compact_words(t), workspace, workspace_bytes));
+  CHECK(check_table(t, true, t.pages / 2, kv_compact_words(t), workspace, workspace_bytes));
   kv_compact((hipStream_t)hip_stream, t);
   return launched();
 }

@@ -430,14 +430,14 @@ class KvScores:
             if t is not None:
                 _expect(t, dtype, 1)
         self._keep = (slopes, begin, end)
+        self._heads, self._tokens = (None if slopes is None else len(slopes)), [len(t) for t in (begin, end) if t is not None]
         self.c = Scores(cap, _ptr_of(slopes), window, _ptr_of(begin), _ptr_of(end))
         self.ref = C.byref(self.c)
 
     def expect(self, heads: int, tokens: int):
         """Raises unless the arrays are those of so many heads and tokens."""
-        for t, n in zip(self._keep, (heads, tokens, tokens)):
-            if t is not None and len(t) != n:
-                raise ValueError(f"expected an entry for each of {n} heads or tokens")
+        if self._heads not in (None, heads) or any(n != tokens for n in self._tokens):
+            raise ValueError(f"expected slopes of {heads} heads, begin and end of {tokens} tokens")
 
 
 class KvCache:

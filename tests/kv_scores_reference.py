@@ -107,7 +107,7 @@ class Rows:
     """Ragged rows of a cache, on the host in float64 and in pages on the device.  Pages are dealt out in random order; what no token
     was filed to is garbage (NaN bits, exponents of NaN)."""
 
-    def __init__(self, elem, H, dh, page, past, new, seed=0, spare=0):
+    def __init__(self, elem, H, dh, page, past, new, seed=0, spare=0, fill=0xff):
         g = torch.Generator().manual_seed(seed)
         self.elem, self.H, self.dh, self.page, self.past, self.new = elem, H, dh, page, past, new
         self.total = [p + n for p, n in zip(past, new)]
@@ -117,7 +117,7 @@ class Rows:
         for r, n in enumerate(need):
             for i in range(n):
                 self.table[r, i] = order.pop()
-        self.pool = garbage(elem, sum(need) + 1, H, dh, page)
+        self.pool = garbage(elem, sum(need) + 1, H, dh, page, fill)
         self.cache = skd.KvCache(self.pool, self.table.cuda(), H, dh, page, elem)
         gain = 0.2 + 3 * torch.rand(H, dh, generator=g)
         self.k = [(torch.randn(t, H, dh, generator=g) * gain).bfloat16() for t in self.total]
@@ -174,11 +174,12 @@ class Rows:
             at += n
 
 
-def garbage(elem, pages, H, dh, page):
+def garbage(elem, pages, H, dh, page, fill=0xff):
+    """fill: bytes of 4-bit pages (as exponents 0xff is NaN, 0xfd and 0xfe with most codes infinity)."""
     if elem == BF16:
         return torch.full((pages, H * page * 2 * dh), float("nan"), dtype=torch.bfloat16, device="cuda")
     size = H * page * (2 * dh + 2) if elem == FP8 else H * page // 32 * 34 * dh
-    return torch.full((pages, size), 0x7f if elem == FP8 else 0xff, dtype=torch.uint8, device="cuda")
+    return torch.full((pages, size), 0x7f if elem == FP8 else fill, dtype=torch.uint8, device="cuda")
 
 
 # ---------------------------------------------------------------------------------------------- block tables

@@ -120,6 +120,16 @@ def test_attention(H, group, dh, page, past, new):
     assert torch.equal(k.double(), c.held(c.k, [0] * len(past), c.total)) and torch.equal(v.double(), c.held(c.v, [0] * len(past), c.total))
 
 
+@pytest.mark.parametrize("fill", [0xfd, 0xfe, 0x7f, 0x00])
+@pytest.mark.parametrize("past,new", [([31, 20], [1, 1]), ([100, 0], [9, 4]), ([3, 40], [70, 33]), ([1000, 31], [200, 257])])
+def test_places_that_nobody_wrote_may_hold_anything(fill, past, new):
+    c = S.Rows(S.FP4, 2, 128, 96, past, new, seed=17, spare=1, fill=fill)
+    q = torch.randn(sum(new), 4, 128, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    c.append([0, 0], past)
+    c.check(q, c.attend(q, files=True))
+    c.check(q, c.attend(q, window=20), window=20)
+
+
 @pytest.mark.parametrize("scale,size", [(0.01, 1.0), (1.0, 1.0), (0.125, 8.0)])
 def test_attention_of_flat_and_sharp_scores(scale, size):
     c = S.Rows(S.FP4, 2, 64, 64, [200, 65], [40, 33], seed=21)
@@ -136,10 +146,23 @@ def test_attention_to_values_at_the_ends(size):
     q = torch.randn(3, 2, 128, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
     c.append([0, 0], c.total)
     out = c.attend(q)
-    for o, v in ((out, c.v),):
-        ref = S.Rows.check
-        c.v = [x / size for x in v]
-        ref(c, q, o.float() / size if size > 1 else (o.double() / size))
+    c.v = [x / size for x in c.v]                                    # (exact, and so is what is held)
+    c.check(q, out.double() / size)
+
+
+@pytest.mark.parametrize("new", [1, 20, 130])
+def test_attention_to_the_largest_values(new):
+    """Exponents of 126, whose codes end at 3: finite where they are seen and where they are not."""
+    c = S.Rows(S.FP4, 1, 64, 32, [40], [new], seed=27)
+    big = torch.finfo(torch.bfloat16).max
+    c.v[0][41:] = torch.where(c.v[0][41:] > 0, big, -big)
+    c.append([0], c.total)
+    q = torch.randn(new, 2, 64, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    out = c.attend(q, window=1)                                      # each token's own value, as it is held
+    want = c.held(c.v, c.past, c.new)[:, :1].expand(-1, 2, -1)
+    assert torch.equal(out.double(), want)
+    first = c.attend(q, end=[41] * new)                              # those before alone
+    c.check(q, first, end=[41] * new)
 
 
 @pytest.mark.parametrize("new", [1, 4, 70])

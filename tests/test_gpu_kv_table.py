@@ -1,5 +1,6 @@
 """Block tables on the device (skd_kv_assign, skd_kv_compact, skd_kv_copy_pages), against their definition entry by entry, and a
 batch that is forked, grown, cut and compacted while it is filed to and attended to."""
+import ctypes as C
 import math
 import random
 
@@ -97,6 +98,32 @@ def test_many_pages_and_rows():
     length = [length[s] for s in source]
     assert t.assign(length, more, source) == padded(S.assign(table, pages, page, length, more, source), rows)
     assert t.compact() == padded(S.compact(table, pages), pages // 2)
+
+
+@pytest.mark.parametrize("pages", [8, 5000])
+def test_pages_of_half_a_billion_positions(pages):
+    """Places of positions near the end of 32 bits: one page a row, of 2^29 positions, and small rows of many."""
+    for page, table in ((1 << 29, [[3], [-1], [3], [0]]), ((1 << 30) // 96, [[1] * 70 + [-1] * 25, [-1] * 95])):
+        rows, width = len(table), len(table[0])
+        for length, more, source in (([5, 0, 5, 1 << 29], [1, 2, 0, 1], [0, 1, 0, 3]), ([(1 << 30) - 1] * 4, [1 << 29] * 4, [0, 1, 2, 3]), ([1 << 28] * 4, [2 ** 31 - 1] * 4, [0, 0, 0, 0])):
+            length, more, source = length[:rows], more[:rows], [min(x, rows - 1) for x in source[:rows]]
+            dev, out = ints(table), torch.full((rows, width), 77, dtype=torch.int32, device="cuda")
+            kv = skd.Kv(S.BF16, 1, 64, page // 32 * 32, pages, rows, width, None, dev.data_ptr())
+            args = [ints(x) for x in (source, length, more)]
+            copies, counts = torch.zeros(rows, 2, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+            ws = torch.zeros(1 << 18, dtype=torch.uint8, device="cuda")
+            rc = skd.lib().skd_kv_assign(C.byref(kv), *[x.data_ptr() for x in args], out.data_ptr(), copies.data_ptr(), counts.data_ptr(), ws.data_ptr(), 1 << 18, None)
+            assert rc == skd.OK
+            assert (out.tolist(), copies.tolist(), counts.tolist()) == padded(S.assign(table, pages, page // 32 * 32, length, more, source), rows)
+
+
+def test_a_pool_of_one_page():
+    t = Table([[0], [-1]], 1)
+    none = torch.zeros(0, 2, dtype=torch.int32, device="cuda")
+    out, counts = torch.zeros_like(t.dev), torch.zeros(3, dtype=torch.int32, device="cuda")
+    t.cache.compact(out, none, counts, workspace=torch.zeros(t.cache.compact_workspace(), dtype=torch.uint8, device="cuda"))
+    assert out.tolist() == [[0], [-1]] and counts.tolist() == [1, 0, 0]
+    t.cache.copy_pages(none, counts[2:])
 
 
 def test_no_rows():
