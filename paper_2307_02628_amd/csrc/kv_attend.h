@@ -319,79 +319,116 @@ struct Share {
     s.q0 = (tiles - 1 - tile) * NQ;
     s.any = s.q0 < s.R;
     s.held = s.t.past + (files ? 0 : s.t.n);
-    int first = 0, nblk;
-    if constexpr (SC) {
-      // what the queries see together and each of them, by every wave
-      int from = 1 << 30, upto = 0;
-      s.whole_lo = 0;
-      s.whole_hi = 1 << 30;
-      for (int q = s.q0 + (threadIdx.x & 63); q < min(s.q0 + NQ, s.R); q += 64) {
-        const Range x = s.range<SC>(a, q);
-        if (x.lo < x.hi) from = min(from, x.lo);
-        upto = max(upto, x.hi);
-        s.whole_lo = max(s.whole_lo, x.lo < x.hi ? x.lo : 1 << 30);
-        s.whole_hi = min(s.whole_hi, x.hi);
-      }
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) {
-        from = min(from, __shfl_xor(from, o));
-        upto = max(upto, __shfl_xor(upto, o));
-        s.whole_lo = max(s.whole_lo, __shfl_xor(s.whole_lo, o));
-        s.whole_hi = min(s.whole_hi, __shfl_xor(s.whole_hi, o));
-      }
-      auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-      nblk = one((min(upto, s.held) + 31) >> 5);
-      first = min(one(from >> 5), nblk);
-      s.whole_lo = one((s.whole_lo + 31) >> 5);
-      if constexpr (SC & SC_SLOPES) s.whole_hi = min(s.whole_hi, s.seen(a, s.q0));  // (where distances have a sign)
-      s.whole_hi = one(min(s.whole_hi, s.held) >> 5);
-    } else {
-      nblk = (min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held) + 31) >> 5;
-      s.whole_lo = 0;
+    s.lo = s.hi = s.whole_lo = s.whole_hi = 0;
+    if constexpr (!SC) {
       s.whole_hi = min(s.seen(a, s.q0), s.held) >> 5;
-    }
-    const int per = (nblk - first + a.splits - 1) / a.splits;
-    s.lo = first + (int)blockIdx.y * per;
-    s.hi = min(s.lo + per, nblk);
-    if constexpr (SC) {
-      s.whole_lo = min(max(s.whole_lo, s.lo), max(s.hi, s.lo));
-      s.whole_hi = max(min(s.whole_hi, s.hi), s.whole_lo);
+      s.take(a, 0, min(s.seen(a, min(s.q0 + NQ, s.R) - 1), s.held));
     }
     return s;
+  }
+  // blocks with positions from .. upto - 1, of them this workgroup's share
+  __device__ void take(const KvAttend &a, int from, int upto) {
+    const int nblk = (upto + 31) >> 5, first = min(from >> 5, nblk), per = (nblk - first + a.splits - 1) / a.splits;
+    lo = first + (int)blockIdx.y * per;
+    hi = min(lo + per, nblk);
   }
   // SC: the blocks that every query sees whole come first, the others, before and behind them, then: masks are in the code once.
   __device__ int wholes() const { return whole_hi - whole_lo; }
   __device__ int block(int v) const { return v < wholes() ? whole_lo + v : v < whole_hi - lo ? v - wholes() + lo : v + lo; }
-  struct Range {
-    int lo, hi;
-  };
-  // Positions lo .. hi - 1 of those that the row has are seen by query q (lo = hi = 0: none).
-  template <int SC>
-  __device__ Range range(const KvAttend &a, int q) const {
-    if constexpr (!SC) return Range{0, seen(a, q)};
-    const int p = t.past + q / a.group;
-    const long at = token(a, q);
-    Range x{a.sc.begin ? max(a.sc.begin[at], 0) : 0, min(a.sc.end ? a.sc.end[at] : p + 1, t.past + t.n)};
-    if (a.sc.window) x.lo = max(x.lo, p + 1 - a.sc.window);
-    return x.lo < x.hi ? x : Range{0, 0};
-  }
-  template <int SC>
-  __device__ float slope(const KvAttend &a, int q) const { return a.sc.slopes[head(a, q)] * 1.4426950408889634f / factor<SC>(a); }
   __device__ int seen(const KvAttend &a, int q) const { return t.past + q / a.group + 1; }  // positions that query q sees
   __device__ long token(const KvAttend &a, int q) const { return t.at + (long)(q / a.group) * a.tk.step; }
   __device__ int head(const KvAttend &a, int q) const { return h * a.group + q % a.group; }
 };
-// What a lane needs to know of a query: it sees positions low .. limit - 1 of those that the cache holds.
+// What a lane needs to know of a query: it sees positions low .. limit - 1 of those that the row has (none: 0, 0).
 struct Seen {
   int low, limit, pos;
   float slope;  // over what scores are multiplied by
-  template <int SC>
-  __device__ static Seen of(const KvAttend &a, const Share &s, int q) {
-    if (q >= s.R) return Seen{0, 0, 0, 0.f};
-    const Share::Range x = s.range<SC>(a, q);
-    return Seen{x.lo, min(x.hi, s.held), s.t.past + q / a.group, SC & SC_SLOPES ? s.slope<SC>(a, q) : 0.f};
+};
+// of queries q0 + 16 t + col; the loads are on their way together
+template <int SC, int NT>
+__device__ inline void see(const KvAttend &a, const Share &s, int q0, Seen (&x)[NT]) {
+  const int col = threadIdx.x & 15;
+  if constexpr (!SC) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int q = q0 + 16 * t + col;
+      x[t] = Seen{0, q < s.R ? s.seen(a, q) : 0, 0, 0.f};
+    }
+  } else {
+    long at[NT];
+    int lo[NT], hi[NT];
+    float slope[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int q = min(q0 + 16 * t + col, s.R - 1);
+      at[t] = s.token(a, q);
+      x[t].pos = s.seen(a, q) - 1;
+      lo[t] = 0;
+      hi[t] = x[t].pos + 1;
+      if constexpr (SC & SC_SLOPES) slope[t] = a.sc.slopes[s.head(a, q)];
+    }
+    if (a.sc.begin) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) lo[t] = a.sc.begin[at[t]];
+    }
+    if (a.sc.end) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) hi[t] = a.sc.end[at[t]];
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      lo[t] = max(lo[t], a.sc.window ? max(x[t].pos + 1 - a.sc.window, 0) : 0);
+      hi[t] = min(hi[t], s.t.past + s.t.n);
+      const bool is = q0 + 16 * t + col < s.R;
+      x[t].low = is && lo[t] < hi[t] ? lo[t] : 0;
+      x[t].limit = is && lo[t] < hi[t] ? hi[t] : 0;
+      x[t].slope = SC & SC_SLOPES && is ? slope[t] * 1.4426950408889634f / factor<SC>(a) : 0.f;
+    }
+  }
+}
+// What queries see together: some of them positions from .. upto - 1, each of them all .. any - 1.
+struct Span {
+  int from, upto, all, any;
+  __device__ void join(const Span &x) {
+    from = min(from, x.from);
+    upto = max(upto, x.upto);
+    all = max(all, x.all);
+    any = min(any, x.any);
+  }
+  template <int NT>
+  __device__ static Span of(const Share &s, int q0, const Seen (&x)[NT]) {  // of a wave's tiles
+    Span r{1 << 30, 0, 0, 1 << 30};
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      if (q0 + 16 * t + (int)(threadIdx.x & 15) < s.R) {
+        const bool none = x[t].low >= x[t].limit;
+        r.join(Span{none ? 1 << 30 : x[t].low, x[t].limit, none ? 1 << 30 : x[t].low, x[t].limit});
+      }
+    r.join(r.turned<8>());
+    r.join(r.turned<4>());
+    r.join(r.turned<2>());
+    r.join(r.turned<1>());
+    return r.uniform();
+  }
+  template <int N>
+  __device__ Span turned() const {  // that of the lane N places on, of 16
+    auto of = [](int x) { return __builtin_amdgcn_mov_dpp(x, 0x120 + N, 0xF, 0xF, true); };
+    return Span{of(from), of(upto), of(all), of(any)};
+  }
+  __device__ Span uniform() const {
+    auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    return Span{one(from), one(upto), one(all), one(any)};
   }
 };
+// the blocks of a workgroup whose queries see `x` together
+template <int SC>
+__device__ inline void take(const KvAttend &a, Share &s, const Span &x) {
+  s.take(a, x.from, min(x.upto, s.held));
+  // (with slopes: where distances have a sign)
+  const int any = min(SC & SC_SLOPES ? min(x.any, s.seen(a, s.q0)) : x.any, s.held);
+  s.whole_lo = min(max((x.all + 31) >> 5, s.lo), max(s.hi, s.lo));
+  s.whole_hi = max(min(any >> 5, s.hi), s.whole_lo);
+}
 // Where the scores of a block begin; from: distance of the query from the lane's first position; before: no position lies behind it.
 // (A distance is exact up to 2^24, and beyond to 2^-24 of itself.)
 template <int SC>
@@ -459,8 +496,8 @@ template <int DH, typename Tile, int NT>
 __device__ inline bool not_finite(const Tile (&tile)[NT]) { return not_finite_<DH, NT, Tile>(tile); }
 // The numerators of a wave's tiles again, over blocks first, first + step, ... below end (SC: in their order) of bf16 pages, against the references
 // that the wave has arrived at: values without their infinities and NaNs, which are then added.
-template <int DH, int SC, typename Tile, int NT>
-__device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, int q0, int first, int step, int end, Tile (&tile)[NT]) {
+template <int DH, int SC, typename SeenOf, typename Tile, int NT>
+__device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, int q0, SeenOf seen_of, int first, int step, int end, Tile (&tile)[NT]) {
   constexpr int QC = DH / 32, VM = DH / 16;
   const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15, bpp = a.kv.g.page_tokens >> 5;
 #pragma unroll
@@ -476,7 +513,7 @@ __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, in
     for (int t = 0; t < NT; ++t) {
       bf16x8 qf[QC];
       load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf);
-      const Seen x = Seen::of<SC>(a, s, q0 + 16 * t + col);
+      const Seen x = seen_of(t);
       const int lim = x.limit - blk * 32, lo = x.low - blk * 32;
       floatx4 S[2];
       begin_scores<SC, true>(false, x, blk * 32 + 4 * grp, S);
@@ -522,11 +559,12 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   __shared__ bf16x8 sh_q[LDS_Q ? QC * 64 : 1];
   // (and what else is known of a query, if scores are changed)
   __shared__ Seen sh_seen[SC && LDS_Q ? 16 : 1];
+  __shared__ int sh_new[16];                           // (whether it sees the new token; of one tile)
   __shared__ __align__(16) bf16_t sh_k[DH], sh_v[DH];  // the new token
   extern __shared__ float lds[];                       // [NW][cols][DH + 2]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
   const bool files = NT == 1 && a.k.p != nullptr;  // (t.n is 1: the token is not in the cache yet)
-  const Share s = Share::of<NQ, SC>(a, pairs, files);
+  Share s = Share::of<NQ, SC>(a, pairs, files);
   if (!s.any) return;
   const int q0 = s.q0, R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
   // The page that takes the new token, known to the wave that attends to it: without one it is dropped, and nobody sees it.
@@ -547,17 +585,21 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   for (int t = 0; t < NT; ++t) {
     const int q = q0 + 16 * t + col;
     load_queries<DH>(a, s, q, grp, qf[t]);
-    seen[t] = Seen::of<SC>(a, s, q);
     tile[t].clear();
   }
+  see<SC>(a, s, q0, seen);
+  if (SC && NT == 1 && wave == 0 && grp == 0) sh_new[col] = seen[0].low <= s.held && s.held < seen[0].limit;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) seen[t].limit = min(seen[t].limit, s.held);
+  if constexpr (SC) take<SC>(a, s, Span::of(s, q0, seen));
   if constexpr (LDS_Q) {
     if (wave == 0) {
 #pragma unroll
       for (int c = 0; c < QC; ++c) sh_q[c * 64 + lane] = qf[0][c];
       if (SC && grp == 0) sh_seen[col] = seen[0];
     }
-    __syncthreads();
   }
+  if constexpr (LDS_Q || (SC && NT == 1)) __syncthreads();
   typedef KvBlock<DH, EL> Block;
   auto load = [&](int page, int ib, Block &b) {
     const unsigned char *pg = a.kv.pool + (long)page * a.kv.page_bytes;
@@ -590,6 +632,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     asm volatile("" : "+v"(at)::"memory");  // (read where it is needed, not kept, nor its place)
     return sh_seen[at & 15];
   };
+
   // base: first position of the block; valid: positions that the row has
   auto use = [&](auto masked_, int base, Block &b, int valid) {
     constexpr bool masked = decltype(masked_)::value;
@@ -720,7 +763,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     while (blk < end) step(std::true_type());
   }
   if constexpr (EL == EL_BF16) {
-    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, SC ? wave : s.lo + wave, NW, SC ? s.hi - s.lo : s.hi, tile);
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, seen_of, SC ? wave : s.lo + wave, NW, SC ? s.hi - s.lo : s.hi, tile);
   }
   uint32_t ke = 0, ve = 0;  // exponents of the new token
   if constexpr (NT == 1) {
@@ -757,10 +800,9 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       auto &x = tile[0];
       float score = __shfl(S[0], col);
       if constexpr (SC) {  // (at a distance of 0)
-        const Share::Range sees = q0 + col < R ? s.range<SC>(a, q0 + col) : Share::Range{0, 0};
         if constexpr (SC & SC_CAP) score = capped(a.sc.in, score);
         score *= factor<SC>(a);
-        if (!(sees.lo <= s.held && s.held < sees.hi)) score = -INFINITY;
+        if (!sh_new[col]) score = -INFINITY;
       } else {
         score *= a.c;
       }
@@ -899,17 +941,20 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
   constexpr bool LDS_SEEN = SC && DH == 64;
   __shared__ Seen sh_seen[LDS_SEEN ? NQ : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
-  const Share s = Share::of<NQ, SC>(a, pairs, false);
+  Share s = Share::of<NQ, SC>(a, pairs, false);
   if (!s.any) return;
   const int q0 = s.q0 + wave * (16 * NT), R = s.R, h = s.h, H = a.kv.g.H, bpp = a.kv.g.page_tokens >> 5;
   const bool busy = q0 < R;
-  int from_blk = 0, last = busy ? min((s.seen(a, min(q0 + 16 * NT, R) - 1) + 31) >> 5, s.hi) : 0;  // this wave's blocks
   bf16x8 qf[NT][QC];
   Seen seen[NT];
   QueryTile<DH, false> tile[NT];
+  if constexpr (SC) {  // (on their way while the ranges are waited for)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
+  }
+  see<SC>(a, s, q0, seen);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    seen[t] = Seen::of<SC>(a, s, q0 + 16 * t + col);
     if (LDS_SEEN && grp == 0) sh_seen[wave * (16 * NT) + 16 * t + col] = seen[t];  // (read by this wave alone)
     tile[t].clear();
   }
@@ -919,20 +964,19 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
     asm volatile("" : "+v"(at)::"memory");  // (read where it is needed, not kept, nor its place)
     return sh_seen[wave * (16 * NT) + 16 * t + (at & 15)];
   };
+  int from_blk = 0, last = 0;  // this wave's blocks
   if constexpr (SC) {
-    int from = 1 << 30, upto = 0;
+    Span *spans = (Span *)(ring + (NS - 1) * STAGE), mine = Span::of(s, q0, seen);  // (a stage that nothing is requested into before the first barrier of the loop)
+    if (lane == 0) spans[wave] = mine;
+    __syncthreads();
+    Span every = spans[0];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if (seen[t].low < seen[t].limit) from = min(from, seen[t].low);
-      upto = max(upto, seen[t].limit);
-    }
-#pragma unroll
-    for (int o = 1; o < 16; o *= 2) {
-      from = min(from, __shfl_xor(from, o));
-      upto = max(upto, __shfl_xor(upto, o));
-    }
-    from_blk = __builtin_amdgcn_readfirstlane(from >> 5);
-    last = min(__builtin_amdgcn_readfirstlane((upto + 31) >> 5), s.hi);
+    for (int w = 1; w < NW; ++w) every.join(spans[w]);
+    take<SC>(a, s, every.uniform());
+    from_blk = mine.from >> 5;
+    last = min((mine.upto + 31) >> 5, s.hi);
+  } else {
+    last = busy ? min((s.seen(a, min(q0 + 16 * NT, R) - 1) + 31) >> 5, s.hi) : 0;
   }
   // Blocks are requested in order.  Lane l holds page 64 w + l of the row, for the window w of 64 pages that the next block is
   // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked, as is every block from the
@@ -999,15 +1043,21 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
     if (other && ip < ip_end) new_page();
   };
   constexpr int LOADS = LPW + (FP8 || FP4 ? 1 : 0);
+  auto queries_here = [&]() {  // (waited for inside the loop, the queries would make the compiler wait for the ring as well)
+    wait_vmcnt<0>();
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
+  };
+  if constexpr (SC) queries_here();
   for (int i = 0; i < NS - 2; ++i)
     if (asked < asked_end) request();
+  if constexpr (!SC) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
-  wait_vmcnt<0>();  // (waited for inside the loop, the queries would make the compiler wait for the ring as well)
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(qf[t][c]));
+    for (int t = 0; t < NT; ++t) load_queries<DH>(a, s, q0 + 16 * t + col, grp, qf[t]);
+    queries_here();
+  }
 
   // scores of a block: S[t][tl][i] of position 16 tl + 4 grp + i
   auto scores = [&](int stage, int base, bool before, floatx4 (&S)[NT][2]) {
@@ -1241,7 +1291,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
     for (; blk < s.hi; ++blk) single(blk);
   }
   if constexpr (EL == EL_BF16) {
-    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, SC ? 0 : s.lo, 1, SC ? s.hi - s.lo : last, tile);
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, seen_of, SC ? 0 : s.lo, 1, SC ? s.hi - s.lo : last, tile);
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {

@@ -486,13 +486,10 @@ class KvCache:
     def attend(self, chunk: KvChunk, q, out, scale: float, k=None, v=None, workspace=None, stream: int = 0):
         """q, out [tokens][heads][head_dim]; workspace: a device tensor of attend_workspace bytes (None where that is 0)."""
         heads = q.shape[1] if q.dim() == 3 else q.shape[1] // self.dh
-        _check(self._lib.skd_kv_attend(self.ref, chunk.ref, heads, scale, *self._attend_args(chunk, heads, q, out, k, v, workspace), stream),
-               "skd_kv_attend")
-
-    def _attend_args(self, chunk: KvChunk, heads: int, q, out, k, v, workspace):
         kk = (0, 0) if k is None else self._rows_of(chunk, self.heads, k, "torch.bfloat16")
         vv = (0, 0) if v is None else self._rows_of(chunk, self.heads, v, "torch.bfloat16")
-        return (*self._rows_of(chunk, heads, q, "torch.bfloat16"), *kk, *vv, *self._rows_of(chunk, heads, out, "torch.bfloat16"), *_bytes_of(workspace))
+        _check(self._lib.skd_kv_attend(self.ref, chunk.ref, heads, scale, *self._rows_of(chunk, heads, q, "torch.bfloat16"), *kk, *vv,
+                                       *self._rows_of(chunk, heads, out, "torch.bfloat16"), *_bytes_of(workspace), stream), "skd_kv_attend")
 
     def attend_scores_workspace(self, chunk: KvChunk, heads: int, scores: KvScores) -> int:
         return _check(self._lib.skd_kv_attend_scores_workspace(self.ref, chunk.ref, heads, scores.ref), "skd_kv_attend_scores_workspace")
@@ -501,8 +498,10 @@ class KvCache:
         """attend with changed scores and masks; workspace: attend_scores_workspace bytes."""
         heads = q.shape[1] if q.dim() == 3 else q.shape[1] // self.dh
         scores.expect(heads, chunk.tokens)
-        _check(self._lib.skd_kv_attend_scores(self.ref, chunk.ref, heads, scale, scores.ref,
-                                              *self._attend_args(chunk, heads, q, out, k, v, workspace), stream), "skd_kv_attend_scores")
+        kk = (0, 0) if k is None else self._rows_of(chunk, self.heads, k, "torch.bfloat16")
+        vv = (0, 0) if v is None else self._rows_of(chunk, self.heads, v, "torch.bfloat16")
+        _check(self._lib.skd_kv_attend_scores(self.ref, chunk.ref, heads, scale, scores.ref, *self._rows_of(chunk, heads, q, "torch.bfloat16"), *kk, *vv,
+                                              *self._rows_of(chunk, heads, out, "torch.bfloat16"), *_bytes_of(workspace), stream), "skd_kv_attend_scores")
 
     def _table_args(self, table_out, copies, counts, most: int, workspace):
         for t, shape in ((table_out, (self.rows, self.c.max_pages)), (copies, (most, 2)), (counts, (3,))):
