@@ -142,10 +142,12 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads, i
     // not, us: 4 rows of 1000 with 20 new tokens, 32 heads 23.3, 20.0; 16 of 2000 with 5, 32 queries' and 8 kv heads 31.7, 31.1; 24 of
     // 3000 with 6 64.9, 50.9; 16 of 500 with 5 17.7, 14.1; against it 16 of 1000 to 2000 with 5, 27.0, 28.5).
     p.waves = p.nq == 16 && wgs >= 1024 ? 4 : 8;
-    // (4 bits are bound by the vector units: on exactly half of the CUs from three blocks a wave on; six and three, us: 16 rows of 2000 with 5,
-    // 32 queries' and 8 kv heads 20.8, 19.3, capped 25.1, 22.0; on more of the CUs six: 24 of 3000 with 6 27.0, three 34.4.)
-    const int least = p.waves * (p.nq == 32 && wgs >= 128 ? kv.fp4 && wgs == 128 ? 3 : 6 : 1);
-    while (p.splits < 64 && wgs * p.waves * p.splits < 2048 && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
+    // 4 bits are bound by the vector units as much as by bytes: no more than a workgroup a CU, and shares only if every wave keeps three
+    // blocks, of two tiles two (by the rule before, and this one, us, 8 kv heads of 128: 24 rows of 1000 14.4, 10.4, of 4000 26.5, 23.8;
+    // 16 of 1000 11.5, 10.0; 12 of 3000 with 5 26.7, 21.8; 16 of 2000 with 5 20.8, 19.3; against it 1 of 1500 with 5 13.9, 14.5).
+    const int least = p.waves * (kv.fp4 ? (p.nq == 16 ? 3 : 2) : p.nq == 32 && wgs >= 128 ? 6 : 1);
+    auto more = [&]() { return kv.fp4 ? wgs * 2 * p.splits <= 256 : wgs * p.waves * p.splits < 2048; };
+    while (p.splits < 64 && more() && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
   }
   return p;
 }
