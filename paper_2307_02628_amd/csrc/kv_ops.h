@@ -67,9 +67,9 @@ struct KvAttend {
   int splits;               // of the keys of a query tile
   float *part;              // splits > 1: [splits][tokens * heads][dh + 2]: numerators, maximum, denominator
 };
-// window: of the scores, 0 where there is none
-bool kv_attend_fits(const KvView &kv, const KvTokens &tk, int heads, int window = 0);  // in a launch; rows x kv heads must be below 2^31 before
-int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads, int window = 0);
+// window: of changed scores, 0 where they have none; -1: scores as they are
+bool kv_attend_fits(const KvView &kv, const KvTokens &tk, int heads, int window = -1);  // in a launch; rows x kv heads must be below 2^31 before
+int kv_attend_splits(const KvView &kv, const KvTokens &tk, int heads, int window = -1);
 size_t kv_attend_part(const KvView &kv, const KvTokens &tk, int heads, int splits);  // floats
 void kv_attend(hipStream_t s, const KvAttend &a);
 

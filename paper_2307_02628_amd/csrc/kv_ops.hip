@@ -119,7 +119,7 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads, i
   p.nq = R <= 16 ? 16 : R <= (kv.fp8 || kv.fp4 ? 64 : 32) ? 32 : 128;
   p.tiles = (R + p.nq - 1) / p.nq;
   // (all that a tile's queries see: a window for its last token and as many positions as the tile has tokens)
-  if (window) blocks = std::min(blocks, ((long)window + p.nq / (heads / kv.g.H) + 62) / 32);
+  if (window > 0) blocks = std::min(blocks, ((long)window + p.nq / (heads / kv.g.H) + 62) / 32);
   const long n = (long)kv.g.H * kv.rows, wgs = p.tiles * n;
   // Workgroups go to the eight XCDs in turn.  With a multiple of eight places all tiles of a row and kv head are on one of them
   // and find each other's blocks in its L2 (8 prompts of 2048, 32 heads of 128: 586 us with the tiles next to each other, 441
@@ -145,8 +145,11 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads, i
     // 4 bits are bound by the vector units as much as by bytes: no more than a workgroup a CU, and shares only if every wave keeps three
     // blocks, of two tiles two (by the rule before, and this one, us, 8 kv heads of 128: 24 rows of 1000 14.4, 10.4, of 4000 26.5, 23.8;
     // 16 of 1000 11.5, 10.0; 12 of 3000 with 5 26.7, 21.8; 16 of 2000 with 5 20.8, 19.3; against it 1 of 1500 with 5 13.9, 14.5).
-    const int least = p.waves * (kv.fp4 ? (p.nq == 16 ? 3 : 2) : p.nq == 32 && wgs >= 128 ? 6 : 1);
-    auto more = [&]() { return kv.fp4 ? wgs * 2 * p.splits <= 256 : wgs * p.waves * p.splits < 2048; };
+    // Two tiles with changed scores likewise, two blocks from half of the CUs on (12 rows of 3000 with 5, 8 kv heads, capped, bf16 34.0, 30.3,
+    // 8 bits 29.9, 25.6; 16 of 3000 39.3, 35.1 and 32.7, 27.0).  (One tile of theirs is not: 24 rows of 4000, 8 bits, 39.2, 44.9.)
+    const bool one_a_cu = kv.fp4 || (window >= 0 && p.nq == 32);
+    const int least = p.waves * (kv.fp4 ? (p.nq == 16 ? 3 : 2) : p.nq == 32 && wgs >= 128 ? (one_a_cu ? 2 : 6) : 1);
+    auto more = [&]() { return one_a_cu ? wgs * 2 * p.splits <= 256 : wgs * p.waves * p.splits < 2048; };
     while (p.splits < 64 && more() && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
   }
   return p;
@@ -169,7 +172,7 @@ static void merge(hipStream_t s, const KvAttend &a) {
 }
 void kv_attend(hipStream_t s, const KvAttend &call) {
   KvAttend a = call;
-  const AttendPlan p = plan_attend(a.kv, a.tk, a.heads, a.scored ? a.sc.window : 0);
+  const AttendPlan p = plan_attend(a.kv, a.tk, a.heads, a.scored ? a.sc.window : -1);
   if (a.k.p && !(a.tk.max_new == 1 && p.nq == 16)) {  // (one token of few heads: the same launch)
     kv_append(s, a.kv, a.tk, a.k, a.v);
     a.k.p = nullptr;

@@ -149,7 +149,7 @@ static int check_scores(const skd_kv_scores *sc) {
   if (!aligned4({sc->slopes, sc->begin, sc->end})) return SKD_ERR_SHAPE;
   return SKD_OK;
 }
-static int window_of(const skd_kv_scores *sc) { return sc ? std::min(sc->window, 1 << 30) : 0; }  // (no row has as many positions)
+static int window_of(const skd_kv_scores *sc) { return sc ? std::min(sc->window, 1 << 30) : -1; }  // (no row has as many positions)
 static int check_attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, const skd_kv_scores *sc) {
   CHECK(check_call(kv, ch));
   if (heads < 1 || heads % kv->kv_heads) return SKD_ERR_SHAPE;
@@ -204,7 +204,7 @@ static int attend(const skd_kv *kv, const skd_kv_chunk *ch, int32_t heads, float
   a.c = c;
   a.q = rows_of(q, q_stride);
   a.o = rows_of(out, out_stride);
-  a.splits = kv_attend_splits(a.kv, a.tk, heads, a.sc.window);
+  a.splits = kv_attend_splits(a.kv, a.tk, heads, window_of(sc));
   if (a.splits > 1) {
     if (!workspace) return SKD_ERR_NULL;
     if (!aligned(workspace)) return SKD_ERR_SHAPE;
