@@ -115,7 +115,8 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads, i
   // tiles and more (inputs not in the last-level cache, us.  Two tiles of 16 for 17 .. 32 queries: 16 rows of 2000, 8 kv heads of
   // 128, bf16 31.3, 30.9; 40 rows 70.7, 104.9.  33 .. 64 as two of 32 or through LDS: 8 rows of 1000, 32 heads of 128, bf16 58.7,
   // 35.2, 8 bits 38.7, 38.2; 32 rows of 700, 8 kv heads of 64, bf16 23.4, 19.7, 8 bits 15.2, 22.1; one of 20000, 8 of 128, 8 bits
-  // 23.3, 30.5.  65 .. 128: 8 rows of 1000 bf16 107, 38, 8 bits 70, 41.)
+  // 23.3, 30.5.  65 .. 128: 8 rows of 1000 bf16 107, 38, 8 bits 70, 41.  4 bits as 8: 8 rows of 1000, 64 queries 30.8, 35.7, 100 of them
+  // 46.3, 37.5; 32 rows of 700, 8 kv heads of 64, 64 queries 15.5, 20.6.)
   p.nq = R <= 16 ? 16 : R <= (kv.fp8 || kv.fp4 ? 64 : 32) ? 32 : 128;
   p.tiles = (R + p.nq - 1) / p.nq;
   // (all that a tile's queries see: a window for its last token and as many positions as the tile has tokens)
