@@ -461,7 +461,8 @@ typedef struct {
                            itself in both directions); NULL: up to its own */
 } skd_kv_scores;
 
-/* skd_kv_attend with changed scores and masks (`scores`, device arrays in it; finite slopes).  Positions seen are cut to those
+/* skd_kv_attend with changed scores and masks (`scores`, device arrays in it; slopes that are finite in fp32, also times the
+ * distances and over scale, or over cap where there is one).  Positions seen are cut to those
  * that the row has once the call's tokens are filed, so tokens of one call see each other in both directions where `end`
  * says so; a token that sees none gets zeros.  What positions that a token does not see hold, also infinities and NaN,
  * does not reach it.  A cap's function is off by up to 2^-11.4 of a weight (cap 1024; in proportion to it), a distance above

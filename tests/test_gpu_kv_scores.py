@@ -207,6 +207,63 @@ def test_rows_without_pages_holes_and_rows_behind_the_last(elem):
 
 
 @pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("new", [1, 6, 90])
+def test_strided_queries_keys_values_and_outputs(elem, new):
+    """All of them columns of wider rows, as a projection leaves them; what lies between stays."""
+    c = S.Rows(elem, 2, 64, 64, [70, 31], [new, new], seed=19)
+    c.append([0, 0], c.past)
+    T, W = 2 * new, 2 * 64
+    packed = torch.full((T, 4 * W + 8), 9.0, dtype=torch.bfloat16, device="cuda")
+    q, k, v = packed[:, :2 * W], packed[:, 2 * W:3 * W], packed[:, 3 * W:4 * W]
+    q.copy_(queries(T, 4, 64).flatten(1))
+    k.copy_(c.tokens(c.k, c.past, c.new).flatten(1))
+    v.copy_(c.tokens(c.v, c.past, c.new).flatten(1))
+    wide = torch.full((T, 3 * W), 7.0, dtype=torch.bfloat16, device="cuda")
+    ch, how = c.chunk(c.past, c.new), dict(cap=9.0, slopes=[0.1, 0.0, 1.0, 0.02], window=50)
+    sc = c.scores(4, **how)
+    ws = torch.empty(c.cache.attend_scores_workspace(ch, 4, sc), dtype=torch.uint8, device="cuda")
+    c.cache.attend_scores(ch, q, wide[:, 8:8 + 2 * W], 0.125, sc, k, v, workspace=ws)
+    c.check(q.unflatten(1, (4, 64)), wide[:, 8:8 + 2 * W].unflatten(1, (4, 64)).cpu(), 0.125, **how)
+    assert (wide[:, :8] == 7).all() and (wide[:, 8 + 2 * W:] == 7).all() and (packed[:, 4 * W:] == 9).all()
+    kr, vr = c.read([0, 0], c.total)
+    assert torch.equal(kr.double(), c.held(c.k, [0, 0], c.total)) and torch.equal(vr.double(), c.held(c.v, [0, 0], c.total))
+
+
+def test_two_streams_at_once():
+    """Other rows, masks and workspaces on two streams at a time, over one pool, against the same calls one after the other."""
+    c = S.Rows(S.FP4, 4, 128, 64, [3000, 2500], [1, 1], seed=29)
+    c.append([0, 0], c.total)
+    q = queries(2, 16, 128)
+    sc = [c.scores(16, slopes=[0.01 * h for h in range(16)]), c.scores(16, cap=20.0, window=1000)]
+    ch = c.chunk(c.past, c.new)
+    spaces = [torch.empty(c.cache.attend_scores_workspace(ch, 16, x), dtype=torch.uint8, device="cuda") for x in sc]
+    want = [torch.zeros_like(q) for _ in sc]
+    for i in range(2):
+        c.cache.attend_scores(ch, q, want[i], 0.1, sc[i], workspace=spaces[i])
+    outs, streams = [torch.zeros_like(q) for _ in sc], [torch.cuda.Stream() for _ in sc]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            c.cache.attend_scores(ch, q, outs[i], 0.1, sc[i], workspace=spaces[i], stream=streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+    c.check(q, outs[1].cpu(), 0.1, cap=20.0, window=1000)
+
+
+def test_many_rows_of_all_lengths():
+    """More rows than compute units, from none to some hundreds of positions, each with a prefix of its own."""
+    g = np.random.default_rng(5)
+    past, new = g.integers(0, 300, 150).tolist(), g.integers(0, 9, 150).tolist()
+    new[3], past[3] = 0, 0
+    c = S.Rows(S.BF16, 1, 64, 32, past, new, seed=37)
+    c.append([0] * 150, past)
+    q = queries(sum(new), 3, 64)
+    end = [max(p + 1, int(w)) for p, w in zip(positions(past, new), g.integers(0, 400, sum(new)))]
+    out = c.attend(q, files=True, end=end, slopes=[0.5, 0.05, 0.0])
+    c.check(q, out, end=end, slopes=[0.5, 0.05, 0.0])
+
+
+@pytest.mark.parametrize("elem", ELEMS)
 def test_long_rows_in_shares(elem):
     """Shares of the keys joined: windows that end inside shares, distances of a long row."""
     c = S.Rows(elem, 1, 128, 64, [9000], [2], seed=43)
