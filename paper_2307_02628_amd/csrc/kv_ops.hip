@@ -143,13 +143,16 @@ static AttendPlan plan_attend(const KvView &kv, const KvTokens &tk, int heads, i
     // not, us: 4 rows of 1000 with 20 new tokens, 32 heads 23.3, 20.0; 16 of 2000 with 5, 32 queries' and 8 kv heads 31.7, 31.1; 24 of
     // 3000 with 6 64.9, 50.9; 16 of 500 with 5 17.7, 14.1; against it 16 of 1000 to 2000 with 5, 27.0, 28.5).
     p.waves = p.nq == 16 && wgs >= 1024 ? 4 : 8;
-    // 4 bits are bound by the vector units as much as by bytes: no more than a workgroup a CU, and shares only if every wave keeps three
-    // blocks, of two tiles two (by the rule before, and this one, us, 8 kv heads of 128: 24 rows of 1000 14.4, 10.4, of 4000 26.5, 23.8;
-    // 16 of 1000 11.5, 10.0; 12 of 3000 with 5 26.7, 21.8; 16 of 2000 with 5 20.8, 19.3; against it 1 of 1500 with 5 13.9, 14.5).
-    // Two tiles with changed scores likewise, two blocks from half of the CUs on (12 rows of 3000 with 5, 8 kv heads, capped, bf16 34.0, 30.3,
-    // 8 bits 29.9, 25.6; 16 of 3000 39.3, 35.1 and 32.7, 27.0).  (One tile of theirs is not: 24 rows of 4000, 8 bits, 39.2, 44.9.)
+    // 4 bits are bound by the vector units as much as by bytes: no more than a workgroup a CU (by the rule of the others, and this one, us,
+    // 8 kv heads of 128: 24 rows of 1000 14.4, 10.4, of 4000 26.5, 23.8; 12 of 3000 with 5 26.7, 21.8).  Two shares begin where a wave has five
+    // blocks, six if that fills half of the CUs, four if scores are changed or tiles are two (one share, two: one row of 1000 9.2, 9.6, with slopes
+    // 11.2, 10.1; of 1500 11.6, 10.2; 16 of 1500 12.0, 12.6; 3 of 700 8.6, 10.0, with slopes 9.9, 10.8; 16 of 2000 with 5 20.8, 19.3).
+    // Two tiles with changed scores likewise, from four blocks a wave where half of the CUs have one (12 rows of 3000 with 5, 8 kv heads, capped,
+    // bf16 34.0, 30.3, 8 bits 29.9, 25.6; 16 of 3000 39.3, 35.1 and 32.7, 27.0).  (One tile of theirs is not: 24 rows of 4000, 8 bits, 39.2, 44.9.)
     const bool one_a_cu = kv.fp4 || (window >= 0 && p.nq == 32);
-    const int least = p.waves * (kv.fp4 ? (p.nq == 16 ? 3 : 2) : p.nq == 32 && wgs >= 128 ? (one_a_cu ? 2 : 6) : 1);
+    int least = p.waves;  // blocks of half a row
+    if (kv.fp4) least = p.nq == 32 || window >= 0 ? 2 * p.waves : wgs >= 128 ? 3 * p.waves : 5 * p.waves / 2;
+    else if (p.nq == 32 && wgs >= 128) least = (one_a_cu ? 2 : 6) * p.waves;
     auto more = [&]() { return one_a_cu ? wgs * 2 * p.splits <= 256 : wgs * p.waves * p.splits < 2048; };
     while (p.splits < 64 && more() && blocks / (2 * p.splits) >= (p.splits == 1 ? least : p.waves)) p.splits *= 2;
   }
