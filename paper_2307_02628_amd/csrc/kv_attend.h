@@ -544,7 +544,8 @@ __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, in
 
 // Few queries (one or two tiles): a workgroup is NW waves on NT tiles, and a wave takes every NW-th 32-key block, straight from
 // the page into the operand registers, with a softmax of its own; the waves' states are joined in LDS, the shares of several
-// workgroups by k_kv_merge.  Bound by the bytes of the pages.
+// workgroups by k_kv_merge.  Bound by the bytes of the pages; 4 bits by the vector units too (two conversions and a permutation for
+// four values; a step of 128 rows of 1024, 32 heads of 128, 75 us: 5.8 TB/s with the vector units at work in 63 % of all cycles).
 template <int DH, int EL>
 struct KvBlock {
   uint32x4 k[key_pieces(DH, EL)], v[value_pieces(DH, EL)];
@@ -927,7 +928,10 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 // requested before it.  80 KB of stages and up to 256 registers: two workgroups a CU.  Three (168 registers, three stages, a
 // block at a time, fragments requested as they are needed): us, 8 rows of 512 new tokens behind 2048, 32 heads of 128, bf16
 // 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 339.  Bound by the vector units (softmax;
-// conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.
+// conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.  4 bits, 8 rows of
+// 512 behind 2048: 146 us (bf16 139), the vector units at work in 51 % of all cycles, the matrix cores in 25.  What a workgroup with
+// changed scores takes before its first block is its rows' place, the ranges of its tokens and a page's number, one after the other; the
+// queries come meanwhile (2 prompts of 2047 in windows of 1: 24.7 -> 23.4 us, of which their bytes are 16).
 constexpr int rows_stages(int dh, int el) { return el != EL_BF16 ? 8 : dh == 128 ? 5 : 6; }  // (64: three workgroups, 97 -> 77 us for 32 prompts of 512)
 constexpr size_t rows_lds(int dh, int el) { return (size_t)rows_stages(dh, el) * ((key_pieces(dh, el) + value_pieces(dh, el)) * 1024 + (el != EL_BF16 ? 256 : 0)); }
 template <int DH, int EL, int SC>

@@ -10,7 +10,8 @@ namespace {
 // A workgroup files the tokens of one row and kv head that lie in one 32-key block.  DH / 8 lanes take a token: 16 bytes of
 // K and of V each, largest magnitudes over them; K goes to the page as it is, V^T by way of LDS, where the four keys that
 // are neighbours in the page are gathered.  Bound by the bytes of large calls; a block's codes leave as whole words where the
-// row fills them, and element by element at the ends of its tokens, so that what other tokens hold there stays.
+// row fills them, and element by element at the ends of its tokens, so that what other tokens hold there stays.  4 bits: four lanes share an
+// exponent, and the lanes of elements 16 apart join their values' codes, two in a byte.  509 tokens of 8 rows, 32 heads of 128: 17 us.
 template <int DH, int EL>
 __global__ __launch_bounds__(256) void k_kv_append(KvView kv, KvTokens tk, KvRows k, KvRows v, int blocks, uint32_t from) {
   constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
