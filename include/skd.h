@@ -368,8 +368,8 @@ int skd_profile_read(skd_state *st, double *ms, int64_t *launches);
  * what is finite stays so).  A position and head whose values held an
  * infinity or NaN has byte 255, codes 0, and reads as NaN.
  * The bf16 pages of a state have the same layout.
- * SKD_KV_FP4 pages hold 4 bits a value (8.5 bits a position and element of keys and values together, 17 / 32 of
- * SKD_KV_FP8's, 17 / 64 of bf16): e2m1 codes (bits s e e m: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two in a
+ * SKD_KV_FP4 pages hold 4 bits a value (8.5 bits a position and element of keys and values together: 17 / 64 of
+ * bf16, a little over half of SKD_KV_FP8): e2m1 codes (bits s e e m: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two in a
  * byte, and for every 32 neighbouring elements of a position one byte that stands for 2^(byte - 127).  The exponent is the smallest
  * from -124 on with which none of the 32 magnitudes exceeds 6 * 2^exponent; codes are rounded to nearest even (those
  * of exponent 126 end at 3, so that what is finite stays so).  32 elements among which was an infinity or NaN have byte
