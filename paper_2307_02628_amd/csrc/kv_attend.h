@@ -36,7 +36,7 @@ enum { SC_MASK = 1, SC_CAP = 2, SC_SLOPES = 4 };  // what of a call's scoring a 
 // function is applied in place, but for its factor, which takes that place, and for its constant part, which is the same for every position.
 // (Its four instructions, two of them of a quarter of the rate, stand in the code as such: with a branch around them, or around
 // the share, products and exponentials of two blocks no longer mixed: 512 tokens of 8 rows behind 2048, 32 heads of 128, bf16, us:
-// slopes 217, so 162; cap 194, 177; masks alone 156, 144, which is what the plain attention takes.)
+// slopes 217, so 162 (144 with the nearest blocks first); cap 194, 177; masks alone 156, 144, which is what the plain attention takes.)
 
 // bf16x8 of two words of codes, times the power of two whose exponent byte is `e` (255: NaN)
 __device__ inline bf16x8 widen(uint32_t a, uint32_t b, uint32_t e) {
@@ -334,7 +334,11 @@ struct Share {
   }
   // SC: the blocks that every query sees whole come first, the others, before and behind them, then: masks are in the code once.
   __device__ int wholes() const { return whole_hi - whole_lo; }
-  __device__ int block(int v) const { return v < wholes() ? whole_lo + v : v < whole_hi - lo ? v - wholes() + lo : v + lo; }
+  // LAST_FIRST: of the whole ones the last first, where scores fall with the distance: the nearest have the largest ones, and the
+  // reference is not raised again and again (from the first on, and so, us: 512 tokens of 8 rows behind 2048, 32 heads of 128, bf16 165, 144, 8
+  // bits 188, 160; steps of 32 rows of 600 in 4 bits 19.7, 18.5).
+  template <bool LAST_FIRST = false>
+  __device__ int block(int v) const { return v < wholes() ? (LAST_FIRST ? whole_hi - 1 - v : whole_lo + v) : v < whole_hi - lo ? v - wholes() + lo : v + lo; }
   __device__ int seen(const KvAttend &a, int q) const { return t.past + q / a.group + 1; }  // positions that query q sees
   __device__ long token(const KvAttend &a, int q) const { return t.at + (long)(q / a.group) * a.tk.step; }
   __device__ int head(const KvAttend &a, int q) const { return h * a.group + q % a.group; }
@@ -496,7 +500,7 @@ template <int DH, typename Tile, int NT>
 __device__ inline bool not_finite(const Tile (&tile)[NT]) { return not_finite_<DH, NT, Tile>(tile); }
 // The numerators of a wave's tiles again, over blocks first, first + step, ... below end (SC: in their order) of bf16 pages, against the references
 // that the wave has arrived at: values without their infinities and NaNs, which are then added.
-template <int DH, int SC, typename SeenOf, typename Tile, int NT>
+template <int DH, int SC, bool LAST_FIRST, typename SeenOf, typename Tile, int NT>
 __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, int q0, SeenOf seen_of, int first, int step, int end, Tile (&tile)[NT]) {
   constexpr int QC = DH / 32, VM = DH / 16;
   const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15, bpp = a.kv.g.page_tokens >> 5;
@@ -505,7 +509,7 @@ __device__ __forceinline__ void sums_again(const KvAttend &a, const Share &s, in
 #pragma unroll
     for (int m = 0; m < VM; ++m) tile[t].O[m] = floatx4{0.f, 0.f, 0.f, 0.f};
   for (int at = first; at < end; at += step) {
-    const int blk = SC ? s.block(at) : at, page = page_of(a.kv, s.r, blk);
+    const int blk = SC ? s.block<LAST_FIRST>(at) : at, page = page_of(a.kv, s.r, blk);
     if (page < 0) continue;
     const uint32x4 *src = (const uint32x4 *)(a.kv.pool + (long)page * a.kv.page_bytes + ((long)s.h * bpp + blk % bpp) * (128 * DH)) + lane;
     const Keep keep(s.held - blk * 32, grp);
@@ -712,7 +716,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
   int blk = SC ? wave : s.lo + wave, ip, ib;  // (SC: in their order)
   auto place = [&]() {
-    const int b = SC ? s.block(blk) : blk;
+    const int b = SC ? s.block<(SC & SC_SLOPES) != 0>(blk) : blk;
     ip = b / bpp;
     ib = b % bpp;
   };
@@ -724,7 +728,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   auto fetch = [&](Block &b) {
     const bool is = number >= 0 && number < a.kv.pages && ip < a.kv.g.max_pages;
     if (is) load(number, ib, b);
-    const int base = is ? (SC ? s.block(blk) : blk) * 32 : -1;
+    const int base = is ? (SC ? s.block<(SC & SC_SLOPES) != 0>(blk) : blk) * 32 : -1;
     blk += NW;
     if constexpr (SC) {
       place();
@@ -764,7 +768,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
     while (blk < end) step(std::true_type());
   }
   if constexpr (EL == EL_BF16) {
-    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, seen_of, SC ? wave : s.lo + wave, NW, SC ? s.hi - s.lo : s.hi, tile);
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC, (SC & SC_SLOPES) != 0>(a, s, q0, seen_of, SC ? wave : s.lo + wave, NW, SC ? s.hi - s.lo : s.hi, tile);
   }
   uint32_t ke = 0, ve = 0;  // exponents of the new token
   if constexpr (NT == 1) {
@@ -986,7 +990,8 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
   // in, waited for where it is loaded; a block without a page is loaded from page 0 and masked, as is every block from the
   // moment on at which a window has an entry that is no page.
   const int32_t *table = a.kv.table + (long)s.r * a.kv.g.max_pages;
-  const int begin = SC ? s.block(0) : s.lo;
+  constexpr bool BACK = (SC & SC_SLOPES) != 0;     // whole blocks from the last one on
+  const int begin = SC ? s.block<BACK>(0) : s.lo;
   int ip = begin / bpp, ib = begin % bpp, pages = 0, window = -1;
   uint32_t none = 0;                               // a bit for each stage: its block has no page
   int into = 0, from = 0, asked = SC ? 0 : s.lo;   // stages of the next block requested and used; blocks requested (SC: in their order)
@@ -1004,7 +1009,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
       const int at = window * 64 + lane;
       pages = at < a.kv.g.max_pages ? table[at] : -1;
       asm volatile("" : "+v"(pages));
-      gaps |= __any(at >= ip && at < ip_end && (pages < 0 || pages >= a.kv.pages));
+      gaps |= __any(at >= (BACK ? s.lo / bpp : ip) && at < ip_end && (pages < 0 || pages >= a.kv.pages));
     }
     int page = __builtin_amdgcn_readlane(pages, ip & 63);
     is = page >= 0 && page < a.kv.pages;
@@ -1030,6 +1035,13 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
                                        (__attribute__((address_space(3))) void *)(ring + into * STAGE + FR * 64), 4, 0, 0);
     into = next(into);
     ++asked;
+    if constexpr (BACK) {
+      const int blk = s.block<true>(asked);
+      ip = blk / bpp;
+      ib = blk % bpp;
+      if (asked < asked_end) new_page();
+      return;
+    }
     src += block_bytes(DH, EL) / 16;
     ex_src += FP4 ? block_bytes(DH, EL) : 64;
     bool other = ++ib == bpp;  // page
@@ -1038,7 +1050,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
       ++ip;
     }
     if (SC && asked == turn) {  // (behind the whole ones, and where these were)
-      const int blk = s.block(asked);
+      const int blk = s.block<BACK>(asked);
       turn = turn == s.wholes() ? s.whole_hi - s.lo : 0;
       ip = blk / bpp;
       ib = blk % bpp;
@@ -1164,6 +1176,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
   // Two blocks that every query sees whole: one branch for all of their weights, so that from there on exponentials and products
   // are formed side by side, and the values are on their way before.
   auto use_two = [&](int one, int two, int base) {
+    constexpr int STEP = BACK ? -32 : 32;  // from one to the other
     const int stage[2] = {one, two};
     const float c = factor<SC>(a);
     floatx4 S[2][NT][2];
@@ -1174,7 +1187,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       __builtin_amdgcn_s_setprio(1);  // (before the other waves' exponentials: 140 -> 136 us)
-      scores(stage[u], base + 32 * u, true, S[u]);
+      scores(stage[u], base + STEP * u, true, S[u]);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (FP8) {
         factor_words(stage[u], ve[u]);
@@ -1184,7 +1197,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
         for (int i = 0; i < 2; ++i) raise |= (((ve[u][i] & 0x7f7f7f7fu) + 0x01010101u) & ve[u][i] & 0x80808080u) != 0;
       }
 #pragma unroll
-      for (int t = 0; t < NT; ++t) end_scores<SC, false>(a.sc, true, seen_of(t), base + 32 * u + 4 * grp, S[u][t]);
+      for (int t = 0; t < NT; ++t) end_scores<SC, false>(a.sc, true, seen_of(t), base + STEP * u + 4 * grp, S[u][t]);
     }
     values_of(stage[0], vw);
     float p[2][NT][8];
@@ -1272,7 +1285,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
   };
   auto single = [&](int at) {
     open(at, 1);
-    const int blk = SC ? s.block(at) : at;
+    const int blk = SC ? s.block<BACK>(at) : at;
     const bool no_page = none >> from & 1;
     if (!FP4 && (no_page || blk * 32 + 32 > s.held)) clear(no_page ? 0 : s.held - blk * 32);  // (4 bits: codes are finite, exponents are looked at)
     if (blk < last && (!SC || blk >= from_blk)) use(blk, no_page);
@@ -1280,7 +1293,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
   };
   auto pair = [&](int at) {
     open(at, 2);
-    const int blk = SC ? s.whole_lo + at : at;
+    const int blk = SC ? s.block<BACK>(at) : at;
     const int second = next(from);
     if (busy) use_two(from, second, blk * 32);
     from = next(second);
@@ -1295,7 +1308,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
     for (; blk < s.hi; ++blk) single(blk);
   }
   if constexpr (EL == EL_BF16) {
-    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC>(a, s, q0, seen_of, SC ? 0 : s.lo, 1, SC ? s.hi - s.lo : last, tile);
+    if (__builtin_expect(not_finite<DH>(tile), 0)) sums_again<DH, SC, false>(a, s, q0, seen_of, SC ? 0 : s.lo, 1, SC ? s.hi - s.lo : last, tile);
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
