@@ -26,10 +26,11 @@ enum { SC_MASK = 1, SC_CAP = 2, SC_SLOPES = 4 };  // what of a call's scoring a 
 // selection.  Since 0 * infinity is not 0, that leaves values: beyond the row's last position they are cleared (a page may hold
 // anything there); an infinity or NaN that only later queries see makes sums that are not finite, and a wave that ends with such
 // sums forms them once more (sums_again), without such values, which are added for the queries that see them.  8-bit values are
-// finite, what is not is in their scales, which are selected with the weights.
+// finite where they were filed, what is not is in their scales, which are selected with the weights; with changed scores a position
+// that no query sees may never have been filed, so that codes of NaN are looked for (odd_codes).
 // The powers of two of 8-bit keys are an operand of the conversion to bf16, those of values multiply the weights: both exact.
 // Those of 4-bit keys and values are operands of the conversion (32 elements of a value have one each, so that the weights would
-// have to be multiplied for every 32); a value that is not finite is in them, and is added for the queries that see it.
+// have to be multiplied for every 32); a value that is not finite is in them, and is added for the queries that see it (odd_exponents).
 //
 // Changed scores and masks (SC, bits of what a call asks for).  A query sees positions low .. limit - 1 of its own.  The share of
 // the distance, over what scores are multiplied by, is where the matrix instructions' sums begin: one instruction a score.  A cap's
@@ -205,36 +206,65 @@ __device__ inline bf16x8 visible(int low, int limit, int grp) {
   for (int j = 0; j < 8; ++j) v[j] = (__bf16)(hidden<LOW>(j, low, limit, grp) ? 0.0f : 1.0f);
   return v;
 }
-// 4-bit values that are not finite, or that nobody wrote: of a lane's words of exponents, [group][2], those of positions from `valid` of
-// the block on are cleared where their values might not be finite (exponents from 126 on), and where a byte stands for NaN it is
-// cleared and the sums of the queries that see it become NaN.  Rare: out of the way of everything else.
-template <int DH, bool LOW, int NT, typename Tile>
-__device__ inline void odd_exponents(uint32_t (&e)[DH / 16], Tile (&tile)[NT], const int (&low)[NT], const int (&limit)[NT], int valid) {
+// Whether masked blocks look for values that are not finite as they come.  (8 bits with scores as they are: the row's last token sees every position
+// that the row has, so they were all filed, and what lies behind is cleared.  bf16: sums_again.)
+constexpr bool looks(int el, int sc) { return el == EL_FP4 || (el == EL_FP8 && sc); }
+__device__ inline uint32_t bytes_of(uint32_t top) { return (top << 1) - (top >> 7); }  // all bits of the bytes whose upper one is set
+// 4-bit values of a masked block that are not finite, since 0 is no weight for them, wherever they are: a position that holds NaN, or one
+// that nobody wrote.  Of a lane's words of exponents, [group][2], bytes of NaN (and 254, which is never written) are cleared and
+// the sums of the queries that see them become NaN; codes with exponent 126 end at 3, as written ones do.  Rare: out of the way of
+// everything else.
+template <int DH, bool LOW, int NT, int NV, typename Tile>
+__device__ inline void odd_exponents(uint32x4 (&v)[NV], uint32_t (&e)[DH / 16], Tile (&tile)[NT], const int (&low)[NT], const int (&limit)[NT]) {
   auto odd = [&](int i) { return ((e[i] & 0x7f7f7f7fu) + 0x03030303u) & e[i] & 0x80808080u; };  // bytes from 253 on
   uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) any |= odd(i);
   if (__builtin_expect(!__any(any != 0), 1)) return;
-  const int grp = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) {
     if (!__any(odd(i) != 0)) continue;
 #pragma unroll 1
     for (int g = 0; g < 4; ++g) {
-      const uint32_t w = (uint32_t)__shfl((int)e[i], 16 * g);
+      const uint32_t b = (uint32_t)__shfl((int)e[i], 16 * g);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          if ((w >> (8 * y) & 255u) == 255u && !hidden<LOW>(4 * (i & 1) + y, low[t], limit[t], g)) {
+          if ((b >> (8 * y) & 255u) >= 254u && !hidden<LOW>(4 * (i & 1) + y, low[t], limit[t], g)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) tile[t].O[i / 2 * 2 + u] += __uint_as_float(0x7fc00000u);
           }
     }
-#pragma unroll
-    for (int y = 0; y < 4; ++y)
-      if ((e[i] >> (8 * y) & 255u) == 255u || block_pos(4 * (i & 1) + y, grp) >= valid) e[i] &= ~(255u << (8 * y));
+    const uint32_t w = v[i / 4][i % 4], large = w >> 1 & w >> 2 & 0x11111111u & bytes_of(odd(i));  // of the same keys; codes of 4 and 6
+    v[i / 4][i % 4] = (w & ~(large << 1)) | large;
+    e[i] &= ~bytes_of(((e[i] & 0x7f7f7f7fu) + 0x02020202u) & e[i] & 0x80808080u);
   }
+}
+__device__ inline uint32_t over_row(uint32_t x) {  // bits that any of 16 lanes has
+  x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xF, 0xF, true);
+  x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xF, 0xF, true);
+  x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xF, 0xF, true);
+  return x | (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xF, 0xF, true);
+}
+// 8-bit values of a masked block likewise: codes of NaN, which are never filed, are cleared; what is returned says whether there were any, and
+// `bad` where: the bytes of the lane's keys 0 .. 3 and 4 .. 7, as their exponents lie, all bits set.
+template <int NV>
+__device__ inline bool odd_codes(uint32x4 (&v)[NV], uint32_t (&bad)[2]) {
+  auto odd = [](uint32_t w) { return (w & 0x7f7f7f7fu) + 0x01010101u; };  // the upper bit of a byte
+  bad[0] = bad[1] = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bad[j & 1] |= odd(v[i][j]);
+  if (__builtin_expect(!__any(((bad[0] | bad[1]) & 0x80808080u) != 0), 1)) return false;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i][j] &= ~bytes_of(odd(v[i][j]) & 0x80808080u);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) bad[x] = bytes_of(over_row(bad[x]) & 0x80808080u);  // (the elements of a key are in 16 lanes)
+  return true;
 }
 // masks of a lane's eight bf16 values: positions below `valid`
 struct Keep {
@@ -557,7 +587,7 @@ struct KvBlock {
 };
 template <int DH, int EL, int SC, int NT, int NW>
 __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend a, int pairs) {
-  constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
+  constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4, LOOKS = looks(EL, SC);
   constexpr int QC = DH / 32, VM = DH / 16, NQ = 16 * NT;
   // One tile of 128-wide heads keeps its queries in LDS: with them in registers the loop did not fit the 128 of 4 waves a SIMD.
   constexpr bool LDS_Q = NT == 1 && DH == 128;
@@ -656,6 +686,12 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
         for (int t = 0; t < NT; ++t) S[t][tl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, x[t], S[t][tl], 0, 0, 0);
       }
     }
+    if constexpr (FP8 && LOOKS && masked) {  // (positions of such codes hold NaN)
+      if (uint32_t bad[2]; odd_codes(b.v, bad)) {
+        b.ve[0] |= bad[0];
+        b.ve[1] |= bad[1];
+      }
+    }
     float vs[8];
     if constexpr (FP8) {
 #pragma unroll
@@ -669,7 +705,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       pv[t] = tile[t].template weights<FP8, SC != 0>(masked, S[t], factor<SC>(a), x.low - base, x.limit - base, grp, vs);
     }
     if constexpr (FP4) {
-      if (masked) {
+      if constexpr (masked) {
         int from[NT], to[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -677,7 +713,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
           from[t] = x.low - base;
           to[t] = x.limit - base;
         }
-        odd_exponents<DH, SC != 0, NT>(b.ve, tile, from, to, valid - base);
+        odd_exponents<DH, SC != 0, NT>(b.v, b.ve, tile, from, to);
       }
 #pragma unroll
       for (int i = 0; i < DH / 32; ++i) {
@@ -690,7 +726,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       }
       return;
     }
-    if (masked) {
+    if (masked && !LOOKS) {
       const Keep keep(valid - base, grp);
       if constexpr (FP8) {  // (codes of positions that the row does not have may be NaN)
 #pragma unroll
@@ -940,7 +976,7 @@ constexpr int rows_stages(int dh, int el) { return el != EL_BF16 ? 8 : dh == 128
 constexpr size_t rows_lds(int dh, int el) { return (size_t)rows_stages(dh, el) * ((key_pieces(dh, el) + value_pieces(dh, el)) * 1024 + (el != EL_BF16 ? 256 : 0)); }
 template <int DH, int EL, int SC>
 __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(KvAttend a, int pairs) {
-  constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4;
+  constexpr bool FP8 = EL == EL_FP8, FP4 = EL == EL_FP4, LOOKS = looks(EL, SC);
   constexpr int QC = DH / 32, VM = DH / 16, NT = 2, NW = 4, NS = rows_stages(DH, EL), NQ = 16 * NT * NW;
   constexpr int KF = key_pieces(DH, EL), FR = KF + value_pieces(DH, EL), LPW = FR < NW ? 1 : FR / NW;  // fragments a stage, loads of a wave
   constexpr int STAGE = FR * 64 + (FP8 || FP4 ? 16 : 0);  // 16-byte pieces; behind 8- and 4-bit blocks 256 bytes for their exponents
@@ -1157,19 +1193,30 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
     }
     uint32x4 vw[FR - KF];
     values_of(from, vw);
+    int lo[NT], to[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const Seen x = seen_of(t);
+      lo[t] = x.low - base;
+      to[t] = no_page ? 0 : x.limit - base;
+    }
     if constexpr (FP4) {
       uint32_t ve[DH / 16];
-      int lo[NT], to[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const Seen x = seen_of(t);
-        lo[t] = x.low - base;
-        to[t] = no_page ? 0 : x.limit - base;
-      }
       exponents4(from, ve);
-      odd_exponents<DH, SC != 0, NT>(ve, tile, lo, to, no_page ? 0 : s.held - base);
+      odd_exponents<DH, SC != 0, NT>(vw, ve, tile, lo, to);
       add_values4(vw, ve, pv);
     } else {
+      if constexpr (FP8 && LOOKS) {
+        if (uint32_t bad[2]; odd_codes(vw, bad)) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {  // (a weight of NaN for a query that sees any)
+            bool sees = false;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sees |= (bad[j >> 2] >> (8 * (j & 3)) & 255u) && !hidden<SC != 0>(j, lo[t], to[t], grp);
+            if (sees) pv[t][0] = (__bf16)__uint_as_float(0x7fc00000u);
+          }
+        }
+      }
       add_values(vw, pv);
     }
   };
@@ -1287,7 +1334,7 @@ __global__ __launch_bounds__(256, SC && DH == 64 ? 3 : 2) void k_kv_attend_rows(
     open(at, 1);
     const int blk = SC ? s.block<BACK>(at) : at;
     const bool no_page = none >> from & 1;
-    if (!FP4 && (no_page || blk * 32 + 32 > s.held)) clear(no_page ? 0 : s.held - blk * 32);  // (4 bits: codes are finite, exponents are looked at)
+    if (!LOOKS && (no_page || blk * 32 + 32 > s.held)) clear(no_page ? 0 : s.held - blk * 32);
     if (blk < last && (!SC || blk >= from_blk)) use(blk, no_page);
     from = next(from);
   };
