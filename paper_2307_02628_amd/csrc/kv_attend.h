@@ -840,10 +840,11 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
       }
       auto &x = tile[0];
       float score = __shfl(S[0], col);
+      const bool sees = !SC || sh_new[col];
       if constexpr (SC) {  // (at a distance of 0)
         if constexpr (SC & SC_CAP) score = capped(a.sc.in, score);
         score *= factor<SC>(a);
-        if (!sh_new[col]) score = -INFINITY;
+        if (!sees) score = -INFINITY;
       } else {
         score *= a.c;
       }
@@ -876,7 +877,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (SC) {
-            if (p == 0.f) v[i] = 0.f;  // (nobody sees it, or its weight is nothing beside the others': no 0 x infinity)
+            if (!sees) v[i] = 0.f;  // (no 0 x infinity)
           }
           x.O[m][i] = x.O[m][i] * alpha + p * v[i];
         }

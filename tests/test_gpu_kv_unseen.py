@@ -1,5 +1,7 @@
 """Attention with masks over rows of which only what their tokens see was ever filed: what the pages hold at the other positions, before, between
 and behind, does not reach a query, whatever it is (skd_kv_attend_scores), against 64 bits on the CPU."""
+import copy
+
 import pytest
 import torch
 
@@ -58,3 +60,34 @@ def test_places_that_no_token_sees_of_a_long_row_in_shares(elem, fill, new):
     q = queries(new, 4, 128)
     for how in (dict(window=window), dict(window=window, slopes=[0.1, 0.0, 0.01, 1.0], cap=30.0)):
         c.check(q, c.attend(q, files=True, **how), **how)
+
+
+def finite(c):
+    """The same rows with what a page holds as infinity or NaN as zeros."""
+    same = copy.copy(c)
+    held = [torch.from_numpy(S.as_held(x.double().numpy(), c.elem)) for x in c.v]
+    same.v = [torch.where(torch.isfinite(h), x.double(), 0.0).bfloat16() for h, x in zip(held, c.v)]
+    return same
+
+
+@pytest.mark.parametrize("elem", [S.BF16, S.FP8, S.FP4])
+@pytest.mark.parametrize("past", [20, 300])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_a_filed_value_that_is_not_finite_and_weighs_nothing(elem, past, dh):
+    """The token of the call has an infinity and a NaN among its values, and a key of every block a score so much larger that its weight is 0 in 32 bits:
+    queries that see it get no finite result, whether the call files it or the cache holds it, and others are as if it were not there."""
+    c = S.Rows(elem, 2, dh, 64, [past], [1], seed=71)
+    q = queries(1, 2, dh)
+    c.k[0][5:past:16] = 400.0 / dh ** 0.5 * q[0].cpu()               # a score of about 400
+    c.v[0][5:past:16] = c.v[0][5].clone()
+    c.v[0][past, 0, 3], c.v[0][past, 1, 40] = float("inf"), float("nan")
+    c.append([0], [past])
+    for how in (dict(cap=1000.0), dict(window=past), dict(slopes=[2.0 ** -9, 0.0]), dict(slopes=[0.0, 2.0 ** -9], cap=1000.0, end=[past + 1])):
+        for files in (True, False):
+            out = c.attend(q, files=files, **how)[0]
+            lost = torch.isnan(torch.from_numpy(S.as_held(c.v[0][past].double().numpy(), elem))) | torch.isinf(c.v[0][past])
+            assert lost.any() and torch.equal(~torch.isfinite(out), lost), (how, files)
+            finite(c).check(q, torch.where(lost, torch.from_numpy(S.as_held(c.v[0][5].double().numpy(), elem)), out.double())[None], **how)
+    for how in (dict(end=[past]), dict(end=[past], cap=1000.0, slopes=[0.5, 0.0])):
+        for files in (True, False):
+            c.check(q, c.attend(q, files=files, **how), **how)
