@@ -8,28 +8,53 @@ namespace skd {
 
 namespace {
 
+constexpr int PAGE_CHUNKS = 16 * TABLE_CHUNK;  // of pages, whose counts are added up as they are (3 million pages, `over` for more than 1024 chunks: 54 -> 76 us)
+__host__ __device__ inline int chunks_of(int n) { return (int)(((long)n + TABLE_CHUNK - 1) / TABLE_CHUNK); }
+// Counts of n chunks and, beyond `most` of them, of chunks of chunks (`over`), so that who needs the sum of all before a place reads some
+// thousands at most: 2^24 rows are 2^14 chunks, 2^31 pages 2^21.  Atomics add those up, of whole numbers, in any order the same; to a few
+// neighbouring places they take 10 to 20 ns each, so that they are for large numbers alone.
+struct Counts {
+  int32_t *of, *over;
+  int n, most;
+  __device__ bool far() const { return n > most; }
+  __device__ void set(int c, int x) const {
+    of[c] = x;
+    if (far()) atomicAdd(&over[c / TABLE_CHUNK], x);
+  }
+};
 // Work of an assignment: what a page is to the entries of the new table, before any page is dealt out.
 struct AssignWork {
   int32_t *uses;     // [pages]: entries that name it
   int32_t *writes;   // of them those that new tokens go to
   int32_t *loose;    // of them those that hold nothing yet
-  int32_t *lowest;   // the first of those that new tokens go to
-  int32_t *free, *soft;  // [chunks]: pages that no entry names, that none names but loose ones
+  Counts needs, copies;  // `need` and `copy` by chunks of rows
+  Counts free;       // [chunks of pages]: pages that no entry names
+  int32_t *lowest;   // [pages]: the first of those that new tokens go to
+  int32_t *soft;     // [chunks]: pages that none names but loose ones
   int32_t *need, *copy;  // [rows]: pages that the row has to get; 1: one of them as a copy
   int32_t *list;     // free pages, ascending, as many as there could be entries for
-  __host__ __device__ AssignWork(const KvTable &t, int chunks) {
+  __host__ __device__ explicit AssignWork(const KvTable &t) {
+    const int chunks = chunks_of(t.pages), row_chunks = chunks_of(t.rows);
     uses = t.work;
     writes = uses + t.pages;
     loose = writes + t.pages;
-    lowest = loose + t.pages;
-    free = lowest + t.pages;
-    soft = free + chunks;
+    needs.over = loose + t.pages;
+    copies.over = needs.over + chunks_of(row_chunks);
+    free.over = copies.over + chunks_of(row_chunks);
+    lowest = free.over + chunks_of(chunks);  // (all before it begins with 0)
+    needs.of = lowest + t.pages;
+    copies.of = needs.of + row_chunks;
+    free.of = copies.of + row_chunks;
+    soft = free.of + chunks;
     need = soft + chunks;
     copy = need + t.rows;
     list = copy + t.rows;
+    needs.n = copies.n = row_chunks;
+    free.n = chunks;
+    needs.most = copies.most = TABLE_CHUNK;
+    free.most = PAGE_CHUNKS;
   }
 };
-__host__ __device__ inline int chunks_of(int pages) { return (int)(((long)pages + TABLE_CHUNK - 1) / TABLE_CHUNK); }
 __host__ __device__ inline long list_of(const KvTable &t) {
   const long entries = (long)t.rows * t.width;
   return entries < t.pages ? entries : t.pages;
@@ -55,7 +80,7 @@ __global__ __launch_bounds__(256) void k_table_fill(int32_t *w, long zero, long 
 }
 // The rows in their new order, cut to what they will hold, and what every page is to them.
 __global__ __launch_bounds__(256) void k_table_gather(KvTable t) {
-  const AssignWork w(t, chunks_of(t.pages));
+  const AssignWork w(t);
   const uint32_t at = blockIdx.x * 256u + threadIdx.x, all = (uint32_t)t.rows * (uint32_t)t.width;
   if (at >= all) return;
   const int r = (int)(at / t.width), i = (int)(at % t.width);
@@ -87,8 +112,8 @@ __device__ inline int wave_sum_i(int v) {
 }
 // A wave for each row: the pages that it needs; a workgroup for each chunk of pages: the free ones.
 __global__ __launch_bounds__(256) void k_table_count(KvTable t, int rows4) {
-  const int chunks = chunks_of(t.pages), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const AssignWork w(t, chunks);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const AssignWork w(t);
   if ((int)blockIdx.x < rows4) {
     const int r = blockIdx.x * 4 + wave;
     if (r >= t.rows) return;
@@ -126,17 +151,27 @@ __global__ __launch_bounds__(256) void k_table_count(KvTable t, int rows4) {
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    w.free[c] = sum[0][0] + sum[0][1] + sum[0][2] + sum[0][3];
+    w.free.set(c, sum[0][0] + sum[0][1] + sum[0][2] + sum[0][3]);
     w.soft[c] = sum[1][0] + sum[1][1] + sum[1][2] + sum[1][3];
   }
 }
-// Sum of n values over the lanes of a wave.
-__device__ inline long sum_of(const int32_t *x, int n) {
-  long v = 0;
+// Sums over the lanes of a wave (none is above the number of pages, or of entries): a lane's part of n values, and all of them.
+__device__ inline int part_of(const int32_t *x, int n) {
+  int v = 0;
   for (int i = threadIdx.x & 63; i < n; i += 64) v += x[i];
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
   return v;
+}
+__device__ inline int sum_of(const int32_t *x, int n) { return wave_sum_i(part_of(x, n)); }
+__device__ inline int sum_of(const Counts &c) { return c.far() ? sum_of(c.over, chunks_of(c.n)) : sum_of(c.of, c.n); }
+__device__ inline int part_before(const Counts &c, int chunk) {
+  const int o = c.far() ? chunk / TABLE_CHUNK : 0;
+  return part_of(c.over, o) + part_of(c.of + o * TABLE_CHUNK, chunk - o * TABLE_CHUNK);
+}
+__device__ inline int sum_before(const Counts &c, int chunk) { return wave_sum_i(part_before(c, chunk)); }
+// of all values of which x are counts' own, those before place i
+__device__ inline int sum_before(const Counts &c, const int32_t *x, int i) {
+  const int chunk = i / TABLE_CHUNK;
+  return wave_sum_i(part_before(c, chunk) + part_of(x + (long)chunk * TABLE_CHUNK, i - chunk * TABLE_CHUNK));
 }
 // Place of each of a chunk's pages for which `is` holds among them, in f(page, place).  256 threads, four pages each.
 template <typename Is, typename F>
@@ -168,26 +203,36 @@ __device__ inline void each_in_chunk(int c, int pages, Is is, F f) {
       at += has[k];
     }
 }
-// The free pages in ascending order.
+// The free pages in ascending order; behind the workgroups of pages one for each chunk of rows: what they need together.
 __global__ __launch_bounds__(256) void k_table_list(KvTable t) {
-  const AssignWork w(t, chunks_of(t.pages));
-  const long before = sum_of(w.free, blockIdx.x), room = list_of(t);
+  const AssignWork w(t);
+  if ((int)blockIdx.x >= w.free.n) {
+    const int c = blockIdx.x - w.free.n, wave = threadIdx.x >> 6;
+    if (wave < 2) {
+      const int32_t *x = (wave ? w.copy : w.need) + (long)c * TABLE_CHUNK;
+      const int all = sum_of(x, min(TABLE_CHUNK, t.rows - c * TABLE_CHUNK));
+      if ((threadIdx.x & 63) == 0) (wave ? w.copies : w.needs).set(c, all);
+    }
+    return;
+  }
+  const long before = sum_before(w.free, blockIdx.x), room = list_of(t);
   if (before >= room) return;
   each_in_chunk(blockIdx.x, t.pages, [&](long p) { return w.uses[p] == 0; },
                 [&](int p, bool is, int at) {
                   if (is && before + at < room) w.list[before + at] = p;
                 });
 }
-// A wave for each row deals its pages out: those that come behind the needs of the rows before it.
+// A wave for each row deals its pages out: those that come behind the needs of the rows before it, by their chunks' sums (2^18 rows of one
+// page, ms: 0.43, with all rows added up by every row's wave 29; 4096 rows of 16 0.030, 0.048).
 __global__ __launch_bounds__(64) void k_table_deal(KvTable t) {
-  const int chunks = chunks_of(t.pages), r = blockIdx.x, lane = threadIdx.x;
+  const int r = blockIdx.x, lane = threadIdx.x;
   if (t.rows == 0) {
     if (lane < 3) t.counts[lane] = 0;
     return;
   }
-  const AssignWork w(t, chunks);
-  const long free = sum_of(w.free, chunks), before = sum_of(w.need, r), all = before + sum_of(w.need + r, t.rows - r);
-  const long copies_before = sum_of(w.copy, r);
+  const AssignWork w(t);
+  const long free = sum_of(w.free), before = sum_before(w.needs, w.need, r), all = sum_of(w.needs);
+  const long copies_before = sum_before(w.copies, w.copy, r);
   const bool enough = all <= free;
   const Span s = span_of(t, r);
   long place = before;
@@ -211,13 +256,13 @@ __global__ __launch_bounds__(64) void k_table_deal(KvTable t) {
     }
     place += __popcll(who);
   }
-  const long copies = enough ? copies_before + sum_of(w.copy + r, t.rows - r) : 0;
+  const long copies = enough ? sum_of(w.copies) : 0;
   if (lane == 0 && r >= copies) t.copies[2 * (long)r] = t.copies[2 * (long)r + 1] = -1;
   if (r == 0) {
-    const long soft = sum_of(w.soft, chunks);
+    const long soft = sum_of(w.soft, chunks_of(t.pages));
     if (lane == 0) {
       t.counts[0] = (int)(enough ? t.pages - free + all : t.pages - soft);
-      t.counts[1] = (int)(enough ? 0 : min(all - free, 0x7fffffffL));
+      t.counts[1] = (int)(enough ? 0 : all - free);
       t.counts[2] = (int)copies;
     }
   }
@@ -343,25 +388,29 @@ __global__ __launch_bounds__(1024) void k_table_assign_one(KvTable t) {
 // ------------------------------------------------------------------ pages in use moved to the lowest places
 struct CompactWork {
   int32_t *uses, *rank;     // [pages]: 1 if named; place among the pages that move
-  int32_t *used;            // [chunks]
+  Counts used;              // [chunks]
   int32_t *source, *target; // [pages / 2]
-  __host__ __device__ CompactWork(const KvTable &t, int chunks) {
+  __host__ __device__ explicit CompactWork(const KvTable &t) {
+    const int chunks = chunks_of(t.pages);
     uses = t.work;
-    rank = uses + t.pages;
-    used = rank + t.pages;
-    source = used + chunks;
+    used.over = uses + t.pages;
+    used.of = used.over + chunks_of(chunks);  // (all before it begins with 0)
+    rank = used.of + chunks;
+    source = rank + t.pages;
+    used.n = chunks;
+    used.most = PAGE_CHUNKS;
     target = source + t.pages / 2;
   }
 };
 __global__ __launch_bounds__(256) void k_table_mark(KvTable t) {
-  const CompactWork w(t, chunks_of(t.pages));
+  const CompactWork w(t);
   const uint32_t at = blockIdx.x * 256u + threadIdx.x, all = (uint32_t)t.rows * (uint32_t)t.width;
   if (at >= all) return;
   const int page = t.table[at];
   if (page >= 0 && page < t.pages) w.uses[page] = 1;
 }
 __global__ __launch_bounds__(256) void k_table_used(KvTable t) {
-  const CompactWork w(t, chunks_of(t.pages));
+  const CompactWork w(t);
   __shared__ int sum[4];
   int n = 0;
   for (int k = threadIdx.x; k < TABLE_CHUNK; k += 256) {
@@ -371,18 +420,13 @@ __global__ __launch_bounds__(256) void k_table_used(KvTable t) {
   n = wave_sum_i(n);
   if ((threadIdx.x & 63) == 0) sum[threadIdx.x >> 6] = n;
   __syncthreads();
-  if (threadIdx.x == 0) w.used[blockIdx.x] = sum[0] + sum[1] + sum[2] + sum[3];
-}
-// Pages in use before page `n` (of all of them, where n is their number).
-__device__ inline int used_before(const CompactWork &w, int n) {
-  const int c = n / TABLE_CHUNK;
-  return (int)(sum_of(w.used, c) + sum_of(w.uses + (long)c * TABLE_CHUNK, n - c * TABLE_CHUNK));
+  if (threadIdx.x == 0) w.used.set(blockIdx.x, sum[0] + sum[1] + sum[2] + sum[3]);
 }
 // The k-th page in use at or behind the number of all of them goes to the k-th free one before it.
 __global__ __launch_bounds__(256) void k_table_rank(KvTable t) {
-  const int chunks = chunks_of(t.pages), c = blockIdx.x;
-  const CompactWork w(t, chunks);
-  const int used = (int)sum_of(w.used, chunks), below = used_before(w, used), before = (int)sum_of(w.used, c);
+  const int c = blockIdx.x;
+  const CompactWork w(t);
+  const int used = sum_of(w.used), below = sum_before(w.used, w.uses, used), before = sum_before(w.used, c);
   each_in_chunk(c, t.pages, [&](long p) { return w.uses[p] != 0; },
                 [&](int p, bool is, int at) {
                   at += before;  // pages in use before p
@@ -394,9 +438,8 @@ __global__ __launch_bounds__(256) void k_table_rank(KvTable t) {
                 });
 }
 __global__ __launch_bounds__(256) void k_table_move(KvTable t) {
-  const int chunks = chunks_of(t.pages);
-  const CompactWork w(t, chunks);
-  const int used = (int)sum_of(w.used, chunks), moved = used - used_before(w, used);
+  const CompactWork w(t);
+  const int used = sum_of(w.used), moved = used - sum_before(w.used, w.uses, used);
   const uint32_t at = blockIdx.x * 256u + threadIdx.x, all = (uint32_t)t.rows * (uint32_t)t.width;
   if (at < all) {
     const int page = t.table[at];
@@ -487,15 +530,17 @@ unsigned groups_for(long n) { return (unsigned)std::max(1L, (n + 255) / 256); }
 
 }  // namespace
 
+// words of work that begin with 0
+static size_t assign_zeros(const KvTable &t) { return 3 * (size_t)t.pages + 2 * (size_t)chunks_of(chunks_of(t.rows)) + chunks_of(chunks_of(t.pages)); }
+static size_t compact_zeros(const KvTable &t) { return (size_t)t.pages + chunks_of(chunks_of(t.pages)); }
 bool kv_table_fits(const KvTable &t) {
   const long entries = (long)t.rows * t.width;
   return entries < 1L << 31 && launch_fits((long)t.rows + chunks_of(t.pages), 256);
 }
 size_t kv_assign_words(const KvTable &t) {
-  const size_t chunks = chunks_of(t.pages);
-  return 4 * (size_t)t.pages + 2 * chunks + 2 * (size_t)t.rows + (size_t)list_of(t);
+  return assign_zeros(t) + t.pages + 2 * (size_t)chunks_of(t.pages) + 2 * (size_t)chunks_of(t.rows) + 2 * (size_t)t.rows + (size_t)list_of(t);
 }
-size_t kv_compact_words(const KvTable &t) { return 2 * (size_t)t.pages + chunks_of(t.pages) + 2 * (size_t)(t.pages / 2); }
+size_t kv_compact_words(const KvTable &t) { return compact_zeros(t) + t.pages + chunks_of(t.pages) + 2 * (size_t)(t.pages / 2); }
 
 void kv_assign(hipStream_t s, const KvTable &t) {
   const int chunks = chunks_of(t.pages), rows4 = (t.rows + 3) / 4;
@@ -504,10 +549,10 @@ void kv_assign(hipStream_t s, const KvTable &t) {
     SKD_LAUNCH(k_table_assign_one, dim3(1), dim3(1024), 0, s, t);
     return;
   }
-  SKD_LAUNCH(k_table_fill, dim3(std::min(groups_for(4L * t.pages), 1024u)), dim3(256), 0, s, t.work, 3L * t.pages, (long)t.pages);
+  SKD_LAUNCH(k_table_fill, dim3(std::min(groups_for(4L * t.pages), 1024u)), dim3(256), 0, s, t.work, (long)assign_zeros(t), (long)t.pages);
   SKD_LAUNCH(k_table_gather, dim3(groups_for(entries)), dim3(256), 0, s, t);
   SKD_LAUNCH(k_table_count, dim3(rows4 + chunks), dim3(256), 0, s, t, rows4);
-  SKD_LAUNCH(k_table_list, dim3(chunks), dim3(256), 0, s, t);
+  SKD_LAUNCH(k_table_list, dim3(chunks + chunks_of(t.rows)), dim3(256), 0, s, t);
   SKD_LAUNCH(k_table_deal, dim3(std::max(t.rows, 1)), dim3(64), 0, s, t);
 }
 void kv_compact(hipStream_t s, const KvTable &t) {
@@ -517,7 +562,7 @@ void kv_compact(hipStream_t s, const KvTable &t) {
     SKD_LAUNCH(k_table_compact_one, dim3(1), dim3(1024), 0, s, t);
     return;
   }
-  SKD_LAUNCH(k_table_fill, dim3(std::min(groups_for(t.pages), 1024u)), dim3(256), 0, s, t.work, (long)t.pages, 0L);
+  SKD_LAUNCH(k_table_fill, dim3(std::min(groups_for(t.pages), 1024u)), dim3(256), 0, s, t.work, (long)compact_zeros(t), 0L);
   SKD_LAUNCH(k_table_mark, dim3(groups_for(entries)), dim3(256), 0, s, t);
   SKD_LAUNCH(k_table_used, dim3(chunks), dim3(256), 0, s, t);
   SKD_LAUNCH(k_table_rank, dim3(chunks), dim3(256), 0, s, t);
