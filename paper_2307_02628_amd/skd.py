@@ -429,8 +429,8 @@ class KvScores:
         for t, dtype in ((slopes, "float32"), (begin, "int32"), (end, "int32")):
             if t is not None:
                 _expect(t, dtype, 1)
-        if window >= 1 << 31:
-            raise ValueError("expected a window below 2^31")
+        if not -1 << 31 <= window < 1 << 31:
+            raise ValueError("expected a window that fits 32 bits")
         self._keep = (slopes, begin, end)
         self._heads, self._tokens = (None if slopes is None else len(slopes)), [len(t) for t in (begin, end) if t is not None]
         self.c = Scores(cap, _ptr_of(slopes), window, _ptr_of(begin), _ptr_of(end))
