@@ -51,7 +51,7 @@ def test_places_that_no_token_sees(elem, fill, dh, new, group, name):
 
 
 @pytest.mark.parametrize("elem,fill", FILLS)
-@pytest.mark.parametrize("new", [1, 6, 140])
+@pytest.mark.parametrize("new", [1, 6, 40])
 def test_places_that_no_token_sees_of_a_long_row_in_shares(elem, fill, new):
     past, window = 9000, 2000
     c = S.Rows(elem, 1, 128, 64, [past], [new], seed=67)
