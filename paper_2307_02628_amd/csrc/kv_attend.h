@@ -36,8 +36,9 @@ enum { SC_MASK = 1, SC_CAP = 2, SC_SLOPES = 4 };  // what of a call's scoring a 
 // the distance, over what scores are multiplied by, is where the matrix instructions' sums begin: one instruction a score.  A cap's
 // function is applied in place, but for its factor, which takes that place, and for its constant part, which is the same for every position.
 // (Its four instructions, two of them of a quarter of the rate, stand in the code as such: with a branch around them, or around
-// the share, products and exponentials of two blocks no longer mixed: 512 tokens of 8 rows behind 2048, 32 heads of 128, bf16, us:
-// slopes 217, so 162 (144 with the nearest blocks first); cap 194, 177; masks alone 156, 144, which is what the plain attention takes.)
+// the share, products and exponentials of two blocks no longer mixed.  8 rows of up to 512 tokens behind 2048, 32 heads of 128, bf16, us
+// of short runs: slopes 217, so 162; cap 194, 177; masks alone 156, 144.  Of continued ones, side by side: scores as they are 130, masks
+// alone 129, slopes 139 with the nearest blocks first, cap 160, both 175; 8 bits 143, 147, 162, 180, 201; 4 bits 144, 148, 163, 179, 198.)
 
 // bf16x8 of two words of codes, times the power of two whose exponent byte is `e` (255: NaN)
 __device__ inline bf16x8 widen(uint32_t a, uint32_t b, uint32_t e) {
@@ -365,8 +366,8 @@ struct Share {
   // SC: the blocks that every query sees whole come first, the others, before and behind them, then: masks are in the code once.
   __device__ int wholes() const { return whole_hi - whole_lo; }
   // LAST_FIRST: of the whole ones the last first, where scores fall with the distance: the nearest have the largest ones, and the
-  // reference is not raised again and again (from the first on, and so, us: 512 tokens of 8 rows behind 2048, 32 heads of 128, bf16 165, 144, 8
-  // bits 188, 160; steps of 32 rows of 600 in 4 bits 19.7, 18.5).
+  // reference is not raised again and again (from the first on, and so, us: 8 rows of up to 512 tokens behind 2048, 32 heads of 128, bf16 161,
+  // 139, 8 bits 191, 162, 4 bits 184, 163; steps of 32 rows of up to 600 in 4 bits 19.3, 18.2).
   template <bool LAST_FIRST = false>
   __device__ int block(int v) const { return v < wholes() ? (LAST_FIRST ? whole_hi - 1 - v : whole_lo + v) : v < whole_hi - lo ? v - wholes() + lo : v + lo; }
   __device__ int seen(const KvAttend &a, int q) const { return t.past + q / a.group + 1; }  // positions that query q sees
@@ -782,6 +783,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
   if constexpr (FP4 && NT == 1 && DH == 128 && !SC) {
     // Blocks are small: the next one is on its way while one is used (128 rows of 1024, 32 heads: 83 -> 79 us; one row of 32766, 8 kv
     // heads 15.8 -> 15.1).  Where fewer registers are left, or more queries to compute for, it costs: heads of 64 45 -> 49, two tiles 27.6 -> 28.4.
+    // With changed scores, so written, the blocks went through scratch memory: 128 rows of 1023, slopes 96 -> 447, a cap 96 -> 447; 32 rows 30 -> 118.
     Block b;
     int at = blk, base = at < end ? fetch(b) : -1;
     auto step = [&](auto masked_) {
@@ -967,10 +969,10 @@ __global__ __launch_bounds__(NW * 64, NT == 1 ? 4 : 2) void k_kv_attend(KvAttend
 // stages in LDS holds: filled by LDS-direct loads, one bare barrier for two blocks (8-bit blocks stay codes in LDS, and every wave
 // converts what it reads).  Blocks that all queries see whole are taken two at a time with one branch for all weights, the values
 // requested before it.  80 KB of stages and up to 256 registers: two workgroups a CU.  Three (168 registers, three stages, a
-// block at a time, fragments requested as they are needed): us, 8 rows of 512 new tokens behind 2048, 32 heads of 128, bf16
-// 143 -> 136; 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 339.  Bound by the vector units (softmax;
-// conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.  4 bits, 8 rows of
-// 512 behind 2048: 146 us (bf16 139), the vector units at work in 51 % of all cycles, the matrix cores in 25.  What a workgroup with
+// block at a time, fragments requested as they are needed): us of short runs, 8 rows of up to 512 new tokens behind 2048, 32 heads of 128, bf16
+// 143 -> 136 (130 of continued ones); 2 rows of 1023 behind 8193, 32 queries' and 8 kv heads, 8 bits 404 -> 339.  Bound by the vector units (softmax;
+// conversions take two thirds again) and the matrix cores in turns, with two waves a SIMD; four tiles a wave do not fit.  4 bits, the same 8 rows:
+// 144 us (8 bits 143), the vector units at work in 51 % of all cycles, the matrix cores in 25.  What a workgroup with
 // changed scores takes before its first block is its rows' place, the ranges of its tokens and a page's number, one after the other; the
 // queries come meanwhile (2 prompts of 2047 in windows of 1: 24.7 -> 23.4 us, of which their bytes are 16).
 constexpr int rows_stages(int dh, int el) { return el != EL_BF16 ? 8 : dh == 128 ? 5 : 6; }  // (64: three workgroups, 97 -> 77 us for 32 prompts of 512)

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(64) void k_table_deal(KvTable t) {
 }
 
 // A small table by one workgroup: the same steps, what a page is to the entries in LDS, in one launch instead of five (one and five,
-// us: 128 rows of 11 of 1384 pages 7.4, 16.1; 128 of 29 of 3148 10.0, 16.6; compaction, 64 of 122 of 4096 pages 7.3, 16.8).
+// us: 128 rows of 11 of 1384 pages 7.6, 15.6; 128 of 29 of 3148 10.4, 16.4; 64 of 122 of 4096 16.3, 16.0, compacted 7.2, 20.7).
 constexpr int ONE_PAGES = 4096, ONE_ENTRIES = 8192;
 // Sum over the 1024 threads of those before this one; `all`: over all of them.
 __device__ inline int before_in_group(int n, int (&sums)[16], int &all) {
