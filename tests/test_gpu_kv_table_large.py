@@ -113,7 +113,7 @@ class Call:
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("R,W,pages", [(1025, 3, 5000), (5000, 2, 1 << 20), (70001, 2, 200000), (1 << 18, 1, 1 << 19), (3, 5, 3 << 20), (2100000, 1, 2500000)])
+@pytest.mark.parametrize("R,W,pages", [(1025, 3, 5000), (5000, 2, 1 << 20), (70001, 2, 200000), (1 << 18, 1, 1 << 19), (3, 5, 3 << 20), (2100000, 1, 2500000), (1000, 2, (17 << 20) + 5)])
 def test_large_tables(R, W, pages):
     """Around and far beyond a chunk of rows and pages, and a chunk of chunks of either."""
     g = np.random.default_rng(R)
